@@ -215,7 +215,7 @@ def _prepare_linear(c, g):
     return {"op": "linear", "x": x.to(DTYPES[c["x"]]), "m": m, "k": k, "n": n, "w": _pack(codes).contiguous(), "ws": _tile_scales(scales),
             "bias": torch.randn(n, generator=g, device="cuda") * 0.1 if c["bias"] else None, "relu": c["relu"],
             "y": torch.zeros(m, n + pad, dtype=DTYPES[c["y"]], device="cuda"),
-            "scratch": torch.empty(m * nb * 16 + pb + 256, dtype=torch.uint8, device="cuda")}
+            "scratch": torch.empty(m * nb * 16 + pb + 256, dtype=torch.uint8, device="cuda"), "status": torch.zeros(1, dtype=torch.int32, device="cuda")}
 
 
 def prepare(case, seed):
@@ -273,7 +273,7 @@ def _run_own(s):
     else:
         x, y = s["x"], s["y"]
         m.mfet_mx4_linear(x, m.dtype_of(x), x.stride(0), s["m"], s["w"], s["ws"], s["n"], s["k"], s["bias"], m.ACT_RELU if s["relu"] else m.ACT_NONE,
-                          y, m.dtype_of(y), y.stride(0), s["scratch"], s["scratch"].numel(), stream)
+                          y, m.dtype_of(y), y.stride(0), s["scratch"], s["scratch"].numel(), s["status"], stream)
 
 
 def run(state):
@@ -285,7 +285,7 @@ def run(state):
         return {"grads": state["flat"], "norm": state["norm"]}
     if state["op"] == "rows":
         return {"values": state["dst"], "status": state["status"]}
-    return {"y": state["y"][:, :state["n"]]}
+    return {"y": state["y"][:, :state["n"]], "status": state["status"]}
 
 
 # ---------------------------------------------------------------- what it cannot do without ----
@@ -357,4 +357,4 @@ def exact(case, seed):
     y = _values64(s["x"][:, :k].double()) @ _values64(w.double()).T
     if s["bias"] is not None:
         y = y + s["bias"].double()
-    return {"y": torch.clamp(y, min=0) if s["relu"] else y}
+    return {"y": torch.clamp(y, min=0) if s["relu"] else y, "status": None}
