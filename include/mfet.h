@@ -43,7 +43,8 @@ extern "C" {
 typedef struct mfet_tables mfet_tables_t; /* opaque, library-owned */
 typedef void* mfet_stream_t;              /* a cudaStream_t */
 
-enum { MFET_F32 = 0, MFET_F16 = 1, MFET_BF16 = 2, MFET_INT4 = 3 };
+enum { MFET_F32 = 0, MFET_F16 = 1, MFET_BF16 = 2, MFET_INT4 = 3, MFET_MXFP4 = 4 };
+enum { MFET_ACT_NONE = 0, MFET_ACT_RELU = 1 };
 enum { MFET_POOL_SUM = 0, MFET_POOL_MEAN = 1, MFET_POOL_WSUM = 2 };
 enum { MFET_LOC_DEVICE = 0, MFET_LOC_HOST = 1 };
 enum { MFET_VAL_NORMAL = 0, MFET_VAL_GRID = 1 };
@@ -103,8 +104,9 @@ typedef struct {
 } mfet_batch_shape_t;
 
 /* Stored bytes of one row: dim*4 (F32), dim*2 (F16/BF16); INT4: dim/2 nibble
- * bytes + fp16 scale + fp16 bias, rounded up to a multiple of 16 (dim even).
- * Returns 0 for a bad dtype. */
+ * bytes + fp16 scale + fp16 bias, rounded up to a multiple of 16 (dim even);
+ * MXFP4: dim/2 nibble bytes + one scale byte per 32 elements, rounded up to a
+ * multiple of 16. Returns 0 for a bad dtype. */
 MFET_API uint64_t mfet_row_bytes(uint32_t dim, uint32_t dtype);
 
 /* Create a table set on GPU `device` (a CUDA ordinal). Copies the descriptors;
@@ -373,6 +375,99 @@ MFET_API int mfet_host_fetch_rows(mfet_tables_t* t, int32_t table_id, const int6
  * roll-out (Algorithm 1). Default tag: 0. */
 MFET_API int mfet_tables_set_version(mfet_tables_t* t, uint64_t version);
 MFET_API int mfet_tables_version(const mfet_tables_t* t, uint64_t* version /*host*/);
+
+/* ---- after the backward pass: clipping, writing rows back, the first dense layer ----
+ * These calls take no handle: they work on caller memory of the current GPU, with the
+ * sizes, formats and lists that the calls above use. They are asynchronous on `stream`.
+ * `status` is a device word (or NULL) into which the kernels OR MFET_DEV_* bits. */
+
+/* One gradient tensor: rows x cols elements of dtype MFET_F32 / MFET_F16 / MFET_BF16, `ld`
+ * elements apart (0 = cols). n_rows: NULL, or a device count of which at most `rows` rows
+ * are used: what mfet_embedding_bag_backward writes, so that its sparse lists are clipped
+ * without the host learning their length. dst: where the scaled gradient goes, laid out as
+ * src; it may be src itself, or NULL (the tensor only counts for the norm); it must not
+ * overlap src otherwise. Rows beyond the count are neither read nor written. */
+typedef struct {
+  const void* src;
+  void* dst;
+  int64_t rows, cols, ld;
+  const int64_t* n_rows;
+  uint32_t dtype;
+  uint32_t flags;  /* must be 0 */
+} mfet_grad_t;
+
+/* Global 2-norm of all tensors and clipping (paper, Section 4.3: the tables are fine-tuned
+ * with the ranking model, so the gradients of tables and dense parameters are clipped together):
+ *   norm = sqrt(sum of g^2 over all elements of all tensors)
+ *   dst  = g * (norm > max_norm ? max_norm / norm : 1), rounded to the tensor's dtype.
+ * Squares and sums are fp64, in an order that depends only on the list and the GPU. When norm is NaN or
+ * infinite the gradients are passed on unchanged; the caller sees it in *norm.
+ *   grads    host mfet_grad_t[n_grads]; n_grads == 0 gives norm 0
+ *   norm     dev f32[1], or NULL;  max_norm >= 0; infinity: the norm only, dst = g
+ *   scratch  dev, 8-byte aligned, mfet_grad_clip_bytes(n_grads) bytes; needs no initialisation
+ * Errors: INVALID_ARG, ALIGNMENT (a tensor not aligned to its element), WORKSPACE, CUDA. */
+MFET_API uint64_t mfet_grad_clip_bytes(int32_t n_grads);
+MFET_API int mfet_grad_clip(const mfet_grad_t* grads /*host*/, int32_t n_grads, float max_norm, float* norm,
+                            void* scratch, uint64_t scratch_bytes, mfet_stream_t stream);
+
+/* Write rows of values into a table in its own format: row rows[i] of the table becomes
+ * values[i, 0..dim), i < n; and the reverse (paper, Section 4.1.2: tables are quantised after
+ * training). The table is memory of the current GPU, described as for mfet_tables_create
+ * (the memory of a live table set may be given; hash_seed is not used). dtypes:
+ *   MFET_F32 / F16 / BF16: rounded to nearest-even.
+ *   MFET_INT4 (dim % 8 == 0): the format of mfet_table_fill. A row whose scale or bias is not
+ *     finite (a NaN or an infinity among the values, or beyond fp16) reads back as NaN.
+ *   MFET_MXFP4 (dim % 8 == 0): 32 neighbouring elements share a scale 2^(b - 127), b =
+ *     max(0, floor(log2(max |v|)) + 125) as a byte (0 for a block of zeros); an element is the code of v / scale
+ *     in sign + E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6; nearest, ties to the even code, magnitudes above 6
+ *     to 6). Stored as dim/2 bytes of codes (element d in the low nibble of byte d/2 when d is
+ *     even), one scale byte per block, zero padding to a multiple of 16 bytes. A block with a NaN or an infinity
+ *     gets scale byte 255 and reads back as NaN.
+ *   rows    dev i64[n], or NULL: row i. A negative entry is no row: skipped by the write, zeros
+ *           in the read. An entry >= table rows is treated likewise and sets MFET_DEV_ROW_RANGE.
+ *           The entries of a write must be distinct (as mfet_embedding_bag_backward lists them): which one of two writers' bytes a
+ *           row holds is undefined.
+ *   n_dev   dev i64[1], or NULL: the number of entries, if only the device knows it (at most n are used)
+ *   values  dev [n, dim] of dtype MFET_F32 / F16 / BF16, `ld` >= dim elements between rows
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED_DIM, CUDA. */
+MFET_API int mfet_rows_write(const mfet_table_desc_t* table /*host*/, const int64_t* rows, int64_t n, const int64_t* n_dev,
+                             const void* values, uint32_t dtype, int64_t ld, uint32_t* status, mfet_stream_t stream);
+MFET_API int mfet_rows_read(const mfet_table_desc_t* table /*host*/, const int64_t* rows, int64_t n, const int64_t* n_dev,
+                            void* values, uint32_t dtype, int64_t ld, uint32_t* status, mfet_stream_t stream);
+
+/* MXFP4 matrix operands (the element format above). An operand of `rows` rows and k columns is
+ *   codes   [rows][ceil(k/32)][16] bytes, element d of a block in the low nibble of byte d/2 when d
+ *           is even; elements from k up to a multiple of 32 are code 0
+ *   scales  bytes in tiles of 128 rows x 4 blocks: the byte of row r, block c is at
+ *           (r/128 * ceil(k/128) + c/4) * 512 + (r%32)*16 + (r%128)/32*4 + c%4;
+ *           the bytes of blocks from ceil(k/32) up to a multiple of 4 are 0, those of rows past the end are not used
+ * Both 16-byte aligned, mfet_mx4_code_bytes / mfet_mx4_scale_bytes long (0 for a bad size). */
+MFET_API uint64_t mfet_mx4_code_bytes(int64_t rows, int64_t k);
+MFET_API uint64_t mfet_mx4_scale_bytes(int64_t rows, int64_t k);
+
+/* The operand of x dev [rows, k] of dtype MFET_F32 / F16 / BF16, `ld` >= k elements between rows.
+ * k >= 1, rows >= 0. Errors: INVALID_ARG, ALIGNMENT, CUDA. */
+MFET_API int mfet_mx4_quantize(const void* x, uint32_t dtype, int64_t ld, int64_t rows, int64_t k, void* codes,
+                               void* scales, mfet_stream_t stream);
+
+/* y[i, j] = act(sum over k of a[i, k] * w[j, k] + bias[j]), i < m, j < n, for two operands of k
+ * columns; products exact, fp32 sums, rounded once to y's dtype. bias dev f32[n] or NULL; act
+ * MFET_ACT_NONE / MFET_ACT_RELU; y dev [m, n] of dtype MFET_F32 / F16 / BF16, y_ld >= n elements between rows (what
+ * lies between is not written). MFET_DEV_STALLED in *status: a wait inside the kernel ran out (two
+ * seconds) and y is incomplete. Errors: INVALID_ARG, ALIGNMENT, CUDA. */
+MFET_API int mfet_mx4_matmul(const void* a_codes, const void* a_scales, int64_t m, const void* w_codes,
+                             const void* w_scales, int64_t n, int64_t k, const float* bias, uint32_t act, void* y,
+                             uint32_t y_dtype, int64_t y_ld, uint32_t* status, mfet_stream_t stream);
+
+/* The same with x quantised in the call: the first dense layer on the pooled features that
+ * mfet_embedding_bag_forward writes (paper, Section 2.2: they feed the ranking model), with weights
+ * quantised once. scratch dev, 16-byte aligned, mfet_mx4_linear_bytes(m, k) bytes (for m <= 8 and k up
+ * to 10,000 one kernel does it all and scratch may be NULL). Errors: as above, WORKSPACE. */
+MFET_API uint64_t mfet_mx4_linear_bytes(int64_t m, int64_t k);
+MFET_API int mfet_mx4_linear(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t m, const void* w_codes,
+                             const void* w_scales, int64_t n, int64_t k, const float* bias, uint32_t act, void* y,
+                             uint32_t y_dtype, int64_t y_ld, void* scratch, uint64_t scratch_bytes, uint32_t* status,
+                             mfet_stream_t stream);
 
 /* Number of kernels the library has launched on behalf of this handle. */
 MFET_API int mfet_launch_count(const mfet_tables_t* t, uint64_t* launches /*host*/);

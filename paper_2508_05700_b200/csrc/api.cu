@@ -57,6 +57,7 @@ uint64_t mfet_row_bytes(uint32_t dim, uint32_t dtype) {
     case MFET_F16:
     case MFET_BF16: return (uint64_t)dim * 2;
     case MFET_INT4: return ((uint64_t)dim / 2 + 4 + 15) / 16 * 16;
+    case MFET_MXFP4: return ((uint64_t)dim / 2 + ((uint64_t)dim + 31) / 32 + 15) / 16 * 16;
     default: return 0;
   }
 }

@@ -1,0 +1,363 @@
+// Global 2-norm of many gradient tensors, and the gradients scaled so that it is at most max_norm.
+//
+//   norm = sqrt(sum over all elements of g^2),  coef = norm > max_norm ? max_norm / norm : 1,  dst = round(g * coef)
+//
+// Two launches over the same pieces. The first adds up the squares: a block takes pieces of 32 KB, every element
+// is squared and added in double precision (no square of an fp32 value overflows or vanishes there, and the adder
+// is far from being the limit: one conversion and one fused multiply-add per element), and leaves one sum per block. The
+// second adds those sums up - every block the same ones in the same order, which costs less than another launch or a
+// count of finished blocks - and scales. It walks the pieces from the last to the first, because the end of what the
+// first launch has read is still in L2. Nothing depends on which block finishes when: equal inputs give equal bits.
+#include <cmath>
+#include <cstring>
+
+#include "lowbit.cuh"
+
+using namespace mfet;
+
+namespace mfet {
+namespace {
+
+constexpr int kClipThreads = 256;
+constexpr int kClipInFlight = 8;                                  // 16-byte loads that a thread requests together
+constexpr int kPieceVecs = kClipThreads * kClipInFlight;          // 16-byte vectors per piece
+constexpr int kClipBlocksPerSm = 4;
+
+struct GradDev {
+  const uint8_t* src;
+  uint8_t* dst;           // nullptr: only counted
+  const int64_t* n_rows;  // nullptr, or the number of rows on the device
+  int64_t rows, cols, ld;
+  int64_t first_piece;
+  uint32_t dtype;
+  uint32_t lead;          // elements between the 16-byte boundary before src and src; vectors are counted from that boundary
+};
+static_assert(sizeof(GradDev) == 64, "the capacities below count 64-byte entries");
+
+// Tensors per launch: the entries are kernel parameters. The small block keeps the launch of a few tensors cheap.
+constexpr int kFewTensors = 48, kManyTensors = 448;
+template <int N>
+struct GradParams {
+  double* sums;       // all sums of the call
+  float* norm;
+  double max_norm;
+  int64_t pieces;
+  int32_t n;          // tensors of this launch
+  int32_t first_sum;  // where this launch's blocks put theirs
+  int32_t n_sums;     // sums of the call
+  int32_t pad;
+  GradDev t[N];
+};
+static_assert(sizeof(GradParams<kManyTensors>) <= 32000, "kernel parameters are limited to 32764 bytes");
+
+template <class P>
+__device__ __forceinline__ int find_tensor(const P& p, int64_t piece) {
+  int lo = 0, hi = p.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (p.t[mid].first_piece <= piece) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int64_t live_elems(const GradDev& t) {
+  int64_t r = t.rows;
+  if (t.n_rows) {
+    const int64_t v = *t.n_rows;
+    r = v < 0 ? 0 : (v < r ? v : r);
+  }
+  return r * t.cols;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* shared) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_down_sync(0xFFFFFFFFu, v, d);
+  if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double s = 0;
+#pragma unroll
+  for (int w = 0; w < kClipThreads / 32; ++w) s += shared[w];
+  __syncthreads();
+  return s;
+}
+
+// element i of a tensor whose rows are `ld` apart
+__device__ __forceinline__ int64_t strided(const GradDev& t, int64_t i) {
+  const int64_t r = (uint64_t)(i | t.cols) >> 32 ? i / t.cols : (int64_t)((uint32_t)i / (uint32_t)t.cols);
+  return r * t.ld + (i - r * t.cols);
+}
+
+template <int DT>
+__device__ __forceinline__ double vec_squares(const uint4& v) {
+  constexpr int V = 16 / sizeof(typename Elem<DT>::T);
+  typename Elem<DT>::T t[V];
+  memcpy(t, &v, 16);
+  double s = 0;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const double x = (double)Elem<DT>::to(t[j]);
+    s = fma(x, x, s);
+  }
+  return s;
+}
+
+template <int DT>
+__device__ double piece_squares(const GradDev& t, int64_t piece) {
+  using T = typename Elem<DT>::T;
+  constexpr int V = 16 / sizeof(T);
+  const int64_t n = live_elems(t);
+  const T* src = reinterpret_cast<const T*>(t.src);
+  const int64_t v0 = piece * kPieceVecs, end = n + t.lead;  // vectors count from the boundary before src
+  double s = 0;
+  if (v0 * V >= end) return s;
+  if (t.ld == t.cols) {
+    const T* base = src - t.lead;
+    uint4 v[kClipInFlight];
+#pragma unroll
+    for (int j = 0; j < kClipInFlight; ++j) {
+      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
+      v[j] = make_uint4(0, 0, 0, 0);
+      if (a >= t.lead && a + V <= end) v[j] = __ldg(reinterpret_cast<const uint4*>(base + a));
+    }
+#pragma unroll
+    for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
+    // the vectors at the tensor's two ends that belong to it only in part
+#pragma unroll 1
+    for (int j = 0; j < kClipInFlight; ++j) {
+      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
+      if (a + V <= t.lead || a >= end || (a >= t.lead && a + V <= end)) continue;
+      for (int64_t i = a > t.lead ? a : t.lead; i < a + V && i < end; ++i) {
+        const double x = (double)Elem<DT>::to(base[i]);
+        s = fma(x, x, s);
+      }
+    }
+  } else {
+    for (int64_t i = v0 * V + threadIdx.x; i < (v0 + kPieceVecs) * V && i < n; i += kClipThreads) {
+      const double x = (double)Elem<DT>::to(src[strided(t, i)]);
+      s = fma(x, x, s);
+    }
+  }
+  return s;
+}
+
+// x * coef rounded to its type; without clipping the bits are handed on (a product with 1 would change a NaN's)
+struct Factor {
+  bool clip;
+  float coef;
+};
+template <int DT>
+__device__ __forceinline__ typename Elem<DT>::T scaled(typename Elem<DT>::T x, Factor f) {
+  return f.clip ? Elem<DT>::from(Elem<DT>::to(x) * f.coef) : x;
+}
+
+template <int DT>
+__device__ void piece_scale(const GradDev& t, int64_t piece, Factor f) {
+  using T = typename Elem<DT>::T;
+  constexpr int V = 16 / sizeof(T);
+  const int64_t n = live_elems(t);
+  const T* src = reinterpret_cast<const T*>(t.src);
+  T* dst = reinterpret_cast<T*>(t.dst);
+  const int64_t v0 = piece * kPieceVecs, end = n + t.lead;
+  if (v0 * V >= end) return;
+  if (t.ld == t.cols) {
+    const T* from = src - t.lead;
+    T* to = dst - t.lead;
+    const bool same = ((reinterpret_cast<uintptr_t>(to)) & 15u) == 0;  // dst sits on its boundary as src does
+    uint4 v[kClipInFlight];
+#pragma unroll
+    for (int j = 0; j < kClipInFlight; ++j) {
+      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
+      if (a >= t.lead && a + V <= end) v[j] = *reinterpret_cast<const uint4*>(from + a);
+    }
+#pragma unroll
+    for (int j = 0; j < kClipInFlight; ++j) {
+      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
+      if (a + V <= t.lead || a >= end) continue;
+      if (a >= t.lead && a + V <= end) {
+        T x[V];
+        memcpy(x, &v[j], 16);
+#pragma unroll
+        for (int q = 0; q < V; ++q) x[q] = scaled<DT>(x[q], f);
+        if (same) {
+          uint4 r;
+          memcpy(&r, x, 16);
+          *reinterpret_cast<uint4*>(to + a) = r;
+        } else {
+#pragma unroll
+          for (int q = 0; q < V; ++q) to[a + q] = x[q];
+        }
+      } else {
+        for (int64_t i = a > t.lead ? a : t.lead; i < a + V && i < end; ++i)
+          to[i] = scaled<DT>(from[i], f);
+      }
+    }
+  } else {
+    for (int64_t i = v0 * V + threadIdx.x; i < (v0 + kPieceVecs) * V && i < n; i += kClipThreads) {
+      const int64_t at = strided(t, i);
+      dst[at] = scaled<DT>(src[at], f);
+    }
+  }
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads) grad_squares_kernel(const __grid_constant__ GradParams<N> p) {
+  __shared__ double shared[kClipThreads / 32];
+  double s = 0;
+  for (int64_t k = blockIdx.x; k < p.pieces; k += gridDim.x) {
+    const GradDev& t = p.t[find_tensor(p, k)];
+    const int64_t piece = k - t.first_piece;
+    if (t.dtype == MFET_F32) s += piece_squares<MFET_F32>(t, piece);
+    else if (t.dtype == MFET_F16) s += piece_squares<MFET_F16>(t, piece);
+    else s += piece_squares<MFET_BF16>(t, piece);
+  }
+  s = block_sum(s, shared);
+  if (threadIdx.x == 0) p.sums[p.first_sum + blockIdx.x] = s;
+  asm volatile("griddepcontrol.launch_dependents;");
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads) grad_scale_kernel(const __grid_constant__ GradParams<N> p) {
+  __shared__ double shared[kClipThreads / 32];
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the sums of the launch before this one
+  double s = 0;
+  for (int i = threadIdx.x; i < p.n_sums; i += kClipThreads) s += __ldcg(p.sums + i);
+  const double norm = sqrt(block_sum(s, shared));
+  if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
+  // a norm that is infinite or NaN leaves the gradients as they are
+  const bool clip = norm > p.max_norm && norm < INFINITY;
+  Factor f{clip, (float)(p.max_norm / norm)};
+  asm volatile("" : "+f"(f.coef));  // else "clip ? x * coef : x" may be folded into one product
+  for (int64_t k = p.pieces - 1 - blockIdx.x; k >= 0; k -= gridDim.x) {
+    const GradDev& t = p.t[find_tensor(p, k)];
+    if (!t.dst || (!clip && t.dst == t.src)) continue;
+    const int64_t piece = k - t.first_piece;
+    if (t.dtype == MFET_F32) piece_scale<MFET_F32>(t, piece, f);
+    else if (t.dtype == MFET_F16) piece_scale<MFET_F16>(t, piece, f);
+    else piece_scale<MFET_BF16>(t, piece, f);
+  }
+}
+
+int64_t blocks_of(int64_t pieces) {
+  const int64_t most = (int64_t)sm_count() * kClipBlocksPerSm;
+  return pieces < most ? pieces : most;
+}
+
+int check_grad(const mfet_grad_t& g) {
+  if (g.dtype > MFET_BF16 || g.flags != 0 || g.rows < 0 || g.cols < 0) return MFET_ERR_INVALID_ARG;
+  if (g.rows >= (1ll << 48) || g.cols >= (1ll << 48) || g.ld >= (1ll << 48)) return MFET_ERR_INVALID_ARG;
+  if (g.cols > 0 && g.rows > (1ll << 56) / g.cols) return MFET_ERR_INVALID_ARG;
+  if (g.rows > 0 && g.cols > 0 && !g.src) return MFET_ERR_INVALID_ARG;
+  if (g.ld != 0 && g.ld < g.cols) return MFET_ERR_INVALID_ARG;
+  const uintptr_t mask = g.dtype == MFET_F32 ? 3u : 1u;
+  if (((uintptr_t)g.src & mask) || ((uintptr_t)g.dst & mask) || ((uintptr_t)g.n_rows & 7u)) return MFET_ERR_ALIGNMENT;
+  return MFET_OK;
+}
+
+// the tensors [at, at + n) as kernel parameters; returns how many of them fit
+template <int N>
+int32_t fill_params(const mfet_grad_t* g, int32_t n_grads, int32_t at, GradParams<N>* p) {
+  p->n = 0;
+  p->pieces = 0;
+  int32_t i = at;
+  for (; i < n_grads && p->n < N; ++i) {
+    if (g[i].rows == 0 || g[i].cols == 0) continue;
+    GradDev& t = p->t[p->n++];
+    const int64_t size = g[i].dtype == MFET_F32 ? 4 : 2;
+    t.src = (const uint8_t*)g[i].src;
+    t.dst = (uint8_t*)g[i].dst;
+    t.n_rows = g[i].n_rows;
+    t.rows = g[i].rows;
+    t.cols = g[i].cols;
+    t.ld = g[i].ld && g[i].rows > 1 ? g[i].ld : g[i].cols;
+    t.dtype = g[i].dtype;
+    t.lead = t.ld == t.cols ? (uint32_t)(((uintptr_t)t.src & 15u) / size) : 0u;
+    t.first_piece = p->pieces;
+    p->pieces += (t.rows * t.cols + t.lead + kPieceVecs * (16 / size) - 1) / (kPieceVecs * (16 / size));
+  }
+  return i - at;
+}
+
+template <int N>
+cudaError_t launch_squares(const GradParams<N>& p, cudaStream_t s) {
+  grad_squares_kernel<N><<<(unsigned)blocks_of(p.pieces), kClipThreads, 0, s>>>(p);
+  return cudaGetLastError();
+}
+
+template <int N>
+cudaError_t launch_scale(const GradParams<N>& p, cudaStream_t s) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.blockDim = dim3(kClipThreads);
+  cfg.gridDim = dim3((unsigned)(p.pieces > 0 ? blocks_of(p.pieces) : 1));
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, grad_scale_kernel<N>, p);
+}
+
+// Tensors are taken in groups that fit the kernel parameters: first the squares of all groups, then the scaling of each.
+template <int N>
+int run_clip(const mfet_grad_t* g, int32_t n_grads, double max_norm, float* norm, double* sums, int64_t room,
+             cudaStream_t s) {
+  GradParams<N> p;
+  p.sums = sums;
+  p.norm = norm;
+  p.max_norm = max_norm;
+  p.pad = 0;
+  p.first_sum = 0;
+  int64_t n_sums = 0;
+  for (int32_t at = 0; at < n_grads;) {
+    at += fill_params<N>(g, n_grads, at, &p);
+    n_sums += blocks_of(p.pieces);
+  }
+  if (n_sums > room) return MFET_ERR_WORKSPACE;
+  p.n_sums = (int32_t)n_sums;
+  const bool one_group = n_grads <= N;  // p holds it already
+  if (n_grads == 0) p.n = 0, p.pieces = 0;
+  for (int32_t at = 0; at < n_grads;) {
+    at += one_group ? n_grads : fill_params<N>(g, n_grads, at, &p);
+    if (p.pieces == 0) continue;
+    if (launch_squares(p, s) != cudaSuccess) return MFET_ERR_CUDA;
+    p.first_sum += (int32_t)blocks_of(p.pieces);
+  }
+  for (int32_t at = 0; at < n_grads;) {
+    at += one_group ? n_grads : fill_params<N>(g, n_grads, at, &p);
+    bool any = false;
+    for (int32_t i = 0; i < p.n; ++i) any |= p.t[i].dst != nullptr;
+    if (!any) continue;
+    if (launch_scale(p, s) != cudaSuccess) return MFET_ERR_CUDA;
+    p.norm = nullptr;  // written once
+  }
+  if (p.norm) {  // nothing to scale: the norm alone
+    p.pieces = 0;
+    if (launch_scale(p, s) != cudaSuccess) return MFET_ERR_CUDA;
+  }
+  return MFET_OK;
+}
+
+}  // namespace
+}  // namespace mfet
+
+extern "C" uint64_t mfet_grad_clip_bytes(int32_t n_grads) {
+  if (n_grads < 0) return 0;
+  const uint64_t groups = ((uint64_t)n_grads + kManyTensors - 1) / kManyTensors;
+  return (groups ? groups : 1) * (uint64_t)sm_count() * kClipBlocksPerSm * sizeof(double);
+}
+
+extern "C" int mfet_grad_clip(const mfet_grad_t* grads, int32_t n_grads, float max_norm, float* norm, void* scratch,
+                              uint64_t scratch_bytes, mfet_stream_t stream) {
+  if (n_grads < 0 || (n_grads > 0 && !grads) || !(max_norm >= 0.f)) return MFET_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n_grads; ++i) {
+    const int rc = check_grad(grads[i]);
+    if (rc != MFET_OK) return rc;
+  }
+  if (((uintptr_t)scratch & 7u) != 0 || ((uintptr_t)norm & 3u) != 0) return MFET_ERR_ALIGNMENT;
+  if (!scratch) scratch_bytes = 0;
+  const int64_t room = (int64_t)(scratch_bytes / sizeof(double));
+  double* sums = static_cast<double*>(scratch);
+  if (n_grads <= kFewTensors) return run_clip<kFewTensors>(grads, n_grads, max_norm, norm, sums, room, (cudaStream_t)stream);
+  return run_clip<kManyTensors>(grads, n_grads, max_norm, norm, sums, room, (cudaStream_t)stream);
+}

@@ -1,0 +1,694 @@
+// MXFP4 matrices: quantisation of a matrix into an operand, and the product of two operands,
+//
+//   y[i, j] = act(sum over k of a[i, k] * w[j, k] + bias[j])
+//
+// An operand of r rows and k columns is its codes, row by row (16 bytes per block of 32 values, the last block filled up
+// with zeros), and its scale bytes in tiles of 128 rows x 4 blocks = 512 bytes, tile by tile along a row of tiles: byte
+// (r % 32) * 16 + (r % 128) / 32 * 4 + block % 4 of a tile. That is the order in which the tensor cores read
+// scales, so a tile goes from global to shared to tensor memory as it lies. Codes and scales are defined in lowbit.cuh.
+//
+// Two kernels for the product. A few rows (mx4_few_kernel): the weights are read once and nothing else costs bandwidth,
+// so a warp per output column and integer dot products suffice, and x is quantised in the same launch. More rows
+// (mx4_gemm_kernel): block-scaled 5th-generation tensor-core instructions with the weights as the 128-row operand.
+#include <cuda.h>
+
+#include <atomic>
+#include <cstring>
+
+#include "lowbit.cuh"
+
+using namespace mfet;
+
+namespace mfet {
+namespace {
+
+constexpr unsigned kAll = 0xFFFFFFFFu;
+
+// ------------------------------------------------------------------ quantisation ----
+
+constexpr int kQuantThreads = 256;
+constexpr int kQuantInFlight = 4;  // pieces of 128 values that a half-warp requests together
+
+struct QuantParams {
+  const uint8_t* x;
+  int64_t ld;
+  int64_t rows;
+  int64_t units;     // rows * groups
+  uint32_t k, blocks, groups;  // values, blocks of 32, groups of 4 blocks per row
+  uint8_t* codes;
+  uint8_t* scales;
+};
+
+// A half-warp takes one row's 128 values (4 blocks): 8 values per lane, 4 lanes per block, 64 bytes of codes, and the four
+// scale bytes as one word. Bound by reading x.
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kQuantThreads) mx4_quantize_kernel(const __grid_constant__ QuantParams p) {
+  using T = typename Elem<DT>::T;
+  asm volatile("griddepcontrol.launch_dependents;");  // the product may set itself up; it waits for this grid's end
+  const int lane = threadIdx.x & 31, sub = lane & 15;
+  const int64_t warp = ((int64_t)blockIdx.x * kQuantThreads + threadIdx.x) >> 5;
+  const int64_t step = (int64_t)gridDim.x * (kQuantThreads / 32) * 2 * kQuantInFlight;
+  for (int64_t u0 = warp * 2 * kQuantInFlight; u0 < p.units; u0 += step) {
+    Raw8<DT> raw[kQuantInFlight];
+    int64_t row[kQuantInFlight];
+    uint32_t group[kQuantInFlight];
+    int count[kQuantInFlight];
+#pragma unroll
+    for (int u = 0; u < kQuantInFlight; ++u) {
+      const int64_t i = u0 + 2 * u + (lane >> 4);
+      row[u] = (uint64_t)i >> 32 ? i / p.groups : (int64_t)((uint32_t)i / p.groups);
+      group[u] = (uint32_t)(i - row[u] * p.groups);
+      const uint32_t at = group[u] * 128 + sub * 8;
+      count[u] = i < p.units && at < p.k ? (int)min(8u, p.k - at) : 0;
+      if (count[u] > 0) raw[u] = load8<DT, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kQuantInFlight; ++u) {
+      float v[8] = {};
+      if (count[u] > 0) widen8<DT>(raw[u], v);
+      uint32_t m = amax8(v);
+      m = max(m, __shfl_xor_sync(kAll, m, 1));
+      m = max(m, __shfl_xor_sync(kAll, m, 2));
+      const uint32_t b = mx_scale_byte(m);
+      uint32_t word = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) word |= __shfl_sync(kAll, b, (lane & 16) + 4 * j) << (8 * j);
+      if (u0 + 2 * u + (lane >> 4) < p.units) {
+        const uint32_t c = group[u] * 16 + sub;  // chunk of 8 values within the row
+        if (c < p.blocks * 4)
+          *reinterpret_cast<uint32_t*>(p.codes + row[u] * ((int64_t)p.blocks * 16) + c * 4) =
+              b == kMxNan ? 0u : mx_encode8(v, mx_inv_scale(b));
+        if (sub == 0)
+          *reinterpret_cast<uint32_t*>(p.scales + ((row[u] >> 7) * p.groups + group[u]) * 512 + (row[u] & 31) * 16 +
+                                       ((row[u] & 127) >> 5) * 4) = word;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ epilogue ----
+
+struct OutParams {
+  uint8_t* y;
+  int64_t ld;
+  const float* bias;
+  uint32_t dtype;
+  uint32_t relu;
+};
+
+__device__ __forceinline__ float activate(float v, float bias, uint32_t relu) {
+  v += bias;
+  return relu && v < 0.f ? 0.f : v;  // a NaN stays one
+}
+
+__device__ __forceinline__ void put(const OutParams& o, int64_t i, int64_t j, float v) {
+  const int64_t at = i * o.ld + j;
+  if (o.dtype == MFET_F32) reinterpret_cast<float*>(o.y)[at] = v;
+  else if (o.dtype == MFET_F16) reinterpret_cast<__half*>(o.y)[at] = __float2half_rn(v);
+  else reinterpret_cast<__nv_bfloat16*>(o.y)[at] = __float2bfloat16_rn(v);
+}
+
+// ------------------------------------------------------------------ a few rows ----
+
+constexpr int kFewThreads = 256;
+constexpr int kFewMost = 8;  // rows of x
+
+struct FewParams {
+  const uint8_t* x;
+  int64_t ld;
+  const uint8_t* codes;
+  const uint8_t* scales;
+  int64_t n;
+  uint32_t k, blocks, groups;
+  int32_t m;
+  uint32_t x_dtype, vec;
+  OutParams out;
+};
+
+// twice the values of codes 0..3 of `codes`' low half, as signed bytes. A code's low three bits pick the magnitude
+// 0,1,2,3,4,6,8,12; prmt reads the code's sign bit as "replicate the sign of the picked byte", which is 0 for these tables,
+// so `pos` holds the non-negative codes and `neg` the magnitudes of the others.
+__device__ __forceinline__ uint32_t pick4(uint32_t codes) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(0x03020100u), "r"(0x0C080604u), "r"(codes));  // reads 16 bits of codes
+  return r;
+}
+__device__ __forceinline__ uint32_t twice4(uint32_t codes) {
+  const uint32_t pos = pick4(codes), neg = pick4(codes ^ 0x8888u);
+  return ((pos | 0x80808080u) - neg) ^ 0x80808080u;  // no borrow crosses a byte
+}
+
+template <int DT>
+__device__ __forceinline__ void few_stage(const FewParams& p, int mt, int4* sx, float* ss, uint32_t padded) {
+  // 4 lanes per block of x; the block's 32 signed bytes go to two arrays of 16-byte halves, so that neighbouring lanes'
+  // reads of neighbouring blocks hit neighbouring banks
+  using T = typename Elem<DT>::T;
+  const uint32_t units = (uint32_t)mt * padded * 4;  // chunks of 8 values; `padded` is a multiple of 32: whole warps
+  for (uint32_t i = threadIdx.x; i < units; i += kFewThreads) {
+    const uint32_t row = i / (padded * 4), c = i - row * padded * 4, b = c >> 2;
+    const int count = (int)row < p.m && c * 8 < p.k ? (int)min(8u, p.k - c * 8) : 0;
+    float v[8] = {};
+    if (count > 0) {
+      const T* at = reinterpret_cast<const T*>(p.x) + (int64_t)row * p.ld + c * 8;
+      const Raw8<DT> raw = p.vec ? load8<DT, true>(at, count) : load8<DT, false>(at, count);
+      widen8<DT>(raw, v);
+    }
+    uint32_t m = amax8(v);
+    m = max(m, __shfl_xor_sync(kAll, m, 1));
+    m = max(m, __shfl_xor_sync(kAll, m, 2));
+    const uint32_t s = mx_scale_byte(m);
+    const uint32_t codes = s == kMxNan ? 0u : mx_encode8(v, mx_inv_scale(s));
+    const uint32_t half = (c >> 1) & 1;
+    uint2* dst = reinterpret_cast<uint2*>(sx + (row * 2 + half) * padded + b) + (c & 1);
+    *dst = make_uint2(twice4(codes), twice4(codes >> 16));
+    if ((c & 3) == 0) ss[row * padded + b] = mx_scale(s);
+  }
+}
+
+// A warp per output column: lane b takes block b, b + 32, ... of the column's weights (16 bytes each, 512 bytes per warp and
+// load) against the same block of all MT rows of x from shared memory: 8 integer dot products of 4 values per
+// row and block, exact, then one fp32 multiply-add with the two scales.
+template <int MT>
+__global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_constant__ FewParams p) {
+  extern __shared__ int4 sx[];  // [MT][2][padded] 16-byte halves, then [MT][padded] scales
+  const uint32_t padded = (p.blocks + 31) & ~31u;
+  float* ss = reinterpret_cast<float*>(sx + (size_t)MT * 2 * padded);
+  const int lane = threadIdx.x & 31;
+  const int64_t first = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5);
+  const int64_t step = (int64_t)gridDim.x * (kFewThreads / 32);
+  auto weights = [&](int64_t j, uint32_t b, uint4* w, uint32_t* s) {
+    const bool in = j < p.n && b < p.blocks;
+    *w = in ? __ldg(reinterpret_cast<const uint4*>(p.codes + (j * p.blocks + b) * 16)) : make_uint4(0, 0, 0, 0);
+    *s = in ? (uint32_t)__ldg(p.scales + ((j >> 7) * p.groups + (b >> 2)) * 512 + (j & 31) * 16 + ((j & 127) >> 5) * 4 + (b & 3))
+            : 0u;
+  };
+  // the first weights do not depend on x: they are under way while x is quantised
+  uint4 w;
+  uint32_t s;
+  weights(first, lane, &w, &s);
+  if (p.x_dtype == MFET_F32) few_stage<MFET_F32>(p, MT, sx, ss, padded);
+  else if (p.x_dtype == MFET_F16) few_stage<MFET_F16>(p, MT, sx, ss, padded);
+  else few_stage<MFET_BF16>(p, MT, sx, ss, padded);
+  __syncthreads();
+  for (int64_t j = first; j < p.n; j += step) {
+    float acc[MT];
+#pragma unroll
+    for (int r = 0; r < MT; ++r) acc[r] = 0.f;
+    for (uint32_t b = lane; b < padded; b += 32) {
+      const uint4 wn = w;
+      const float sw = mx_scale(s) * 0.25f;  // both factors of the integer product are doubled
+      // the next block's weights, or the next column's first ones
+      if (b + 32 < padded) weights(j, b + 32, &w, &s);
+      else weights(j + step, lane, &w, &s);
+      const uint32_t c[4] = {wn.x, wn.y, wn.z, wn.w};
+      uint32_t v[8];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[2 * q] = twice4(c[q]), v[2 * q + 1] = twice4(c[q] >> 16);
+#pragma unroll
+      for (int r = 0; r < MT; ++r) {
+        const int4 x0 = sx[(r * 2) * padded + b], x1 = sx[(r * 2 + 1) * padded + b];
+        int d = __dp4a((int)v[0], x0.x, 0);
+        d = __dp4a((int)v[1], x0.y, d);
+        d = __dp4a((int)v[2], x0.z, d);
+        d = __dp4a((int)v[3], x0.w, d);
+        d = __dp4a((int)v[4], x1.x, d);
+        d = __dp4a((int)v[5], x1.y, d);
+        d = __dp4a((int)v[6], x1.z, d);
+        d = __dp4a((int)v[7], x1.w, d);
+        acc[r] = fmaf((float)d * sw, ss[r * padded + b], acc[r]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) acc[r] += __shfl_xor_sync(kAll, acc[r], d);
+    }
+    float mine = acc[0];
+#pragma unroll
+    for (int r = 1; r < MT; ++r)
+      if (lane == r) mine = acc[r];
+    if (lane < p.m) put(p.out, lane, j, activate(mine, p.out.bias ? p.out.bias[j] : 0.f, p.out.relu));
+  }
+}
+
+// ------------------------------------------------------------------ tensor cores ----
+
+constexpr int kGemmThreads = 192;  // warp 0 loads, warp 1 issues the products, warps 2..5 write results
+constexpr int kTileN = 128;        // weights' rows (output columns) per tile: lanes of tensor memory
+constexpr int kSlab = 256;         // k per stage: 128 bytes of codes per row, four instructions of k = 64
+constexpr uint64_t kStallNs = 2000000000ull;
+
+template <int TM>  // rows of x per tile: columns of tensor memory
+struct GemmShape {
+  static constexpr uint32_t a_bytes = kTileN * 128, b_bytes = TM * 128, s_bytes = 1024;  // 2 scale tiles of 512 bytes
+  static constexpr uint32_t stage_bytes = a_bytes + b_bytes + 2 * s_bytes;
+  static constexpr int stages = 6;
+  static constexpr uint32_t smem = stage_bytes * stages + 1024;  // + room to align to 1024
+  static constexpr uint32_t acc_cols = TM;                       // two accumulators, then 16 columns of scales per stage
+  static constexpr uint32_t scale_col = 2 * TM;
+  static_assert(scale_col + 16 * stages <= 512, "tensor memory has 512 columns");
+};
+
+struct GemmParams {
+  const uint8_t* a_scales;  // weights
+  const uint8_t* b_scales;  // x
+  int64_t m, n;
+  uint32_t k, groups, slabs;
+  uint32_t n_tiles;
+  int64_t tiles;
+  uint32_t* status;
+  OutParams out;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\t"
+               "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+               "selp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok)
+               : "r"(bar), "r"(parity)
+               : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// Waits for the phase `parity` of a barrier, two seconds at most; false: it did not come (or another role gave up)
+__device__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+  if (bar_try(bar, parity)) return true;
+  const uint64_t t0 = now_ns();
+  for (uint32_t i = 0;; ++i) {
+    if (bar_try(bar, parity)) return true;
+    if ((i & 63) == 63) {
+      if (*dead) return false;
+      if (now_ns() - t0 > kStallNs) {
+        *dead = 1;
+        return false;
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// Shared-memory matrix descriptor, K-major rows of 128 bytes with the 128-byte swizzle: groups of 8 rows are 1024 bytes apart
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
+  return (uint64_t)((addr >> 4) & 0x3FFF) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// 32 rows of 16 bytes without a swizzle (a scale tile): groups of 8 rows are 128 bytes apart
+__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
+  return (uint64_t)((addr >> 4) & 0x3FFF) | (8ull << 16) | (8ull << 32) | (1ull << 46);
+}
+// Instruction descriptor: both operands E2M1, K-major, scales UE8M0, fp32 accumulator; `id`: which two of a row's four scale
+// bytes (0 or 2) this instruction's two blocks use
+template <int TM>
+__device__ __forceinline__ uint32_t inst_desc(uint32_t id) {
+  return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TM >> 3) << 17) | (1u << 23) | ((uint32_t)(kTileN >> 7) << 27) | (id << 29);
+}
+
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t inst, uint32_t sa, uint32_t sb, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\t"
+               "setp.ne.b32 p, %6, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+               "l"(a), "l"(b), "r"(inst), "r"(sa), "r"(sb), "r"(add)
+               : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"  // in one statement: nothing may use the registers before the wait
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr)
+      : "memory");
+}
+
+// One block per SM walks over the tiles (128 output columns x TM rows of x); output columns run fastest, so that the blocks at
+// work share the rows of x in L2. Stages of k = 256 go through a ring of shared memory; two accumulators in tensor memory, so
+// that a tile is written while the next one is computed. The weights are the 128-row operand: a lane of tensor memory is an
+// output column, and the 32 lanes of a warp write 32 neighbouring values of one row of y.
+template <int TM>
+__global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap a_map,
+                                                                  const __grid_constant__ CUtensorMap b_map,
+                                                                  const __grid_constant__ GemmParams p) {
+  using G = GemmShape<TM>;
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ __align__(8) uint64_t bars[2 * G::stages + 5];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int dead;
+  const uint32_t base = (smem_addr(raw_smem) + 1023) & ~1023u;
+  const uint32_t bar0 = smem_addr(bars);
+  auto full = [&](int s) { return bar0 + 8 * s; };
+  auto empty = [&](int s) { return bar0 + 8 * (G::stages + s); };
+  auto acc_full = [&](int a) { return bar0 + 8 * (2 * G::stages + a); };
+  auto acc_empty = [&](int a) { return bar0 + 8 * (2 * G::stages + 2 + a); };
+  const uint32_t drained = bar0 + 8 * (2 * G::stages + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < G::stages; ++s) bar_init(full(s), 1), bar_init(empty(s), 1);
+    for (int a = 0; a < 2; ++a) bar_init(acc_full(a), 1), bar_init(acc_empty(a), 4);
+    bar_init(drained, 1);
+    dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
+
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // x may be the result of the launch before this one
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;  // stages filled so far
+      bool ok = true;
+      for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+        const int64_t tm = t / p.n_tiles, tn = t - tm * p.n_tiles;
+        const uint8_t* sa = p.a_scales + (size_t)tn * p.groups * 512;
+        const uint8_t* sb = p.b_scales + (size_t)(tm * TM >> 7) * p.groups * 512;
+        for (uint32_t s = 0; s < p.slabs; ++s, ++it) {
+          const int st = it % G::stages;
+          if (it >= G::stages && !(ok = bar_wait(empty(st), (it / G::stages - 1) & 1, &dead))) break;
+          const uint32_t at = base + st * G::stage_bytes;
+          const uint32_t sc = min(2u, p.groups - 2 * s) * 512;  // scale bytes of this slab, per operand
+          bar_expect(full(st), G::a_bytes + G::b_bytes + 2 * sc);
+          tma_load(at, &a_map, (int32_t)(s * 128), (int32_t)(tn * kTileN), full(st));
+          tma_load(at + G::a_bytes, &b_map, (int32_t)(s * 128), (int32_t)(tm * TM), full(st));
+          bulk_load(at + G::a_bytes + G::b_bytes, sa + (size_t)s * 1024, sc, full(st));
+          bulk_load(at + G::a_bytes + G::b_bytes + G::s_bytes, sb + (size_t)s * 1024, sc, full(st));
+        }
+      }
+      // Every copy that this thread started has to land before the block ends. The products wait for each of them; only
+      // when a wait has run out are they waited for here.
+      if (!ok || dead) {
+        volatile int none = 0;
+        const uint32_t from = it > G::stages ? it - G::stages : 0;
+        for (uint32_t i = from; i < it; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t it = 0, done = 0;
+      bool ok = true;
+      for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x, ++done) {
+        const int acc = done & 1;
+        if (done >= 2 && !(ok = bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem + acc * G::acc_cols;
+        for (uint32_t s = 0; s < p.slabs; ++s, ++it) {
+          const int st = it % G::stages;
+          if (!(ok = bar_wait(full(st), (it / G::stages) & 1, &dead))) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t at = base + st * G::stage_bytes, sc = at + G::a_bytes + G::b_bytes;
+          const uint32_t sfa = tmem + G::scale_col + 16 * st, sfb = sfa + 8;
+          const uint32_t left = p.k - s * kSlab;
+          const int steps = left >= (uint32_t)kSlab ? 4 : (int)((left + 63) / 64);
+          const int pairs = (steps + 1) / 2;
+          for (int g = 0; g < pairs; ++g) {
+            copy_scales(sfa + 4 * g, scale_desc(sc + 512 * g));
+            copy_scales(sfb + 4 * g, scale_desc(sc + G::s_bytes + 512 * g));
+          }
+          for (int j = 0; j < steps; ++j)
+            mma_mx4(d, tile_desc(at + 32 * j), tile_desc(at + G::a_bytes + 32 * j), inst_desc<TM>((j & 1) * 2), sfa + 4 * (j >> 1),
+                    sfb + 4 * (j >> 1), s > 0 || j > 0);
+          mma_commit(empty(st));
+        }
+        if (ok) mma_commit(acc_full(acc));
+      }
+      if (!ok || dead) {  // the products under way read shared memory and write tensor memory: let them end
+        volatile int none = 0;
+        mma_commit(drained);
+        bar_wait(drained, 0, &none);
+      }
+    }
+  } else {
+    const int quarter = warp & 3;  // the 32 lanes of tensor memory that this warp may read
+    uint32_t done = 0;
+    for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x, ++done) {
+      const int acc = done & 1;
+      const bool ok = bar_wait(acc_full(acc), (done / 2) & 1, &dead);
+      if (!__all_sync(kAll, ok)) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const int64_t tm = t / p.n_tiles, tn = t - tm * p.n_tiles;
+      const int64_t j = tn * kTileN + quarter * 32 + lane, i0 = tm * TM;
+      const bool in = j < p.n;
+      const float bias = in && p.out.bias ? p.out.bias[j] : 0.f;
+#pragma unroll 1
+      for (int c = 0; c < TM; c += 32) {
+        uint32_t r[32];
+        tmem_load32(tmem + acc * G::acc_cols + c + ((uint32_t)(quarter * 32) << 16), r);
+        if (c + 32 >= TM) {  // the accumulator is read: the next tile but one may overwrite it
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(acc_empty(acc));
+        }
+#pragma unroll
+        for (int q = 0; q < 32; ++q)
+          if (in && i0 + c + q < p.m) put(p.out, i0 + c + q, j, activate(__uint_as_float(r[q]), bias, p.out.relu));
+      }
+    }
+  }
+  __syncwarp();  // the one lane that loaded or issued rejoins its warp
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (dead && threadIdx.x == 0 && p.status) atomicOr(p.status, (uint32_t)MFET_DEV_STALLED);
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+// ------------------------------------------------------------------ host side ----
+
+struct Dims {
+  uint32_t blocks, groups;
+};
+Dims dims_of(int64_t k) { return {(uint32_t)((k + 31) / 32), (uint32_t)((k + 127) / 128)}; }
+
+bool bad_size(int64_t rows, int64_t k) { return rows < 0 || rows >= (1ll << 31) || k < 1 || k >= (1ll << 30); }
+
+uint64_t code_bytes(int64_t rows, int64_t k) { return (uint64_t)rows * dims_of(k).blocks * 16; }
+uint64_t scale_bytes(int64_t rows, int64_t k) { return (uint64_t)((rows + 127) / 128) * dims_of(k).groups * 512; }
+
+bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+uint32_t size_of(uint32_t dtype) { return dtype == MFET_F32 ? 4 : 2; }
+
+template <int DT>
+cudaError_t launch_quantize(const QuantParams& p, bool vec, cudaStream_t s) {
+  const int64_t per_block = (int64_t)(kQuantThreads / 32) * 2 * kQuantInFlight;
+  const int64_t want = (p.units + per_block - 1) / per_block, most = (int64_t)sm_count() * 16;
+  const unsigned b = (unsigned)(want < most ? want : most);
+  if (vec) mx4_quantize_kernel<DT, true><<<b, kQuantThreads, 0, s>>>(p);
+  else mx4_quantize_kernel<DT, false><<<b, kQuantThreads, 0, s>>>(p);
+  return cudaGetLastError();
+}
+
+int quantize(const void* x, uint32_t dtype, int64_t rows, int64_t k, int64_t ld, void* codes, void* scales, cudaStream_t s) {
+  const Dims d = dims_of(k);
+  QuantParams p{(const uint8_t*)x, ld, rows, rows * (int64_t)d.groups, (uint32_t)k, d.blocks, d.groups, (uint8_t*)codes,
+                (uint8_t*)scales};
+  const bool vec = aligned(x, 16) && (uint64_t)ld * size_of(dtype) % 16 == 0;
+  cudaError_t e;
+  switch (dtype) {
+    case MFET_F32: e = launch_quantize<MFET_F32>(p, vec, s); break;
+    case MFET_F16: e = launch_quantize<MFET_F16>(p, vec, s); break;
+    default: e = launch_quantize<MFET_BF16>(p, vec, s); break;
+  }
+  return e == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static std::atomic<void*> found{nullptr};
+  void* f = found.load(std::memory_order_acquire);
+  if (!f) {
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    found.store(f, std::memory_order_release);
+  }
+  return reinterpret_cast<EncodeTiled>(f);
+}
+
+// codes [rows, blocks * 16 bytes] read in boxes of `box` rows x 128 bytes; what lies outside reads as code 0
+bool code_map(CUtensorMap* map, const void* codes, int64_t rows, uint32_t blocks, uint32_t box) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const cuuint64_t size[2] = {(cuuint64_t)blocks * 16, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)blocks * 16};
+  const cuuint32_t boxes[2] = {128, box}, ones[2] = {1, 1};
+  return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), size, stride, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int TM>
+int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
+         uint32_t* status, bool after_quantize, cudaStream_t s) {
+  const Dims d = dims_of(k);
+  CUtensorMap a, b;
+  if (!code_map(&a, wc, n, d.blocks, kTileN) || !code_map(&b, xc, m, d.blocks, TM)) return MFET_ERR_CUDA;
+  GemmParams p;
+  p.a_scales = (const uint8_t*)ws;
+  p.b_scales = (const uint8_t*)xs;
+  p.m = m;
+  p.n = n;
+  p.k = (uint32_t)k;
+  p.groups = d.groups;
+  p.slabs = (uint32_t)((k + kSlab - 1) / kSlab);
+  p.n_tiles = (uint32_t)((n + kTileN - 1) / kTileN);
+  p.tiles = (m + TM - 1) / TM * p.n_tiles;
+  p.status = status;
+  p.out = out;
+  static std::atomic<uint64_t> ready{0};  // one bit per GPU: the kernel may use this much shared memory there
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return MFET_ERR_CUDA;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    if (cudaFuncSetAttribute(mx4_gemm_kernel<TM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GemmShape<TM>::smem) != cudaSuccess)
+      return MFET_ERR_CUDA;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.gridDim = dim3((unsigned)(p.tiles < sm_count() ? p.tiles : sm_count()));
+  cfg.dynamicSmemBytes = GemmShape<TM>::smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = after_quantize ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<TM>, a, b, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+}
+
+int product(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
+            uint32_t* status, bool after_quantize, cudaStream_t s) {
+  if (m <= 32) return gemm<32>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+  if (m <= 64) return gemm<64>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+  return gemm<128>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+}
+
+template <int MT>
+cudaError_t launch_few(const FewParams& p, cudaStream_t s) {
+  const size_t padded = (p.blocks + 31) & ~31u;
+  const size_t smem = MT * padded * (32 + 4);
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(mx4_few_kernel<MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  const int64_t want = (p.n + kFewThreads / 32 - 1) / (kFewThreads / 32), most = (int64_t)sm_count() * 4;
+  mx4_few_kernel<MT><<<(unsigned)(want < most ? want : most), kFewThreads, smem, s>>>(p);
+  return cudaGetLastError();
+}
+
+int check_out(int64_t m, int64_t n, const float* bias, uint32_t act, const void* y, uint32_t dtype, int64_t ld) {
+  if (dtype > MFET_BF16 || act > MFET_ACT_RELU || ld < n || ld >= (1ll << 31) || (m > 0 && n > 0 && !y)) return MFET_ERR_INVALID_ARG;
+  if (!aligned(y, size_of(dtype)) || !aligned(bias, 4)) return MFET_ERR_ALIGNMENT;
+  return MFET_OK;
+}
+
+}  // namespace
+}  // namespace mfet
+
+extern "C" {
+
+uint64_t mfet_mx4_code_bytes(int64_t rows, int64_t k) { return bad_size(rows, k) ? 0 : code_bytes(rows, k); }
+uint64_t mfet_mx4_scale_bytes(int64_t rows, int64_t k) { return bad_size(rows, k) ? 0 : scale_bytes(rows, k); }
+
+int mfet_mx4_quantize(const void* x, uint32_t dtype, int64_t ld, int64_t rows, int64_t k, void* codes, void* scales,
+                      mfet_stream_t stream) {
+  if (dtype > MFET_BF16 || bad_size(rows, k) || ld < k || ld >= (1ll << 31)) return MFET_ERR_INVALID_ARG;
+  if (rows == 0) return MFET_OK;
+  if (!x || !codes || !scales) return MFET_ERR_INVALID_ARG;
+  if (!aligned(x, size_of(dtype)) || !aligned(codes, 16) || !aligned(scales, 16)) return MFET_ERR_ALIGNMENT;
+  return quantize(x, dtype, rows, k, ld, codes, scales, (cudaStream_t)stream);
+}
+
+int mfet_mx4_matmul(const void* a_codes, const void* a_scales, int64_t m, const void* w_codes, const void* w_scales, int64_t n,
+                    int64_t k, const float* bias, uint32_t act, void* y, uint32_t y_dtype, int64_t y_ld, uint32_t* status,
+                    mfet_stream_t stream) {
+  if (bad_size(m, k) || bad_size(n, k)) return MFET_ERR_INVALID_ARG;
+  const int rc = check_out(m, n, bias, act, y, y_dtype, y_ld);
+  if (rc != MFET_OK) return rc;
+  if (m == 0 || n == 0) return MFET_OK;
+  if (!a_codes || !a_scales || !w_codes || !w_scales) return MFET_ERR_INVALID_ARG;
+  if (!aligned(a_codes, 16) || !aligned(a_scales, 16) || !aligned(w_codes, 16) || !aligned(w_scales, 16)) return MFET_ERR_ALIGNMENT;
+  const OutParams out{(uint8_t*)y, y_ld, bias, y_dtype, act == MFET_ACT_RELU};
+  return product(a_codes, a_scales, m, w_codes, w_scales, n, k, out, status, false, (cudaStream_t)stream);
+}
+
+uint64_t mfet_mx4_linear_bytes(int64_t m, int64_t k) {
+  if (bad_size(m, k)) return 0;
+  return scale_bytes(m, k) + code_bytes(m, k);
+}
+
+int mfet_mx4_linear(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t m, const void* w_codes, const void* w_scales, int64_t n,
+                    int64_t k, const float* bias, uint32_t act, void* y, uint32_t y_dtype, int64_t y_ld, void* scratch,
+                    uint64_t scratch_bytes, uint32_t* status, mfet_stream_t stream) {
+  if (x_dtype > MFET_BF16 || bad_size(m, k) || bad_size(n, k) || x_ld < k || x_ld >= (1ll << 31)) return MFET_ERR_INVALID_ARG;
+  int rc = check_out(m, n, bias, act, y, y_dtype, y_ld);
+  if (rc != MFET_OK) return rc;
+  if (m == 0 || n == 0) return MFET_OK;
+  if (!x || !w_codes || !w_scales) return MFET_ERR_INVALID_ARG;
+  if (!aligned(x, size_of(x_dtype)) || !aligned(w_codes, 16) || !aligned(w_scales, 16)) return MFET_ERR_ALIGNMENT;
+  const OutParams out{(uint8_t*)y, y_ld, bias, y_dtype, act == MFET_ACT_RELU};
+  const Dims d = dims_of(k);
+  cudaStream_t s = (cudaStream_t)stream;
+  // the quantised x of a few rows has to fit shared memory (k up to 10,000 for 8 rows)
+  const uint32_t mt = m == 1 ? 1 : m == 2 ? 2 : m <= 4 ? 4 : 8;
+  if (m <= kFewMost && (uint64_t)mt * ((d.blocks + 31) & ~31u) * 36 <= 96 * 1024) {
+    FewParams p{(const uint8_t*)x, x_ld, (const uint8_t*)w_codes, (const uint8_t*)w_scales, n, (uint32_t)k, d.blocks, d.groups,
+                (int32_t)m, x_dtype, aligned(x, 16) && (uint64_t)x_ld * size_of(x_dtype) % 16 == 0, out};
+    const cudaError_t e = mt == 1 ? launch_few<1>(p, s) : mt == 2 ? launch_few<2>(p, s) : mt == 4 ? launch_few<4>(p, s) : launch_few<8>(p, s);
+    return e == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+  }
+  if (!scratch || scratch_bytes < scale_bytes(m, k) + code_bytes(m, k)) return MFET_ERR_WORKSPACE;
+  if (!aligned(scratch, 16)) return MFET_ERR_ALIGNMENT;
+  uint8_t* scales = (uint8_t*)scratch;
+  uint8_t* codes = scales + scale_bytes(m, k);
+  rc = quantize(x, x_dtype, m, k, x_ld, codes, scales, s);
+  if (rc != MFET_OK) return rc;
+  return product(codes, scales, m, w_codes, w_scales, n, k, out, status, true, s);
+}
+
+}  // extern "C"

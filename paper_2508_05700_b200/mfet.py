@@ -18,7 +18,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # MFET_LIBRARY selects another build of the same library (the bounds-checked one, libmfet_checked.so)
 LIB_PATH = os.environ.get("MFET_LIBRARY") or os.path.join(_HERE, "libmfet.so")
 
-F32, F16, BF16, INT4 = 0, 1, 2, 3
+F32, F16, BF16, INT4, MXFP4 = 0, 1, 2, 3, 4
+ACT_NONE, ACT_RELU = 0, 1
 POOL_SUM, POOL_MEAN, POOL_WSUM = 0, 1, 2
 LOC_DEVICE, LOC_HOST = 0, 1
 VAL_NORMAL, VAL_GRID = 0, 1
@@ -40,6 +41,8 @@ EXPORTS = [
     "mfet_launch_count", "mfet_status_string", "mfet_dedup_rows_static", "mfet_profile_read", "mfet_host_path_counts", "mfet_tables_set_version", "mfet_tables_version",
     "mfet_host_prefetch", "mfet_embedding_bag_backward", "mfet_embedding_bag_forward_host_async",
     "mfet_host_path_result", "mfet_host_fetch_rows",
+    "mfet_grad_clip_bytes", "mfet_grad_clip", "mfet_rows_write", "mfet_rows_read", "mfet_mx4_code_bytes",
+    "mfet_mx4_scale_bytes", "mfet_mx4_quantize", "mfet_mx4_matmul", "mfet_mx4_linear_bytes", "mfet_mx4_linear",
 ]
 BATCH_IDS_ARE_ROWS, BATCH_PREFETCHED = 1, 2
 STATIC_DEDUP_MAX_IDS = 262144
@@ -54,6 +57,11 @@ class TableDesc(C.Structure):
 class BatchShape(C.Structure):
     _fields_ = [("batch", C.c_int32), ("n_features", C.c_int32), ("n_slots", C.c_int32),
                 ("flags", C.c_int32), ("slot_feature", C.POINTER(C.c_int32)), ("out_ld", C.c_int64)]
+
+
+class Grad(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64),
+                ("n_rows", C.c_void_p), ("dtype", C.c_uint32), ("flags", C.c_uint32)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -94,8 +102,20 @@ _lib.mfet_tables_version.argtypes = [_P, C.POINTER(C.c_uint64)]
 _lib.mfet_host_prefetch.argtypes = [_P, C.POINTER(BatchShape), _P, _P, _P, _P]
 _lib.mfet_embedding_bag_backward.argtypes = [_P, C.POINTER(BatchShape), _P, _P, _P, _P, _P, _P, C.c_int32, _P, _P, _P, _P]
 _lib.mfet_launch_count.argtypes = [_P, C.POINTER(C.c_uint64)]
+_lib.mfet_grad_clip.argtypes = [C.POINTER(Grad), C.c_int32, C.c_float, _P, _P, C.c_uint64, _P]
+_lib.mfet_rows_write.argtypes = [C.POINTER(TableDesc), _P, C.c_int64, _P, _P, C.c_uint32, C.c_int64, _P, _P]
+_lib.mfet_rows_read.argtypes = _lib.mfet_rows_write.argtypes
+_lib.mfet_mx4_quantize.argtypes = [_P, C.c_uint32, C.c_int64, C.c_int64, C.c_int64, _P, _P, _P]
+_lib.mfet_mx4_matmul.argtypes = [_P, _P, C.c_int64, _P, _P, C.c_int64, C.c_int64, _P, C.c_uint32, _P, C.c_uint32, C.c_int64, _P,
+                                 _P]
+_lib.mfet_mx4_linear.argtypes = [_P, C.c_uint32, C.c_int64, C.c_int64, _P, _P, C.c_int64, C.c_int64, _P, C.c_uint32, _P,
+                                 C.c_uint32, C.c_int64, _P, C.c_uint64, _P, _P]
+_BYTES = ("mfet_grad_clip_bytes", "mfet_mx4_code_bytes", "mfet_mx4_scale_bytes", "mfet_mx4_linear_bytes")
+for _n in _BYTES:
+    getattr(_lib, _n).restype = C.c_uint64
+    getattr(_lib, _n).argtypes = [C.c_int32] if _n == "mfet_grad_clip_bytes" else [C.c_int64, C.c_int64]
 for _n in EXPORTS:
-    if _n not in ("mfet_row_bytes", "mfet_status_string"):
+    if _n not in ("mfet_row_bytes", "mfet_status_string") + _BYTES:
         getattr(_lib, _n).restype = C.c_int
 
 
@@ -295,3 +315,79 @@ def mfet_launch_count(h) -> int:
     n = C.c_uint64()
     _check(_lib.mfet_launch_count(h, C.byref(n)), "mfet_launch_count")
     return int(n.value)
+
+
+def dtype_of(t) -> int:
+    """MFET_F32 / F16 / BF16 of a torch tensor."""
+    name = str(t.dtype)
+    if name not in _TORCH_DTYPES:
+        raise MfetError(ERR_INVALID_ARG, "dtype_of(%s)" % name)
+    return _TORCH_DTYPES[name]
+
+
+_TORCH_DTYPES = {"torch.float32": F32, "torch.float16": F16, "torch.bfloat16": BF16}
+
+
+def make_grads(src, dst, counts=None):
+    """The list of gradient tensors of mfet_grad_clip, to be kept and used for every step: `src` and `dst` (entries may be
+    None, or the source itself) are torch tensors of one or two dimensions whose last one is dense; counts: i64 device
+    tensor with the number of live rows of every tensor, or None."""
+    arr = (Grad * max(len(src), 1))()
+    for i, (a, b) in enumerate(zip(src, dst)):
+        if b is not None and (b.dtype != a.dtype or b.shape != a.shape or b.stride() != a.stride()):
+            raise MfetError(ERR_INVALID_ARG, "make_grads: tensor %d and its destination differ in type, shape or strides" % i)
+        two = a if a.dim() == 2 else a.reshape(1, -1) if a.is_contiguous() else None
+        if two is None or (two.shape[1] > 1 and two.stride(1) != 1):
+            raise MfetError(ERR_INVALID_ARG, "make_grads: tensor %d is not rows of neighbouring elements" % i)
+        rows, cols = two.shape
+        ld = two.stride(0) if rows > 1 else cols
+        arr[i] = Grad(_ptr(a), _ptr(b), rows, cols, ld, None if counts is None else _ptr(counts) + 8 * i, dtype_of(a), 0)
+    return arr, len(src)
+
+
+def mfet_grad_clip_bytes(n_grads: int) -> int:
+    return int(_lib.mfet_grad_clip_bytes(n_grads))
+
+
+def mfet_grad_clip(grads, max_norm: float, norm, scratch, scratch_bytes: int, stream=None) -> None:
+    """grads: what make_grads gave."""
+    arr, n = grads
+    _check(_lib.mfet_grad_clip(arr, n, max_norm, _ptr(norm), _ptr(scratch), scratch_bytes, _ptr(stream)), "mfet_grad_clip")
+
+
+def mfet_rows_write(table: TableDesc, rows, n: int, n_dev, values, dtype: int, ld: int, status=None, stream=None) -> None:
+    _check(_lib.mfet_rows_write(C.byref(table), _ptr(rows), n, _ptr(n_dev), _ptr(values), dtype, ld, _ptr(status),
+                                _ptr(stream)), "mfet_rows_write")
+
+
+def mfet_rows_read(table: TableDesc, rows, n: int, n_dev, values, dtype: int, ld: int, status=None, stream=None) -> None:
+    _check(_lib.mfet_rows_read(C.byref(table), _ptr(rows), n, _ptr(n_dev), _ptr(values), dtype, ld, _ptr(status),
+                               _ptr(stream)), "mfet_rows_read")
+
+
+def mfet_mx4_code_bytes(rows: int, k: int) -> int:
+    return int(_lib.mfet_mx4_code_bytes(rows, k))
+
+
+def mfet_mx4_scale_bytes(rows: int, k: int) -> int:
+    return int(_lib.mfet_mx4_scale_bytes(rows, k))
+
+
+def mfet_mx4_linear_bytes(m: int, k: int) -> int:
+    return int(_lib.mfet_mx4_linear_bytes(m, k))
+
+
+def mfet_mx4_quantize(x, dtype: int, ld: int, rows: int, k: int, codes, scales, stream=None) -> None:
+    _check(_lib.mfet_mx4_quantize(_ptr(x), dtype, ld, rows, k, _ptr(codes), _ptr(scales), _ptr(stream)), "mfet_mx4_quantize")
+
+
+def mfet_mx4_matmul(a_codes, a_scales, m: int, w_codes, w_scales, n: int, k: int, bias, act: int, y, y_dtype: int, y_ld: int,
+                    status=None, stream=None) -> None:
+    _check(_lib.mfet_mx4_matmul(_ptr(a_codes), _ptr(a_scales), m, _ptr(w_codes), _ptr(w_scales), n, k, _ptr(bias), act, _ptr(y),
+                                y_dtype, y_ld, _ptr(status), _ptr(stream)), "mfet_mx4_matmul")
+
+
+def mfet_mx4_linear(x, x_dtype: int, x_ld: int, m: int, w_codes, w_scales, n: int, k: int, bias, act: int, y, y_dtype: int,
+                    y_ld: int, scratch, scratch_bytes: int, status=None, stream=None) -> None:
+    _check(_lib.mfet_mx4_linear(_ptr(x), x_dtype, x_ld, m, _ptr(w_codes), _ptr(w_scales), n, k, _ptr(bias), act, _ptr(y), y_dtype,
+                                y_ld, _ptr(scratch), scratch_bytes, _ptr(status), _ptr(stream)), "mfet_mx4_linear")

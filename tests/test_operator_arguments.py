@@ -1,0 +1,132 @@
+"""Refusals of the clipping, row and matrix calls: found on the host, before anything is launched (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+from tests.helpers import mfet
+
+
+def status(call, *args):
+    m = mfet()
+    with pytest.raises(m.MfetError) as e:
+        call(*args)
+    return e.value.status
+
+
+def test_rows_refusals():
+    m = mfet()
+    A = 1 << 20  # an address that is never followed
+
+    def desc(**kw):
+        v = dict(data=A, rows=100, dim=64, dtype=m.MXFP4, loc=m.LOC_DEVICE, flags=0, seed=0, stride=0)
+        v.update(kw)
+        return m.TableDesc(v["data"], v["rows"], v["dim"], v["dtype"], v["loc"], v["flags"], v["seed"], v["stride"])
+
+    for call in (m.mfet_rows_write, m.mfet_rows_read):
+        def st(d, n=5, mem=A, dtype=m.F32, ld=64):
+            return status(call, d, A, n, None, mem, dtype, ld)
+        assert st(desc(data=None)) == m.ERR_INVALID_ARG
+        assert st(desc(rows=0)) == m.ERR_INVALID_ARG
+        assert st(desc(rows=1 << 63)) == m.ERR_INVALID_ARG
+        assert st(desc(dim=0)) == m.ERR_INVALID_ARG
+        assert st(desc(flags=1)) == m.ERR_INVALID_ARG
+        assert st(desc(dtype=5)) == m.ERR_INVALID_ARG
+        assert st(desc(loc=m.LOC_HOST)) == m.ERR_INVALID_ARG
+        assert st(desc(), n=-1) == m.ERR_INVALID_ARG
+        assert st(desc(), mem=None) == m.ERR_INVALID_ARG
+        assert st(desc(), dtype=m.INT4) == m.ERR_INVALID_ARG
+        assert st(desc(), ld=63) == m.ERR_INVALID_ARG
+        assert st(desc(dim=60, dtype=m.MXFP4)) == m.ERR_UNSUPPORTED_DIM
+        assert st(desc(dim=60, dtype=m.INT4)) == m.ERR_UNSUPPORTED_DIM
+        assert st(desc(dim=60, dtype=m.F16)) == m.ERR_UNSUPPORTED_DIM
+        assert st(desc(stride=40)) == m.ERR_INVALID_ARG
+        assert st(desc(stride=56)) == m.ERR_ALIGNMENT
+        assert st(desc(data=A + 8)) == m.ERR_ALIGNMENT
+        assert st(desc(), mem=A + 2) == m.ERR_ALIGNMENT
+        assert st(desc(), mem=A + 1, dtype=m.BF16) == m.ERR_ALIGNMENT
+        call(desc(), A, 0, None, None, m.F32, 64)  # nothing to do: no launch, no GPU
+    assert m.row_bytes(64, m.MXFP4) == 48 and m.row_bytes(32, m.MXFP4) == 32 and m.row_bytes(128, m.MXFP4) == 80
+    assert m.row_bytes(40, m.MXFP4) == 32 and m.row_bytes(8, m.MXFP4) == 16
+
+
+def test_grad_clip_refusals():
+    m = mfet()
+    A = 1 << 20
+
+    def st(max_norm=1.0, norm=A, scratch=A, nbytes=1 << 20, **kw):
+        v = dict(src=A, dst=A, rows=4, cols=8, ld=0, n_rows=None, dtype=m.F32, flags=0)
+        v.update(kw)
+        arr = (m.Grad * 1)(m.Grad(v["src"], v["dst"], v["rows"], v["cols"], v["ld"], v["n_rows"], v["dtype"], v["flags"]))
+        return status(m.mfet_grad_clip, (arr, 1), max_norm, norm, scratch, nbytes)
+    assert st(max_norm=-1.0) == m.ERR_INVALID_ARG
+    assert st(max_norm=float("nan")) == m.ERR_INVALID_ARG
+    assert st(src=None) == m.ERR_INVALID_ARG
+    assert st(rows=-1) == m.ERR_INVALID_ARG
+    assert st(cols=-1) == m.ERR_INVALID_ARG
+    assert st(ld=7) == m.ERR_INVALID_ARG
+    assert st(rows=1 << 40, cols=1 << 40) == m.ERR_INVALID_ARG
+    assert st(dtype=m.INT4) == m.ERR_INVALID_ARG
+    assert st(flags=1) == m.ERR_INVALID_ARG
+    assert st(src=A + 2) == m.ERR_ALIGNMENT
+    assert st(dst=A + 1, dtype=m.F16) == m.ERR_ALIGNMENT
+    assert st(n_rows=A + 4) == m.ERR_ALIGNMENT
+    assert st(norm=A + 2) == m.ERR_ALIGNMENT
+    assert st(scratch=A + 4) == m.ERR_ALIGNMENT
+    assert st(nbytes=0) == m.ERR_WORKSPACE
+    assert st(scratch=None) == m.ERR_WORKSPACE
+    assert status(m.mfet_grad_clip, (None, 1), 1.0, A, A, 1 << 20) == m.ERR_INVALID_ARG
+    assert status(m.mfet_grad_clip, (None, -1), 1.0, A, A, 1 << 20) == m.ERR_INVALID_ARG
+    assert m.mfet_grad_clip_bytes(-1) == 0 and m.mfet_grad_clip_bytes(1) > 0
+    assert m.mfet_grad_clip_bytes(5000) > m.mfet_grad_clip_bytes(400)
+
+
+def test_make_grads_refusals():
+    import torch
+    m = mfet()
+    a = torch.zeros(4, 6)
+    assert status(m.make_grads, [a], [a.half()]) == m.ERR_INVALID_ARG
+    assert status(m.make_grads, [a], [a[:3]]) == m.ERR_INVALID_ARG
+    assert status(m.make_grads, [a.t()], [a.t()]) == m.ERR_INVALID_ARG
+    assert status(m.make_grads, [a.double()], [None]) == m.ERR_INVALID_ARG
+    arr, n = m.make_grads([a, a[:, :5], a[0]], [None, a[:, :5], a[0]])
+    assert n == 3 and (arr[0].rows, arr[0].cols, arr[0].ld) == (4, 6, 6) and arr[0].dst is None
+    assert (arr[1].rows, arr[1].cols, arr[1].ld) == (4, 5, 6) and (arr[2].rows, arr[2].cols) == (1, 6)
+
+
+def test_mx4_refusals():
+    m = mfet()
+    A = 1 << 20
+    assert m.mfet_mx4_code_bytes(3, 33) == 3 * 2 * 16 and m.mfet_mx4_scale_bytes(129, 129) == 2 * 2 * 512
+    assert m.mfet_mx4_code_bytes(-1, 5) == 0 and m.mfet_mx4_scale_bytes(5, 0) == 0 and m.mfet_mx4_linear_bytes(5, 0) == 0
+
+    def q(x=A, dtype=m.F32, ld=64, rows=4, k=64, codes=A, scales=A):
+        return status(m.mfet_mx4_quantize, x, dtype, ld, rows, k, codes, scales)
+    assert q(x=None) == m.ERR_INVALID_ARG and q(codes=None) == m.ERR_INVALID_ARG and q(scales=None) == m.ERR_INVALID_ARG
+    assert q(dtype=m.INT4) == m.ERR_INVALID_ARG and q(ld=63) == m.ERR_INVALID_ARG and q(rows=-1) == m.ERR_INVALID_ARG
+    assert q(k=0) == m.ERR_INVALID_ARG
+    assert q(x=A + 2) == m.ERR_ALIGNMENT and q(codes=A + 8) == m.ERR_ALIGNMENT and q(scales=A + 4) == m.ERR_ALIGNMENT
+    m.mfet_mx4_quantize(None, m.F32, 64, 0, 64, None, None)
+
+    def mm(a=A, asc=A, rows=200, w=A, wsc=A, n=64, k=64, bias=None, act=0, y=A, yd=m.F32, ld=64):
+        return status(m.mfet_mx4_matmul, a, asc, rows, w, wsc, n, k, bias, act, y, yd, ld)
+    for kw in (dict(a=None), dict(asc=None), dict(w=None), dict(wsc=None), dict(y=None), dict(rows=-1), dict(n=-1), dict(k=0),
+               dict(act=2), dict(yd=m.INT4), dict(ld=63)):
+        assert mm(**kw) == m.ERR_INVALID_ARG, kw
+    for kw in (dict(a=A + 8), dict(asc=A + 8), dict(w=A + 4), dict(wsc=A + 1), dict(y=A + 2), dict(bias=A + 2)):
+        assert mm(**kw) == m.ERR_ALIGNMENT, kw
+    m.mfet_mx4_matmul(None, None, 0, None, None, 64, 64, None, 0, None, m.F32, 64)
+
+    def li(x=A, xd=m.F32, xld=64, rows=200, w=A, wsc=A, n=64, k=64, bias=None, act=0, y=A, yd=m.F32, ld=64, scratch=A, nbytes=1 << 20):
+        return status(m.mfet_mx4_linear, x, xd, xld, rows, w, wsc, n, k, bias, act, y, yd, ld, scratch, nbytes)
+    for kw in (dict(x=None), dict(w=None), dict(wsc=None), dict(y=None), dict(rows=-1), dict(n=-1), dict(k=0), dict(act=2),
+               dict(xd=m.INT4), dict(yd=m.INT4), dict(ld=63), dict(xld=63)):
+        assert li(**kw) == m.ERR_INVALID_ARG, kw
+    for kw in (dict(x=A + 2), dict(w=A + 4), dict(wsc=A + 1), dict(y=A + 2), dict(bias=A + 2), dict(scratch=A + 8)):
+        assert li(**kw) == m.ERR_ALIGNMENT, kw
+    assert li(scratch=None) == m.ERR_WORKSPACE and li(nbytes=100) == m.ERR_WORKSPACE
+    m.mfet_mx4_linear(None, m.F32, 64, 0, None, None, 64, 64, None, 0, None, m.F32, 64, None, 0)
+
+
+def test_struct_layout():
+    m = mfet()
+    assert C.sizeof(m.Grad) == 56 and m.Grad.n_rows.offset == 40 and m.Grad.dtype.offset == 48
