@@ -2,9 +2,8 @@
 //
 //   norm = sqrt(sum over all elements of g^2),  coef = norm > max_norm ? max_norm / norm : 1,  dst = round(g * coef)
 //
-// Two launches over the same pieces. The first adds up the squares: a block takes pieces of 32 KB, every element
-// is squared and added in double precision (no square of an fp32 value overflows or vanishes there, and the adder
-// is far from being the limit: one conversion and one fused multiply-add per element), and leaves one sum per block. The
+// Two launches over the same pieces of 32 KB. The first adds up the squares in fp64, a few of them at a time in fp32, and leaves one
+// sum per block. The
 // second adds those sums up - every block the same ones in the same order, which costs less than another launch or a
 // count of finished blocks - and scales. It walks the pieces from the last to the first, because the end of what the
 // first launch has read is still in L2. Nothing depends on which block finishes when: equal inputs give equal bits.
@@ -88,56 +87,21 @@ __device__ __forceinline__ int64_t strided(const GradDev& t, int64_t i) {
   return r * t.ld + (i - r * t.cols);
 }
 
+// Sum of the squares of 16 bytes. The four or eight products are added in fp32, which is exact enough for so few (2^-22
+// relative at worst) and leaves one conversion to fp64 per 16 bytes; where a product may leave fp32's range they are added in fp64.
 template <int DT>
-__device__ __forceinline__ double vec_squares(const uint4& v) {
-  constexpr int V = 16 / sizeof(typename Elem<DT>::T);
-  typename Elem<DT>::T t[V];
-  memcpy(t, &v, 16);
+__device__ __forceinline__ double vec_squares(const uint4& w) {
+  constexpr int V = 16 / (int)sizeof(typename Elem<DT>::T);
+  float v[V];
+  widen16<DT>(w, v);
+  float q = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) q = fmaf(v[j], v[j], q);
+  if (q > 1e-20f && q < 1e38f) return (double)q;
+  if (((w.x | w.y | w.z | w.w) & (DT == MFET_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0u) return 0.0;
   double s = 0;
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const double x = (double)Elem<DT>::to(t[j]);
-    s = fma(x, x, s);
-  }
-  return s;
-}
-
-template <int DT>
-__device__ double piece_squares(const GradDev& t, int64_t piece) {
-  using T = typename Elem<DT>::T;
-  constexpr int V = 16 / sizeof(T);
-  const int64_t n = live_elems(t);
-  const T* src = reinterpret_cast<const T*>(t.src);
-  const int64_t v0 = piece * kPieceVecs, end = n + t.lead;  // vectors count from the boundary before src
-  double s = 0;
-  if (v0 * V >= end) return s;
-  if (t.ld == t.cols) {
-    const T* base = src - t.lead;
-    uint4 v[kClipInFlight];
-#pragma unroll
-    for (int j = 0; j < kClipInFlight; ++j) {
-      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
-      v[j] = make_uint4(0, 0, 0, 0);
-      if (a >= t.lead && a + V <= end) v[j] = __ldg(reinterpret_cast<const uint4*>(base + a));
-    }
-#pragma unroll
-    for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
-    // the vectors at the tensor's two ends that belong to it only in part
-#pragma unroll 1
-    for (int j = 0; j < kClipInFlight; ++j) {
-      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
-      if (a + V <= t.lead || a >= end || (a >= t.lead && a + V <= end)) continue;
-      for (int64_t i = a > t.lead ? a : t.lead; i < a + V && i < end; ++i) {
-        const double x = (double)Elem<DT>::to(base[i]);
-        s = fma(x, x, s);
-      }
-    }
-  } else {
-    for (int64_t i = v0 * V + threadIdx.x; i < (v0 + kPieceVecs) * V && i < n; i += kClipThreads) {
-      const double x = (double)Elem<DT>::to(src[strided(t, i)]);
-      s = fma(x, x, s);
-    }
-  }
+  for (int j = 0; j < V; ++j) s = fma((double)v[j], (double)v[j], s);
   return s;
 }
 
@@ -148,13 +112,65 @@ struct Factor {
 };
 template <int DT>
 __device__ __forceinline__ typename Elem<DT>::T scaled(typename Elem<DT>::T x, Factor f) {
-  return f.clip ? Elem<DT>::from(Elem<DT>::to(x) * f.coef) : x;
+  return f.clip ? Elem<DT>::from(to_float<DT>(x) * f.coef) : x;
+}
+template <int DT>
+__device__ __forceinline__ uint4 scaled16(const uint4& w, Factor f) {
+  if (!f.clip) return w;
+  constexpr int V = 16 / (int)sizeof(typename Elem<DT>::T);
+  float v[V];
+  widen16<DT>(w, v);
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] *= f.coef;
+  return narrow16<DT>(v);
 }
 
 template <int DT>
-__device__ void piece_scale(const GradDev& t, int64_t piece, Factor f) {
+__device__ __forceinline__ double piece_squares(const GradDev& t, int64_t piece) {
   using T = typename Elem<DT>::T;
-  constexpr int V = 16 / sizeof(T);
+  constexpr int V = 16 / (int)sizeof(T);
+  const int64_t n = live_elems(t);
+  const T* src = reinterpret_cast<const T*>(t.src);
+  const int64_t v0 = piece * kPieceVecs, end = n + t.lead;  // vectors count from the boundary before src
+  double s = 0;
+  if (v0 * V >= end) return s;
+  if (t.ld == t.cols) {
+    const T* base = src - t.lead;
+    const uint4* at = reinterpret_cast<const uint4*>(base) + v0 + threadIdx.x;
+    if (v0 * V >= t.lead && (v0 + kPieceVecs) * V <= end) {  // a whole piece
+      uint4 v[kClipInFlight];
+#pragma unroll
+      for (int j = 0; j < kClipInFlight; ++j) v[j] = __ldg(at + j * kClipThreads);
+#pragma unroll
+      for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
+      return s;
+    }
+#pragma unroll 1
+    for (int j = 0; j < kClipInFlight; ++j) {
+      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
+      if (a + V <= t.lead || a >= end) continue;
+      if (a >= t.lead && a + V <= end) {
+        s += vec_squares<DT>(__ldg(at + j * kClipThreads));
+      } else {  // a vector that belongs to the tensor only in part
+        for (int64_t i = a > t.lead ? a : t.lead; i < a + V && i < end; ++i) {
+          const double x = (double)to_float<DT>(base[i]);
+          s = fma(x, x, s);
+        }
+      }
+    }
+  } else {
+    for (int64_t i = v0 * V + threadIdx.x; i < (v0 + kPieceVecs) * V && i < n; i += kClipThreads) {
+      const double x = (double)to_float<DT>(src[strided(t, i)]);
+      s = fma(x, x, s);
+    }
+  }
+  return s;
+}
+
+template <int DT>
+__device__ __forceinline__ void piece_scale(const GradDev& t, int64_t piece, Factor f) {
+  using T = typename Elem<DT>::T;
+  constexpr int V = 16 / (int)sizeof(T);
   const int64_t n = live_elems(t);
   const T* src = reinterpret_cast<const T*>(t.src);
   T* dst = reinterpret_cast<T*>(t.dst);
@@ -163,33 +179,28 @@ __device__ void piece_scale(const GradDev& t, int64_t piece, Factor f) {
   if (t.ld == t.cols) {
     const T* from = src - t.lead;
     T* to = dst - t.lead;
+    const uint4* in = reinterpret_cast<const uint4*>(from) + v0 + threadIdx.x;
+    uint4* out = reinterpret_cast<uint4*>(to) + v0 + threadIdx.x;
     const bool same = ((reinterpret_cast<uintptr_t>(to)) & 15u) == 0;  // dst sits on its boundary as src does
-    uint4 v[kClipInFlight];
+    if (same && v0 * V >= t.lead && (v0 + kPieceVecs) * V <= end) {
 #pragma unroll
-    for (int j = 0; j < kClipInFlight; ++j) {
-      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
-      if (a >= t.lead && a + V <= end) v[j] = *reinterpret_cast<const uint4*>(from + a);
+      for (int h = 0; h < kClipInFlight; h += 4) {
+        uint4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __ldcs(in + (h + j) * kClipThreads);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) __stcs(out + (h + j) * kClipThreads, scaled16<DT>(v[j], f));
+      }
+      return;
     }
-#pragma unroll
+#pragma unroll 1
     for (int j = 0; j < kClipInFlight; ++j) {
       const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
       if (a + V <= t.lead || a >= end) continue;
-      if (a >= t.lead && a + V <= end) {
-        T x[V];
-        memcpy(x, &v[j], 16);
-#pragma unroll
-        for (int q = 0; q < V; ++q) x[q] = scaled<DT>(x[q], f);
-        if (same) {
-          uint4 r;
-          memcpy(&r, x, 16);
-          *reinterpret_cast<uint4*>(to + a) = r;
-        } else {
-#pragma unroll
-          for (int q = 0; q < V; ++q) to[a + q] = x[q];
-        }
+      if (same && a >= t.lead && a + V <= end) {
+        out[j * kClipThreads] = scaled16<DT>(in[j * kClipThreads], f);
       } else {
-        for (int64_t i = a > t.lead ? a : t.lead; i < a + V && i < end; ++i)
-          to[i] = scaled<DT>(from[i], f);
+        for (int64_t i = a > t.lead ? a : t.lead; i < a + V && i < end; ++i) to[i] = scaled<DT>(from[i], f);
       }
     }
   } else {
@@ -201,7 +212,7 @@ __device__ void piece_scale(const GradDev& t, int64_t piece, Factor f) {
 }
 
 template <int N>
-__global__ void __launch_bounds__(kClipThreads) grad_squares_kernel(const __grid_constant__ GradParams<N> p) {
+__global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) grad_squares_kernel(const __grid_constant__ GradParams<N> p) {
   __shared__ double shared[kClipThreads / 32];
   double s = 0;
   for (int64_t k = blockIdx.x; k < p.pieces; k += gridDim.x) {
@@ -217,7 +228,7 @@ __global__ void __launch_bounds__(kClipThreads) grad_squares_kernel(const __grid
 }
 
 template <int N>
-__global__ void __launch_bounds__(kClipThreads) grad_scale_kernel(const __grid_constant__ GradParams<N> p) {
+__global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) grad_scale_kernel(const __grid_constant__ GradParams<N> p) {
   __shared__ double shared[kClipThreads / 32];
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the sums of the launch before this one
   double s = 0;

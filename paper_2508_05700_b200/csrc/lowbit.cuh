@@ -1,5 +1,5 @@
-// The element formats that the row and matrix kernels share: conversion of 8 neighbouring values to and
-// from MXFP4 and INT4 codes, and loads / stores of 8 values of an fp32, fp16 or bf16 array.
+// The element formats that the row, matrix and clipping kernels share: MXFP4 scales and codes, and loads, conversions
+// and stores of a few neighbouring values of an fp32, fp16 or bf16 array.
 //
 // MXFP4: 32 neighbouring values of a row are a block with one scale 2^(b - 127), stored as the byte b. With
 // amax the block's largest magnitude, b - 127 = floor(log2(amax)) - 2, not below -127; since amax = 1.f * 2^(E - 127)
@@ -65,76 +65,135 @@ struct Elem;
 template <>
 struct Elem<MFET_F32> {
   using T = float;
-  static __device__ __forceinline__ float to(T x) { return x; }
   static __device__ __forceinline__ T from(float x) { return x; }
 };
 template <>
 struct Elem<MFET_F16> {
   using T = __half;
-  static __device__ __forceinline__ float to(T x) { return __half2float(x); }
   static __device__ __forceinline__ T from(float x) { return __float2half_rn(x); }
+  static __device__ __forceinline__ float2 widen(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
 };
 template <>
 struct Elem<MFET_BF16> {
   using T = __nv_bfloat16;
-  static __device__ __forceinline__ float to(T x) { return __bfloat162float(x); }
   static __device__ __forceinline__ T from(float x) { return __float2bfloat16_rn(x); }
-};
-
-// Eight neighbouring values as they lie in memory: 16 bytes of a 16-bit type, 32 bytes of fp32.
-template <int DT>
-struct Raw8 {
-  static constexpr int words = DT == MFET_F32 ? 2 : 1;
-  uint4 w[words];
-};
-
-// The first `count` (<= 8) values at p, the rest 0. VEC: p is 16-byte aligned and full chunks are read in 16-byte pieces.
-// The values are read once, so they are kept out of L1.
-template <int DT, bool VEC>
-__device__ __forceinline__ Raw8<DT> load8(const typename Elem<DT>::T* p, int count) {
-  Raw8<DT> r;
-  if (VEC && count == 8) {
-#pragma unroll
-    for (int i = 0; i < Raw8<DT>::words; ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-    return r;
+  static __device__ __forceinline__ float2 widen(uint32_t w) { return make_float2(bf16lo(w), bf16hi(w)); }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
   }
-  typename Elem<DT>::T t[8];
+};
+
+template <int DT>
+__device__ __forceinline__ float to_float(typename Elem<DT>::T x) {
+  if constexpr (DT == MFET_F32) return x;
+  else if constexpr (DT == MFET_F16) return __half2float(x);
+  else return __bfloat162float(x);
+}
+
+// E neighbouring values as they lie in memory
+template <int DT, int E>
+struct Raw {
+  static constexpr int bytes = E * (int)sizeof(typename Elem<DT>::T);
+  static constexpr int pieces = bytes / 16, per = 16 / (int)sizeof(typename Elem<DT>::T);
+  uint4 w[pieces];
+};
+
+// The first `count` values at p, the rest 0. VEC: p is 16-byte aligned, and whole pieces of 16 bytes are read as such. The values
+// are read once: they do not displace anything in the caches.
+template <int DT, int E, bool VEC>
+__device__ __forceinline__ Raw<DT, E> load_raw(const typename Elem<DT>::T* p, int count) {
+  using R = Raw<DT, E>;
+  R r;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) t[j] = j < count ? p[j] : Elem<DT>::from(0.f);
-  memcpy(&r, t, sizeof(t));
+  for (int i = 0; i < R::pieces; ++i) {
+    if (VEC && count >= (i + 1) * R::per) {
+      r.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    } else {
+      typename Elem<DT>::T t[R::per];
+#pragma unroll
+      for (int j = 0; j < R::per; ++j) t[j] = i * R::per + j < count ? p[i * R::per + j] : Elem<DT>::from(0.f);
+      memcpy(&r.w[i], t, 16);
+    }
+  }
   return r;
 }
 
+// the values of 16 bytes
 template <int DT>
-__device__ __forceinline__ void widen8(const Raw8<DT>& r, float* v) {
-  typename Elem<DT>::T t[8];
-  memcpy(t, &r, sizeof(t));
+__device__ __forceinline__ void widen16(const uint4& w, float* v) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = Elem<DT>::to(t[j]);
-}
-
-template <int DT, bool VEC>
-__device__ __forceinline__ void store8(typename Elem<DT>::T* p, const float* v, int count) {
-  typename Elem<DT>::T t[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) t[j] = Elem<DT>::from(v[j]);
-  if (VEC && count == 8) {
-    Raw8<DT> r;
-    memcpy(&r, t, sizeof(t));
-#pragma unroll
-    for (int i = 0; i < Raw8<DT>::words; ++i) reinterpret_cast<uint4*>(p)[i] = r.w[i];
-    return;
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (DT == MFET_F32) {
+      v[j] = __uint_as_float(x[j]);
+    } else {
+      const float2 f = Elem<DT>::widen(x[j]);
+      v[2 * j] = f.x;
+      v[2 * j + 1] = f.y;
+    }
   }
+}
+template <int DT>
+__device__ __forceinline__ uint4 narrow16(const float* v) {
+  uint32_t x[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < count) p[j] = t[j];
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (DT == MFET_F32) x[j] = __float_as_uint(v[j]);
+    else x[j] = Elem<DT>::pack(v[2 * j], v[2 * j + 1]);
+  }
+  return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
-__device__ __forceinline__ uint32_t amax8(const float* v) {
-  uint32_t m = 0;
+template <int DT, int E>
+__device__ __forceinline__ void widen_raw(const Raw<DT, E>& r, float* v) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);  // a NaN's bits are above infinity's
-  return m;
+  for (int i = 0; i < Raw<DT, E>::pieces; ++i) widen16<DT>(r.w[i], v + i * Raw<DT, E>::per);
+}
+
+template <int DT, int E, bool VEC>
+__device__ __forceinline__ void store_values(typename Elem<DT>::T* p, const float* v, int count) {
+  using R = Raw<DT, E>;
+#pragma unroll
+  for (int i = 0; i < R::pieces; ++i) {
+    if (VEC && count >= (i + 1) * R::per) {
+      reinterpret_cast<uint4*>(p)[i] = narrow16<DT>(v + i * R::per);
+    } else {
+#pragma unroll
+      for (int j = 0; j < R::per; ++j)
+        if (i * R::per + j < count) p[i * R::per + j] = Elem<DT>::from(v[i * R::per + j]);
+    }
+  }
+}
+
+// Bits of the largest magnitude as fp32; above infinity's when there is a NaN among the values. 16-bit values are
+// compared as integers two at a time, which orders magnitudes, infinity and NaN alike.
+template <int DT, int E>
+__device__ __forceinline__ uint32_t amax_raw(const Raw<DT, E>& r) {
+  if constexpr (DT == MFET_F32) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < Raw<DT, E>::pieces; ++i) {
+      const uint32_t x[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(fabsf(__uint_as_float(x[j]))));
+    }
+    return __float_as_uint(m);
+  } else {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < Raw<DT, E>::pieces; ++i) {
+      const uint32_t x[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(x[j] & 0x7FFF7FFFu));
+    }
+    const float2 f = Elem<DT>::widen(max(m >> 16, m & 0xFFFFu));
+    return __float_as_uint(f.x);
+  }
 }
 
 }  // namespace mfet

@@ -9,7 +9,7 @@
 //
 // Two kernels for the product. A few rows (mx4_few_kernel): the weights are read once and nothing else costs bandwidth,
 // so a warp per output column and integer dot products suffice, and x is quantised in the same launch. More rows
-// (mx4_gemm_kernel): block-scaled 5th-generation tensor-core instructions with the weights as the 128-row operand.
+// (mx4_gemm_kernel): block-scaled 5th-generation tensor-core instructions.
 #include <cuda.h>
 
 #include <atomic>
@@ -27,7 +27,7 @@ constexpr unsigned kAll = 0xFFFFFFFFu;
 // ------------------------------------------------------------------ quantisation ----
 
 constexpr int kQuantThreads = 256;
-constexpr int kQuantInFlight = 4;  // pieces of 128 values that a half-warp requests together
+constexpr int kQuantInFlight = 4;  // loads of 32 bytes that a lane requests together
 
 struct QuantParams {
   const uint8_t* x;
@@ -39,45 +39,53 @@ struct QuantParams {
   uint8_t* scales;
 };
 
-// A half-warp takes one row's 128 values (4 blocks): 8 values per lane, 4 lanes per block, 64 bytes of codes, and the four
-// scale bytes as one word. Bound by reading x.
+// A lane takes 32 bytes of x (8 fp32 or 16 16-bit values), and the lanes of 128 values (4 blocks) write 64 bytes of codes and the
+// four scale bytes as one word. Bound by reading x.
 template <int DT, bool VEC>
-__global__ void __launch_bounds__(kQuantThreads) mx4_quantize_kernel(const __grid_constant__ QuantParams p) {
+__global__ void __launch_bounds__(kQuantThreads, 4) mx4_quantize_kernel(const __grid_constant__ QuantParams p) {
   using T = typename Elem<DT>::T;
+  constexpr int E = 32 / (int)sizeof(T), LPB = kMxBlock / E, LPU = 4 * LPB;  // values per lane, lanes per block and per 128 values
+  constexpr int U = kQuantInFlight;
   asm volatile("griddepcontrol.launch_dependents;");  // the product may set itself up; it waits for this grid's end
-  const int lane = threadIdx.x & 31, sub = lane & 15;
+  const int lane = threadIdx.x & 31, sub = lane % LPU;
   const int64_t warp = ((int64_t)blockIdx.x * kQuantThreads + threadIdx.x) >> 5;
-  const int64_t step = (int64_t)gridDim.x * (kQuantThreads / 32) * 2 * kQuantInFlight;
-  for (int64_t u0 = warp * 2 * kQuantInFlight; u0 < p.units; u0 += step) {
-    Raw8<DT> raw[kQuantInFlight];
-    int64_t row[kQuantInFlight];
-    uint32_t group[kQuantInFlight];
-    int count[kQuantInFlight];
+  const int64_t step = (int64_t)gridDim.x * (kQuantThreads / 32) * (32 / LPU) * U;
+  for (int64_t u0 = warp * (32 / LPU) * U; u0 < p.units; u0 += step) {
+    Raw<DT, E> raw[U];
+    int64_t row[U];
+    uint32_t group[U];
 #pragma unroll
-    for (int u = 0; u < kQuantInFlight; ++u) {
-      const int64_t i = u0 + 2 * u + (lane >> 4);
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = u0 + u * (32 / LPU) + lane / LPU;
       row[u] = (uint64_t)i >> 32 ? i / p.groups : (int64_t)((uint32_t)i / p.groups);
       group[u] = (uint32_t)(i - row[u] * p.groups);
-      const uint32_t at = group[u] * 128 + sub * 8;
-      count[u] = i < p.units && at < p.k ? (int)min(8u, p.k - at) : 0;
-      if (count[u] > 0) raw[u] = load8<DT, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count[u]);
+      const uint32_t at = group[u] * 128 + sub * E;
+      const int count = i < p.units && at < p.k ? (int)min((uint32_t)E, p.k - at) : 0;
+      if (count > 0) raw[u] = load_raw<DT, E, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count);
+      else memset(&raw[u], 0, sizeof(raw[u]));
     }
 #pragma unroll
-    for (int u = 0; u < kQuantInFlight; ++u) {
-      float v[8] = {};
-      if (count[u] > 0) widen8<DT>(raw[u], v);
-      uint32_t m = amax8(v);
-      m = max(m, __shfl_xor_sync(kAll, m, 1));
-      m = max(m, __shfl_xor_sync(kAll, m, 2));
-      const uint32_t b = mx_scale_byte(m);
-      uint32_t word = 0;
+    for (int u = 0; u < U; ++u) {
+      uint32_t m = amax_raw<DT, E>(raw[u]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) word |= __shfl_sync(kAll, b, (lane & 16) + 4 * j) << (8 * j);
-      if (u0 + 2 * u + (lane >> 4) < p.units) {
-        const uint32_t c = group[u] * 16 + sub;  // chunk of 8 values within the row
-        if (c < p.blocks * 4)
-          *reinterpret_cast<uint32_t*>(p.codes + row[u] * ((int64_t)p.blocks * 16) + c * 4) =
-              b == kMxNan ? 0u : mx_encode8(v, mx_inv_scale(b));
+      for (int d = 1; d < LPB; d <<= 1) m = max(m, __shfl_xor_sync(kAll, m, d));
+      const uint32_t b = mx_scale_byte(m);
+      uint32_t word = b << (8 * (sub / LPB));
+      word |= __shfl_xor_sync(kAll, word, LPB);
+      word |= __shfl_xor_sync(kAll, word, 2 * LPB);
+      float v[E];
+      widen_raw<DT, E>(raw[u], v);
+      const float inv = b == kMxNan ? 0.f : mx_inv_scale(b);
+      uint32_t codes[E / 8];
+#pragma unroll
+      for (int j = 0; j < E / 8; ++j) codes[j] = b == kMxNan ? 0u : mx_encode8(v + 8 * j, inv);
+      if (u0 + u * (32 / LPU) + lane / LPU < p.units) {
+        const uint32_t c = group[u] * LPU + sub;
+        if (c < p.blocks * LPB) {
+          uint8_t* dst = p.codes + row[u] * ((int64_t)p.blocks * 16) + c * (E / 2);
+          if constexpr (E == 16) *reinterpret_cast<uint2*>(dst) = make_uint2(codes[0], codes[E / 8 - 1]);
+          else *reinterpret_cast<uint32_t*>(dst) = codes[0];
+        }
         if (sub == 0)
           *reinterpret_cast<uint32_t*>(p.scales + ((row[u] >> 7) * p.groups + group[u]) * 512 + (row[u] & 31) * 16 +
                                        ((row[u] & 127) >> 5) * 4) = word;
@@ -147,13 +155,13 @@ __device__ __forceinline__ void few_stage(const FewParams& p, int mt, int4* sx, 
   for (uint32_t i = threadIdx.x; i < units; i += kFewThreads) {
     const uint32_t row = i / (padded * 4), c = i - row * padded * 4, b = c >> 2;
     const int count = (int)row < p.m && c * 8 < p.k ? (int)min(8u, p.k - c * 8) : 0;
-    float v[8] = {};
-    if (count > 0) {
-      const T* at = reinterpret_cast<const T*>(p.x) + (int64_t)row * p.ld + c * 8;
-      const Raw8<DT> raw = p.vec ? load8<DT, true>(at, count) : load8<DT, false>(at, count);
-      widen8<DT>(raw, v);
-    }
-    uint32_t m = amax8(v);
+    Raw<DT, 8> raw;
+    const T* at = reinterpret_cast<const T*>(p.x) + (int64_t)row * p.ld + c * 8;
+    if (count > 0) raw = p.vec ? load_raw<DT, 8, true>(at, count) : load_raw<DT, 8, false>(at, count);
+    else memset(&raw, 0, sizeof(raw));
+    float v[8];
+    widen_raw<DT, 8>(raw, v);
+    uint32_t m = amax_raw<DT, 8>(raw);
     m = max(m, __shfl_xor_sync(kAll, m, 1));
     m = max(m, __shfl_xor_sync(kAll, m, 2));
     const uint32_t s = mx_scale_byte(m);
@@ -234,33 +242,62 @@ __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_const
 // ------------------------------------------------------------------ tensor cores ----
 
 constexpr int kGemmThreads = 192;  // warp 0 loads, warp 1 issues the products, warps 2..5 write results
-constexpr int kTileN = 128;        // weights' rows (output columns) per tile: lanes of tensor memory
+constexpr int kTileM = 128;        // rows of x per tile: lanes of tensor memory
 constexpr int kSlab = 256;         // k per stage: 128 bytes of codes per row, four instructions of k = 64
 constexpr uint64_t kStallNs = 2000000000ull;
 
-template <int TM>  // rows of x per tile: columns of tensor memory
+template <int TN>  // output columns per tile
 struct GemmShape {
-  static constexpr uint32_t a_bytes = kTileN * 128, b_bytes = TM * 128, s_bytes = 1024;  // 2 scale tiles of 512 bytes
+  static constexpr uint32_t a_bytes = kTileM * 128, b_bytes = TN * 128, s_bytes = 1024;  // 2 scale tiles of 512 bytes
   static constexpr uint32_t stage_bytes = a_bytes + b_bytes + 2 * s_bytes;
-  static constexpr int stages = 6;
-  static constexpr uint32_t smem = stage_bytes * stages + 1024;  // + room to align to 1024
-  static constexpr uint32_t acc_cols = TM;                       // two accumulators, then 16 columns of scales per stage
-  static constexpr uint32_t scale_col = 2 * TM;
+  static constexpr int stages = TN == 128 ? 5 : 6;
+  static constexpr uint32_t out_at = stage_bytes * stages;                    // two pieces of 32 rows x 128 bytes per warp
+  static constexpr uint32_t bias_at = out_at + 4 * 2 * 4096;
+  static constexpr uint32_t smem = bias_at + 4 * TN * 4 + 1024;  // + room to align to 1024
+  static constexpr uint32_t acc_cols = TN;                       // two accumulators, then 16 columns of scales per stage
+  static constexpr uint32_t scale_col = 2 * TN;
   static_assert(scale_col + 16 * stages <= 512, "tensor memory has 512 columns");
 };
 
 struct GemmParams {
-  const uint8_t* a_scales;  // weights
-  const uint8_t* b_scales;  // x
+  const uint8_t* a_scales;  // x
+  const uint8_t* b_scales;  // weights
   int64_t m, n;
   uint32_t k, groups, slabs;
   uint32_t n_tiles;
+  uint32_t bulk_y;          // y can be written by bulk copies (16-byte aligned rows)
   int64_t tiles;
   uint32_t* status;
   OutParams out;
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// True in one lane of a converged warp. Instructions of the tensor cores and the copy engine take their operands from uniform
+// registers; under a branch on this the compiler knows that one lane runs and moves them there directly (under `lane == 0`
+// each such instruction took 110 cycles to issue).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+// The tiles of a block, one after the other: column tiles run fastest
+struct TileWalk {
+  int64_t t;
+  uint32_t tm, tn, n_tiles, dm, dn;
+  __device__ __forceinline__ explicit TileWalk(uint32_t n_tiles_) : t(blockIdx.x), n_tiles(n_tiles_) {
+    tm = blockIdx.x / n_tiles;
+    tn = blockIdx.x - tm * n_tiles;
+    dm = gridDim.x / n_tiles;
+    dn = gridDim.x - dm * n_tiles;
+  }
+  __device__ __forceinline__ void next() {
+    t += gridDim.x;
+    tm += dm;
+    tn += dn;
+    if (tn >= n_tiles) tn -= n_tiles, ++tm;
+  }
+};
 
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -286,15 +323,17 @@ __device__ __forceinline__ uint64_t now_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// Waits for the phase `parity` of a barrier, two seconds at most; false: it did not come (or another role gave up)
-__device__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  if (bar_try(bar, parity)) return true;
-  const uint64_t t0 = now_ns();
-  for (uint32_t i = 0;; ++i) {
+// Waits for the phase `parity` of a barrier, two seconds at most; false: it did not come (or another role gave up). The
+// clock is not read before a wait has failed often: reading it takes longer than most waits.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 1;; ++i) {
     if (bar_try(bar, parity)) return true;
-    if ((i & 63) == 63) {
+    if ((i & 255) == 0) {
       if (*dead) return false;
-      if (now_ns() - t0 > kStallNs) {
+      const uint64_t t = now_ns();
+      if (t0 == 0) t0 = t;
+      if (t - t0 > kStallNs) {
         *dead = 1;
         return false;
       }
@@ -313,6 +352,11 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
+__device__ __forceinline__ void bulk_store(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
+               : "memory");
+}
+
 // Shared-memory matrix descriptor, K-major rows of 128 bytes with the 128-byte swizzle: groups of 8 rows are 1024 bytes apart
 __device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
   return (uint64_t)((addr >> 4) & 0x3FFF) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
@@ -323,9 +367,9 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
 }
 // Instruction descriptor: both operands E2M1, K-major, scales UE8M0, fp32 accumulator; `id`: which two of a row's four scale
 // bytes (0 or 2) this instruction's two blocks use
-template <int TM>
+template <int TN>
 __device__ __forceinline__ uint32_t inst_desc(uint32_t id) {
-  return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TM >> 3) << 17) | (1u << 23) | ((uint32_t)(kTileN >> 7) << 27) | (id << 29);
+  return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TN >> 3) << 17) | (1u << 23) | ((uint32_t)(kTileM >> 7) << 27) | (id << 29);
 }
 
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
@@ -355,20 +399,26 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
       : "memory");
 }
 
-// One block per SM walks over the tiles (128 output columns x TM rows of x); output columns run fastest, so that the blocks at
-// work share the rows of x in L2. Stages of k = 256 go through a ring of shared memory; two accumulators in tensor memory, so
-// that a tile is written while the next one is computed. The weights are the 128-row operand: a lane of tensor memory is an
-// output column, and the 32 lanes of a warp write 32 neighbouring values of one row of y.
-template <int TM>
+// One block per SM walks over the tiles (128 rows of x times TN output columns); output columns run fastest, so that the blocks
+// at work share the rows of x in L2. Stages of k = 256 go through a ring of shared memory, scales from there to tensor memory ahead
+// of the products that use them; two accumulators in tensor memory, so that a tile is written while the next one is computed. A
+// lane of tensor memory is a row of x: each of the four writing warps takes its 32 rows in pieces of 128 bytes, adds the bias, rounds, and
+// leaves the piece in shared memory (128-byte swizzle: a lane writes 16 bytes of its own row without bank conflicts), from where
+// one bulk copy writes 32 rows and clips what lies beyond y; a y whose rows do not start on 16 bytes is written by plain
+// stores from there.
+template <int TN, int DT>
 __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap a_map,
                                                                   const __grid_constant__ CUtensorMap b_map,
+                                                                  const __grid_constant__ CUtensorMap y_map,
                                                                   const __grid_constant__ GemmParams p) {
-  using G = GemmShape<TM>;
+  using G = GemmShape<TN>;
+  using T = typename Elem<DT>::T;
   extern __shared__ uint8_t raw_smem[];
   __shared__ __align__(8) uint64_t bars[2 * G::stages + 5];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int dead;
   const uint32_t base = (smem_addr(raw_smem) + 1023) & ~1023u;
+  uint8_t* const smem = raw_smem + (base - smem_addr(raw_smem));
   const uint32_t bar0 = smem_addr(bars);
   auto full = [&](int s) { return bar0 + 8 * s; };
   auto empty = [&](int s) { return bar0 + 8 * (G::stages + s); };
@@ -397,94 +447,147 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
   asm volatile("griddepcontrol.wait;" ::: "memory");  // x may be the result of the launch before this one
 
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t it = 0;  // stages filled so far
-      bool ok = true;
-      for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-        const int64_t tm = t / p.n_tiles, tn = t - tm * p.n_tiles;
-        const uint8_t* sa = p.a_scales + (size_t)tn * p.groups * 512;
-        const uint8_t* sb = p.b_scales + (size_t)(tm * TM >> 7) * p.groups * 512;
-        for (uint32_t s = 0; s < p.slabs; ++s, ++it) {
-          const int st = it % G::stages;
-          if (it >= G::stages && !(ok = bar_wait(empty(st), (it / G::stages - 1) & 1, &dead))) break;
+    uint32_t it = 0;  // stages filled so far
+    bool ok = true;
+    for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next()) {
+      const uint8_t* sa = p.a_scales + (size_t)w.tm * p.groups * 512;
+      const uint8_t* sb = p.b_scales + (size_t)(w.tn * (uint32_t)TN >> 7) * p.groups * 512;
+      for (uint32_t s = 0; s < p.slabs; ++s, ++it) {
+        const int st = it % G::stages;
+        if (it >= G::stages && !(ok = __all_sync(kAll, bar_wait(empty(st), (it / G::stages - 1) & 1, &dead)))) break;
+        if (elect_one()) {
           const uint32_t at = base + st * G::stage_bytes;
           const uint32_t sc = min(2u, p.groups - 2 * s) * 512;  // scale bytes of this slab, per operand
           bar_expect(full(st), G::a_bytes + G::b_bytes + 2 * sc);
-          tma_load(at, &a_map, (int32_t)(s * 128), (int32_t)(tn * kTileN), full(st));
-          tma_load(at + G::a_bytes, &b_map, (int32_t)(s * 128), (int32_t)(tm * TM), full(st));
+          tma_load(at, &a_map, (int32_t)(s * 128), (int32_t)(w.tm * kTileM), full(st));
+          tma_load(at + G::a_bytes, &b_map, (int32_t)(s * 128), (int32_t)(w.tn * TN), full(st));
           bulk_load(at + G::a_bytes + G::b_bytes, sa + (size_t)s * 1024, sc, full(st));
           bulk_load(at + G::a_bytes + G::b_bytes + G::s_bytes, sb + (size_t)s * 1024, sc, full(st));
         }
+        __syncwarp();
       }
-      // Every copy that this thread started has to land before the block ends. The products wait for each of them; only
-      // when a wait has run out are they waited for here.
-      if (!ok || dead) {
-        volatile int none = 0;
-        const uint32_t from = it > G::stages ? it - G::stages : 0;
-        for (uint32_t i = from; i < it; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
-      }
+    }
+    // Every copy that this warp started has to land before the block ends. The products wait for each of them; only
+    // when a wait has run out are they waited for here.
+    if (!ok || dead) {
+      volatile int none = 0;
+      const uint32_t from = it > G::stages ? it - G::stages : 0;
+      for (uint32_t i = from; i < it; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t it = 0, done = 0;
-      bool ok = true;
-      for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x, ++done) {
-        const int acc = done & 1;
-        if (done >= 2 && !(ok = bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead))) break;
+    uint32_t it = 0, done = 0;
+    bool ok = true;
+    for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next(), ++done) {
+      const int acc = done & 1;
+      if (done >= 2 && !(ok = __all_sync(kAll, bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead)))) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t d = tmem + acc * G::acc_cols;
+      // a tile of 64 columns that starts in the middle of a scale tile uses the upper half of its four columns
+      const uint32_t half = TN == 64 ? (w.tn & 1) * 2 : 0;
+      for (uint32_t s = 0; s < p.slabs; ++s, ++it) {
+        const int st = it % G::stages;
+        if (!(ok = __all_sync(kAll, bar_wait(full(st), (it / G::stages) & 1, &dead)))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + acc * G::acc_cols;
-        for (uint32_t s = 0; s < p.slabs; ++s, ++it) {
-          const int st = it % G::stages;
-          if (!(ok = bar_wait(full(st), (it / G::stages) & 1, &dead))) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t at = base + st * G::stage_bytes, sc = at + G::a_bytes + G::b_bytes;
-          const uint32_t sfa = tmem + G::scale_col + 16 * st, sfb = sfa + 8;
-          const uint32_t left = p.k - s * kSlab;
-          const int steps = left >= (uint32_t)kSlab ? 4 : (int)((left + 63) / 64);
-          const int pairs = (steps + 1) / 2;
-          for (int g = 0; g < pairs; ++g) {
-            copy_scales(sfa + 4 * g, scale_desc(sc + 512 * g));
-            copy_scales(sfb + 4 * g, scale_desc(sc + G::s_bytes + 512 * g));
-          }
-          for (int j = 0; j < steps; ++j)
-            mma_mx4(d, tile_desc(at + 32 * j), tile_desc(at + G::a_bytes + 32 * j), inst_desc<TM>((j & 1) * 2), sfa + 4 * (j >> 1),
-                    sfb + 4 * (j >> 1), s > 0 || j > 0);
+        const uint32_t at = base + st * G::stage_bytes, sc = at + G::a_bytes + G::b_bytes;
+        const uint32_t sfa = tmem + G::scale_col + 16 * st, sfb = sfa + 8;
+        const uint32_t left = p.k - s * kSlab;
+        const int steps = left >= (uint32_t)kSlab ? 4 : (int)((left + 63) / 64);
+        if (elect_one()) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+            if (2 * g < steps) {
+              copy_scales(sfa + 4 * g, scale_desc(sc + 512 * g));
+              copy_scales(sfb + 4 * g, scale_desc(sc + G::s_bytes + 512 * g));
+            }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (j < steps)
+              mma_mx4(d, tile_desc(at + 32 * j), tile_desc(at + G::a_bytes + 32 * j), inst_desc<TN>((j & 1) * 2), sfa + 4 * (j >> 1),
+                      sfb + 4 * (j >> 1) + half, s > 0 || j > 0);
           mma_commit(empty(st));
+          if (s + 1 == p.slabs) mma_commit(acc_full(acc));
         }
-        if (ok) mma_commit(acc_full(acc));
-      }
-      if (!ok || dead) {  // the products under way read shared memory and write tensor memory: let them end
-        volatile int none = 0;
-        mma_commit(drained);
-        bar_wait(drained, 0, &none);
+        __syncwarp();
       }
     }
+    if (!ok || dead) {  // the products under way read shared memory and write tensor memory: let them end
+      volatile int none = 0;
+      if (elect_one()) mma_commit(drained);
+      __syncwarp();
+      bar_wait(drained, 0, &none);
+    }
   } else {
-    const int quarter = warp & 3;  // the 32 lanes of tensor memory that this warp may read
-    uint32_t done = 0;
-    for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x, ++done) {
+    constexpr int kCols = 128 / (int)sizeof(T);  // output columns of a piece
+    const int quarter = warp & 3;                // the 32 lanes of tensor memory that this warp may read
+    const uint32_t out0 = base + G::out_at + quarter * 8192;
+    uint8_t* const out_ptr = smem + G::out_at + quarter * 8192;
+    float* const bias = reinterpret_cast<float*>(smem + G::bias_at) + quarter * TN;
+    uint32_t done = 0, pieces = 0;
+    for (TileWalk w(p.n_tiles); w.t < p.tiles; w.next(), ++done) {
       const int acc = done & 1;
+      const int64_t i0 = (int64_t)w.tm * kTileM + quarter * 32, j0 = (int64_t)w.tn * TN;
+      for (int c = lane; c < TN; c += 32) bias[c] = p.out.bias && j0 + c < p.n ? p.out.bias[j0 + c] : 0.f;
+      __syncwarp();
       const bool ok = bar_wait(acc_full(acc), (done / 2) & 1, &dead);
       if (!__all_sync(kAll, ok)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int64_t tm = t / p.n_tiles, tn = t - tm * p.n_tiles;
-      const int64_t j = tn * kTileN + quarter * 32 + lane, i0 = tm * TM;
-      const bool in = j < p.n;
-      const float bias = in && p.out.bias ? p.out.bias[j] : 0.f;
 #pragma unroll 1
-      for (int c = 0; c < TM; c += 32) {
-        uint32_t r[32];
-        tmem_load32(tmem + acc * G::acc_cols + c + ((uint32_t)(quarter * 32) << 16), r);
-        if (c + 32 >= TM) {  // the accumulator is read: the next tile but one may overwrite it
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) bar_arrive(acc_empty(acc));
-        }
+      for (int c = 0; c < TN; c += kCols, ++pieces) {
+        const uint32_t buf = (pieces & 1) * 4096;
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // the piece before the last has left its half
+        __syncwarp();
 #pragma unroll
-        for (int q = 0; q < 32; ++q)
-          if (in && i0 + c + q < p.m) put(p.out, i0 + c + q, j, activate(__uint_as_float(r[q]), bias, p.out.relu));
+        for (int h = 0; h < kCols; h += 32) {
+          uint32_t r[32];
+          tmem_load32(tmem + acc * G::acc_cols + c + h + ((uint32_t)(quarter * 32) << 16), r);
+          if (c + h + 32 >= TN) {  // the accumulator is read: the next tile but one may overwrite it
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(acc_empty(acc));
+          }
+          float v[32];
+#pragma unroll
+          for (int q = 0; q < 32; q += 4) {
+            const float4 b4 = *reinterpret_cast<const float4*>(bias + c + h + q);
+            v[q] = activate(__uint_as_float(r[q]), b4.x, p.out.relu);
+            v[q + 1] = activate(__uint_as_float(r[q + 1]), b4.y, p.out.relu);
+            v[q + 2] = activate(__uint_as_float(r[q + 2]), b4.z, p.out.relu);
+            v[q + 3] = activate(__uint_as_float(r[q + 3]), b4.w, p.out.relu);
+          }
+          constexpr int kPer = 16 / (int)sizeof(T);  // values per 16 bytes
+#pragma unroll
+          for (int q = 0; q < 32; q += kPer) {
+            const uint4 w = narrow16<DT>(v + q);
+            const int sixteen = (h + q) / kPer;  // which 16 bytes of the row's 128
+            *reinterpret_cast<uint4*>(out_ptr + buf + lane * 128 + ((sixteen ^ (lane & 7)) << 4)) = w;
+          }
+        }
+        if (p.bulk_y) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (i0 < p.m && j0 + c < p.n && elect_one()) bulk_store(&y_map, out0 + buf, (int32_t)(j0 + c), (int32_t)i0);
+          __syncwarp();
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");  // a group of its own in the lane that stored, empty ones elsewhere
+        } else {
+          __syncwarp();
+          T* y = reinterpret_cast<T*>(p.out.y);
+          constexpr int kOwn = 4 / (int)sizeof(T);  // values per lane and row
+          const int64_t j = j0 + c + lane * kOwn;
+#pragma unroll 4
+          for (int i = 0; i < 32; ++i) {
+            T two[kOwn];
+            memcpy(two, out_ptr + buf + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4, 4);
+            if (i0 + i < p.m) {
+#pragma unroll
+              for (int q = 0; q < kOwn; ++q)
+                if (j + q < p.n) y[(i0 + i) * p.out.ld + j + q] = two[q];
+            }
+          }
+          __syncwarp();
+        }
       }
     }
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // shared memory outlives the copies that read it
   }
   __syncwarp();  // the one lane that loaded or issued rejoins its warp
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -511,7 +614,8 @@ uint32_t size_of(uint32_t dtype) { return dtype == MFET_F32 ? 4 : 2; }
 
 template <int DT>
 cudaError_t launch_quantize(const QuantParams& p, bool vec, cudaStream_t s) {
-  const int64_t per_block = (int64_t)(kQuantThreads / 32) * 2 * kQuantInFlight;
+  constexpr int kLanesPerUnit = 4 * (int)sizeof(typename Elem<DT>::T);  // 128 values, 32 bytes per lane
+  const int64_t per_block = (int64_t)(kQuantThreads / kLanesPerUnit) * kQuantInFlight;
   const int64_t want = (p.units + per_block - 1) / per_block, most = (int64_t)sm_count() * 16;
   const unsigned b = (unsigned)(want < most ? want : most);
   if (vec) mx4_quantize_kernel<DT, true><<<b, kQuantThreads, 0, s>>>(p);
@@ -561,30 +665,51 @@ bool code_map(CUtensorMap* map, const void* codes, int64_t rows, uint32_t blocks
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int TM>
+// y [m, n] written in boxes of 32 rows x 128 bytes
+bool out_map(CUtensorMap* map, const OutParams& o, int64_t m, int64_t n) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const uint32_t size = size_of(o.dtype);
+  const cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)m}, stride[1] = {(cuuint64_t)o.ld * size};
+  const cuuint32_t boxes[2] = {128 / size, 32}, ones[2] = {1, 1};
+  const CUtensorMapDataType t = o.dtype == MFET_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                : o.dtype == MFET_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                      : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return f(map, t, 2, o.y, dims, stride, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int TN, int DT>
 int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
          uint32_t* status, bool after_quantize, cudaStream_t s) {
   const Dims d = dims_of(k);
-  CUtensorMap a, b;
-  if (!code_map(&a, wc, n, d.blocks, kTileN) || !code_map(&b, xc, m, d.blocks, TM)) return MFET_ERR_CUDA;
+  CUtensorMap a, b, y;
+  if (!code_map(&a, xc, m, d.blocks, kTileM) || !code_map(&b, wc, n, d.blocks, TN)) return MFET_ERR_CUDA;
   GemmParams p;
-  p.a_scales = (const uint8_t*)ws;
-  p.b_scales = (const uint8_t*)xs;
+  p.a_scales = (const uint8_t*)xs;
+  p.b_scales = (const uint8_t*)ws;
   p.m = m;
   p.n = n;
   p.k = (uint32_t)k;
   p.groups = d.groups;
   p.slabs = (uint32_t)((k + kSlab - 1) / kSlab);
-  p.n_tiles = (uint32_t)((n + kTileN - 1) / kTileN);
-  p.tiles = (m + TM - 1) / TM * p.n_tiles;
+  p.n_tiles = (uint32_t)((n + TN - 1) / TN);
+  p.tiles = (m + kTileM - 1) / kTileM * p.n_tiles;
   p.status = status;
   p.out = out;
+  p.bulk_y = aligned(out.y, 16) && (uint64_t)out.ld * size_of(out.dtype) % 16 == 0;
+  if (p.bulk_y) {
+    if (!out_map(&y, out, m, n)) return MFET_ERR_CUDA;
+  } else {
+    y = a;  // not used
+  }
   static std::atomic<uint64_t> ready{0};  // one bit per GPU: the kernel may use this much shared memory there
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return MFET_ERR_CUDA;
   const uint64_t bit = dev < 64 ? 1ull << dev : 0;
   if (!(ready.load(std::memory_order_relaxed) & bit)) {
-    if (cudaFuncSetAttribute(mx4_gemm_kernel<TM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GemmShape<TM>::smem) != cudaSuccess)
+    if (cudaFuncSetAttribute(mx4_gemm_kernel<TN, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GemmShape<TN>::smem) !=
+        cudaSuccess)
       return MFET_ERR_CUDA;
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
@@ -594,18 +719,29 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   cudaLaunchConfig_t cfg{};
   cfg.blockDim = dim3(kGemmThreads);
   cfg.gridDim = dim3((unsigned)(p.tiles < sm_count() ? p.tiles : sm_count()));
-  cfg.dynamicSmemBytes = GemmShape<TM>::smem;
+  cfg.dynamicSmemBytes = GemmShape<TN>::smem;
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = after_quantize ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<TM>, a, b, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<TN, DT>, a, b, y, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+}
+
+template <int DT>
+int product_dt(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
+               uint32_t* status, bool after_quantize, cudaStream_t s) {
+  // tiles of 128 columns when there is one for every SM, else of 64: twice the blocks
+  const int64_t tiles = (m + kTileM - 1) / kTileM * ((n + 127) / 128);
+  if (tiles >= sm_count()) return gemm<128, DT>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+  return gemm<64, DT>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
 }
 
 int product(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
             uint32_t* status, bool after_quantize, cudaStream_t s) {
-  if (m <= 32) return gemm<32>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
-  if (m <= 64) return gemm<64>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
-  return gemm<128>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+  switch (out.dtype) {
+    case MFET_F32: return product_dt<MFET_F32>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+    case MFET_F16: return product_dt<MFET_F16>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+    default: return product_dt<MFET_BF16>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+  }
 }
 
 template <int MT>

@@ -1,8 +1,9 @@
 // Rows of values written into a table in its own format (quantised as they are written), and rows read back.
 //
-// Both kernels move each byte once; a lane owns 8 neighbouring values of a row, the lanes of a row are the
-// power of two that covers it (4 .. 32; wider rows take several rounds of a whole warp), and a warp keeps kRowsInFlight
-// rows per lane group in flight, because the table rows are scattered and a warp has to cover their latency.
+// Both kernels move each byte once. A lane owns 32 bytes of a row of values (8 fp32 or 16 16-bit values), the lanes of a row are the
+// power of two that covers it (wider rows take several rounds of a whole warp), and a lane group works on kRowsInFlight rows at a
+// time, the list entries of the next ones under way: the table rows are scattered, and what the kernels wait for is their
+// latency. What is left after that is instructions: conversions go two values at a time where the type allows.
 #include <cstring>
 
 #include "lowbit.cuh"
@@ -14,7 +15,8 @@ namespace {
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kRowsThreads = 256;
-constexpr int kRowsInFlight = 4;
+constexpr int kRowsInFlight = 2;
+constexpr int kRowsBlocksPerSm = 4;
 
 struct RowsParams {
   uint8_t* table;
@@ -34,15 +36,16 @@ __device__ __forceinline__ int64_t live_count(const RowsParams& p) {
   return v < 0 ? 0 : (v < p.n ? v : p.n);
 }
 
-// Table row of list entry i; -1: no row (beyond the list, a negative entry, or one past the table, which is reported)
+// Entry i of the list; -1 beyond its end
 __device__ __forceinline__ int64_t entry(const RowsParams& p, int64_t i, int64_t n) {
-  if (i >= n) return -1;
-  int64_t r = p.list ? p.list[i] : i;
-  if (r >= 0 && (uint64_t)r >= p.rows) {
-    if (p.status) atomicOr(p.status, (uint32_t)MFET_DEV_ROW_RANGE);
-    r = -1;
-  }
-  return r < 0 ? -1 : r;
+  return i < n ? (p.list ? __ldg(reinterpret_cast<const long long*>(p.list) + i) : i) : -1;
+}
+// The table row that an entry names, or -1: a negative entry, or one past the table, which is reported
+__device__ __forceinline__ int64_t checked(const RowsParams& p, int64_t r) {
+  if (r < 0) return -1;
+  if ((uint64_t)r < p.rows) return r;
+  if (p.status) atomicOr(p.status, (uint32_t)MFET_DEV_ROW_RANGE);
+  return -1;
 }
 
 // code of x in an INT4 row: clamp(rint((x - bias) / scale), 0, 15) with the quotient rounded once in double precision, as
@@ -55,170 +58,217 @@ __device__ __forceinline__ uint32_t int4_code(float x, float scale, float bias, 
   return (uint32_t)(int)fminf(15.f, fmaxf(0.f, rintf(q)));
 }
 
-template <int TD, int SD, bool VEC>
-__global__ void __launch_bounds__(kRowsThreads) rows_write_kernel(const __grid_constant__ RowsParams p) {
+// ONE: a row takes one round (up to 256 values of fp32, 512 of a 16-bit type)
+template <int TD, int SD, bool VEC, bool ONE>
+__global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_kernel(const __grid_constant__ RowsParams p) {
   using S = typename Elem<SD>::T;
+  constexpr int E = 32 / (int)sizeof(S), LPB = kMxBlock / E;  // values per lane, lanes per block of 32
+  constexpr int U = kRowsInFlight;
   const int64_t n = live_count(p);
   const int lane = threadIdx.x & 31;
   const int lanes = 1 << p.lanes_log2, per_warp = 32 >> p.lanes_log2;
   const int sub = lane & (lanes - 1), group = lane >> p.lanes_log2;
-  const int64_t warp = ((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5;
-  const int64_t step = (int64_t)gridDim.x * (kRowsThreads / 32) * per_warp * kRowsInFlight;
-  for (int64_t w0 = warp * per_warp * kRowsInFlight; w0 < n; w0 += step) {
-    int64_t row[kRowsInFlight];
-    const S* src[kRowsInFlight];
+  const int64_t step = (int64_t)gridDim.x * (kRowsThreads / 32) * per_warp * U;
+  const uint32_t rounds = ONE ? 1 : p.rounds;
+  int64_t w0 = (((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5) * per_warp * U;
+  int64_t next[U];
 #pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) {
+  for (int u = 0; u < U; ++u) next[u] = entry(p, w0 + u * per_warp + group, n);
+  for (; w0 < n; w0 += step) {
+    int64_t row[U];
+    const S* src[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
       const int64_t i = w0 + u * per_warp + group;
-      row[u] = entry(p, i, n);
-      src[u] = reinterpret_cast<const S*>(p.mem) + i * p.ld;
+      row[u] = next[u];
+      next[u] = entry(p, i + step, n);
+      src[u] = reinterpret_cast<const S*>(p.mem) + (i < n ? i : 0) * p.ld;
     }
-    float lo[kRowsInFlight], hi[kRowsInFlight];  // INT4: the whole row's smallest and largest value
+    float lo[U], hi[U];  // INT4: the whole row's smallest and largest value
     if constexpr (TD == MFET_INT4) {
 #pragma unroll
-      for (int u = 0; u < kRowsInFlight; ++u) lo[u] = INFINITY, hi[u] = -INFINITY;
-      for (uint32_t rd = 0; rd < p.rounds; ++rd) {
-        const uint32_t c = rd * 32 + sub;
-        Raw8<SD> raw[kRowsInFlight];
+      for (int u = 0; u < U; ++u) lo[u] = INFINITY, hi[u] = -INFINITY;
+      for (uint32_t rd = 0; rd < rounds; ++rd) {
+        const uint32_t at = (rd * 32 + sub) * E;
+        const int count = at < p.dim ? (int)min((uint32_t)E, p.dim - at) : 0;
+        Raw<SD, E> raw[U];
 #pragma unroll
-        for (int u = 0; u < kRowsInFlight; ++u)
-          if (row[u] >= 0 && c * 8 < p.dim) raw[u] = load8<SD, VEC>(src[u] + c * 8, 8);
+        for (int u = 0; u < U; ++u)
+          if (count > 0) raw[u] = load_raw<SD, E, VEC>(src[u] + at, count);
 #pragma unroll
-        for (int u = 0; u < kRowsInFlight; ++u)
-          if (row[u] >= 0 && c * 8 < p.dim) {
-            float v[8];
-            widen8<SD>(raw[u], v);
+        for (int u = 0; u < U; ++u)
+          if (count > 0) {
+            float v[E];
+            widen_raw<SD, E>(raw[u], v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              // a NaN has to reach the row's scale: fminf would drop it
-              lo[u] = v[j] != v[j] ? v[j] : (lo[u] != lo[u] ? lo[u] : fminf(lo[u], v[j]));
-              hi[u] = fmaxf(hi[u], v[j]);
-            }
+            for (int j = 0; j < E; ++j)
+              if (j < count) {
+                // a NaN has to reach the row's scale: fminf would drop it
+                lo[u] = v[j] != v[j] ? v[j] : (lo[u] != lo[u] ? lo[u] : fminf(lo[u], v[j]));
+                hi[u] = fmaxf(hi[u], v[j]);
+              }
           }
       }
 #pragma unroll
-      for (int u = 0; u < kRowsInFlight; ++u)
+      for (int u = 0; u < U; ++u)
         for (int d = 1; d < lanes; d <<= 1) {
           const float l = __shfl_xor_sync(kAll, lo[u], d), h = __shfl_xor_sync(kAll, hi[u], d);
           lo[u] = (l != l || lo[u] != lo[u]) ? NAN : fminf(lo[u], l);
           hi[u] = fmaxf(hi[u], h);
         }
     }
-    for (uint32_t rd = 0; rd < p.rounds; ++rd) {
-      const uint32_t c = rd * 32 + sub;
-      const int count = c * 8 < p.dim ? (int)min(8u, p.dim - c * 8) : 0;
-      Raw8<SD> raw[kRowsInFlight];
+    for (uint32_t rd = 0; rd < rounds; ++rd) {
+      const uint32_t c = rd * 32 + sub, at = c * E;
+      const int count = at < p.dim ? (int)min((uint32_t)E, p.dim - at) : 0;
+      Raw<SD, E> raw[U];
 #pragma unroll
-      for (int u = 0; u < kRowsInFlight; ++u)
-        if (row[u] >= 0 && count > 0) raw[u] = load8<SD, VEC>(src[u] + c * 8, count);
+      for (int u = 0; u < U; ++u)
+        if (count > 0) raw[u] = load_raw<SD, E, VEC>(src[u] + at, count);  // does not wait for the list entry
+        else memset(&raw[u], 0, sizeof(raw[u]));
 #pragma unroll
-      for (int u = 0; u < kRowsInFlight; ++u) {
-        const bool live = row[u] >= 0 && count > 0;
-        uint8_t* out = p.table + (uint64_t)(row[u] >= 0 ? row[u] : 0) * p.stride;
-        float v[8] = {};
-        if (live) widen8<SD>(raw[u], v);
+      for (int u = 0; u < U; ++u) {
+        const int64_t r = checked(p, row[u]);
+        const bool ok = r >= 0;
+        uint8_t* out = p.table + (uint64_t)(ok ? r : 0) * p.stride;
         if constexpr (TD == MFET_MXFP4) {
-          uint32_t m = amax8(v);  // 0 where the row has ended: a short last block counts what it has
-          m = max(m, __shfl_xor_sync(kAll, m, 1));
-          m = max(m, __shfl_xor_sync(kAll, m, 2));
-          const uint32_t b = mx_scale_byte(m);
-          if (live) *reinterpret_cast<uint32_t*>(out + c * 4) = b == kMxNan ? 0u : mx_encode8(v, mx_inv_scale(b));
-          // the scale bytes and the padding behind them, as words: this round's blocks are 4 lanes apart
-          const int first = lane - sub;
-          const uint32_t tail = (p.row_bytes - p.dim / 2) / 4, w = rd * 2 + sub;
-          const uint32_t blocks = (p.dim + kMxBlock - 1) / kMxBlock;
-          uint32_t word = 0;
+          uint32_t m = amax_raw<SD, E>(raw[u]);  // 0 where the row has ended: a short last block counts what it has
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t s = __shfl_sync(kAll, b, first + ((4 * sub + j) * 4 & (lanes - 1)));
-            if (4 * w + j < blocks) word |= s << (8 * j);
+          for (int d = 1; d < LPB; d <<= 1) m = max(m, __shfl_xor_sync(kAll, m, d));
+          const uint32_t b = mx_scale_byte(m);
+          // the scale bytes of four neighbouring blocks as one word
+          uint32_t word = b << (8 * ((sub / LPB) & 3));
+          if (lanes > LPB) word |= __shfl_xor_sync(kAll, word, LPB);
+          if (lanes > 2 * LPB) word |= __shfl_xor_sync(kAll, word, 2 * LPB);
+          float v[E];
+          widen_raw<SD, E>(raw[u], v);
+          const float inv = b == kMxNan ? 0.f : mx_inv_scale(b);
+          if (ok && count > 0) {
+            uint32_t codes[E / 8];
+#pragma unroll
+            for (int j = 0; j < E / 8; ++j) codes[j] = b == kMxNan ? 0u : mx_encode8(v + 8 * j, inv);
+            uint32_t* dst = reinterpret_cast<uint32_t*>(out + at / 2);
+            if (E == 16 && count == 16) *reinterpret_cast<uint2*>(dst) = make_uint2(codes[0], codes[E / 8 - 1]);
+            else *dst = codes[0];
           }
-          const bool last = rd + 1 == p.rounds;
-          if (row[u] >= 0 && w < tail && (last || sub < 2)) *reinterpret_cast<uint32_t*>(out + p.dim / 2 + 4 * w) = word;
+          if (ok) {
+            uint32_t* tail = reinterpret_cast<uint32_t*>(out + p.dim / 2);
+            const uint32_t tail_words = (p.row_bytes - p.dim / 2) / 4, data_words = (p.dim + 127) / 128;
+            const uint32_t w = c / (4 * LPB);
+            if (c % (4 * LPB) == 0 && w < data_words) tail[w] = word;
+            if (rd + 1 == rounds)
+              for (uint32_t x = data_words + sub; x < tail_words; x += lanes) tail[x] = 0u;  // the padding
+          }
         } else if constexpr (TD == MFET_INT4) {
+          float v[E];
+          widen_raw<SD, E>(raw[u], v);
           const __half sh = __float2half_rn(__fdiv_rn(__fsub_rn(hi[u], lo[u]), 15.0f)), bh = __float2half_rn(lo[u]);
           const float scale = __half2float(sh), bias = __half2float(bh);
           const bool fine = isfinite(scale) && isfinite(bias);
-          uint32_t word = 0;
-          if (fine && scale > 0.f) {
-            const float inv = __fdiv_rn(1.f, scale);
+          const float inv = __fdiv_rn(1.f, scale);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) word |= int4_code(v[j], scale, bias, inv) << (4 * j);
+          for (int q = 0; q < E / 8; ++q) {
+            uint32_t word = 0;
+            if (fine && scale > 0.f) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) word |= int4_code(v[8 * q + j], scale, bias, inv) << (4 * j);
+            }
+            if (ok && count >= 8 * (q + 1)) reinterpret_cast<uint32_t*>(out + at / 2)[q] = word;
           }
-          if (live) *reinterpret_cast<uint32_t*>(out + c * 4) = word;
-          const uint32_t tail = (p.row_bytes - p.dim / 2) / 4, w = rd * 32 + sub;
-          // scale and bias, then zeros up to the row's end (at most 16 bytes: one round writes them all)
-          if (row[u] >= 0 && rd == 0 && w < tail)
-            *reinterpret_cast<uint32_t*>(out + p.dim / 2 + 4 * w) =
-                w > 0 ? 0u
-                      : (fine ? (uint32_t)__half_as_ushort(sh) | ((uint32_t)__half_as_ushort(bh) << 16) : 0x7E007E00u);
+          // scale and bias, then zeros up to the row's end
+          if (ok && rd == 0)
+            for (uint32_t x = sub; x < (p.row_bytes - p.dim / 2) / 4; x += lanes)
+              reinterpret_cast<uint32_t*>(out + p.dim / 2)[x] =
+                  x > 0 ? 0u : (fine ? (uint32_t)__half_as_ushort(sh) | ((uint32_t)__half_as_ushort(bh) << 16) : 0x7E007E00u);
         } else {
-          if (live) store8<TD, true>(reinterpret_cast<typename Elem<TD>::T*>(out) + c * 8, v, count);
+          float v[E];
+          widen_raw<SD, E>(raw[u], v);
+          if (ok && count > 0) store_values<TD, E, true>(reinterpret_cast<typename Elem<TD>::T*>(out) + at, v, count);
         }
       }
     }
   }
 }
 
-template <int TD, int DD, bool VEC>
-__global__ void __launch_bounds__(kRowsThreads) rows_read_kernel(const __grid_constant__ RowsParams p) {
+template <int TD, int DD, bool VEC, bool ONE>
+__global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_read_kernel(const __grid_constant__ RowsParams p) {
   using D = typename Elem<DD>::T;
+  constexpr int E = 32 / (int)sizeof(D), LPB = kMxBlock / E;
+  constexpr int U = kRowsInFlight;
   const int64_t n = live_count(p);
   const int lane = threadIdx.x & 31;
   const int lanes = 1 << p.lanes_log2, per_warp = 32 >> p.lanes_log2;
   const int sub = lane & (lanes - 1), group = lane >> p.lanes_log2;
-  const int64_t warp = ((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5;
-  const int64_t step = (int64_t)gridDim.x * (kRowsThreads / 32) * per_warp * kRowsInFlight;
+  const int64_t step = (int64_t)gridDim.x * (kRowsThreads / 32) * per_warp * U;
+  const uint32_t rounds = ONE ? 1 : p.rounds;
   constexpr bool kCodes = TD == MFET_MXFP4 || TD == MFET_INT4;
   constexpr int kTable = kCodes ? MFET_F32 : TD;  // element type of a row that is stored plainly
-  for (int64_t w0 = warp * per_warp * kRowsInFlight; w0 < n; w0 += step) {
-    int64_t row[kRowsInFlight];
+  int64_t w0 = (((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5) * per_warp * U;
+  int64_t next[U];
 #pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) row[u] = entry(p, w0 + u * per_warp + group, n);
-    for (uint32_t rd = 0; rd < p.rounds; ++rd) {
-      const uint32_t c = rd * 32 + sub;
-      const int count = c * 8 < p.dim ? (int)min(8u, p.dim - c * 8) : 0;
-      uint32_t codes[kRowsInFlight], meta[kRowsInFlight];
-      Raw8<kTable> raw[kRowsInFlight];
+  for (int u = 0; u < U; ++u) next[u] = entry(p, w0 + u * per_warp + group, n);
+  for (; w0 < n; w0 += step) {
+    int64_t row[U];
 #pragma unroll
-      for (int u = 0; u < kRowsInFlight; ++u) {
-        codes[u] = meta[u] = 0;
+    for (int u = 0; u < U; ++u) {
+      row[u] = checked(p, next[u]);
+      next[u] = entry(p, w0 + step + u * per_warp + group, n);
+    }
+    for (uint32_t rd = 0; rd < rounds; ++rd) {
+      const uint32_t c = rd * 32 + sub, at = c * E;
+      const int count = at < p.dim ? (int)min((uint32_t)E, p.dim - at) : 0;
+      uint32_t codes[U][E / 8], meta[U];
+      Raw<kTable, E> raw[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int j = 0; j < E / 8; ++j) codes[u][j] = 0;
+        meta[u] = 0;
         if (row[u] >= 0 && count > 0) {
-          const uint8_t* at = p.table + (uint64_t)row[u] * p.stride;
+          const uint8_t* from = p.table + (uint64_t)row[u] * p.stride;
           if constexpr (kCodes) {
-            codes[u] = *reinterpret_cast<const uint32_t*>(at + c * 4);
-            meta[u] = TD == MFET_MXFP4 ? (uint32_t)at[p.dim / 2 + c / 4] : *reinterpret_cast<const uint32_t*>(at + p.dim / 2);
+            // 16 codes are read together; behind the last 8 of a row lie its scales, which are not used as codes
+            if constexpr (E == 16) {
+              const uint2 two = *reinterpret_cast<const uint2*>(from + at / 2);
+              codes[u][0] = two.x;
+              codes[u][E / 8 - 1] = two.y;
+            } else {
+              codes[u][0] = *reinterpret_cast<const uint32_t*>(from + at / 2);
+            }
+            meta[u] = TD == MFET_MXFP4 ? (uint32_t)from[p.dim / 2 + c / LPB] : *reinterpret_cast<const uint32_t*>(from + p.dim / 2);
           } else {
-            raw[u] = load8<kTable, true>(reinterpret_cast<const typename Elem<kTable>::T*>(at) + c * 8, count);
+            raw[u] = load_raw<kTable, E, true>(reinterpret_cast<const typename Elem<kTable>::T*>(from) + at, count);
           }
         }
       }
 #pragma unroll
-      for (int u = 0; u < kRowsInFlight; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int64_t i = w0 + u * per_warp + group;
         if (i >= n || count == 0) continue;
-        float v[8] = {};
+        float v[E] = {};
         if (row[u] >= 0) {
           if constexpr (TD == MFET_MXFP4) {
-            mx_decode8(codes[u], mx_scale(meta[u]), v);
+            const float scale = mx_scale(meta[u]);
+#pragma unroll
+            for (int j = 0; j < E / 8; ++j) mx_decode8(codes[u][j], scale, v + 8 * j);
           } else if constexpr (TD == MFET_INT4) {
             const float2 sb = __half22float2(*reinterpret_cast<const __half2*>(&meta[u]));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = fmaf((float)((codes[u] >> (4 * j)) & 15u), sb.x, sb.y);
+            for (int j = 0; j < E; ++j) v[j] = fmaf((float)((codes[u][j / 8] >> (4 * (j % 8))) & 15u), sb.x, sb.y);
           } else {
-            widen8<kTable>(raw[u], v);
+            widen_raw<kTable, E>(raw[u], v);
           }
         }
-        store8<DD, VEC>(reinterpret_cast<D*>(p.mem) + i * p.ld + c * 8, v, count);
+        store_values<DD, E, VEC>(reinterpret_cast<D*>(p.mem) + i * p.ld + at, v, count);
       }
     }
   }
 }
 
-// the narrowest lane group that covers a row, and how many rounds a wider row takes
-void lanes_of(uint32_t dim, RowsParams* p) {
-  const uint32_t chunks = (dim + 31) / 32 * 4;  // whole blocks of 32 values
-  uint32_t l = 2;
+// the narrowest lane group that covers a row (32 bytes of values per lane, whole blocks of 32 values), and how many rounds
+// a wider row takes
+void lanes_of(uint32_t dim, uint32_t mem_dtype, RowsParams* p) {
+  const uint32_t per_block = mem_dtype == MFET_F32 ? 4 : 2, chunks = (dim + 31) / 32 * per_block;
+  uint32_t l = per_block == 4 ? 2 : 1;
   while ((1u << l) < chunks && l < 5) ++l;
   p->lanes_log2 = l;
   p->rounds = (chunks + (1u << l) - 1) >> l;
@@ -247,7 +297,7 @@ int check(const mfet_table_desc_t* d, const int64_t* list, int64_t n, const void
   p->ld = ld;
   p->dim = d->dim;
   p->row_bytes = (uint32_t)rb;
-  lanes_of(d->dim, p);
+  lanes_of(d->dim, mem_dtype, p);
   return MFET_OK;
 }
 
@@ -258,21 +308,22 @@ bool vectors(const RowsParams& p, uint32_t dtype) {
 
 unsigned blocks_for(const RowsParams& p) {
   const int64_t per_block = (int64_t)(kRowsThreads >> p.lanes_log2) * kRowsInFlight;
-  const int64_t want = (p.n + per_block - 1) / per_block, most = (int64_t)sm_count() * 16;
+  const int64_t want = (p.n + per_block - 1) / per_block, most = (int64_t)sm_count() * kRowsBlocksPerSm;
   return (unsigned)(want < most ? want : most);
+}
+
+template <int TD, int MD, bool VEC, bool ONE>
+void launch_as(const RowsParams& p, bool write, cudaStream_t s) {
+  const unsigned b = blocks_for(p);
+  if (write) rows_write_kernel<TD, MD, VEC, ONE><<<b, kRowsThreads, 0, s>>>(p);
+  else rows_read_kernel<TD, MD, VEC, ONE><<<b, kRowsThreads, 0, s>>>(p);
 }
 
 template <int TD, int MD>
 cudaError_t launch_one(const RowsParams& p, bool write, cudaStream_t s) {
-  const unsigned b = blocks_for(p);
-  const bool vec = vectors(p, MD);
-  if (write) {
-    if (vec) rows_write_kernel<TD, MD, true><<<b, kRowsThreads, 0, s>>>(p);
-    else rows_write_kernel<TD, MD, false><<<b, kRowsThreads, 0, s>>>(p);
-  } else {
-    if (vec) rows_read_kernel<TD, MD, true><<<b, kRowsThreads, 0, s>>>(p);
-    else rows_read_kernel<TD, MD, false><<<b, kRowsThreads, 0, s>>>(p);
-  }
+  const bool vec = vectors(p, MD), one = p.rounds == 1;
+  if (vec) one ? launch_as<TD, MD, true, true>(p, write, s) : launch_as<TD, MD, true, false>(p, write, s);
+  else one ? launch_as<TD, MD, false, true>(p, write, s) : launch_as<TD, MD, false, false>(p, write, s);
   return cudaGetLastError();
 }
 

@@ -127,12 +127,14 @@ class MfetError(RuntimeError):
 
 def _ptr(x) -> Optional[int]:
     """Address of a torch tensor, numpy array, ctypes pointer or int; None stays NULL."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
-    if hasattr(x, "data_ptr"):
-        return int(x.data_ptr())
+    try:
+        return x.data_ptr()  # what most arguments are: no look-up ahead of the call
+    except AttributeError:
+        pass
+    if isinstance(x, int):
+        return int(x)
     if isinstance(x, np.ndarray):
         return int(x.ctypes.data)
     return C.cast(x, C.c_void_p).value
@@ -317,15 +319,18 @@ def mfet_launch_count(h) -> int:
     return int(n.value)
 
 
+_DTYPES = {}  # torch dtype -> MFET_*, filled as dtypes are met
+
+
 def dtype_of(t) -> int:
     """MFET_F32 / F16 / BF16 of a torch tensor."""
-    name = str(t.dtype)
-    if name not in _TORCH_DTYPES:
-        raise MfetError(ERR_INVALID_ARG, "dtype_of(%s)" % name)
-    return _TORCH_DTYPES[name]
-
-
-_TORCH_DTYPES = {"torch.float32": F32, "torch.float16": F16, "torch.bfloat16": BF16}
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        d = {"torch.float32": F32, "torch.float16": F16, "torch.bfloat16": BF16}.get(str(t.dtype))
+        if d is None:
+            raise MfetError(ERR_INVALID_ARG, "dtype_of(%s)" % t.dtype)
+        _DTYPES[t.dtype] = d
+    return d
 
 
 def make_grads(src, dst, counts=None):
