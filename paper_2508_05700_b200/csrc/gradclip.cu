@@ -27,7 +27,7 @@ struct GradDev {
   uint8_t* dst;           // nullptr: only counted
   const int64_t* n_rows;  // nullptr, or the number of rows on the device
   int64_t rows, cols, ld;
-  int64_t first_piece;
+  int64_t pad;
   uint32_t dtype;
   uint32_t lead;          // elements between the 16-byte boundary before src and src; vectors are counted from that boundary
 };
@@ -49,25 +49,71 @@ struct GradParams {
 };
 static_assert(sizeof(GradParams<kManyTensors>) <= 32000, "kernel parameters are limited to 32764 bytes");
 
-template <class P>
-__device__ __forceinline__ int find_tensor(const P& p, int64_t piece) {
-  int lo = 0, hi = p.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (p.t[mid].first_piece <= piece) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
+// What a block works on: its share of the pieces that hold elements. The counts on the device are read once per block, the pieces of
+// the tensors before each one are added up in shared memory, and the block goes along: no search per piece, and a list that is half
+// empty spreads as evenly as a full one.
+template <int N>
+struct Share {
+  int64_t live[N];    // elements
+  int32_t first[N];   // pieces of the tensors before
+  int32_t warp_sum[kClipThreads / 32];
+  int32_t total;
 
-__device__ __forceinline__ int64_t live_elems(const GradDev& t) {
-  int64_t r = t.rows;
-  if (t.n_rows) {
-    const int64_t v = *t.n_rows;
-    r = v < 0 ? 0 : (v < r ? v : r);
+  template <class P>
+  __device__ __forceinline__ void fill(const P& p) {
+    // Every thread has an entry of its own here. Constant loads would go through the entries one by one (20 us for 300 tensors):
+    // behind this the compiler no longer knows where they are, and uses ordinary ones.
+    const GradDev* entries = p.t;
+    asm volatile("" : "+l"(entries));
+    constexpr int kPer = (N + kClipThreads - 1) / kClipThreads;
+    int32_t mine[kPer], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = (int)threadIdx.x * kPer + j;
+      mine[j] = 0;
+      if (i < p.n) {
+        const GradDev& t = entries[i];
+        int64_t r = t.rows;
+        if (t.n_rows) {
+          const int64_t v = *t.n_rows;
+          r = v < 0 ? 0 : (v < r ? v : r);
+        }
+        const int64_t e = r * t.cols, per = kPieceVecs * (t.dtype == MFET_F32 ? 4 : 8);
+        live[i] = e;
+        mine[j] = e > 0 ? (int32_t)((e + t.lead + per - 1) / per) : 0;
+      }
+      sum += mine[j];
+    }
+    int32_t before = sum;  // inclusive over the warp, then over the block
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int32_t o = __shfl_up_sync(0xFFFFFFFFu, before, d);
+      if ((int)(threadIdx.x & 31) >= d) before += o;
+    }
+    if ((threadIdx.x & 31) == 31) warp_sum[threadIdx.x >> 5] = before;
+    __syncthreads();
+    int32_t at = before - sum;
+    for (int w = 0; w < (int)(threadIdx.x >> 5); ++w) at += warp_sum[w];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = (int)threadIdx.x * kPer + j;
+      if (i < p.n) first[i] = at;
+      at += mine[j];
+    }
+    if (threadIdx.x == kClipThreads - 1) total = at;
+    __syncthreads();
   }
-  return r * t.cols;
-}
+  // the last tensor that starts at or before piece k (an empty one is followed by one that starts there too)
+  __device__ __forceinline__ int tensor_of(int n, int32_t k) const {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= k) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
 
 __device__ __forceinline__ double block_sum(double v, double* shared) {
 #pragma unroll
@@ -125,11 +171,25 @@ __device__ __forceinline__ uint4 scaled16(const uint4& w, Factor f) {
   return narrow16<DT>(v);
 }
 
+// A tensor's vectors are counted from the 16-byte boundary at or before its start; `end` is its end in elements from there.
+template <int V>
+__device__ __forceinline__ bool whole_vector(const GradDev& t, int64_t vec, int64_t end) {
+  return vec * V >= t.lead && (vec + 1) * V <= end;
+}
+// The first and the last vector of a tensor may belong to it only in part: their elements, one to a thread, or -1.
+template <int V>
+__device__ __forceinline__ int64_t edge_element(const GradDev& t, int64_t v0, int64_t end) {
+  const int64_t tail = end / V;
+  if (threadIdx.x < V) return v0 == 0 && t.lead > 0 && threadIdx.x >= t.lead && threadIdx.x < end ? (int64_t)threadIdx.x : -1;
+  const int64_t e = tail * V + (int64_t)threadIdx.x - 32;
+  if (threadIdx.x < 32 || threadIdx.x >= 32 + V || e >= end) return -1;
+  return tail >= v0 && tail < v0 + kPieceVecs && !(tail == 0 && t.lead > 0) ? e : -1;
+}
+
 template <int DT>
-__device__ __forceinline__ double piece_squares(const GradDev& t, int64_t piece) {
+__device__ __forceinline__ double piece_squares(const GradDev& t, int64_t n, int64_t piece) {
   using T = typename Elem<DT>::T;
   constexpr int V = 16 / (int)sizeof(T);
-  const int64_t n = live_elems(t);
   const T* src = reinterpret_cast<const T*>(t.src);
   const int64_t v0 = piece * kPieceVecs, end = n + t.lead;  // vectors count from the boundary before src
   double s = 0;
@@ -145,18 +205,16 @@ __device__ __forceinline__ double piece_squares(const GradDev& t, int64_t piece)
       for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
       return s;
     }
-#pragma unroll 1
-    for (int j = 0; j < kClipInFlight; ++j) {
-      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
-      if (a + V <= t.lead || a >= end) continue;
-      if (a >= t.lead && a + V <= end) {
-        s += vec_squares<DT>(__ldg(at + j * kClipThreads));
-      } else {  // a vector that belongs to the tensor only in part
-        for (int64_t i = a > t.lead ? a : t.lead; i < a + V && i < end; ++i) {
-          const double x = (double)to_float<DT>(base[i]);
-          s = fma(x, x, s);
-        }
-      }
+    uint4 v[kClipInFlight];
+#pragma unroll
+    for (int j = 0; j < kClipInFlight; ++j)
+      v[j] = whole_vector<V>(t, v0 + j * kClipThreads + threadIdx.x, end) ? __ldg(at + j * kClipThreads) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
+    const int64_t e = edge_element<V>(t, v0, end);
+    if (e >= 0) {
+      const double x = (double)to_float<DT>(base[e]);
+      s = fma(x, x, s);
     }
   } else {
     for (int64_t i = v0 * V + threadIdx.x; i < (v0 + kPieceVecs) * V && i < n; i += kClipThreads) {
@@ -168,10 +226,9 @@ __device__ __forceinline__ double piece_squares(const GradDev& t, int64_t piece)
 }
 
 template <int DT>
-__device__ __forceinline__ void piece_scale(const GradDev& t, int64_t piece, Factor f) {
+__device__ __forceinline__ void piece_scale(const GradDev& t, int64_t n, int64_t piece, Factor f) {
   using T = typename Elem<DT>::T;
   constexpr int V = 16 / (int)sizeof(T);
-  const int64_t n = live_elems(t);
   const T* src = reinterpret_cast<const T*>(t.src);
   T* dst = reinterpret_cast<T*>(t.dst);
   const int64_t v0 = piece * kPieceVecs, end = n + t.lead;
@@ -183,26 +240,33 @@ __device__ __forceinline__ void piece_scale(const GradDev& t, int64_t piece, Fac
     uint4* out = reinterpret_cast<uint4*>(to) + v0 + threadIdx.x;
     const bool same = ((reinterpret_cast<uintptr_t>(to)) & 15u) == 0;  // dst sits on its boundary as src does
     if (same && v0 * V >= t.lead && (v0 + kPieceVecs) * V <= end) {
+      uint4 v[kClipInFlight];
 #pragma unroll
-      for (int h = 0; h < kClipInFlight; h += 4) {
-        uint4 v[4];
+      for (int j = 0; j < kClipInFlight; ++j) v[j] = __ldcs(in + j * kClipThreads);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __ldcs(in + (h + j) * kClipThreads);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) __stcs(out + (h + j) * kClipThreads, scaled16<DT>(v[j], f));
-      }
+      for (int j = 0; j < kClipInFlight; ++j) __stcs(out + j * kClipThreads, scaled16<DT>(v[j], f));
       return;
     }
-#pragma unroll 1
+    uint4 v[kClipInFlight];
+#pragma unroll
+    for (int j = 0; j < kClipInFlight; ++j)
+      if (whole_vector<V>(t, v0 + j * kClipThreads + threadIdx.x, end)) v[j] = __ldcs(in + j * kClipThreads);
+#pragma unroll
     for (int j = 0; j < kClipInFlight; ++j) {
-      const int64_t a = (v0 + j * kClipThreads + threadIdx.x) * V;
-      if (a + V <= t.lead || a >= end) continue;
-      if (same && a >= t.lead && a + V <= end) {
-        out[j * kClipThreads] = scaled16<DT>(in[j * kClipThreads], f);
+      const int64_t vec = v0 + j * kClipThreads + threadIdx.x;
+      if (!whole_vector<V>(t, vec, end)) continue;
+      const uint4 r = scaled16<DT>(v[j], f);
+      if (same) {
+        __stcs(out + j * kClipThreads, r);
       } else {
-        for (int64_t i = a > t.lead ? a : t.lead; i < a + V && i < end; ++i) to[i] = scaled<DT>(from[i], f);
+        T x[V];
+        memcpy(x, &r, 16);
+#pragma unroll
+        for (int q = 0; q < V; ++q) to[vec * V + q] = x[q];
       }
     }
+    const int64_t e = edge_element<V>(t, v0, end);
+    if (e >= 0) to[e] = scaled<DT>(from[e], f);
   } else {
     for (int64_t i = v0 * V + threadIdx.x; i < (v0 + kPieceVecs) * V && i < n; i += kClipThreads) {
       const int64_t at = strided(t, i);
@@ -211,42 +275,82 @@ __device__ __forceinline__ void piece_scale(const GradDev& t, int64_t piece, Fac
   }
 }
 
+// Block `b` of `g` takes every g-th piece, in ascending order here and in descending order when it scales.
+template <int N>
+__device__ __forceinline__ double share_squares(const GradParams<N>& p, const Share<N>& share, int b, int g) {
+  double s = 0;
+  int32_t k = b;
+  for (int i = k < share.total ? share.tensor_of(p.n, k) : 0; k < share.total; k += g) {
+    while (i + 1 < p.n && share.first[i + 1] <= k) ++i;
+    const GradDev& t = p.t[i];
+    const int64_t piece = k - share.first[i];
+    if (t.dtype == MFET_F32) s += piece_squares<MFET_F32>(t, share.live[i], piece);
+    else if (t.dtype == MFET_F16) s += piece_squares<MFET_F16>(t, share.live[i], piece);
+    else s += piece_squares<MFET_BF16>(t, share.live[i], piece);
+  }
+  return s;
+}
+
+template <int N>
+__device__ __forceinline__ void share_scale(const GradParams<N>& p, const Share<N>& share, int b, int g, double norm) {
+  if (p.norm && b == 0 && threadIdx.x == 0) *p.norm = (float)norm;
+  // a norm that is infinite or NaN leaves the gradients as they are
+  const bool clip = norm > p.max_norm && norm < INFINITY;
+  Factor f{clip, (float)(p.max_norm / norm)};
+  asm volatile("" : "+f"(f.coef));  // else "clip ? x * coef : x" may be folded into one product
+  int32_t k = b < share.total ? (share.total - 1 - b) / g * g + b : -1;
+  for (int i = k >= 0 ? share.tensor_of(p.n, k) : 0; k >= 0; k -= g) {
+    while (share.first[i] > k) --i;
+    const GradDev& t = p.t[i];
+    if (!t.dst || (!clip && t.dst == t.src)) continue;
+    const int64_t piece = k - share.first[i];
+    if (t.dtype == MFET_F32) piece_scale<MFET_F32>(t, share.live[i], piece, f);
+    else if (t.dtype == MFET_F16) piece_scale<MFET_F16>(t, share.live[i], piece, f);
+    else piece_scale<MFET_BF16>(t, share.live[i], piece, f);
+  }
+}
+
 template <int N>
 __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) grad_squares_kernel(const __grid_constant__ GradParams<N> p) {
   __shared__ double shared[kClipThreads / 32];
-  double s = 0;
-  for (int64_t k = blockIdx.x; k < p.pieces; k += gridDim.x) {
-    const GradDev& t = p.t[find_tensor(p, k)];
-    const int64_t piece = k - t.first_piece;
-    if (t.dtype == MFET_F32) s += piece_squares<MFET_F32>(t, piece);
-    else if (t.dtype == MFET_F16) s += piece_squares<MFET_F16>(t, piece);
-    else s += piece_squares<MFET_BF16>(t, piece);
-  }
-  s = block_sum(s, shared);
+  __shared__ Share<N> share;
+  asm volatile("griddepcontrol.launch_dependents;");  // the scaling may set itself up; it waits for this grid's end
+  share.fill(p);
+  const double s = block_sum(share_squares(p, share, blockIdx.x, gridDim.x), shared);
   if (threadIdx.x == 0) p.sums[p.first_sum + blockIdx.x] = s;
-  asm volatile("griddepcontrol.launch_dependents;");
 }
 
 template <int N>
 __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) grad_scale_kernel(const __grid_constant__ GradParams<N> p) {
   __shared__ double shared[kClipThreads / 32];
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // the sums of the launch before this one
+  __shared__ Share<N> share;
+  share.fill(p);  // what the call was given: not written by the launch before this one
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // its sums are
   double s = 0;
   for (int i = threadIdx.x; i < p.n_sums; i += kClipThreads) s += __ldcg(p.sums + i);
-  const double norm = sqrt(block_sum(s, shared));
-  if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
-  // a norm that is infinite or NaN leaves the gradients as they are
-  const bool clip = norm > p.max_norm && norm < INFINITY;
-  Factor f{clip, (float)(p.max_norm / norm)};
-  asm volatile("" : "+f"(f.coef));  // else "clip ? x * coef : x" may be folded into one product
-  for (int64_t k = p.pieces - 1 - blockIdx.x; k >= 0; k -= gridDim.x) {
-    const GradDev& t = p.t[find_tensor(p, k)];
-    if (!t.dst || (!clip && t.dst == t.src)) continue;
-    const int64_t piece = k - t.first_piece;
-    if (t.dtype == MFET_F32) piece_scale<MFET_F32>(t, piece, f);
-    else if (t.dtype == MFET_F16) piece_scale<MFET_F16>(t, piece, f);
-    else piece_scale<MFET_BF16>(t, piece, f);
+  share_scale(p, share, blockIdx.x, gridDim.x, sqrt(block_sum(s, shared)));
+}
+
+// Few pieces: both steps in one launch of one cluster, whose blocks exchange their sums through distributed shared memory. A launch
+// costs more than such a call's work.
+constexpr int kSmallBlocks = 8, kSmallPieces = 4 * kSmallBlocks;
+__global__ void __cluster_dims__(kSmallBlocks, 1, 1) __launch_bounds__(kClipThreads, kClipBlocksPerSm)
+    grad_small_kernel(const __grid_constant__ GradParams<kFewTensors> p) {
+  __shared__ double shared[kClipThreads / 32];
+  __shared__ double all[kSmallBlocks];
+  __shared__ Share<kFewTensors> share;
+  share.fill(p);
+  const double s = block_sum(share_squares(p, share, blockIdx.x, kSmallBlocks), shared);
+  if (threadIdx.x < kSmallBlocks) {  // into every block's list
+    uint32_t to;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&all[blockIdx.x])), "r"(threadIdx.x));
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(s) : "memory");
   }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  double total = 0;
+#pragma unroll
+  for (int b = 0; b < kSmallBlocks; ++b) total += all[b];
+  share_scale(p, share, blockIdx.x, kSmallBlocks, sqrt(total));
 }
 
 int64_t blocks_of(int64_t pieces) {
@@ -283,7 +387,7 @@ int32_t fill_params(const mfet_grad_t* g, int32_t n_grads, int32_t at, GradParam
     t.ld = g[i].ld && g[i].rows > 1 ? g[i].ld : g[i].cols;
     t.dtype = g[i].dtype;
     t.lead = t.ld == t.cols ? (uint32_t)(((uintptr_t)t.src & 15u) / size) : 0u;
-    t.first_piece = p->pieces;
+    t.pad = 0;
     p->pieces += (t.rows * t.cols + t.lead + kPieceVecs * (16 / size) - 1) / (kPieceVecs * (16 / size));
   }
   return i - at;
@@ -322,11 +426,18 @@ int run_clip(const mfet_grad_t* g, int32_t n_grads, double max_norm, float* norm
   int64_t n_sums = 0;
   for (int32_t at = 0; at < n_grads;) {
     at += fill_params<N>(g, n_grads, at, &p);
+    if (p.pieces > 0x7FFFFFFF) return MFET_ERR_INVALID_ARG;
     n_sums += blocks_of(p.pieces);
   }
   if (n_sums > room) return MFET_ERR_WORKSPACE;
   p.n_sums = (int32_t)n_sums;
   const bool one_group = n_grads <= N;  // p holds it already
+  if constexpr (N == kFewTensors) {
+    if (n_grads > 0 && p.pieces <= kSmallPieces) {
+      grad_small_kernel<<<kSmallBlocks, kClipThreads, 0, s>>>(p);
+      return cudaGetLastError() == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+    }
+  }
   if (n_grads == 0) p.n = 0, p.pieces = 0;
   for (int32_t at = 0; at < n_grads;) {
     at += one_group ? n_grads : fill_params<N>(g, n_grads, at, &p);

@@ -103,12 +103,30 @@ struct Raw {
   uint4 w[pieces];
 };
 
-// The first `count` values at p, the rest 0. VEC: p is 16-byte aligned, and whole pieces of 16 bytes are read as such. The values
-// are read once: they do not displace anything in the caches.
+// 32 bytes, aligned to that: whole sectors in one instruction
+__device__ __forceinline__ void load32(const void* p, uint4* a, uint4* b) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(a->x), "=r"(a->y), "=r"(a->z), "=r"(a->w), "=r"(b->x), "=r"(b->y), "=r"(b->z), "=r"(b->w)
+               : "l"(p));
+}
+__device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w),
+               "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+               : "memory");
+}
+
+// The first `count` values at p, the rest 0. VEC: p is 16-byte aligned, and whole pieces of 16 bytes are read as such; wide: it is
+// 32-byte aligned. The values are read once: they do not displace anything in the caches.
 template <int DT, int E, bool VEC>
-__device__ __forceinline__ Raw<DT, E> load_raw(const typename Elem<DT>::T* p, int count) {
+__device__ __forceinline__ Raw<DT, E> load_raw(const typename Elem<DT>::T* p, int count, bool wide = false) {
   using R = Raw<DT, E>;
   R r;
+  if constexpr (VEC && R::pieces == 2) {
+    if (wide && count == E) {
+      load32(p, &r.w[0], &r.w[1]);
+      return r;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < R::pieces; ++i) {
     if (VEC && count >= (i + 1) * R::per) {
@@ -121,6 +139,61 @@ __device__ __forceinline__ Raw<DT, E> load_raw(const typename Elem<DT>::T* p, in
     }
   }
   return r;
+}
+
+// The same for p at any address of its element type: the 16-byte pieces that hold the values are read whole and shifted into place.
+// Only memory of the array [lo, hi) is read: a piece that reaches over its ends is read value by value.
+template <int DT, int E>
+__device__ __forceinline__ Raw<DT, E> load_shifted(const typename Elem<DT>::T* p, int count, const void* lo, const void* hi) {
+  using R = Raw<DT, E>;
+  using T = typename Elem<DT>::T;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p), from = at & ~(uintptr_t)15;
+  const uint32_t d = (uint32_t)(at & 15);
+  uint32_t w[4 * (R::pieces + 1)];
+#pragma unroll
+  for (int i = 0; i <= R::pieces; ++i) {
+    const uintptr_t a = from + 16 * i;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (a < at + count * sizeof(T)) {
+      if (a >= reinterpret_cast<uintptr_t>(lo) && a + 16 <= reinterpret_cast<uintptr_t>(hi)) {
+        v = __ldg(reinterpret_cast<const uint4*>(a));  // a neighbour reads most of it again
+      } else {
+        T t[R::per];
+#pragma unroll
+        for (int j = 0; j < R::per; ++j) {
+          const T* e = reinterpret_cast<const T*>(a) + j;
+          t[j] = e >= p && e < p + count ? *e : Elem<DT>::from(0.f);
+        }
+        memcpy(&v, t, 16);
+      }
+    }
+    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+  }
+#pragma unroll
+  for (int i = 0; i < 4 * R::pieces + 2; ++i) w[i] = (d & 8) ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 4 * R::pieces + 1; ++i) w[i] = (d & 4) ? w[i + 1] : w[i];
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 4 * R::pieces; ++i) w[i] = __byte_perm(w[i], w[i + 1], (d & 2) ? 0x5432 : 0x3210);
+  }
+  if (count < E) {  // what follows the values
+#pragma unroll
+    for (int i = 0; i < 4 * R::pieces; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = i < count ? w[i] : 0u;
+      else w[i] = 2 * i + 1 < count ? w[i] : (2 * i < count ? w[i] & 0xFFFFu : 0u);
+    }
+  }
+  R r;
+#pragma unroll
+  for (int i = 0; i < R::pieces; ++i) r.w[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  return r;
+}
+
+template <int DT, int E, bool VEC>
+__device__ __forceinline__ Raw<DT, E> load_any(const typename Elem<DT>::T* p, int count, const void* lo, const void* hi, bool wide = false) {
+  if constexpr (VEC) return load_raw<DT, E, true>(p, count, wide);
+  else return load_shifted<DT, E>(p, count, lo, hi);
 }
 
 // the values of 16 bytes
@@ -156,8 +229,14 @@ __device__ __forceinline__ void widen_raw(const Raw<DT, E>& r, float* v) {
 }
 
 template <int DT, int E, bool VEC>
-__device__ __forceinline__ void store_values(typename Elem<DT>::T* p, const float* v, int count) {
+__device__ __forceinline__ void store_values(typename Elem<DT>::T* p, const float* v, int count, bool wide = false) {
   using R = Raw<DT, E>;
+  if constexpr (VEC && R::pieces == 2) {
+    if (wide && count == E) {
+      store32(p, narrow16<DT>(v), narrow16<DT>(v + R::per));
+      return;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < R::pieces; ++i) {
     if (VEC && count >= (i + 1) * R::per) {

@@ -34,9 +34,11 @@ struct QuantParams {
   int64_t ld;
   int64_t rows;
   int64_t units;     // rows * groups
+  const void* x_end;
   uint32_t k, blocks, groups;  // values, blocks of 32, groups of 4 blocks per row
   uint8_t* codes;
   uint8_t* scales;
+  bool wide;         // every row of x starts on a 32-byte boundary
 };
 
 // A lane takes 32 bytes of x (8 fp32 or 16 16-bit values), and the lanes of 128 values (4 blocks) write 64 bytes of codes and the
@@ -45,7 +47,7 @@ template <int DT, bool VEC>
 __global__ void __launch_bounds__(kQuantThreads, 4) mx4_quantize_kernel(const __grid_constant__ QuantParams p) {
   using T = typename Elem<DT>::T;
   constexpr int E = 32 / (int)sizeof(T), LPB = kMxBlock / E, LPU = 4 * LPB;  // values per lane, lanes per block and per 128 values
-  constexpr int U = kQuantInFlight;
+  constexpr int U = VEC ? kQuantInFlight : 2;
   asm volatile("griddepcontrol.launch_dependents;");  // the product may set itself up; it waits for this grid's end
   const int lane = threadIdx.x & 31, sub = lane % LPU;
   const int64_t warp = ((int64_t)blockIdx.x * kQuantThreads + threadIdx.x) >> 5;
@@ -61,11 +63,12 @@ __global__ void __launch_bounds__(kQuantThreads, 4) mx4_quantize_kernel(const __
       group[u] = (uint32_t)(i - row[u] * p.groups);
       const uint32_t at = group[u] * 128 + sub * E;
       const int count = i < p.units && at < p.k ? (int)min((uint32_t)E, p.k - at) : 0;
-      if (count > 0) raw[u] = load_raw<DT, E, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count);
+      if (count > 0) raw[u] = load_any<DT, E, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count, p.x, p.x_end, p.wide);
       else memset(&raw[u], 0, sizeof(raw[u]));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if (u0 + u * (32 / LPU) >= p.units) break;  // the same for the whole warp
       uint32_t m = amax_raw<DT, E>(raw[u]);
 #pragma unroll
       for (int d = 1; d < LPB; d <<= 1) m = max(m, __shfl_xor_sync(kAll, m, d));
@@ -106,7 +109,8 @@ struct OutParams {
 
 __device__ __forceinline__ float activate(float v, float bias, uint32_t relu) {
   v += bias;
-  return relu && v < 0.f ? 0.f : v;  // a NaN stays one
+  if (relu) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v));  // a NaN stays one
+  return v;
 }
 
 __device__ __forceinline__ void put(const OutParams& o, int64_t i, int64_t j, float v) {
@@ -130,6 +134,7 @@ struct FewParams {
   uint32_t k, blocks, groups;
   int32_t m;
   uint32_t x_dtype, vec;
+  const void* x_end;
   OutParams out;
 };
 
@@ -146,31 +151,45 @@ __device__ __forceinline__ uint32_t twice4(uint32_t codes) {
   return ((pos | 0x80808080u) - neg) ^ 0x80808080u;  // no borrow crosses a byte
 }
 
+// The block's copy of x: a block's 32 signed bytes go to two arrays of 16-byte halves, so that neighbouring lanes' reads of
+// neighbouring blocks hit neighbouring banks. `padded` blocks per row, a multiple of 32. kFewInFlight loads are under way at a time:
+// this phase is nothing but their latency.
+constexpr int kFewInFlight = 4;
+template <int DT, bool VEC>
+__device__ __forceinline__ void few_stage(const FewParams& p, int mt, int4* sx, float* ss, uint32_t padded) {
+  using T = typename Elem<DT>::T;
+  constexpr int U = VEC ? kFewInFlight : 2;
+  const uint32_t units = (uint32_t)mt * padded * 4;  // chunks of 8 values: whole warps
+  for (uint32_t i0 = threadIdx.x; i0 < units; i0 += kFewThreads * U) {
+    Raw<DT, 8> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t i = i0 + u * kFewThreads, row = i / (padded * 4), c = i - row * padded * 4;
+      const int count = i < units && (int)row < p.m && c * 8 < p.k ? (int)min(8u, p.k - c * 8) : 0;
+      if (count > 0) raw[u] = load_any<DT, 8, VEC>(reinterpret_cast<const T*>(p.x) + (int64_t)row * p.ld + c * 8, count, p.x, p.x_end);
+      else memset(&raw[u], 0, sizeof(raw[u]));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t i = i0 + u * kFewThreads, row = i / (padded * 4), c = i - row * padded * 4;
+      if (i >= units) break;  // the same for a whole warp
+      float v[8];
+      widen_raw<DT, 8>(raw[u], v);
+      uint32_t m = amax_raw<DT, 8>(raw[u]);
+      m = max(m, __shfl_xor_sync(kAll, m, 1));
+      m = max(m, __shfl_xor_sync(kAll, m, 2));
+      const uint32_t s = mx_scale_byte(m);
+      const uint32_t codes = s == kMxNan ? 0u : mx_encode8(v, mx_inv_scale(s));
+      uint2* dst = reinterpret_cast<uint2*>(sx + (row * 2 + ((c >> 1) & 1)) * padded + (c >> 2)) + (c & 1);
+      *dst = make_uint2(twice4(codes), twice4(codes >> 16));
+      if ((c & 3) == 0) ss[row * padded + (c >> 2)] = mx_scale(s);
+    }
+  }
+}
 template <int DT>
 __device__ __forceinline__ void few_stage(const FewParams& p, int mt, int4* sx, float* ss, uint32_t padded) {
-  // 4 lanes per block of x; the block's 32 signed bytes go to two arrays of 16-byte halves, so that neighbouring lanes'
-  // reads of neighbouring blocks hit neighbouring banks
-  using T = typename Elem<DT>::T;
-  const uint32_t units = (uint32_t)mt * padded * 4;  // chunks of 8 values; `padded` is a multiple of 32: whole warps
-  for (uint32_t i = threadIdx.x; i < units; i += kFewThreads) {
-    const uint32_t row = i / (padded * 4), c = i - row * padded * 4, b = c >> 2;
-    const int count = (int)row < p.m && c * 8 < p.k ? (int)min(8u, p.k - c * 8) : 0;
-    Raw<DT, 8> raw;
-    const T* at = reinterpret_cast<const T*>(p.x) + (int64_t)row * p.ld + c * 8;
-    if (count > 0) raw = p.vec ? load_raw<DT, 8, true>(at, count) : load_raw<DT, 8, false>(at, count);
-    else memset(&raw, 0, sizeof(raw));
-    float v[8];
-    widen_raw<DT, 8>(raw, v);
-    uint32_t m = amax_raw<DT, 8>(raw);
-    m = max(m, __shfl_xor_sync(kAll, m, 1));
-    m = max(m, __shfl_xor_sync(kAll, m, 2));
-    const uint32_t s = mx_scale_byte(m);
-    const uint32_t codes = s == kMxNan ? 0u : mx_encode8(v, mx_inv_scale(s));
-    const uint32_t half = (c >> 1) & 1;
-    uint2* dst = reinterpret_cast<uint2*>(sx + (row * 2 + half) * padded + b) + (c & 1);
-    *dst = make_uint2(twice4(codes), twice4(codes >> 16));
-    if ((c & 3) == 0) ss[row * padded + b] = mx_scale(s);
-  }
+  if (p.vec) few_stage<DT, true>(p, mt, sx, ss, padded);
+  else few_stage<DT, false>(p, mt, sx, ss, padded);
 }
 
 // A warp per output column: lane b takes block b, b + 32, ... of the column's weights (16 bytes each, 512 bytes per warp and
@@ -241,31 +260,41 @@ __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_const
 
 // ------------------------------------------------------------------ tensor cores ----
 
-constexpr int kGemmThreads = 192;  // warp 0 loads, warp 1 issues the products, warps 2..5 write results
+constexpr int kGemmThreads = 320;  // warp 0 loads, warp 1 issues the products, warps 2..9 write results
 constexpr int kTileM = 128;        // rows of x per tile: lanes of tensor memory
-constexpr int kSlab = 256;         // k per stage: 128 bytes of codes per row, four instructions of k = 64
+constexpr int kSlab = 256;         // k of a 128-byte row of codes: four instructions
 constexpr uint64_t kStallNs = 2000000000ull;
 
-template <int TN>  // output columns per tile
+template <int TN>  // output columns per tile: 64 or 128
 struct GemmShape {
-  static constexpr uint32_t a_bytes = kTileM * 128, b_bytes = TN * 128, s_bytes = 1024;  // 2 scale tiles of 512 bytes
-  static constexpr uint32_t stage_bytes = a_bytes + b_bytes + 2 * s_bytes;
-  static constexpr int stages = TN == 128 ? 5 : 6;
-  static constexpr uint32_t out_at = stage_bytes * stages;                    // two pieces of 32 rows x 128 bytes per warp
-  static constexpr uint32_t bias_at = out_at + 4 * 2 * 4096;
-  static constexpr uint32_t smem = bias_at + 4 * TN * 4 + 1024;  // + room to align to 1024
-  static constexpr uint32_t acc_cols = TN;                       // two accumulators, then 16 columns of scales per stage
-  static constexpr uint32_t scale_col = 2 * TN;
-  static_assert(scale_col + 16 * stages <= 512, "tensor memory has 512 columns");
+  // A stage holds `slabs` pieces of k = 256: 128 bytes of codes per row each, four instructions of k = 64. What the issuing lane
+  // does per stage besides issuing (waiting, electing, committing) takes as long as eight instructions run, hence two for
+  // the tile that large products use.
+  static constexpr int slabs = TN == 64 ? 1 : 2;
+  static constexpr uint32_t a_slab = kTileM * 128, b_slab = TN * 128;
+  static constexpr uint32_t b_at = slabs * a_slab, scale_at = b_at + slabs * b_slab;  // a stage: codes of x, of the weights, scales
+  static constexpr uint32_t scale_bytes = slabs * 1024;                              // per operand: 512 bytes per 128 rows and k = 128
+  static constexpr uint32_t stage_bytes = scale_at + 2 * scale_bytes;
+  static constexpr int stages = TN == 64 ? 6 : 3;
+  static constexpr uint32_t out_at = stage_bytes * stages;  // a piece of 32 rows x 64 bytes per writing warp
+  static constexpr uint32_t bias_at = out_at + 8 * 2048;
+  static constexpr uint32_t smem = bias_at + 8 * (TN / 2) * 4 + 1024;  // + room to align to 1024
+  // Tensor memory: two accumulators, then two sets of scales (copies and products run in the order of their issue, so a set may be
+  // overwritten by the copies of the stage after the next)
+  static constexpr uint32_t acc_cols = TN, scale_col = 2 * TN, scale_cols = slabs * 16;
+  static_assert(scale_col + 2 * scale_cols <= 512, "tensor memory has 512 columns");
+  static_assert(smem <= 227 * 1024, "shared memory of a block");
+  // 64 columns: an odd tile starts in the middle of a tile of scales, two of its four columns further on
+  static __device__ __forceinline__ uint32_t half_shift(uint32_t tn) { return TN % 128 ? (tn & 1) * 2 : 0; }
 };
 
 struct GemmParams {
   const uint8_t* a_scales;  // x
   const uint8_t* b_scales;  // weights
   int64_t m, n;
-  uint32_t k, groups, slabs;
+  uint32_t k, groups, stages_k;  // stages_k: stages that cover k
   uint32_t n_tiles;
-  uint32_t bulk_y;          // y can be written by bulk copies (16-byte aligned rows)
+  uint32_t wide_y;          // every row of y starts on a 32-byte boundary
   int64_t tiles;
   uint32_t* status;
   OutParams out;
@@ -311,7 +340,7 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile("{\n\t.reg .pred p;\n\t"
-               "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+               "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
                "selp.u32 %0, 1, 0, p;\n\t}"
                : "=r"(ok)
                : "r"(bar), "r"(parity)
@@ -323,13 +352,13 @@ __device__ __forceinline__ uint64_t now_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// Waits for the phase `parity` of a barrier, two seconds at most; false: it did not come (or another role gave up). The
-// clock is not read before a wait has failed often: reading it takes longer than most waits.
+// Waits for the phase `parity` of a barrier, two seconds at most; false: it did not come (or another role gave up). It polls (a
+// suspended wait took longer to come back: 2 us of 47 for a 16384 x 2048 x 2048 product), and reads the clock rarely.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
   uint64_t t0 = 0;
   for (uint32_t i = 1;; ++i) {
     if (bar_try(bar, parity)) return true;
-    if ((i & 255) == 0) {
+    if ((i & 0xFFFF) == 0) {
       if (*dead) return false;
       const uint64_t t = now_ns();
       if (t0 == 0) t0 = t;
@@ -352,19 +381,13 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-__device__ __forceinline__ void bulk_store(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
-               : "memory");
-}
-
-// Shared-memory matrix descriptor, K-major rows of 128 bytes with the 128-byte swizzle: groups of 8 rows are 1024 bytes apart
-__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
-  return (uint64_t)((addr >> 4) & 0x3FFF) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
-}
-// 32 rows of 16 bytes without a swizzle (a scale tile): groups of 8 rows are 128 bytes apart
-__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
-  return (uint64_t)((addr >> 4) & 0x3FFF) | (8ull << 16) | (8ull << 32) | (1ull << 46);
-}
+// Shared-memory matrix descriptors; the low word holds the address, the high word is constant.
+// Codes: K-major rows of 128 bytes with the 128-byte swizzle, groups of 8 rows 1024 bytes apart.
+constexpr uint32_t kTileDescHi = 64u | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t tile_desc_lo(uint32_t addr) { return (addr >> 4) | (1u << 16); }
+// Scales: 32 rows of 16 bytes without a swizzle, groups of 8 rows 128 bytes apart.
+constexpr uint32_t kScaleDescHi = 8u | (1u << 14);
+__device__ __forceinline__ uint32_t scale_desc_lo(uint32_t addr) { return (addr >> 4) | (8u << 16); }
 // Instruction descriptor: both operands E2M1, K-major, scales UE8M0, fp32 accumulator; `id`: which two of a row's four scale
 // bytes (0 or 2) this instruction's two blocks use
 template <int TN>
@@ -372,14 +395,20 @@ __device__ __forceinline__ uint32_t inst_desc(uint32_t id) {
   return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TN >> 3) << 17) | (1u << 23) | ((uint32_t)(kTileM >> 7) << 27) | (id << 29);
 }
 
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t desc_lo) {
+  asm volatile("{\n\t.reg .b64 d;\n\t"
+               "mov.b64 d, {%1, %2};\n\t"
+               "tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}" ::"r"(tmem),
+               "r"(desc_lo), "n"(kScaleDescHi)
+               : "memory");
 }
-__device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t inst, uint32_t sa, uint32_t sb, uint32_t add) {
-  asm volatile("{\n\t.reg .pred p;\n\t"
+__device__ __forceinline__ void mma_mx4(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t inst, uint32_t sa, uint32_t sb, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
                "setp.ne.b32 p, %6, 0;\n\t"
-               "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-               "l"(a), "l"(b), "r"(inst), "r"(sa), "r"(sb), "r"(add)
+               "mov.b64 a, {%1, %7};\n\t"
+               "mov.b64 b, {%2, %7};\n\t"
+               "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+               "r"(a_lo), "r"(b_lo), "r"(inst), "r"(sa), "r"(sb), "r"(add), "n"(kTileDescHi)
                : "memory");
 }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
@@ -400,16 +429,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
 }
 
 // One block per SM walks over the tiles (128 rows of x times TN output columns); output columns run fastest, so that the blocks
-// at work share the rows of x in L2. Stages of k = 256 go through a ring of shared memory, scales from there to tensor memory ahead
+// at work share the rows of x in L2. Stages go through a ring of shared memory, scales from there to tensor memory ahead
 // of the products that use them; two accumulators in tensor memory, so that a tile is written while the next one is computed. A
-// lane of tensor memory is a row of x: each of the four writing warps takes its 32 rows in pieces of 128 bytes, adds the bias, rounds, and
-// leaves the piece in shared memory (128-byte swizzle: a lane writes 16 bytes of its own row without bank conflicts), from where
-// one bulk copy writes 32 rows and clips what lies beyond y; a y whose rows do not start on 16 bytes is written by plain
-// stores from there.
+// lane of tensor memory is a row of x: each of the eight writing warps takes its 32 rows and half of the columns, adds the bias, rounds, and a lane stores 32
+// bytes of its row at a time, whole sectors. A y whose rows do not start on 32 bytes goes through shared memory instead
+// (16-byte pieces exchanged between rows, so that there are no bank conflicts), and half a warp writes a row's columns.
 template <int TN, int DT>
 __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap a_map,
                                                                   const __grid_constant__ CUtensorMap b_map,
-                                                                  const __grid_constant__ CUtensorMap y_map,
                                                                   const __grid_constant__ GemmParams p) {
   using G = GemmShape<TN>;
   using T = typename Elem<DT>::T;
@@ -429,7 +456,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < G::stages; ++s) bar_init(full(s), 1), bar_init(empty(s), 1);
-    for (int a = 0; a < 2; ++a) bar_init(acc_full(a), 1), bar_init(acc_empty(a), 4);
+    for (int a = 0; a < 2; ++a) bar_init(acc_full(a), 1), bar_init(acc_empty(a), 8);
     bar_init(drained, 1);
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -447,67 +474,83 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
   asm volatile("griddepcontrol.wait;" ::: "memory");  // x may be the result of the launch before this one
 
   if (warp == 0) {
-    uint32_t it = 0;  // stages filled so far
+    uint32_t st = 0, phase = 0;
+    uint64_t filled = 0;
     bool ok = true;
     for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next()) {
       const uint8_t* sa = p.a_scales + (size_t)w.tm * p.groups * 512;
       const uint8_t* sb = p.b_scales + (size_t)(w.tn * (uint32_t)TN >> 7) * p.groups * 512;
-      for (uint32_t s = 0; s < p.slabs; ++s, ++it) {
-        const int st = it % G::stages;
-        if (it >= G::stages && !(ok = __all_sync(kAll, bar_wait(empty(st), (it / G::stages - 1) & 1, &dead)))) break;
+      for (uint32_t s = 0; s < p.stages_k; ++s) {
+        if (filled >= (uint64_t)G::stages && !(ok = __all_sync(kAll, bar_wait(empty(st), phase ^ 1, &dead)))) break;
         if (elect_one()) {
-          const uint32_t at = base + st * G::stage_bytes;
-          const uint32_t sc = min(2u, p.groups - 2 * s) * 512;  // scale bytes of this slab, per operand
-          bar_expect(full(st), G::a_bytes + G::b_bytes + 2 * sc);
-          tma_load(at, &a_map, (int32_t)(s * 128), (int32_t)(w.tm * kTileM), full(st));
-          tma_load(at + G::a_bytes, &b_map, (int32_t)(s * 128), (int32_t)(w.tn * TN), full(st));
-          bulk_load(at + G::a_bytes + G::b_bytes, sa + (size_t)s * 1024, sc, full(st));
-          bulk_load(at + G::a_bytes + G::b_bytes + G::s_bytes, sb + (size_t)s * 1024, sc, full(st));
+          const uint32_t at = base + st * G::stage_bytes, sc_at = at + G::scale_at;
+          const uint32_t slabs = min((uint32_t)G::slabs, (p.groups + 1) / 2 - G::slabs * s);          // pieces of k = 256 that exist
+          const uint32_t sc = min((uint32_t)G::slabs * 2, p.groups - G::slabs * 2 * s) * 512;  // scale bytes per operand
+          bar_expect(full(st), slabs * (G::a_slab + G::b_slab) + 2 * sc);
+          for (uint32_t h = 0; h < slabs; ++h) {
+            tma_load(at + h * G::a_slab, &a_map, (int32_t)((s * G::slabs + h) * 128), (int32_t)(w.tm * kTileM), full(st));
+            tma_load(at + G::b_at + h * G::b_slab, &b_map, (int32_t)((s * G::slabs + h) * 128), (int32_t)(w.tn * TN), full(st));
+          }
+          bulk_load(sc_at, sa + (size_t)s * G::scale_bytes, sc, full(st));
+          bulk_load(sc_at + G::scale_bytes, sb + (size_t)s * G::scale_bytes, sc, full(st));
         }
         __syncwarp();
+        ++filled;
+        if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
       }
     }
     // Every copy that this warp started has to land before the block ends. The products wait for each of them; only
     // when a wait has run out are they waited for here.
     if (!ok || dead) {
       volatile int none = 0;
-      const uint32_t from = it > G::stages ? it - G::stages : 0;
-      for (uint32_t i = from; i < it; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
+      const uint64_t from = filled > G::stages ? filled - G::stages : 0;
+      for (uint64_t i = from; i < filled; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
     }
   } else if (warp == 1) {
-    uint32_t it = 0, done = 0;
-    bool ok = true;
+    // What one lane can issue bounds this role (an instruction takes it some 40 cycles), so everything else is kept short:
+    // stage and phase are counted along, and the next stage's barrier is asked while the instructions of this one are issued.
+    uint32_t st = 0, phase = 0, done = 0;
+    bool ok = true, ready = bar_try(full(0), 0);
     for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next(), ++done) {
       const int acc = done & 1;
       if (done >= 2 && !(ok = __all_sync(kAll, bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead)))) break;
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t d = tmem + acc * G::acc_cols;
-      // a tile of 64 columns that starts in the middle of a scale tile uses the upper half of its four columns
-      const uint32_t half = TN == 64 ? (w.tn & 1) * 2 : 0;
-      for (uint32_t s = 0; s < p.slabs; ++s, ++it) {
-        const int st = it % G::stages;
-        if (!(ok = __all_sync(kAll, bar_wait(full(st), (it / G::stages) & 1, &dead)))) break;
+      const uint32_t half = G::half_shift(w.tn);
+      for (uint32_t s = 0; s < p.stages_k; ++s) {
+        if (!__all_sync(kAll, ready) && !(ok = __all_sync(kAll, bar_wait(full(st), phase, &dead)))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t at = base + st * G::stage_bytes, sc = at + G::a_bytes + G::b_bytes;
-        const uint32_t sfa = tmem + G::scale_col + 16 * st, sfb = sfa + 8;
-        const uint32_t left = p.k - s * kSlab;
-        const int steps = left >= (uint32_t)kSlab ? 4 : (int)((left + 63) / 64);
+        const uint32_t at = base + st * G::stage_bytes;
+        const uint32_t this_empty = empty(st);
+        const uint32_t sf = tmem + G::scale_col + G::scale_cols * (s & 1);
+        if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
         if (elect_one()) {
+          const uint32_t a_lo = tile_desc_lo(at), b_lo = tile_desc_lo(at + G::b_at), sc_lo = scale_desc_lo(at + G::scale_at);
+          // copies of scales for k = 128 (two instructions), and instruction j of the stage
+          auto scales = [&](int g) {
+            copy_scales(sf + 8 * g, sc_lo + 32 * g);
+            copy_scales(sf + 8 * g + 4, sc_lo + (G::scale_bytes >> 4) + 32 * g);
+          };
+          auto product = [&](int j) {
+            mma_mx4(d, a_lo + (j >> 2) * (G::a_slab >> 4) + 2 * (j & 3), b_lo + (j >> 2) * (G::b_slab >> 4) + 2 * (j & 3),
+                    inst_desc<TN>((j & 1) * 2), sf + 8 * (j >> 1), sf + 8 * (j >> 1) + 4 + half, s | j);
+          };
+          constexpr int kSteps = 4 * G::slabs;
+          const uint32_t left = p.k - s * (G::slabs * kSlab);
+          if (left > 64u * (kSteps - 1)) {
 #pragma unroll
-          for (int g = 0; g < 2; ++g)
-            if (2 * g < steps) {
-              copy_scales(sfa + 4 * g, scale_desc(sc + 512 * g));
-              copy_scales(sfb + 4 * g, scale_desc(sc + G::s_bytes + 512 * g));
-            }
+            for (int g = 0; g < kSteps / 2; ++g) scales(g);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (j < steps)
-              mma_mx4(d, tile_desc(at + 32 * j), tile_desc(at + G::a_bytes + 32 * j), inst_desc<TN>((j & 1) * 2), sfa + 4 * (j >> 1),
-                      sfb + 4 * (j >> 1) + half, s > 0 || j > 0);
-          mma_commit(empty(st));
-          if (s + 1 == p.slabs) mma_commit(acc_full(acc));
+            for (int j = 0; j < kSteps; ++j) product(j);
+          } else {
+            const int steps = (int)((left + 63) / 64);
+            for (int g = 0; 2 * g < steps; ++g) scales(g);
+            for (int j = 0; j < steps; ++j) product(j);
+          }
+          mma_commit(this_empty);
+          if (s + 1 == p.stages_k) mma_commit(acc_full(acc));
         }
         __syncwarp();
+        ready = bar_try(full(st), phase);
       }
     }
     if (!ok || dead) {  // the products under way read shared memory and write tensor memory: let them end
@@ -517,77 +560,66 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
       bar_wait(drained, 0, &none);
     }
   } else {
-    constexpr int kCols = 128 / (int)sizeof(T);  // output columns of a piece
     const int quarter = warp & 3;                // the 32 lanes of tensor memory that this warp may read
-    const uint32_t out0 = base + G::out_at + quarter * 8192;
-    uint8_t* const out_ptr = smem + G::out_at + quarter * 8192;
-    float* const bias = reinterpret_cast<float*>(smem + G::bias_at) + quarter * TN;
-    uint32_t done = 0, pieces = 0;
+    const int c0 = warp < 6 ? 0 : TN / 2;        // two warps share them, each takes half of the columns
+    uint8_t* const out_ptr = smem + G::out_at + (warp - 2) * 2048;
+    float* const bias = reinterpret_cast<float*>(smem + G::bias_at) + (warp - 2) * (TN / 2);
+    uint32_t done = 0;
     for (TileWalk w(p.n_tiles); w.t < p.tiles; w.next(), ++done) {
       const int acc = done & 1;
-      const int64_t i0 = (int64_t)w.tm * kTileM + quarter * 32, j0 = (int64_t)w.tn * TN;
-      for (int c = lane; c < TN; c += 32) bias[c] = p.out.bias && j0 + c < p.n ? p.out.bias[j0 + c] : 0.f;
+      const int64_t i0 = (int64_t)w.tm * kTileM + quarter * 32, j0 = (int64_t)w.tn * TN + c0;
+      for (int c = lane; c < TN / 2; c += 32) bias[c] = p.out.bias && j0 + c < p.n ? p.out.bias[j0 + c] : 0.f;
       __syncwarp();
       const bool ok = bar_wait(acc_full(acc), (done / 2) & 1, &dead);
       if (!__all_sync(kAll, ok)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const bool mine = i0 + lane < p.m;
+      T* const own = reinterpret_cast<T*>(p.out.y) + (mine ? i0 + lane : 0) * p.out.ld + j0;
 #pragma unroll 1
-      for (int c = 0; c < TN; c += kCols, ++pieces) {
-        const uint32_t buf = (pieces & 1) * 4096;
-        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // the piece before the last has left its half
-        __syncwarp();
-#pragma unroll
-        for (int h = 0; h < kCols; h += 32) {
-          uint32_t r[32];
-          tmem_load32(tmem + acc * G::acc_cols + c + h + ((uint32_t)(quarter * 32) << 16), r);
-          if (c + h + 32 >= TN) {  // the accumulator is read: the next tile but one may overwrite it
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) bar_arrive(acc_empty(acc));
-          }
-          float v[32];
-#pragma unroll
-          for (int q = 0; q < 32; q += 4) {
-            const float4 b4 = *reinterpret_cast<const float4*>(bias + c + h + q);
-            v[q] = activate(__uint_as_float(r[q]), b4.x, p.out.relu);
-            v[q + 1] = activate(__uint_as_float(r[q + 1]), b4.y, p.out.relu);
-            v[q + 2] = activate(__uint_as_float(r[q + 2]), b4.z, p.out.relu);
-            v[q + 3] = activate(__uint_as_float(r[q + 3]), b4.w, p.out.relu);
-          }
-          constexpr int kPer = 16 / (int)sizeof(T);  // values per 16 bytes
-#pragma unroll
-          for (int q = 0; q < 32; q += kPer) {
-            const uint4 w = narrow16<DT>(v + q);
-            const int sixteen = (h + q) / kPer;  // which 16 bytes of the row's 128
-            *reinterpret_cast<uint4*>(out_ptr + buf + lane * 128 + ((sixteen ^ (lane & 7)) << 4)) = w;
-          }
+      for (int c = 0; c < TN / 2; c += 32) {
+        uint32_t r[32];
+        tmem_load32(tmem + acc * G::acc_cols + c0 + c + ((uint32_t)(quarter * 32) << 16), r);
+        if (c + 32 >= TN / 2) {  // the accumulator is read: the next tile but one may overwrite it
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(acc_empty(acc));
         }
-        if (p.bulk_y) {
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (i0 < p.m && j0 + c < p.n && elect_one()) bulk_store(&y_map, out0 + buf, (int32_t)(j0 + c), (int32_t)i0);
-          __syncwarp();
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");  // a group of its own in the lane that stored, empty ones elsewhere
-        } else {
-          __syncwarp();
-          T* y = reinterpret_cast<T*>(p.out.y);
-          constexpr int kOwn = 4 / (int)sizeof(T);  // values per lane and row
-          const int64_t j = j0 + c + lane * kOwn;
-#pragma unroll 4
-          for (int i = 0; i < 32; ++i) {
-            T two[kOwn];
-            memcpy(two, out_ptr + buf + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4, 4);
-            if (i0 + i < p.m) {
+        float v[32];
 #pragma unroll
-              for (int q = 0; q < kOwn; ++q)
-                if (j + q < p.n) y[(i0 + i) * p.out.ld + j + q] = two[q];
-            }
+        for (int q = 0; q < 32; q += 4) {
+          const float4 b4 = *reinterpret_cast<const float4*>(bias + c + q);
+          v[q] = activate(__uint_as_float(r[q]), b4.x, p.out.relu);
+          v[q + 1] = activate(__uint_as_float(r[q + 1]), b4.y, p.out.relu);
+          v[q + 2] = activate(__uint_as_float(r[q + 2]), b4.z, p.out.relu);
+          v[q + 3] = activate(__uint_as_float(r[q + 3]), b4.w, p.out.relu);
+        }
+        constexpr int kPer = 16 / (int)sizeof(T);  // values per 16 bytes
+        if (p.wide_y && j0 + c + 32 <= p.n) {
+          if (mine) {
+#pragma unroll
+            for (int q = 0; q < 32; q += 2 * kPer) store32(own + c + q, narrow16<DT>(v + q), narrow16<DT>(v + q + kPer));
           }
-          __syncwarp();
+        } else {
+          // 16 columns at a time through shared memory: then half a warp has a row's 16 columns
+          const int64_t j = j0 + c + (lane & 15);
+          T* y = reinterpret_cast<T*>(p.out.y) + (i0 + (lane >> 4)) * p.out.ld + j;
+#pragma unroll
+          for (int h = 0; h < 32; h += 16) {
+#pragma unroll
+            for (int q = 0; q < 16; q += kPer)
+              *reinterpret_cast<uint4*>(out_ptr + lane * 64 + (((q / kPer) ^ ((lane >> 1) & 3)) << 4)) = narrow16<DT>(v + h + q);
+            __syncwarp();
+#pragma unroll 8
+            for (int i = 0; i < 32; i += 2) {
+              const int row = i + (lane >> 4), col = lane & 15;
+              const T x = *reinterpret_cast<const T*>(out_ptr + row * 64 + (((col / kPer) ^ ((row >> 1) & 3)) << 4) + (col % kPer) * sizeof(T));
+              if (i0 + row < p.m && j + h < p.n) y[i * p.out.ld + h] = x;
+            }
+            __syncwarp();
+          }
         }
       }
     }
-    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // shared memory outlives the copies that read it
   }
   __syncwarp();  // the one lane that loaded or issued rejoins its warp
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -615,7 +647,8 @@ uint32_t size_of(uint32_t dtype) { return dtype == MFET_F32 ? 4 : 2; }
 template <int DT>
 cudaError_t launch_quantize(const QuantParams& p, bool vec, cudaStream_t s) {
   constexpr int kLanesPerUnit = 4 * (int)sizeof(typename Elem<DT>::T);  // 128 values, 32 bytes per lane
-  const int64_t per_block = (int64_t)(kQuantThreads / kLanesPerUnit) * kQuantInFlight;
+  // a warp takes several units at a time only when there are enough for every SM
+  const int64_t per_block = (int64_t)(kQuantThreads / kLanesPerUnit);
   const int64_t want = (p.units + per_block - 1) / per_block, most = (int64_t)sm_count() * 16;
   const unsigned b = (unsigned)(want < most ? want : most);
   if (vec) mx4_quantize_kernel<DT, true><<<b, kQuantThreads, 0, s>>>(p);
@@ -625,8 +658,9 @@ cudaError_t launch_quantize(const QuantParams& p, bool vec, cudaStream_t s) {
 
 int quantize(const void* x, uint32_t dtype, int64_t rows, int64_t k, int64_t ld, void* codes, void* scales, cudaStream_t s) {
   const Dims d = dims_of(k);
-  QuantParams p{(const uint8_t*)x, ld, rows, rows * (int64_t)d.groups, (uint32_t)k, d.blocks, d.groups, (uint8_t*)codes,
-                (uint8_t*)scales};
+  QuantParams p{(const uint8_t*)x, ld, rows, rows * (int64_t)d.groups, (const uint8_t*)x + ((rows - 1) * ld + k) * size_of(dtype),
+                (uint32_t)k, d.blocks, d.groups, (uint8_t*)codes, (uint8_t*)scales,
+                aligned(x, 32) && (uint64_t)ld * size_of(dtype) % 32 == 0};
   const bool vec = aligned(x, 16) && (uint64_t)ld * size_of(dtype) % 16 == 0;
   cudaError_t e;
   switch (dtype) {
@@ -665,25 +699,11 @@ bool code_map(CUtensorMap* map, const void* codes, int64_t rows, uint32_t blocks
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// y [m, n] written in boxes of 32 rows x 128 bytes
-bool out_map(CUtensorMap* map, const OutParams& o, int64_t m, int64_t n) {
-  const EncodeTiled f = encode_tiled();
-  if (!f) return false;
-  const uint32_t size = size_of(o.dtype);
-  const cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)m}, stride[1] = {(cuuint64_t)o.ld * size};
-  const cuuint32_t boxes[2] = {128 / size, 32}, ones[2] = {1, 1};
-  const CUtensorMapDataType t = o.dtype == MFET_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                : o.dtype == MFET_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
-                                                      : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  return f(map, t, 2, o.y, dims, stride, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-           CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int TN, int DT>
 int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
          uint32_t* status, bool after_quantize, cudaStream_t s) {
   const Dims d = dims_of(k);
-  CUtensorMap a, b, y;
+  CUtensorMap a, b;
   if (!code_map(&a, xc, m, d.blocks, kTileM) || !code_map(&b, wc, n, d.blocks, TN)) return MFET_ERR_CUDA;
   GemmParams p;
   p.a_scales = (const uint8_t*)xs;
@@ -692,17 +712,12 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   p.n = n;
   p.k = (uint32_t)k;
   p.groups = d.groups;
-  p.slabs = (uint32_t)((k + kSlab - 1) / kSlab);
+  p.stages_k = (uint32_t)((k + GemmShape<TN>::slabs * kSlab - 1) / (GemmShape<TN>::slabs * kSlab));
   p.n_tiles = (uint32_t)((n + TN - 1) / TN);
   p.tiles = (m + kTileM - 1) / kTileM * p.n_tiles;
   p.status = status;
   p.out = out;
-  p.bulk_y = aligned(out.y, 16) && (uint64_t)out.ld * size_of(out.dtype) % 16 == 0;
-  if (p.bulk_y) {
-    if (!out_map(&y, out, m, n)) return MFET_ERR_CUDA;
-  } else {
-    y = a;  // not used
-  }
+  p.wide_y = aligned(out.y, 32) && (uint64_t)out.ld * size_of(out.dtype) % 32 == 0;
   static std::atomic<uint64_t> ready{0};  // one bit per GPU: the kernel may use this much shared memory there
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return MFET_ERR_CUDA;
@@ -723,15 +738,15 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = after_quantize ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<TN, DT>, a, b, y, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<TN, DT>, a, b, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
 }
 
 template <int DT>
 int product_dt(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
                uint32_t* status, bool after_quantize, cudaStream_t s) {
   // tiles of 128 columns when there is one for every SM, else of 64: twice the blocks
-  const int64_t tiles = (m + kTileM - 1) / kTileM * ((n + 127) / 128);
-  if (tiles >= sm_count()) return gemm<128, DT>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
+  if ((m + kTileM - 1) / kTileM * ((n + 127) / 128) >= sm_count())
+    return gemm<128, DT>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
   return gemm<64, DT>(xc, xs, m, wc, ws, n, k, out, status, after_quantize, s);
 }
 
@@ -814,7 +829,8 @@ int mfet_mx4_linear(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t m, co
   const uint32_t mt = m == 1 ? 1 : m == 2 ? 2 : m <= 4 ? 4 : 8;
   if (m <= kFewMost && (uint64_t)mt * ((d.blocks + 31) & ~31u) * 36 <= 96 * 1024) {
     FewParams p{(const uint8_t*)x, x_ld, (const uint8_t*)w_codes, (const uint8_t*)w_scales, n, (uint32_t)k, d.blocks, d.groups,
-                (int32_t)m, x_dtype, aligned(x, 16) && (uint64_t)x_ld * size_of(x_dtype) % 16 == 0, out};
+                (int32_t)m, x_dtype, aligned(x, 16) && (uint64_t)x_ld * size_of(x_dtype) % 16 == 0,
+                (const uint8_t*)x + ((m - 1) * x_ld + k) * size_of(x_dtype), out};
     const cudaError_t e = mt == 1 ? launch_few<1>(p, s) : mt == 2 ? launch_few<2>(p, s) : mt == 4 ? launch_few<4>(p, s) : launch_few<8>(p, s);
     return e == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
   }

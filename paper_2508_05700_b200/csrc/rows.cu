@@ -15,7 +15,8 @@ namespace {
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kRowsThreads = 256;
-constexpr int kRowsInFlight = 2;
+constexpr int kRowsInFlight = 2;   // rows that a lane group writes at a time
+constexpr int kRowsReadAhead = 4;  // ... and reads: a row of codes takes fewer registers
 constexpr int kRowsBlocksPerSm = 4;
 
 struct RowsParams {
@@ -25,9 +26,11 @@ struct RowsParams {
   int64_t n;
   const int64_t* n_dev;  // nullptr, or the number of entries on the device (at most n are used)
   uint8_t* mem;          // values in (write) or out (read)
+  const uint8_t* mem_end;
   int64_t ld;            // elements between the rows of mem
   uint32_t* status;
   uint32_t dim, row_bytes, lanes_log2, rounds;
+  bool wide;             // every row of mem starts on a 32-byte boundary
 };
 
 __device__ __forceinline__ int64_t live_count(const RowsParams& p) {
@@ -94,7 +97,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
         Raw<SD, E> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (count > 0) raw[u] = load_raw<SD, E, VEC>(src[u] + at, count);
+          if (count > 0) raw[u] = load_any<SD, E, VEC>(src[u] + at, count, p.mem, p.mem_end, p.wide);
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (count > 0) {
@@ -123,7 +126,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
       Raw<SD, E> raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (count > 0) raw[u] = load_raw<SD, E, VEC>(src[u] + at, count);  // does not wait for the list entry
+        if (count > 0) raw[u] = load_any<SD, E, VEC>(src[u] + at, count, p.mem, p.mem_end, p.wide);  // does not wait for the list entry
         else memset(&raw[u], 0, sizeof(raw[u]));
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -193,7 +196,7 @@ template <int TD, int DD, bool VEC, bool ONE>
 __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_read_kernel(const __grid_constant__ RowsParams p) {
   using D = typename Elem<DD>::T;
   constexpr int E = 32 / (int)sizeof(D), LPB = kMxBlock / E;
-  constexpr int U = kRowsInFlight;
+  constexpr int U = kRowsReadAhead;
   const int64_t n = live_count(p);
   const int lane = threadIdx.x & 31;
   const int lanes = 1 << p.lanes_log2, per_warp = 32 >> p.lanes_log2;
@@ -258,7 +261,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_read_kern
             widen_raw<kTable, E>(raw[u], v);
           }
         }
-        store_values<DD, E, VEC>(reinterpret_cast<D*>(p.mem) + i * p.ld + at, v, count);
+        store_values<DD, E, VEC>(reinterpret_cast<D*>(p.mem) + i * p.ld + at, v, count, p.wide);
       }
     }
   }
@@ -295,8 +298,10 @@ int check(const mfet_table_desc_t* d, const int64_t* list, int64_t n, const void
   p->n = n;
   p->mem = static_cast<uint8_t*>(const_cast<void*>(mem));
   p->ld = ld;
+  p->mem_end = n > 0 ? p->mem + ((n - 1) * ld + d->dim) * (mem_dtype == MFET_F32 ? 4 : 2) : p->mem;
   p->dim = d->dim;
   p->row_bytes = (uint32_t)rb;
+  p->wide = (reinterpret_cast<uintptr_t>(mem) & 31u) == 0 && (ld * (mem_dtype == MFET_F32 ? 4 : 2)) % 32 == 0;
   lanes_of(d->dim, mem_dtype, p);
   return MFET_OK;
 }
