@@ -294,7 +294,7 @@ struct GemmParams {
   int64_t m, n;
   uint32_t k, groups, stages_k;  // stages_k: stages that cover k
   uint32_t n_tiles;
-  uint32_t wide_y;          // every row of y starts on a 32-byte boundary
+  uint32_t bulk_y;          // every row of y starts on a 16-byte boundary
   int64_t tiles;
   uint32_t* status;
   OutParams out;
@@ -381,6 +381,11 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
+__device__ __forceinline__ void bulk_store(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
+               : "memory");
+}
+
 // Shared-memory matrix descriptors; the low word holds the address, the high word is constant.
 // Codes: K-major rows of 128 bytes with the 128-byte swizzle, groups of 8 rows 1024 bytes apart.
 constexpr uint32_t kTileDescHi = 64u | (1u << 14) | (2u << 29);
@@ -431,12 +436,15 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
 // One block per SM walks over the tiles (128 rows of x times TN output columns); output columns run fastest, so that the blocks
 // at work share the rows of x in L2. Stages go through a ring of shared memory, scales from there to tensor memory ahead
 // of the products that use them; two accumulators in tensor memory, so that a tile is written while the next one is computed. A
-// lane of tensor memory is a row of x: each of the eight writing warps takes its 32 rows and half of the columns, adds the bias, rounds, and a lane stores 32
-// bytes of its row at a time, whole sectors. A y whose rows do not start on 32 bytes goes through shared memory instead
-// (16-byte pieces exchanged between rows, so that there are no bank conflicts), and half a warp writes a row's columns.
+// lane of tensor memory is a row of x: each of the eight writing warps takes its 32 rows and half of the columns, adds the bias, rounds,
+// and leaves 64 bytes per row at a time in shared memory (16-byte pieces swizzled over the rows: no bank conflicts), from where a bulk
+// copy writes them and clips what lies beyond y. (Stores straight from the registers touch a line per lane, and the barriers of
+// the other roles wait behind them: 43 us instead of 35 for 16384 x 2048 x 2048.) A y whose rows do not start on 16 bytes is written by
+// plain stores from there.
 template <int TN, int DT>
 __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap a_map,
                                                                   const __grid_constant__ CUtensorMap b_map,
+                                                                  const __grid_constant__ CUtensorMap y_map,
                                                                   const __grid_constant__ GemmParams p) {
   using G = GemmShape<TN>;
   using T = typename Elem<DT>::T;
@@ -507,24 +515,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
       for (uint64_t i = from; i < filled; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
     }
   } else if (warp == 1) {
-    // What one lane can issue bounds this role (an instruction takes it some 40 cycles), so everything else is kept short:
-    // stage and phase are counted along, and the next stage's barrier is asked while the instructions of this one are issued.
-    uint32_t st = 0, phase = 0, done = 0;
-    bool ok = true, ready = bar_try(full(0), 0);
-    for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next(), ++done) {
-      const int acc = done & 1;
-      if (done >= 2 && !(ok = __all_sync(kAll, bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead)))) break;
-      const uint32_t d = tmem + acc * G::acc_cols;
-      const uint32_t half = G::half_shift(w.tn);
-      for (uint32_t s = 0; s < p.stages_k; ++s) {
-        if (!__all_sync(kAll, ready) && !(ok = __all_sync(kAll, bar_wait(full(st), phase, &dead)))) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t at = base + st * G::stage_bytes;
-        const uint32_t this_empty = empty(st);
-        const uint32_t sf = tmem + G::scale_col + G::scale_cols * (s & 1);
-        if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-        if (elect_one()) {
+    // One lane runs this role from end to end. The tensor cores' queue is short, so what the lane does between the instructions of two
+    // stages has to be short too: stage and phase are counted along, and the next stage's barrier is asked between this one's instructions.
+    if (elect_one()) {
+      uint32_t st = 0, phase = 0, done = 0;
+      bool ok = true, ready = false;
+      for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next(), ++done) {
+        const int acc = done & 1;
+        if (done >= 2 && !(ok = bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead))) break;
+        const uint32_t d = tmem + acc * G::acc_cols;
+        const uint32_t half = G::half_shift(w.tn);
+        for (uint32_t s = 0; s < p.stages_k; ++s) {
+          if (!ready && !(ok = bar_wait(full(st), phase, &dead))) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t at = base + st * G::stage_bytes;
+          const uint32_t this_empty = empty(st);
+          const uint32_t sf = tmem + G::scale_col + G::scale_cols * (s & 1);
           const uint32_t a_lo = tile_desc_lo(at), b_lo = tile_desc_lo(at + G::b_at), sc_lo = scale_desc_lo(at + G::scale_at);
+          if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
           // copies of scales for k = 128 (two instructions), and instruction j of the stage
           auto scales = [&](int g) {
             copy_scales(sf + 8 * g, sc_lo + 32 * g);
@@ -540,29 +548,31 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
 #pragma unroll
             for (int g = 0; g < kSteps / 2; ++g) scales(g);
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j) product(j);
+            for (int j = 0; j < kSteps / 2; ++j) product(j);
+            ready = bar_try(full(st), phase);
+#pragma unroll
+            for (int j = kSteps / 2; j < kSteps; ++j) product(j);
           } else {
             const int steps = (int)((left + 63) / 64);
             for (int g = 0; 2 * g < steps; ++g) scales(g);
             for (int j = 0; j < steps; ++j) product(j);
+            ready = bar_try(full(st), phase);
           }
           mma_commit(this_empty);
           if (s + 1 == p.stages_k) mma_commit(acc_full(acc));
         }
-        __syncwarp();
-        ready = bar_try(full(st), phase);
       }
-    }
-    if (!ok || dead) {  // the products under way read shared memory and write tensor memory: let them end
-      volatile int none = 0;
-      if (elect_one()) mma_commit(drained);
-      __syncwarp();
-      bar_wait(drained, 0, &none);
+      if (!ok || dead) {  // the products under way read shared memory and write tensor memory: let them end
+        volatile int none = 0;
+        mma_commit(drained);
+        bar_wait(drained, 0, &none);
+      }
     }
   } else {
     const int quarter = warp & 3;                // the 32 lanes of tensor memory that this warp may read
     const int c0 = warp < 6 ? 0 : TN / 2;        // two warps share them, each takes half of the columns
     uint8_t* const out_ptr = smem + G::out_at + (warp - 2) * 2048;
+    const uint32_t out_at = base + G::out_at + (warp - 2) * 2048;
     float* const bias = reinterpret_cast<float*>(smem + G::bias_at) + (warp - 2) * (TN / 2);
     uint32_t done = 0;
     for (TileWalk w(p.n_tiles); w.t < p.tiles; w.next(), ++done) {
@@ -573,8 +583,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
       const bool ok = bar_wait(acc_full(acc), (done / 2) & 1, &dead);
       if (!__all_sync(kAll, ok)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const bool mine = i0 + lane < p.m;
-      T* const own = reinterpret_cast<T*>(p.out.y) + (mine ? i0 + lane : 0) * p.out.ld + j0;
 #pragma unroll 1
       for (int c = 0; c < TN / 2; c += 32) {
         uint32_t r[32];
@@ -594,32 +602,39 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
           v[q + 3] = activate(__uint_as_float(r[q + 3]), b4.w, p.out.relu);
         }
         constexpr int kPer = 16 / (int)sizeof(T);  // values per 16 bytes
-        if (p.wide_y && j0 + c + 32 <= p.n) {
-          if (mine) {
+        constexpr int kCols = 64 / (int)sizeof(T);  // columns of a piece
 #pragma unroll
-            for (int q = 0; q < 32; q += 2 * kPer) store32(own + c + q, narrow16<DT>(v + q), narrow16<DT>(v + q + kPer));
-          }
-        } else {
-          // 16 columns at a time through shared memory: then half a warp has a row's 16 columns
-          const int64_t j = j0 + c + (lane & 15);
-          T* y = reinterpret_cast<T*>(p.out.y) + (i0 + (lane >> 4)) * p.out.ld + j;
-#pragma unroll
-          for (int h = 0; h < 32; h += 16) {
-#pragma unroll
-            for (int q = 0; q < 16; q += kPer)
-              *reinterpret_cast<uint4*>(out_ptr + lane * 64 + (((q / kPer) ^ ((lane >> 1) & 3)) << 4)) = narrow16<DT>(v + h + q);
+        for (int h = 0; h < 32; h += kCols) {
+          if (p.bulk_y) {  // the piece before has left
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             __syncwarp();
+          }
+#pragma unroll
+          for (int q = 0; q < kCols; q += kPer)
+            *reinterpret_cast<uint4*>(out_ptr + lane * 64 + (((q / kPer) ^ ((lane >> 1) & 3)) << 4)) = narrow16<DT>(v + h + q);
+          if (p.bulk_y) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (i0 < p.m && j0 + c + h < p.n && elect_one()) bulk_store(&y_map, out_at, (int32_t)(j0 + c + h), (int32_t)i0);
+            __syncwarp();
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          } else {
+            __syncwarp();
+            // a warp takes one row's 32 columns (16 bits) or two rows' 16 (fp32)
+            const int64_t j = j0 + c + h + lane % kCols;
+            T* y = reinterpret_cast<T*>(p.out.y) + i0 * p.out.ld + j;
 #pragma unroll 8
-            for (int i = 0; i < 32; i += 2) {
-              const int row = i + (lane >> 4), col = lane & 15;
+            for (int i = 0; i < 32; i += 32 / kCols) {
+              const int row = i + lane / kCols, col = lane % kCols;
               const T x = *reinterpret_cast<const T*>(out_ptr + row * 64 + (((col / kPer) ^ ((row >> 1) & 3)) << 4) + (col % kPer) * sizeof(T));
-              if (i0 + row < p.m && j + h < p.n) y[i * p.out.ld + h] = x;
+              if (i0 + row < p.m && j < p.n) y[row * p.out.ld] = x;
             }
             __syncwarp();
           }
         }
       }
     }
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // shared memory outlives the copies that read it
   }
   __syncwarp();  // the one lane that loaded or issued rejoins its warp
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -699,11 +714,25 @@ bool code_map(CUtensorMap* map, const void* codes, int64_t rows, uint32_t blocks
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// y [m, n] written in boxes of 32 rows x 64 bytes
+bool out_map(CUtensorMap* map, const OutParams& o, int64_t m, int64_t n) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const uint32_t size = size_of(o.dtype);
+  const cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)m}, stride[1] = {(cuuint64_t)o.ld * size};
+  const cuuint32_t boxes[2] = {64 / size, 32}, ones[2] = {1, 1};
+  const CUtensorMapDataType t = o.dtype == MFET_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                : o.dtype == MFET_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                      : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return f(map, t, 2, o.y, dims, stride, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+           CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int TN, int DT>
 int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
          uint32_t* status, bool after_quantize, cudaStream_t s) {
   const Dims d = dims_of(k);
-  CUtensorMap a, b;
+  CUtensorMap a, b, y;
   if (!code_map(&a, xc, m, d.blocks, kTileM) || !code_map(&b, wc, n, d.blocks, TN)) return MFET_ERR_CUDA;
   GemmParams p;
   p.a_scales = (const uint8_t*)xs;
@@ -717,7 +746,9 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   p.tiles = (m + kTileM - 1) / kTileM * p.n_tiles;
   p.status = status;
   p.out = out;
-  p.wide_y = aligned(out.y, 32) && (uint64_t)out.ld * size_of(out.dtype) % 32 == 0;
+  p.bulk_y = aligned(out.y, 16) && (uint64_t)out.ld * size_of(out.dtype) % 16 == 0;
+  if (!p.bulk_y) y = a;  // not used
+  else if (!out_map(&y, out, m, n)) return MFET_ERR_CUDA;
   static std::atomic<uint64_t> ready{0};  // one bit per GPU: the kernel may use this much shared memory there
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return MFET_ERR_CUDA;
@@ -738,7 +769,7 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = after_quantize ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<TN, DT>, a, b, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<TN, DT>, a, b, y, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
 }
 
 template <int DT>
