@@ -4,11 +4,13 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmfet.so")
 LIB_CHECKED = os.path.join(HERE, "libmfet_checked.so")  # the same library with -DMFET_CHECKED (see common.cuh)
+FASTCALL = os.path.join(HERE, "_fastcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))  # Python entry of the hot calls
 SOURCES = ["api.cu", "bag.cu", "hash_fill.cu", "dedup.cu", "hostpath.cu", "backward.cu", "rows.cu",
            "gradclip.cu", "mx4.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O3", "-lineinfo",
@@ -19,9 +21,22 @@ def _newest(paths):
     return max(os.path.getmtime(p) for p in paths)
 
 
+def build_fastcall(force: bool = False) -> str:
+    """The binding's extension (host code: csrc/fastcall.c)."""
+    src = os.path.join(CSRC, "fastcall.c")
+    deps = [src, os.path.join(HERE, "..", "include", "mfet.h")]
+    if force or not os.path.exists(FASTCALL) or os.path.getmtime(FASTCALL) < _newest(deps):
+        tmp = FASTCALL + ".tmp.%d" % os.getpid()
+        subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
+                               src, "-o", tmp])
+        os.replace(tmp, FASTCALL)
+    return FASTCALL
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
     """Builds (if out of date) and returns the library; checked=True: the bounds-checked build, in
     which every kernel tests its indices and reports a violation through MFET_DEV_BOUNDS."""
+    build_fastcall(force)
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
     deps = srcs + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "dedup_layout.cuh"), os.path.join(CSRC, "lowbit.cuh"),

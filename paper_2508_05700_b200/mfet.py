@@ -68,6 +68,7 @@ if not os.path.exists(LIB_PATH):
     raise ImportError("libmfet.so is missing: build it with `python -m paper_2508_05700_b200.build` "
                       "(there is no fallback path)")
 _lib = C.CDLL(LIB_PATH)
+from . import _fastcall  # noqa: E402  (built with the library)
 
 _P = C.c_void_p
 _lib.mfet_row_bytes.restype = C.c_uint64
@@ -102,14 +103,6 @@ _lib.mfet_tables_version.argtypes = [_P, C.POINTER(C.c_uint64)]
 _lib.mfet_host_prefetch.argtypes = [_P, C.POINTER(BatchShape), _P, _P, _P, _P]
 _lib.mfet_embedding_bag_backward.argtypes = [_P, C.POINTER(BatchShape), _P, _P, _P, _P, _P, _P, C.c_int32, _P, _P, _P, _P]
 _lib.mfet_launch_count.argtypes = [_P, C.POINTER(C.c_uint64)]
-_lib.mfet_grad_clip.argtypes = [C.POINTER(Grad), C.c_int32, C.c_float, _P, _P, C.c_uint64, _P]
-_lib.mfet_rows_write.argtypes = [C.POINTER(TableDesc), _P, C.c_int64, _P, _P, C.c_uint32, C.c_int64, _P, _P]
-_lib.mfet_rows_read.argtypes = _lib.mfet_rows_write.argtypes
-_lib.mfet_mx4_quantize.argtypes = [_P, C.c_uint32, C.c_int64, C.c_int64, C.c_int64, _P, _P, _P]
-_lib.mfet_mx4_matmul.argtypes = [_P, _P, C.c_int64, _P, _P, C.c_int64, C.c_int64, _P, C.c_uint32, _P, C.c_uint32, C.c_int64, _P,
-                                 _P]
-_lib.mfet_mx4_linear.argtypes = [_P, C.c_uint32, C.c_int64, C.c_int64, _P, _P, C.c_int64, C.c_int64, _P, C.c_uint32, _P,
-                                 C.c_uint32, C.c_int64, _P, C.c_uint64, _P, _P]
 _BYTES = ("mfet_grad_clip_bytes", "mfet_mx4_code_bytes", "mfet_mx4_scale_bytes", "mfet_mx4_linear_bytes")
 for _n in _BYTES:
     getattr(_lib, _n).restype = C.c_uint64
@@ -354,22 +347,6 @@ def mfet_grad_clip_bytes(n_grads: int) -> int:
     return int(_lib.mfet_grad_clip_bytes(n_grads))
 
 
-def mfet_grad_clip(grads, max_norm: float, norm, scratch, scratch_bytes: int, stream=None) -> None:
-    """grads: what make_grads gave."""
-    arr, n = grads
-    _check(_lib.mfet_grad_clip(arr, n, max_norm, _ptr(norm), _ptr(scratch), scratch_bytes, _ptr(stream)), "mfet_grad_clip")
-
-
-def mfet_rows_write(table: TableDesc, rows, n: int, n_dev, values, dtype: int, ld: int, status=None, stream=None) -> None:
-    _check(_lib.mfet_rows_write(C.byref(table), _ptr(rows), n, _ptr(n_dev), _ptr(values), dtype, ld, _ptr(status),
-                                _ptr(stream)), "mfet_rows_write")
-
-
-def mfet_rows_read(table: TableDesc, rows, n: int, n_dev, values, dtype: int, ld: int, status=None, stream=None) -> None:
-    _check(_lib.mfet_rows_read(C.byref(table), _ptr(rows), n, _ptr(n_dev), _ptr(values), dtype, ld, _ptr(status),
-                               _ptr(stream)), "mfet_rows_read")
-
-
 def mfet_mx4_code_bytes(rows: int, k: int) -> int:
     return int(_lib.mfet_mx4_code_bytes(rows, k))
 
@@ -382,17 +359,17 @@ def mfet_mx4_linear_bytes(m: int, k: int) -> int:
     return int(_lib.mfet_mx4_linear_bytes(m, k))
 
 
-def mfet_mx4_quantize(x, dtype: int, ld: int, rows: int, k: int, codes, scales, stream=None) -> None:
-    _check(_lib.mfet_mx4_quantize(_ptr(x), dtype, ld, rows, k, _ptr(codes), _ptr(scales), _ptr(stream)), "mfet_mx4_quantize")
+# The calls that a step makes many times go through a small extension instead of ctypes (csrc/fastcall.c): same names, arguments
+# and errors.
+def _fail(status: int, where: str) -> None:
+    raise MfetError(status, where)
 
 
-def mfet_mx4_matmul(a_codes, a_scales, m: int, w_codes, w_scales, n: int, k: int, bias, act: int, y, y_dtype: int, y_ld: int,
-                    status=None, stream=None) -> None:
-    _check(_lib.mfet_mx4_matmul(_ptr(a_codes), _ptr(a_scales), m, _ptr(w_codes), _ptr(w_scales), n, k, _ptr(bias), act, _ptr(y),
-                                y_dtype, y_ld, _ptr(status), _ptr(stream)), "mfet_mx4_matmul")
-
-
-def mfet_mx4_linear(x, x_dtype: int, x_ld: int, m: int, w_codes, w_scales, n: int, k: int, bias, act: int, y, y_dtype: int,
-                    y_ld: int, scratch, scratch_bytes: int, status=None, stream=None) -> None:
-    _check(_lib.mfet_mx4_linear(_ptr(x), x_dtype, x_ld, m, _ptr(w_codes), _ptr(w_scales), n, k, _ptr(bias), act, _ptr(y), y_dtype,
-                                y_ld, _ptr(scratch), scratch_bytes, _ptr(status), _ptr(stream)), "mfet_mx4_linear")
+_FAST = ("mfet_grad_clip", "mfet_rows_write", "mfet_rows_read", "mfet_mx4_quantize", "mfet_mx4_matmul", "mfet_mx4_linear")
+_fastcall.bind(_fail, *(C.cast(getattr(_lib, _n), C.c_void_p).value for _n in _FAST))
+mfet_grad_clip = _fastcall.mfet_grad_clip
+mfet_rows_write = _fastcall.mfet_rows_write
+mfet_rows_read = _fastcall.mfet_rows_read
+mfet_mx4_quantize = _fastcall.mfet_mx4_quantize
+mfet_mx4_matmul = _fastcall.mfet_mx4_matmul
+mfet_mx4_linear = _fastcall.mfet_mx4_linear
