@@ -121,9 +121,10 @@ template <int DT, int E, bool VEC>
 __device__ __forceinline__ Raw<DT, E> load_raw(const typename Elem<DT>::T* p, int count, bool wide = false) {
   using R = Raw<DT, E>;
   R r;
-  if constexpr (VEC && R::pieces == 2) {
+  if constexpr (VEC && R::pieces % 2 == 0) {
     if (wide && count == E) {
-      load32(p, &r.w[0], &r.w[1]);
+#pragma unroll
+      for (int i = 0; i < R::pieces; i += 2) load32(reinterpret_cast<const char*>(p) + 16 * i, &r.w[i], &r.w[i + 1]);
       return r;
     }
   }

@@ -27,70 +27,65 @@ constexpr unsigned kAll = 0xFFFFFFFFu;
 // ------------------------------------------------------------------ quantisation ----
 
 constexpr int kQuantThreads = 256;
-constexpr int kQuantInFlight = 4;  // loads of 32 bytes that a lane requests together
 
 struct QuantParams {
   const uint8_t* x;
   int64_t ld;
-  int64_t rows;
-  int64_t units;     // rows * groups
+  int64_t units;     // rows * 4 * groups
   const void* x_end;
   uint32_t k, blocks, groups;  // values, blocks of 32, groups of 4 blocks per row
+  bool wide;         // every row of x starts on a 32-byte boundary
   uint8_t* codes;
   uint8_t* scales;
-  bool wide;         // every row of x starts on a 32-byte boundary
 };
 
-// A lane takes 32 bytes of x (8 fp32 or 16 16-bit values), and the lanes of 128 values (4 blocks) write 64 bytes of codes and the
-// four scale bytes as one word. Bound by reading x.
+// A lane takes a block of 32 values: no exchange for its scale, and 16 bytes of codes in one store. Four lanes write their scale
+// bytes as one word (a row's blocks are counted up to a multiple of four). Bound by reading x; with fewer values per lane the
+// instructions around them were the limit (16384 x 2048 bf16: 19 us with 16 values per lane).
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kQuantThreads, 4) mx4_quantize_kernel(const __grid_constant__ QuantParams p) {
   using T = typename Elem<DT>::T;
-  constexpr int E = 32 / (int)sizeof(T), LPB = kMxBlock / E, LPU = 4 * LPB;  // values per lane, lanes per block and per 128 values
-  constexpr int U = VEC ? kQuantInFlight : 2;
+  constexpr int U = VEC && DT != MFET_F32 ? 2 : 1;  // blocks that a lane requests together
   asm volatile("griddepcontrol.launch_dependents;");  // the product may set itself up; it waits for this grid's end
-  const int lane = threadIdx.x & 31, sub = lane % LPU;
-  const int64_t warp = ((int64_t)blockIdx.x * kQuantThreads + threadIdx.x) >> 5;
-  const int64_t step = (int64_t)gridDim.x * (kQuantThreads / 32) * (32 / LPU) * U;
-  for (int64_t u0 = warp * (32 / LPU) * U; u0 < p.units; u0 += step) {
-    Raw<DT, E> raw[U];
+  const int lane = threadIdx.x & 31;
+  const uint32_t per_row = p.groups * 4;
+  const int64_t step = (int64_t)gridDim.x * kQuantThreads * U;
+  for (int64_t u0 = ((int64_t)blockIdx.x * kQuantThreads + (threadIdx.x & ~31u)) * U; u0 < p.units; u0 += step) {
+    Raw<DT, 32> raw[U];
     int64_t row[U];
-    uint32_t group[U];
+    uint32_t c[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t i = u0 + u * (32 / LPU) + lane / LPU;
-      row[u] = (uint64_t)i >> 32 ? i / p.groups : (int64_t)((uint32_t)i / p.groups);
-      group[u] = (uint32_t)(i - row[u] * p.groups);
-      const uint32_t at = group[u] * 128 + sub * E;
-      const int count = i < p.units && at < p.k ? (int)min((uint32_t)E, p.k - at) : 0;
-      if (count > 0) raw[u] = load_any<DT, E, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count, p.x, p.x_end, p.wide);
+      const int64_t i = u0 + 32 * u + lane;
+      row[u] = (uint64_t)i >> 32 ? i / per_row : (int64_t)((uint32_t)i / per_row);
+      c[u] = (uint32_t)(i - row[u] * per_row);
+      const uint32_t at = c[u] * 32;
+      const int count = i < p.units && at < p.k ? (int)min(32u, p.k - at) : 0;
+      if (count > 0) raw[u] = load_any<DT, 32, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count, p.x, p.x_end, p.wide);
       else memset(&raw[u], 0, sizeof(raw[u]));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (u0 + u * (32 / LPU) >= p.units) break;  // the same for the whole warp
-      uint32_t m = amax_raw<DT, E>(raw[u]);
+      if (u0 + 32 * u >= p.units) break;  // the same for the whole warp
+      const uint32_t e = mx_scale_byte(amax_raw<DT, 32>(raw[u]));
+      uint32_t word = e << (8 * (lane & 3));
+      word |= __shfl_xor_sync(kAll, word, 1);
+      word |= __shfl_xor_sync(kAll, word, 2);
+      const float inv = mx_inv_scale(e == kMxNan ? 0u : e);
+      uint32_t codes[4];
 #pragma unroll
-      for (int d = 1; d < LPB; d <<= 1) m = max(m, __shfl_xor_sync(kAll, m, d));
-      const uint32_t b = mx_scale_byte(m);
-      uint32_t word = b << (8 * (sub / LPB));
-      word |= __shfl_xor_sync(kAll, word, LPB);
-      word |= __shfl_xor_sync(kAll, word, 2 * LPB);
-      float v[E];
-      widen_raw<DT, E>(raw[u], v);
-      const float inv = b == kMxNan ? 0.f : mx_inv_scale(b);
-      uint32_t codes[E / 8];
+      for (int q = 0; q < 4; ++q) {
+        float v[8];
 #pragma unroll
-      for (int j = 0; j < E / 8; ++j) codes[j] = b == kMxNan ? 0u : mx_encode8(v + 8 * j, inv);
-      if (u0 + u * (32 / LPU) + lane / LPU < p.units) {
-        const uint32_t c = group[u] * LPU + sub;
-        if (c < p.blocks * LPB) {
-          uint8_t* dst = p.codes + row[u] * ((int64_t)p.blocks * 16) + c * (E / 2);
-          if constexpr (E == 16) *reinterpret_cast<uint2*>(dst) = make_uint2(codes[0], codes[E / 8 - 1]);
-          else *reinterpret_cast<uint32_t*>(dst) = codes[0];
-        }
-        if (sub == 0)
-          *reinterpret_cast<uint32_t*>(p.scales + ((row[u] >> 7) * p.groups + group[u]) * 512 + (row[u] & 31) * 16 +
+        for (int h = 0; h < 8 / Raw<DT, 32>::per; ++h) widen16<DT>(raw[u].w[q * (8 / Raw<DT, 32>::per) + h], v + h * Raw<DT, 32>::per);
+        codes[q] = mx_encode8(v, inv);
+      }
+      if (e == kMxNan) codes[0] = codes[1] = codes[2] = codes[3] = 0u;
+      if (u0 + 32 * u + lane < p.units) {
+        if (c[u] < p.blocks)
+          *reinterpret_cast<uint4*>(p.codes + (row[u] * p.blocks + c[u]) * 16) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+        if ((lane & 3) == 0)
+          *reinterpret_cast<uint32_t*>(p.scales + ((row[u] >> 7) * p.groups + (c[u] >> 2)) * 512 + (row[u] & 31) * 16 +
                                        ((row[u] & 127) >> 5) * 4) = word;
       }
     }
@@ -661,10 +656,7 @@ uint32_t size_of(uint32_t dtype) { return dtype == MFET_F32 ? 4 : 2; }
 
 template <int DT>
 cudaError_t launch_quantize(const QuantParams& p, bool vec, cudaStream_t s) {
-  constexpr int kLanesPerUnit = 4 * (int)sizeof(typename Elem<DT>::T);  // 128 values, 32 bytes per lane
-  // a warp takes several units at a time only when there are enough for every SM
-  const int64_t per_block = (int64_t)(kQuantThreads / kLanesPerUnit);
-  const int64_t want = (p.units + per_block - 1) / per_block, most = (int64_t)sm_count() * 16;
+  const int64_t want = (p.units + kQuantThreads - 1) / kQuantThreads, most = (int64_t)sm_count() * 16;
   const unsigned b = (unsigned)(want < most ? want : most);
   if (vec) mx4_quantize_kernel<DT, true><<<b, kQuantThreads, 0, s>>>(p);
   else mx4_quantize_kernel<DT, false><<<b, kQuantThreads, 0, s>>>(p);
@@ -673,9 +665,9 @@ cudaError_t launch_quantize(const QuantParams& p, bool vec, cudaStream_t s) {
 
 int quantize(const void* x, uint32_t dtype, int64_t rows, int64_t k, int64_t ld, void* codes, void* scales, cudaStream_t s) {
   const Dims d = dims_of(k);
-  QuantParams p{(const uint8_t*)x, ld, rows, rows * (int64_t)d.groups, (const uint8_t*)x + ((rows - 1) * ld + k) * size_of(dtype),
-                (uint32_t)k, d.blocks, d.groups, (uint8_t*)codes, (uint8_t*)scales,
-                aligned(x, 32) && (uint64_t)ld * size_of(dtype) % 32 == 0};
+  QuantParams p{(const uint8_t*)x, ld, rows * 4 * (int64_t)d.groups, (const uint8_t*)x + ((rows - 1) * ld + k) * size_of(dtype),
+                (uint32_t)k, d.blocks, d.groups, aligned(x, 32) && (uint64_t)ld * size_of(dtype) % 32 == 0, (uint8_t*)codes,
+                (uint8_t*)scales};
   const bool vec = aligned(x, 16) && (uint64_t)ld * size_of(dtype) % 16 == 0;
   cudaError_t e;
   switch (dtype) {
