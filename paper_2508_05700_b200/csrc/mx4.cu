@@ -257,30 +257,31 @@ __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_const
 
 constexpr int kGemmThreads = 320;  // warp 0 loads, warp 1 issues the products, warps 2..9 write results
 constexpr int kTileM = 128;        // rows of x per tile: lanes of tensor memory
-constexpr int kSlab = 256;         // k of a 128-byte row of codes: four instructions
+constexpr int kSlab = 256;         // k per stage: 128 bytes of codes per row, four instructions of k = 64
 constexpr uint64_t kStallNs = 2000000000ull;
 
-template <int TN>  // output columns per tile: 64 or 128
+template <int TN, int DT>  // output columns per tile: 64 or 128; type of y
 struct GemmShape {
-  // A stage holds `slabs` pieces of k = 256: 128 bytes of codes per row each, four instructions of k = 64. What the issuing lane
-  // does per stage besides issuing (waiting, electing, committing) takes as long as eight instructions run, hence two for
-  // the tile that large products use.
-  static constexpr int slabs = TN == 64 ? 1 : 2;
-  static constexpr uint32_t a_slab = kTileM * 128, b_slab = TN * 128;
-  static constexpr uint32_t b_at = slabs * a_slab, scale_at = b_at + slabs * b_slab;  // a stage: codes of x, of the weights, scales
-  static constexpr uint32_t scale_bytes = slabs * 1024;                              // per operand: 512 bytes per 128 rows and k = 128
-  static constexpr uint32_t stage_bytes = scale_at + 2 * scale_bytes;
-  static constexpr int stages = TN == 64 ? 6 : 3;
-  static constexpr uint32_t out_at = stage_bytes * stages;  // a piece of 32 rows x 64 bytes per writing warp
-  static constexpr uint32_t bias_at = out_at + 8 * 2048;
+  static constexpr uint32_t a_bytes = kTileM * 128, b_bytes = TN * 128, s_bytes = 1024;  // a stage: k = 256; two tiles of scales each
+  static constexpr uint32_t b_at = a_bytes, scale_at = a_bytes + b_bytes, stage_bytes = scale_at + 2 * s_bytes;
+  static constexpr int stages = TN == 64 ? 6 : 5;
+  // Results leave in pieces of 32 rows x 32 columns (wider ones of 16-bit values were slower: 46 instead of 41 us for 16384 x 2048 x 2048)
+  static constexpr int piece_row = 32 * (int)sizeof(typename Elem<DT>::T);  // 64 or 128 bytes
+  static constexpr int pieces = 4096 / (32 * piece_row);                    // that a warp has room for
+  static constexpr uint32_t out_at = stage_bytes * stages;
+  static constexpr uint32_t bias_at = out_at + 8 * 4096;
   static constexpr uint32_t smem = bias_at + 8 * (TN / 2) * 4 + 1024;  // + room to align to 1024
   // Tensor memory: two accumulators, then two sets of scales (copies and products run in the order of their issue, so a set may be
   // overwritten by the copies of the stage after the next)
-  static constexpr uint32_t acc_cols = TN, scale_col = 2 * TN, scale_cols = slabs * 16;
-  static_assert(scale_col + 2 * scale_cols <= 512, "tensor memory has 512 columns");
-  static_assert(smem <= 227 * 1024, "shared memory of a block");
+  static constexpr uint32_t acc_cols = TN, scale_col = 2 * TN;
+  static_assert(scale_col + 2 * 16 <= 512, "tensor memory has 512 columns");
+  static_assert(smem <= 227 * 1024 - 256, "shared memory of a block");
   // 64 columns: an odd tile starts in the middle of a tile of scales, two of its four columns further on
   static __device__ __forceinline__ uint32_t half_shift(uint32_t tn) { return TN % 128 ? (tn & 1) * 2 : 0; }
+  // the 16 bytes `q` of row `row` of a piece, where the bulk copy's swizzle expects them: no bank conflicts among eight rows
+  static __device__ __forceinline__ int at(int row, int q) {
+    return row * piece_row + ((piece_row == 128 ? q ^ (row & 7) : q ^ ((row >> 1) & 3)) << 4);
+  }
 };
 
 struct GemmParams {
@@ -432,7 +433,7 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
 // at work share the rows of x in L2. Stages go through a ring of shared memory, scales from there to tensor memory ahead
 // of the products that use them; two accumulators in tensor memory, so that a tile is written while the next one is computed. A
 // lane of tensor memory is a row of x: each of the eight writing warps takes its 32 rows and half of the columns, adds the bias, rounds,
-// and leaves 64 bytes per row at a time in shared memory (16-byte pieces swizzled over the rows: no bank conflicts), from where a bulk
+// and leaves 32 columns at a time in shared memory (swizzled: no bank conflicts), from where a bulk
 // copy writes them and clips what lies beyond y. (Stores straight from the registers touch a line per lane, and the barriers of
 // the other roles wait behind them: 43 us instead of 35 for 16384 x 2048 x 2048.) A y whose rows do not start on 16 bytes is written by
 // plain stores from there.
@@ -441,7 +442,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
                                                                   const __grid_constant__ CUtensorMap b_map,
                                                                   const __grid_constant__ CUtensorMap y_map,
                                                                   const __grid_constant__ GemmParams p) {
-  using G = GemmShape<TN>;
+  using G = GemmShape<TN, DT>;
   using T = typename Elem<DT>::T;
   extern __shared__ uint8_t raw_smem[];
   __shared__ __align__(8) uint64_t bars[2 * G::stages + 5];
@@ -477,43 +478,41 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
   asm volatile("griddepcontrol.wait;" ::: "memory");  // x may be the result of the launch before this one
 
   if (warp == 0) {
-    uint32_t st = 0, phase = 0;
-    uint64_t filled = 0;
-    bool ok = true;
-    for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next()) {
-      const uint8_t* sa = p.a_scales + (size_t)w.tm * p.groups * 512;
-      const uint8_t* sb = p.b_scales + (size_t)(w.tn * (uint32_t)TN >> 7) * p.groups * 512;
-      for (uint32_t s = 0; s < p.stages_k; ++s) {
-        if (filled >= (uint64_t)G::stages && !(ok = __all_sync(kAll, bar_wait(empty(st), phase ^ 1, &dead)))) break;
-        if (elect_one()) {
-          const uint32_t at = base + st * G::stage_bytes, sc_at = at + G::scale_at;
-          const uint32_t slabs = min((uint32_t)G::slabs, (p.groups + 1) / 2 - G::slabs * s);          // pieces of k = 256 that exist
-          const uint32_t sc = min((uint32_t)G::slabs * 2, p.groups - G::slabs * 2 * s) * 512;  // scale bytes per operand
-          bar_expect(full(st), slabs * (G::a_slab + G::b_slab) + 2 * sc);
-          for (uint32_t h = 0; h < slabs; ++h) {
-            tma_load(at + h * G::a_slab, &a_map, (int32_t)((s * G::slabs + h) * 128), (int32_t)(w.tm * kTileM), full(st));
-            tma_load(at + G::b_at + h * G::b_slab, &b_map, (int32_t)((s * G::slabs + h) * 128), (int32_t)(w.tn * TN), full(st));
-          }
-          bulk_load(sc_at, sa + (size_t)s * G::scale_bytes, sc, full(st));
-          bulk_load(sc_at + G::scale_bytes, sb + (size_t)s * G::scale_bytes, sc, full(st));
+    // One lane runs this role from end to end: what it does per stage is on the critical path of a product with many tiles.
+    if (elect_one()) {
+      uint32_t st = 0, phase = 1;  // an empty barrier's phase before the first is taken as complete
+      uint64_t filled = 0;
+      bool ok = true;
+      for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next()) {
+        const int32_t ya = (int32_t)(w.tm * kTileM), yb = (int32_t)(w.tn * TN);
+        const uint8_t* sa = p.a_scales + (size_t)w.tm * p.groups * 512;
+        const uint8_t* sb = p.b_scales + (size_t)((uint32_t)yb >> 7) * p.groups * 512;
+        for (uint32_t s = 0; s < p.stages_k; ++s) {
+          if (!(ok = bar_wait(empty(st), phase, &dead))) break;
+          const uint32_t at = base + st * G::stage_bytes, bar = full(st);
+          const uint32_t sc = min(2u, p.groups - 2 * s) * 512;  // scale bytes per operand
+          bar_expect(bar, G::a_bytes + G::b_bytes + 2 * sc);
+          tma_load(at, &a_map, (int32_t)(s * 128), ya, bar);
+          tma_load(at + G::b_at, &b_map, (int32_t)(s * 128), yb, bar);
+          bulk_load(at + G::scale_at, sa + (size_t)s * 1024, sc, bar);
+          bulk_load(at + G::scale_at + G::s_bytes, sb + (size_t)s * 1024, sc, bar);
+          ++filled;
+          if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
         }
-        __syncwarp();
-        ++filled;
-        if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
       }
-    }
-    // Every copy that this warp started has to land before the block ends. The products wait for each of them; only
-    // when a wait has run out are they waited for here.
-    if (!ok || dead) {
-      volatile int none = 0;
-      const uint64_t from = filled > G::stages ? filled - G::stages : 0;
-      for (uint64_t i = from; i < filled; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
+      // Every copy that this lane started has to land before the block ends. The products wait for each of them; only
+      // when a wait has run out are they waited for here.
+      if (!ok || dead) {
+        volatile int none = 0;
+        const uint64_t from = filled > G::stages ? filled - G::stages : 0;
+        for (uint64_t i = from; i < filled; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
+      }
     }
   } else if (warp == 1) {
     // One lane runs this role from end to end. The tensor cores' queue is short, so what the lane does between the instructions of two
     // stages has to be short too: stage and phase are counted along, and the next stage's barrier is asked between this one's instructions.
     if (elect_one()) {
-      uint32_t st = 0, phase = 0, done = 0;
+      uint32_t st = 0, phase = 0, done = 0, set = 0;
       bool ok = true, ready = false;
       for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next(), ++done) {
         const int acc = done & 1;
@@ -525,28 +524,26 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = base + st * G::stage_bytes;
           const uint32_t this_empty = empty(st);
-          const uint32_t sf = tmem + G::scale_col + G::scale_cols * (s & 1);
+          const uint32_t sf = tmem + G::scale_col + 16 * (set ^= 1);
           const uint32_t a_lo = tile_desc_lo(at), b_lo = tile_desc_lo(at + G::b_at), sc_lo = scale_desc_lo(at + G::scale_at);
           if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-          // copies of scales for k = 128 (two instructions), and instruction j of the stage
+          // the scales of k = 128 (x, then weights), and instruction j of the stage
           auto scales = [&](int g) {
             copy_scales(sf + 8 * g, sc_lo + 32 * g);
-            copy_scales(sf + 8 * g + 4, sc_lo + (G::scale_bytes >> 4) + 32 * g);
+            copy_scales(sf + 8 * g + 4, sc_lo + (G::s_bytes >> 4) + 32 * g);
           };
           auto product = [&](int j) {
-            mma_mx4(d, a_lo + (j >> 2) * (G::a_slab >> 4) + 2 * (j & 3), b_lo + (j >> 2) * (G::b_slab >> 4) + 2 * (j & 3),
-                    inst_desc<TN>((j & 1) * 2), sf + 8 * (j >> 1), sf + 8 * (j >> 1) + 4 + half, s | j);
+            mma_mx4(d, a_lo + 2 * j, b_lo + 2 * j, inst_desc<TN>((j & 1) * 2), sf + 8 * (j >> 1), sf + 8 * (j >> 1) + 4 + half, s | j);
           };
-          constexpr int kSteps = 4 * G::slabs;
-          const uint32_t left = p.k - s * (G::slabs * kSlab);
-          if (left > 64u * (kSteps - 1)) {
-#pragma unroll
-            for (int g = 0; g < kSteps / 2; ++g) scales(g);
-#pragma unroll
-            for (int j = 0; j < kSteps / 2; ++j) product(j);
+          const uint32_t left = p.k - s * kSlab;
+          if (left > 192u) {
+            scales(0);
+            scales(1);
+            product(0);
+            product(1);
             ready = bar_try(full(st), phase);
-#pragma unroll
-            for (int j = kSteps / 2; j < kSteps; ++j) product(j);
+            product(2);
+            product(3);
           } else {
             const int steps = (int)((left + 63) / 64);
             for (int g = 0; 2 * g < steps; ++g) scales(g);
@@ -566,10 +563,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
   } else {
     const int quarter = warp & 3;                // the 32 lanes of tensor memory that this warp may read
     const int c0 = warp < 6 ? 0 : TN / 2;        // two warps share them, each takes half of the columns
-    uint8_t* const out_ptr = smem + G::out_at + (warp - 2) * 2048;
-    const uint32_t out_at = base + G::out_at + (warp - 2) * 2048;
+    uint8_t* const out_ptr = smem + G::out_at + (warp - 2) * 4096;
+    const uint32_t out_at = base + G::out_at + (warp - 2) * 4096;
     float* const bias = reinterpret_cast<float*>(smem + G::bias_at) + (warp - 2) * (TN / 2);
-    uint32_t done = 0;
+    uint32_t done = 0, turn = 0;
     for (TileWalk w(p.n_tiles); w.t < p.tiles; w.next(), ++done) {
       const int acc = done & 1;
       const int64_t i0 = (int64_t)w.tm * kTileM + quarter * 32, j0 = (int64_t)w.tn * TN + c0;
@@ -597,35 +594,30 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
           v[q + 3] = activate(__uint_as_float(r[q + 3]), b4.w, p.out.relu);
         }
         constexpr int kPer = 16 / (int)sizeof(T);  // values per 16 bytes
-        constexpr int kCols = 64 / (int)sizeof(T);  // columns of a piece
+        const uint32_t piece = (turn++ % G::pieces) * (32 * G::piece_row);
+        uint8_t* const to = out_ptr + piece;
+        if (p.bulk_y) {  // what this piece's memory held before has left
+          asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(G::pieces - 1) : "memory");
+          __syncwarp();
+        }
 #pragma unroll
-        for (int h = 0; h < 32; h += kCols) {
-          if (p.bulk_y) {  // the piece before has left
-            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            __syncwarp();
-          }
-#pragma unroll
-          for (int q = 0; q < kCols; q += kPer)
-            *reinterpret_cast<uint4*>(out_ptr + lane * 64 + (((q / kPer) ^ ((lane >> 1) & 3)) << 4)) = narrow16<DT>(v + h + q);
-          if (p.bulk_y) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (i0 < p.m && j0 + c + h < p.n && elect_one()) bulk_store(&y_map, out_at, (int32_t)(j0 + c + h), (int32_t)i0);
-            __syncwarp();
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          } else {
-            __syncwarp();
-            // a warp takes one row's 32 columns (16 bits) or two rows' 16 (fp32)
-            const int64_t j = j0 + c + h + lane % kCols;
-            T* y = reinterpret_cast<T*>(p.out.y) + i0 * p.out.ld + j;
+        for (int q = 0; q < 32; q += kPer) *reinterpret_cast<uint4*>(to + G::at(lane, q / kPer)) = narrow16<DT>(v + q);
+        const int64_t j1 = j0 + c;
+        if (p.bulk_y) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (i0 < p.m && j1 < p.n && elect_one()) bulk_store(&y_map, out_at + piece, (int32_t)j1, (int32_t)i0);
+          __syncwarp();
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        } else {
+          __syncwarp();
+          T* y = reinterpret_cast<T*>(p.out.y) + i0 * p.out.ld + j1 + lane;
 #pragma unroll 8
-            for (int i = 0; i < 32; i += 32 / kCols) {
-              const int row = i + lane / kCols, col = lane % kCols;
-              const T x = *reinterpret_cast<const T*>(out_ptr + row * 64 + (((col / kPer) ^ ((row >> 1) & 3)) << 4) + (col % kPer) * sizeof(T));
-              if (i0 + row < p.m && j < p.n) y[row * p.out.ld] = x;
-            }
-            __syncwarp();
+          for (int i = 0; i < 32; ++i) {  // a warp writes a row's 32 columns
+            const T x = *reinterpret_cast<const T*>(to + G::at(i, lane / kPer) + lane % kPer * sizeof(T));
+            if (i0 + i < p.m && j1 + lane < p.n) y[i * p.out.ld] = x;
           }
+          __syncwarp();
         }
       }
     }
@@ -706,17 +698,17 @@ bool code_map(CUtensorMap* map, const void* codes, int64_t rows, uint32_t blocks
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// y [m, n] written in boxes of 32 rows x 64 bytes
-bool out_map(CUtensorMap* map, const OutParams& o, int64_t m, int64_t n) {
+// y [m, n] written in boxes of 32 rows x `row` bytes (64 or 128)
+bool out_map(CUtensorMap* map, const OutParams& o, int64_t m, int64_t n, uint32_t row) {
   const EncodeTiled f = encode_tiled();
   if (!f) return false;
   const uint32_t size = size_of(o.dtype);
   const cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)m}, stride[1] = {(cuuint64_t)o.ld * size};
-  const cuuint32_t boxes[2] = {64 / size, 32}, ones[2] = {1, 1};
+  const cuuint32_t boxes[2] = {row / size, 32}, ones[2] = {1, 1};
   const CUtensorMapDataType t = o.dtype == MFET_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                 : o.dtype == MFET_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                       : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  return f(map, t, 2, o.y, dims, stride, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+  return f(map, t, 2, o.y, dims, stride, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -733,20 +725,20 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   p.n = n;
   p.k = (uint32_t)k;
   p.groups = d.groups;
-  p.stages_k = (uint32_t)((k + GemmShape<TN>::slabs * kSlab - 1) / (GemmShape<TN>::slabs * kSlab));
+  p.stages_k = (uint32_t)((k + kSlab - 1) / kSlab);
   p.n_tiles = (uint32_t)((n + TN - 1) / TN);
   p.tiles = (m + kTileM - 1) / kTileM * p.n_tiles;
   p.status = status;
   p.out = out;
   p.bulk_y = aligned(out.y, 16) && (uint64_t)out.ld * size_of(out.dtype) % 16 == 0;
   if (!p.bulk_y) y = a;  // not used
-  else if (!out_map(&y, out, m, n)) return MFET_ERR_CUDA;
+  else if (!out_map(&y, out, m, n, GemmShape<TN, DT>::piece_row)) return MFET_ERR_CUDA;
   static std::atomic<uint64_t> ready{0};  // one bit per GPU: the kernel may use this much shared memory there
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return MFET_ERR_CUDA;
   const uint64_t bit = dev < 64 ? 1ull << dev : 0;
   if (!(ready.load(std::memory_order_relaxed) & bit)) {
-    if (cudaFuncSetAttribute(mx4_gemm_kernel<TN, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GemmShape<TN>::smem) !=
+    if (cudaFuncSetAttribute(mx4_gemm_kernel<TN, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GemmShape<TN, DT>::smem) !=
         cudaSuccess)
       return MFET_ERR_CUDA;
     ready.fetch_or(bit, std::memory_order_relaxed);
@@ -757,7 +749,7 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   cudaLaunchConfig_t cfg{};
   cfg.blockDim = dim3(kGemmThreads);
   cfg.gridDim = dim3((unsigned)(p.tiles < sm_count() ? p.tiles : sm_count()));
-  cfg.dynamicSmemBytes = GemmShape<TN>::smem;
+  cfg.dynamicSmemBytes = GemmShape<TN, DT>::smem;
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = after_quantize ? 1 : 0;

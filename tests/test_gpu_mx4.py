@@ -69,7 +69,9 @@ def test_quantise_is_bit_exact(rows, k, dtype):
 
 SHAPES = [(1, 1, 1), (1, 16, 32), (9, 128, 64), (32, 128, 256), (33, 127, 65), (64, 129, 127), (65, 1, 128), (100, 300, 129),
           (128, 128, 192), (129, 256, 255), (500, 777, 1075), (200, 64, 257), (640, 1000, 896), (1000, 130, 2048), (17, 2048, 31),
-          (300, 96, 4100)]
+          (300, 96, 4100),
+          # enough tiles for pairs of blocks: odd rows, columns and depths, a second block without rows
+          (2305, 1030, 257), (1300, 2000, 1000), (5000, 640, 129), (2561, 1000, 2048), (9345, 300, 33), (130, 9500, 700)]
 
 
 @pytest.mark.parametrize("m_,n,k", SHAPES)
