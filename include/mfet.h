@@ -85,7 +85,8 @@ typedef struct {
                            is supplied later by mfet_host_tables_register).            */
   uint64_t rows;        /* 1 .. 2^63-1                                                  */
   uint32_t dim;         /* elements per row; stored row bytes must be a multiple of 16  */
-  uint32_t dtype;       /* MFET_F32 / MFET_F16 / MFET_BF16 / MFET_INT4 (dim % 8 == 0)          */
+  uint32_t dtype;       /* MFET_F32 / MFET_F16 / MFET_BF16 / MFET_INT4 / MFET_MXFP4 (the last
+                           two: dim % 8 == 0; filled by mfet_rows_write)                 */
   uint32_t location;    /* MFET_LOC_DEVICE / MFET_LOC_HOST                              */
   uint32_t flags;       /* must be 0                                                    */
   uint64_t hash_seed;   /* XORed into the raw ID before hashing; 0 = plain hash         */

@@ -84,8 +84,8 @@ int mfet_tables_create(const mfet_table_desc_t* descs, int32_t n_tables, int32_t
   for (int32_t i = 0; i < n_tables; ++i) {
     const mfet_table_desc_t& d = descs[i];
     if (d.rows == 0 || d.rows >= (1ULL << 63) || d.dim == 0 || d.flags != 0) return MFET_ERR_INVALID_ARG;
-    if (d.dtype > MFET_INT4 || d.location > MFET_LOC_HOST) return MFET_ERR_INVALID_ARG;
-    if (d.dtype == MFET_INT4 && (d.dim % 8u) != 0) return MFET_ERR_UNSUPPORTED_DIM;
+    if (d.dtype > MFET_MXFP4 || d.location > MFET_LOC_HOST) return MFET_ERR_INVALID_ARG;
+    if (d.dtype >= MFET_INT4 && (d.dim % 8u) != 0) return MFET_ERR_UNSUPPORTED_DIM;
     const uint64_t rb = mfet_row_bytes(d.dim, d.dtype);
     if (rb == 0 || rb % 16 != 0) return MFET_ERR_UNSUPPORTED_DIM;
     const uint64_t stride = d.row_stride_bytes ? d.row_stride_bytes : rb;
@@ -438,7 +438,7 @@ int mfet_embedding_bag_forward(mfet_tables_t* t, const mfet_batch_shape_t* shape
     if (n == 0) return MFET_OK;
     // widest rows first: their blocks run longest, so they should not be the last to start
     std::stable_sort(p.slot, p.slot + n, [](const SlotDev& a, const SlotDev& b) {
-      return (uint32_t)a.chunks * (a.dtype == MFET_INT4 ? 4u : 16u) > (uint32_t)b.chunks * (b.dtype == MFET_INT4 ? 4u : 16u);
+      return (uint32_t)a.chunks * (a.dtype >= MFET_INT4 ? 4u : 16u) > (uint32_t)b.chunks * (b.dtype >= MFET_INT4 ? 4u : 16u);
     });
     p.n_slots = n;
     if (launch_bag(p, stream) != cudaSuccess) return MFET_ERR_CUDA;
@@ -460,10 +460,10 @@ int mfet_embedding_bag_forward(mfet_tables_t* t, const mfet_batch_shape_t* shape
       if (use_prefetch) t->consumed += 1;
     } else {
       // rows wider than 512 bytes are covered by several entries of <= 32 chunks
-      // a lane's chunk: 16 bytes, or 4 bytes of codes for INT4 rows
-      const bool int4 = tb.desc.dtype == MFET_INT4;
-      const uint32_t chunk_bytes = int4 ? 4u : 16u;
-      const uint32_t chunks_total = int4 ? tb.desc.dim / 8u : (uint32_t)(tb.row_bytes / 16);
+      // a lane's chunk: 16 bytes, or 4 bytes of codes for INT4 and MXFP4 rows
+      const bool codes = tb.desc.dtype >= MFET_INT4;
+      const uint32_t chunk_bytes = codes ? 4u : 16u;
+      const uint32_t chunks_total = codes ? tb.desc.dim / 8u : (uint32_t)(tb.row_bytes / 16);
       const uint32_t epc = tb.desc.dtype == MFET_F32 ? 4u : 8u;  // elements per chunk
       for (uint32_t c0 = 0; c0 < chunks_total; c0 += 32) {
         if (n == kMaxSlotsPerLaunch) {
@@ -473,7 +473,8 @@ int mfet_embedding_bag_forward(mfet_tables_t* t, const mfet_batch_shape_t* shape
         SlotDev& sd = p.slot[n++];
         const uint32_t ch = chunks_total - c0 < 32 ? chunks_total - c0 : 32;
         sd.table = tb.dev_ptr + (uint64_t)c0 * chunk_bytes;
-        sd.meta_off = int4 ? tb.desc.dim / 2u - c0 * chunk_bytes : 0u;
+        // from the entry's first chunk to the scale/bias pair, or to the scale byte of its first block (4 chunks)
+        sd.meta_off = codes ? tb.desc.dim / 2u - c0 * chunk_bytes + (tb.desc.dtype == MFET_MXFP4 ? c0 / 4u : 0u) : 0u;
         sd.rows = tb.desc.rows;
         sd.magic = tb.magic;
         sd.seed = tb.desc.hash_seed;

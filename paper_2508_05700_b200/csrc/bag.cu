@@ -33,7 +33,7 @@
 #include <queue>
 #include <vector>
 
-#include "common.cuh"
+#include "lowbit.cuh"
 
 namespace mfet {
 
@@ -48,17 +48,18 @@ constexpr int kClassW = (kLongBag + 31) / 32;
 constexpr int kClasses = (kLongBag + kClassW - 1) / kClassW;  // <= 32; class kClasses = long bags
 static_assert(kLongBag >= 1 && kClasses <= 32, "one lane per class of shorter bags");
 
-// A lane's piece of a row: 16 bytes (4 fp32 or 8 fp16/bf16 values), or for INT4 rows
-// 4 bytes (8 four-bit codes) plus the row's fp16 scale/bias pair.
+// A lane's piece of a row: 16 bytes (4 fp32 or 8 fp16/bf16 values), or for INT4 and MXFP4 rows
+// 4 bytes (8 four-bit codes) plus the row's fp16 scale/bias pair or the scale byte of the piece's block.
 template <int DT>
 struct ChunkElems {
   static constexpr int value = (DT == MFET_F32) ? 4 : 8;
-  static constexpr int bytes = (DT == MFET_INT4) ? 4 : 16;
+  static constexpr int bytes = (DT == MFET_INT4 || DT == MFET_MXFP4) ? 4 : 16;
 };
 
 template <int DT>
 __device__ __forceinline__ uint4 load_chunk(const uint8_t* chunk, const uint8_t* meta) {
   if constexpr (DT == MFET_INT4) return make_uint4(ld_row4(chunk), ld_row4(meta), 0u, 0u);
+  else if constexpr (DT == MFET_MXFP4) return make_uint4(ld_row4(chunk), (uint32_t)__ldg(meta), 0u, 0u);
   else return ld_row16(chunk);
 }
 
@@ -92,6 +93,16 @@ __device__ __forceinline__ void accumulate(unsigned long long* acc, const uint4&
       fma2(val, pack2(__float_as_uint(c0), __float_as_uint(c1)), s2);
       fma2(acc[j], val, w2);
     }
+    return;
+  }
+  if constexpr (DT == MFET_MXFP4) {
+    // acc += (w * scale) * level: the scale is a power of two, so this rounds as w * value does
+    float level[8];
+    mx_decode8(v.x, 1.f, level);
+    const float ws = w * mx_scale(v.y);
+    const unsigned long long w2 = pack2(__float_as_uint(ws), __float_as_uint(ws));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) fma2(acc[j], pack2(__float_as_uint(level[2 * j]), __float_as_uint(level[2 * j + 1])), w2);
     return;
   }
   const uint32_t x[4] = {v.x, v.y, v.z, v.w};
@@ -160,7 +171,7 @@ struct Win {
   int b0;                 // first sample of the tile
 };
 
-// Where this lane's chunk (and, INT4, the scale/bias pair) of a staged row is.
+// Where this lane's chunk (and, INT4 and MXFP4, its scale) of a staged row is.
 // Direct tables: base + row * stride. IND: the dedup source index selects the
 // cache (>= 0) or the staging buffer of fetched rows (< 0: -1 - index).
 template <bool IND>
@@ -399,12 +410,13 @@ __device__ __forceinline__ void pool_window(const BagParams& p, const SlotDev& s
   const bool fast_ok = (int)s.chunks == LPR && !(p.flags & 1u) && (IND || s.narrow != 0);
   RowAddr<IND> ra;
   const uint64_t coff = (uint64_t)c * ChunkElems<DT>::bytes;
+  const uint64_t moff = (uint64_t)s.meta_off + (DT == MFET_MXFP4 ? (uint64_t)(c / 4) : 0u);  // a scale byte per 32 elements
   if constexpr (IND) {
     const uint64_t slot_off = reinterpret_cast<uint64_t>(s.table);  // byte offset of the column block in the row
     ra.tbase = ip.cache_data + slot_off + coff;
-    ra.mbase = ip.cache_data + slot_off + s.meta_off;
+    ra.mbase = ip.cache_data + slot_off + moff;
     ra.tbase2 = ip.staging + slot_off + coff;
-    ra.mbase2 = ip.staging + slot_off + s.meta_off;
+    ra.mbase2 = ip.staging + slot_off + moff;
     ra.stride = ip.row_bytes;
     ra.stride32 = (uint32_t)ip.row_bytes;
     ra.wide = false;
@@ -415,7 +427,7 @@ __device__ __forceinline__ void pool_window(const BagParams& p, const SlotDev& s
 #endif
   } else {
     ra.tbase = s.table + coff;
-    ra.mbase = s.table + s.meta_off;
+    ra.mbase = s.table + moff;
     ra.tbase2 = ra.mbase2 = nullptr;
     ra.stride = s.stride;
     ra.stride32 = (uint32_t)s.stride;
@@ -460,9 +472,9 @@ __device__ __forceinline__ void pool_window_dt(const BagParams& p, const SlotDev
 // that their latency overlaps the ordering.
 constexpr int kEarly = 8;
 
-// Q4 = true: the build of the kernel that also decodes INT4 rows (kept apart so that the
-// common kernels stay small).
-template <bool IND, bool Q4>
+// LOW: the build of the kernel that also decodes INT4 rows (1), or INT4 and MXFP4 rows (2); kept apart
+// so that the common kernels stay small.
+template <bool IND, int LOW>
 __device__ __forceinline__ void bag_body(const BagParams& p, const IndirectParams& ip) {
   extern __shared__ __align__(16) uint32_t dyn[];
   __shared__ int64_t soff[kMaxTile + 1];
@@ -679,9 +691,15 @@ __device__ __forceinline__ void bag_body(const BagParams& p, const IndirectParam
 
     const Win w{srow, shi, sw, spos, slen, sbag, &snext, soff, nbw, n_long, b0};
     bool done = false;
-    if constexpr (Q4) {
+    if constexpr (LOW >= 1) {
       if (s.dtype == MFET_INT4) {
         pool_window_dt<MFET_INT4, IND>(p, s, w, ip);
+        done = true;
+      }
+    }
+    if constexpr (LOW >= 2) {
+      if (s.dtype == MFET_MXFP4) {
+        pool_window_dt<MFET_MXFP4, IND>(p, s, w, ip);
         done = true;
       }
     }
@@ -703,30 +721,44 @@ __device__ __forceinline__ void bag_body(const BagParams& p, const IndirectParam
 
 __global__ void __launch_bounds__(256, kMinBlocks) bag_kernel(const __grid_constant__ BagParams p) {
   const IndirectParams none{};
-  bag_body<false, false>(p, none);
+  bag_body<false, 0>(p, none);
 }
 
 __global__ void __launch_bounds__(256, kMinBlocks) bag_q4_kernel(const __grid_constant__ BagParams p) {
   const IndirectParams none{};
-  bag_body<false, true>(p, none);
+  bag_body<false, 1>(p, none);
 }
 
 __global__ void __launch_bounds__(256, kMinBlocks) bag_indirect_kernel(const __grid_constant__ BagParams p,
                                                            const __grid_constant__ IndirectParams ip) {
-  bag_body<true, false>(p, ip);
+  bag_body<true, 0>(p, ip);
 }
 
 __global__ void __launch_bounds__(256, kMinBlocks) bag_indirect_q4_kernel(const __grid_constant__ BagParams p,
                                                               const __grid_constant__ IndirectParams ip) {
-  bag_body<true, true>(p, ip);
+  bag_body<true, 1>(p, ip);
+}
+
+__global__ void __launch_bounds__(256, kMinBlocks) bag_mx4_kernel(const __grid_constant__ BagParams p) {
+  const IndirectParams none{};
+  bag_body<false, 2>(p, none);
+}
+
+__global__ void __launch_bounds__(256, kMinBlocks) bag_indirect_mx4_kernel(const __grid_constant__ BagParams p,
+                                                               const __grid_constant__ IndirectParams ip) {
+  bag_body<true, 2>(p, ip);
 }
 
 }  // namespace
 
-static bool any_int4(const BagParams& p) {
-  for (int i = 0; i < p.n_slots; ++i)
-    if (p.slot[i].dtype == MFET_INT4) return true;
-  return false;
+// which build of the kernel a launch needs: 0, 1 (INT4 rows) or 2 (MXFP4 rows)
+static int low_formats(const BagParams& p) {
+  int low = 0;
+  for (int i = 0; i < p.n_slots; ++i) {
+    if (p.slot[i].dtype == MFET_MXFP4) return 2;
+    if (p.slot[i].dtype == MFET_INT4) low = 1;
+  }
+  return low;
 }
 
 // Samples per block when the caller has not fixed them. The blocks of a launch are handed to
@@ -827,7 +859,7 @@ static size_t stage_bytes(BagParams& p, bool indirect) {
 // blocks need, so that the rest of the SM's array stays L1 for the rows.
 template <typename K>
 static cudaError_t prepare(K kernel, int which, size_t smem) {
-  static std::atomic<long long> configured[4][64];
+  static std::atomic<long long> configured[6][64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = 0;
   const long long want = (long long)smem + 1;
@@ -870,7 +902,12 @@ cudaError_t launch_bag_indirect(const BagParams& p_, const IndirectParams& ip, c
   const size_t smem = stage_bytes(p, true);
   const int64_t blocks = (int64_t)p.n_slots * p.tiles_per_slot;
   cudaError_t e;
-  if (any_int4(p)) {
+  const int low = low_formats(p);
+  if (low == 2) {
+    if ((e = prepare(bag_indirect_mx4_kernel, 4, smem)) != cudaSuccess) return e;
+    return launch(bag_indirect_mx4_kernel, blocks, smem, s, false, p, ip);
+  }
+  if (low == 1) {
     if ((e = prepare(bag_indirect_q4_kernel, 0, smem)) != cudaSuccess) return e;
     return launch(bag_indirect_q4_kernel, blocks, smem, s, false, p, ip);
   }
@@ -885,7 +922,12 @@ cudaError_t launch_bag(const BagParams& p_, cudaStream_t s) {
   const int64_t blocks = (int64_t)p.n_slots * p.tiles_per_slot;
   const bool overlap = (p.flags & 16u) != 0;
   cudaError_t e;
-  if (any_int4(p)) {
+  const int low = low_formats(p);
+  if (low == 2) {
+    if ((e = prepare(bag_mx4_kernel, 5, smem)) != cudaSuccess) return e;
+    return launch(bag_mx4_kernel, blocks, smem, s, overlap, p);
+  }
+  if (low == 1) {
     if ((e = prepare(bag_q4_kernel, 2, smem)) != cudaSuccess) return e;
     return launch(bag_q4_kernel, blocks, smem, s, overlap, p);
   }

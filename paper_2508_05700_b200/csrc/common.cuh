@@ -86,7 +86,7 @@ struct SlotDev {
   uint8_t lpr_log2;      // lanes per row = 1 << lpr_log2 >= chunks
   uint8_t narrow;        // 1: row indices and the stride fit 32 bits
   uint16_t pad;
-  uint32_t meta_off;     // INT4: byte offset of the row's fp16 scale/bias pair from `table`
+  uint32_t meta_off;     // INT4: byte offset of the row's fp16 scale/bias pair from `table`; MXFP4: of the scale byte of the first chunk
 };
 static_assert(sizeof(SlotDev) == 64, "SlotDev must stay 64 bytes");
 
