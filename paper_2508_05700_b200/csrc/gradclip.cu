@@ -6,7 +6,7 @@
 // sum per block. The
 // second adds those sums up - every block the same ones in the same order, which costs less than another launch or a
 // count of finished blocks - and scales. It walks the pieces from the last to the first, because the end of what the
-// first launch has read is still in L2. Nothing depends on which block finishes when: equal inputs give equal bits.
+// first launch has read is still in L2 (which is told to keep the last 64 MB and let the rest go: 214 instead of 222 us for 200 M bf16 values). Nothing depends on which block finishes when: equal inputs give equal bits.
 #include <cmath>
 #include <cstring>
 
@@ -21,6 +21,7 @@ constexpr int kClipThreads = 256;
 constexpr int kClipInFlight = 8;                                  // 16-byte loads that a thread requests together
 constexpr int kPieceVecs = kClipThreads * kClipInFlight;          // 16-byte vectors per piece
 constexpr int kClipBlocksPerSm = 4;
+constexpr int kKeepPieces = 2048;                                 // 64 MB: what L2 can be made to keep for the second launch
 
 struct GradDev {
   const uint8_t* src;
@@ -186,8 +187,23 @@ __device__ __forceinline__ int64_t edge_element(const GradDev& t, int64_t v0, in
   return tail >= v0 && tail < v0 + kPieceVecs && !(tail == 0 && t.lead > 0) ? e : -1;
 }
 
+// 16 bytes through the read-only path, kept in L2 or among the first to leave it
+__device__ __forceinline__ uint64_t l2_policy(bool keep) {
+  uint64_t p;
+  if (keep) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint4 load_with(const uint4* p, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p), "l"(policy));
+  return v;
+}
+
 template <int DT>
-__device__ __forceinline__ double piece_squares(const GradDev& t, int64_t n, int64_t piece) {
+__device__ __forceinline__ double piece_squares(const GradDev& t, int64_t n, int64_t piece, uint64_t policy) {
   using T = typename Elem<DT>::T;
   constexpr int V = 16 / (int)sizeof(T);
   const T* src = reinterpret_cast<const T*>(t.src);
@@ -200,7 +216,7 @@ __device__ __forceinline__ double piece_squares(const GradDev& t, int64_t n, int
     if (v0 * V >= t.lead && (v0 + kPieceVecs) * V <= end) {  // a whole piece
       uint4 v[kClipInFlight];
 #pragma unroll
-      for (int j = 0; j < kClipInFlight; ++j) v[j] = __ldg(at + j * kClipThreads);
+      for (int j = 0; j < kClipInFlight; ++j) v[j] = load_with(at + j * kClipThreads, policy);
 #pragma unroll
       for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
       return s;
@@ -279,14 +295,16 @@ __device__ __forceinline__ void piece_scale(const GradDev& t, int64_t n, int64_t
 template <int N>
 __device__ __forceinline__ double share_squares(const GradParams<N>& p, const Share<N>& share, int b, int g) {
   double s = 0;
+  const uint64_t keep = l2_policy(true), leave = l2_policy(false);
   int32_t k = b;
   for (int i = k < share.total ? share.tensor_of(p.n, k) : 0; k < share.total; k += g) {
     while (i + 1 < p.n && share.first[i + 1] <= k) ++i;
     const GradDev& t = p.t[i];
     const int64_t piece = k - share.first[i];
-    if (t.dtype == MFET_F32) s += piece_squares<MFET_F32>(t, share.live[i], piece);
-    else if (t.dtype == MFET_F16) s += piece_squares<MFET_F16>(t, share.live[i], piece);
-    else s += piece_squares<MFET_BF16>(t, share.live[i], piece);
+    const uint64_t policy = k >= share.total - kKeepPieces ? keep : leave;
+    if (t.dtype == MFET_F32) s += piece_squares<MFET_F32>(t, share.live[i], piece, policy);
+    else if (t.dtype == MFET_F16) s += piece_squares<MFET_F16>(t, share.live[i], piece, policy);
+    else s += piece_squares<MFET_BF16>(t, share.live[i], piece, policy);
   }
   return s;
 }
