@@ -332,7 +332,7 @@ template <int N>
 __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) grad_squares_kernel(const __grid_constant__ GradParams<N> p) {
   __shared__ double shared[kClipThreads / 32];
   __shared__ Share<N> share;
-  asm volatile("griddepcontrol.launch_dependents;");  // the scaling may set itself up; it waits for this grid's end
+  early_launch_wait();
   share.fill(p);
   const double s = block_sum(share_squares(p, share, blockIdx.x, gridDim.x), shared);
   if (threadIdx.x == 0) p.sums[p.first_sum + blockIdx.x] = s;
@@ -342,8 +342,9 @@ template <int N>
 __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) grad_scale_kernel(const __grid_constant__ GradParams<N> p) {
   __shared__ double shared[kClipThreads / 32];
   __shared__ Share<N> share;
-  share.fill(p);  // what the call was given: not written by the launch before this one
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // its sums are
+  // The launch before this one is of the same call, and all before that have ended: the counts can be read, its sums not yet.
+  share.fill(p);
+  early_launch_wait();
   double s = 0;
   for (int i = threadIdx.x; i < p.n_sums; i += kClipThreads) s += __ldcg(p.sums + i);
   share_scale(p, share, blockIdx.x, gridDim.x, sqrt(block_sum(s, shared)));
@@ -357,6 +358,7 @@ __global__ void __cluster_dims__(kSmallBlocks, 1, 1) __launch_bounds__(kClipThre
   __shared__ double shared[kClipThreads / 32];
   __shared__ double all[kSmallBlocks];
   __shared__ Share<kFewTensors> share;
+  early_launch_wait();
   share.fill(p);
   const double s = block_sum(share_squares(p, share, blockIdx.x, kSmallBlocks), shared);
   if (threadIdx.x < kSmallBlocks) {  // into every block's list
@@ -413,22 +415,12 @@ int32_t fill_params(const mfet_grad_t* g, int32_t n_grads, int32_t at, GradParam
 
 template <int N>
 cudaError_t launch_squares(const GradParams<N>& p, cudaStream_t s) {
-  grad_squares_kernel<N><<<(unsigned)blocks_of(p.pieces), kClipThreads, 0, s>>>(p);
-  return cudaGetLastError();
+  return launch_early(grad_squares_kernel<N>, (unsigned)blocks_of(p.pieces), kClipThreads, 0, s, p);
 }
 
 template <int N>
 cudaError_t launch_scale(const GradParams<N>& p, cudaStream_t s) {
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.blockDim = dim3(kClipThreads);
-  cfg.gridDim = dim3((unsigned)(p.pieces > 0 ? blocks_of(p.pieces) : 1));
-  cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, grad_scale_kernel<N>, p);
+  return launch_early(grad_scale_kernel<N>, (unsigned)(p.pieces > 0 ? blocks_of(p.pieces) : 1), kClipThreads, 0, s, p);
 }
 
 // Tensors are taken in groups that fit the kernel parameters: first the squares of all groups, then the scaling of each.
@@ -452,8 +444,7 @@ int run_clip(const mfet_grad_t* g, int32_t n_grads, double max_norm, float* norm
   const bool one_group = n_grads <= N;  // p holds it already
   if constexpr (N == kFewTensors) {
     if (n_grads > 0 && p.pieces <= kSmallPieces) {
-      grad_small_kernel<<<kSmallBlocks, kClipThreads, 0, s>>>(p);
-      return cudaGetLastError() == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+      return launch_early(grad_small_kernel, kSmallBlocks, kClipThreads, 0, s, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
     }
   }
   if (n_grads == 0) p.n = 0, p.pieces = 0;

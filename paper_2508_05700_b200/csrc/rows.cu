@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
   using S = typename Elem<SD>::T;
   constexpr int E = 32 / (int)sizeof(S), LPB = kMxBlock / E;  // values per lane, lanes per block of 32
   constexpr int U = kRowsInFlight;
+  early_launch_wait();
   const int64_t n = live_count(p);
   const int lane = threadIdx.x & 31;
   const int lanes = 1 << p.lanes_log2, per_warp = 32 >> p.lanes_log2;
@@ -197,6 +198,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_read_kern
   using D = typename Elem<DD>::T;
   constexpr int E = 32 / (int)sizeof(D), LPB = kMxBlock / E;
   constexpr int U = kRowsReadAhead;
+  early_launch_wait();
   const int64_t n = live_count(p);
   const int lane = threadIdx.x & 31;
   const int lanes = 1 << p.lanes_log2, per_warp = 32 >> p.lanes_log2;
@@ -318,18 +320,15 @@ unsigned blocks_for(const RowsParams& p) {
 }
 
 template <int TD, int MD, bool VEC, bool ONE>
-void launch_as(const RowsParams& p, bool write, cudaStream_t s) {
-  const unsigned b = blocks_for(p);
-  if (write) rows_write_kernel<TD, MD, VEC, ONE><<<b, kRowsThreads, 0, s>>>(p);
-  else rows_read_kernel<TD, MD, VEC, ONE><<<b, kRowsThreads, 0, s>>>(p);
+cudaError_t launch_as(const RowsParams& p, bool write, cudaStream_t s) {
+  return launch_early(write ? rows_write_kernel<TD, MD, VEC, ONE> : rows_read_kernel<TD, MD, VEC, ONE>, blocks_for(p), kRowsThreads, 0, s, p);
 }
 
 template <int TD, int MD>
 cudaError_t launch_one(const RowsParams& p, bool write, cudaStream_t s) {
   const bool vec = vectors(p, MD), one = p.rounds == 1;
-  if (vec) one ? launch_as<TD, MD, true, true>(p, write, s) : launch_as<TD, MD, true, false>(p, write, s);
-  else one ? launch_as<TD, MD, false, true>(p, write, s) : launch_as<TD, MD, false, false>(p, write, s);
-  return cudaGetLastError();
+  if (vec) return one ? launch_as<TD, MD, true, true>(p, write, s) : launch_as<TD, MD, true, false>(p, write, s);
+  return one ? launch_as<TD, MD, false, true>(p, write, s) : launch_as<TD, MD, false, false>(p, write, s);
 }
 
 template <int TD>
