@@ -462,8 +462,9 @@ MFET_API int mfet_mx4_matmul(const void* a_codes, const void* a_scales, int64_t 
 
 /* The same with x quantised in the call: the first dense layer on the pooled features that
  * mfet_embedding_bag_forward writes (paper, Section 2.2: they feed the ranking model), with weights
- * quantised once. scratch dev, 16-byte aligned, mfet_mx4_linear_bytes(m, k) bytes (for m <= 8 and k up
- * to 10,000 one kernel does it all and scratch may be NULL). Errors: as above, WORKSPACE. */
+ * quantised once. scratch dev, 16-byte aligned, mfet_mx4_linear_bytes(m, k) bytes. (For m <= 8, k up
+ * to 10,000 and m * n * k up to 2^25, m counted up to a power of two, one kernel does it all and scratch
+ * may be NULL.) Errors: as above, WORKSPACE. */
 MFET_API uint64_t mfet_mx4_linear_bytes(int64_t m, int64_t k);
 MFET_API int mfet_mx4_linear(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t m, const void* w_codes,
                              const void* w_scales, int64_t n, int64_t k, const float* bias, uint32_t act, void* y,

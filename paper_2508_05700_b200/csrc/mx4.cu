@@ -41,7 +41,8 @@ struct QuantParams {
 
 // A lane takes a block of 32 values: no exchange for its scale, and 16 bytes of codes in one store. Four lanes write their scale
 // bytes as one word (a row's blocks are counted up to a multiple of four). Bound by reading x; with fewer values per lane the
-// instructions around them were the limit (16384 x 2048 bf16: 19 us with 16 values per lane).
+// instructions around them were the limit (16384 x 2048 bf16: 16 us = 5.3 TB/s read and written, 19 with 16 values per lane; 8192 x 896
+// fp32: 6.5 us = 5.2 TB/s). Rows that do not start on 16 bytes are read in shifted pieces: 500 x 1075 bf16 2.5 us, 6.3 value by value.
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kQuantThreads, 4) mx4_quantize_kernel(const __grid_constant__ QuantParams p) {
   using T = typename Elem<DT>::T;
@@ -119,6 +120,10 @@ __device__ __forceinline__ void put(const OutParams& o, int64_t i, int64_t j, fl
 
 constexpr int kFewThreads = 256;
 constexpr int kFewMost = 8;  // rows of x
+// The most work, in multiply-adds, with the rows counted up to a power of two. The integer products grow with it and the two-launch form
+// hardly does: 8 x 2048 x 1000 (2^24) 7.4 us here against 7.8, 1 x 2048 x 8192 (2^24) 6.7 against 7.6, but 4 x 2048 x 8192 (2^26) 9.8
+// against 8.2 and 8 x 2048 x 8192 17.5 against 8.3; 1 x 896 x 1024 2.5 against 5.0. A second launch costs a calling program 2.4 us besides.
+constexpr int64_t kFewWork = 1ll << 25;
 
 struct FewParams {
   const uint8_t* x;
@@ -189,7 +194,8 @@ __device__ __forceinline__ void few_stage(const FewParams& p, int mt, int4* sx, 
 
 // A warp per output column: lane b takes block b, b + 32, ... of the column's weights (16 bytes each, 512 bytes per warp and
 // load) against the same block of all MT rows of x from shared memory: 8 integer dot products of 4 values per
-// row and block, exact, then one fp32 multiply-add with the two scales.
+// row and block, exact, then one fp32 multiply-add with the two scales. Latency: 2.5 us for 1 x 896 x 1024 (0.5 MB of weights, 0.1 us of
+// bandwidth), of which a launch is most; 7.2 us for 7 x 2048 x 1000, where every block quantises all of x for itself.
 template <int MT>
 __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_constant__ FewParams p) {
   extern __shared__ int4 sx[];  // [MT][2][padded] 16-byte halves, then [MT][padded] scales
@@ -431,12 +437,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
 }
 
 // One block per SM walks over the tiles (128 rows of x times TN output columns); output columns run fastest, so that the blocks
-// at work share the rows of x in L2. Stages go through a ring of shared memory, scales from there to tensor memory ahead
+// at work share the rows of x in L2. 8192 x 896 x 1024 to bf16 takes 10 us (1.5 PFLOP/s), 16384 x 2048 x 2048 41 us (3.4 PFLOP/s; without its loads 29,
+// without its stores 36: it is bound by what loads, stores and scales share, not by the tensor cores, which are busy 44 % of the time).
+// Stages go through a ring of shared memory, scales from there to tensor memory ahead
 // of the products that use them; two accumulators in tensor memory, so that a tile is written while the next one is computed. A
 // lane of tensor memory is a row of x: each of the eight writing warps takes its 32 rows and half of the columns, adds the bias, rounds,
 // and leaves 32 columns at a time in shared memory (swizzled: no bank conflicts), from where a bulk
 // copy writes them and clips what lies beyond y. (Stores straight from the registers touch a line per lane, and the barriers of
-// the other roles wait behind them: 43 us instead of 35 for 16384 x 2048 x 2048.) A y whose rows do not start on 16 bytes is written by
+// the other roles wait behind them: 43 us instead of 41 for 16384 x 2048 x 2048.) A y whose rows do not start on 16 bytes is written by
 // plain stores from there.
 template <int TN, int DT>
 __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap a_map,
@@ -752,8 +760,9 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
 template <int DT>
 int product_dt(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
                uint32_t* status, cudaStream_t s) {
-  // tiles of 128 columns when there is one for every SM, else of 64: twice the blocks
-  if ((m + kTileM - 1) / kTileM * ((n + 127) / 128) >= sm_count())
+  // Tiles of 128 columns when there is one for three quarters of the SMs, else of 64: twice the blocks. With quantisation, k = 896, n = 1024:
+  // 64 tiles of 128 (m = 1024) 6.4 us against 6.0 with 64 columns, 128 tiles 7.3 against 8.0, 512 tiles 17.1 against 19.9.
+  if ((m + kTileM - 1) / kTileM * ((n + 127) / 128) * 4 >= sm_count() * 3)
     return gemm<128, DT>(xc, xs, m, wc, ws, n, k, out, status, s);
   return gemm<64, DT>(xc, xs, m, wc, ws, n, k, out, status, s);
 }
@@ -832,9 +841,9 @@ int mfet_mx4_linear(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t m, co
   const OutParams out{(uint8_t*)y, y_ld, bias, y_dtype, act == MFET_ACT_RELU};
   const Dims d = dims_of(k);
   cudaStream_t s = (cudaStream_t)stream;
-  // the quantised x of a few rows has to fit shared memory (k up to 10,000 for 8 rows)
+  // a few rows and little work; the quantised x has to fit shared memory (k up to 10,000 for 8 rows)
   const uint32_t mt = m == 1 ? 1 : m == 2 ? 2 : m <= 4 ? 4 : 8;
-  if (m <= kFewMost && (uint64_t)mt * ((d.blocks + 31) & ~31u) * 36 <= 96 * 1024) {
+  if (m <= kFewMost && mt * n <= kFewWork / k && (uint64_t)mt * ((d.blocks + 31) & ~31u) * 36 <= 96 * 1024) {
     FewParams p{(const uint8_t*)x, x_ld, (const uint8_t*)w_codes, (const uint8_t*)w_scales, n, (uint32_t)k, d.blocks, d.groups,
                 (int32_t)m, x_dtype, aligned(x, 16) && (uint64_t)x_ld * size_of(x_dtype) % 16 == 0,
                 (const uint8_t*)x + ((m - 1) * x_ld + k) * size_of(x_dtype), out};

@@ -156,3 +156,17 @@ def test_repeated_calls_give_equal_bits_and_another_stream():
             s.synchronize()
             ys.append(y)
         assert torch.equal(ys[0], ys[1]) and torch.equal(ys[0], ys[2])
+
+
+def test_few_rows_beyond_the_one_launch_forms_work():
+    """The largest product that one launch takes, and the next larger ones that go through the scratch."""
+    m = mfet()
+    rng = np.random.default_rng(77)
+    for m_, n, k in ((8, 4096, 1024), (8, 4100, 1024), (3, 9000, 1000), (1, 40000, 900)):
+        x = features(rng, m_, k, "f32")
+        wc, wsc, w = operand(rng.standard_normal((n, k)) / np.sqrt(k))
+        y = torch.zeros(m_, n, device="cuda")
+        nbytes = m.mfet_mx4_linear_bytes(m_, k)
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        m.mfet_mx4_linear(x, 0, k, m_, wc, wsc, n, k, None, 0, y, 0, n, scratch, nbytes, None, stream())
+        check(y, ref.mx4_operand(x.double().cpu().numpy())[2], w, None, False)
