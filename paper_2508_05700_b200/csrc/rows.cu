@@ -3,8 +3,8 @@
 // Both kernels move each byte once. A lane owns 32 bytes of a row of values (8 fp32 or 16 16-bit values), the lanes of a row are the
 // power of two that covers it (wider rows take several rounds of a whole warp), and a lane group works on kRowsInFlight rows at a
 // time, the list entries of the next ones under way: the table rows are scattered, and what the kernels wait for is their
-// latency. 2 M rows of 64 bf16 values into an 8 M-row MXFP4 table: 117 us for 421 MB of DRAM traffic; 4 M rows read from it: 206 us for
-// 1.1 GB (5.35 TB/s, 0.83 of a copy): a 48-byte row costs two DRAM lines as often as one. 37 k rows of 128 fp32 values written and 74 k read:
+// latency. 2 M rows of 64 bf16 values into an 8 M-row MXFP4 table and 4 M rows read from it: 338 us for 1.52 GB of DRAM traffic (4.5 TB/s; the
+// read alone 5.2): a 48-byte row costs 128 to 160 bytes of DRAM reads. 37 k rows of 128 fp32 values written and 74 k read:
 // 19 us, a few dependent loads per launch. More rows in flight or more blocks changed that by 4 % at most, and a whole block of 32 values
 // per lane made it slower (404 instead of 358 us, 30 instead of 19.5).
 #include <cstring>
@@ -64,8 +64,7 @@ __device__ __forceinline__ uint32_t int4_code(float x, float scale, float bias, 
   return (uint32_t)(int)fminf(15.f, fmaxf(0.f, rintf(q)));
 }
 
-// ONE: a row takes one round (up to 256 values of fp32, 512 of a 16-bit type)
-template <int TD, int SD, bool VEC, bool ONE>
+template <int TD, int SD, bool VEC>
 __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_kernel(const __grid_constant__ RowsParams p) {
   using S = typename Elem<SD>::T;
   constexpr int E = 32 / (int)sizeof(S), LPB = kMxBlock / E;  // values per lane, lanes per block of 32
@@ -76,7 +75,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
   const int lanes = 1 << p.lanes_log2, per_warp = 32 >> p.lanes_log2;
   const int sub = lane & (lanes - 1), group = lane >> p.lanes_log2;
   const int64_t step = (int64_t)gridDim.x * (kRowsThreads / 32) * per_warp * U;
-  const uint32_t rounds = ONE ? 1 : p.rounds;
+  const uint32_t rounds = p.rounds;
   int64_t w0 = (((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5) * per_warp * U;
   int64_t next[U];
 #pragma unroll
@@ -196,7 +195,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
   }
 }
 
-template <int TD, int DD, bool VEC, bool ONE>
+template <int TD, int DD, bool VEC>
 __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_read_kernel(const __grid_constant__ RowsParams p) {
   using D = typename Elem<DD>::T;
   constexpr int E = 32 / (int)sizeof(D), LPB = kMxBlock / E;
@@ -207,7 +206,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_read_kern
   const int lanes = 1 << p.lanes_log2, per_warp = 32 >> p.lanes_log2;
   const int sub = lane & (lanes - 1), group = lane >> p.lanes_log2;
   const int64_t step = (int64_t)gridDim.x * (kRowsThreads / 32) * per_warp * U;
-  const uint32_t rounds = ONE ? 1 : p.rounds;
+  const uint32_t rounds = p.rounds;
   constexpr bool kCodes = TD == MFET_MXFP4 || TD == MFET_INT4;
   constexpr int kTable = kCodes ? MFET_F32 : TD;  // element type of a row that is stored plainly
   int64_t w0 = (((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5) * per_warp * U;
@@ -322,16 +321,14 @@ unsigned blocks_for(const RowsParams& p) {
   return (unsigned)(want < most ? want : most);
 }
 
-template <int TD, int MD, bool VEC, bool ONE>
+template <int TD, int MD, bool VEC>
 cudaError_t launch_as(const RowsParams& p, bool write, cudaStream_t s) {
-  return launch_early(write ? rows_write_kernel<TD, MD, VEC, ONE> : rows_read_kernel<TD, MD, VEC, ONE>, blocks_for(p), kRowsThreads, 0, s, p);
+  return launch_early(write ? rows_write_kernel<TD, MD, VEC> : rows_read_kernel<TD, MD, VEC>, blocks_for(p), kRowsThreads, 0, s, p);
 }
 
 template <int TD, int MD>
 cudaError_t launch_one(const RowsParams& p, bool write, cudaStream_t s) {
-  const bool vec = vectors(p, MD), one = p.rounds == 1;
-  if (vec) return one ? launch_as<TD, MD, true, true>(p, write, s) : launch_as<TD, MD, true, false>(p, write, s);
-  return one ? launch_as<TD, MD, false, true>(p, write, s) : launch_as<TD, MD, false, false>(p, write, s);
+  return vectors(p, MD) ? launch_as<TD, MD, true>(p, write, s) : launch_as<TD, MD, false>(p, write, s);
 }
 
 template <int TD>
