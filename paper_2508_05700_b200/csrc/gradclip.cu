@@ -355,15 +355,19 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) grad_scale_ker
 // Few pieces: both steps in one launch of one cluster, whose blocks exchange their sums through distributed shared memory. On the device
 // one launch wins up to a piece per block (8000 fp32 values: 5.8 us against 6.6; 65536: 7.2 against 7.0; 131072: 8.4 against 7.0; 262144:
 // 11.1 against 6.9), but the second launch costs the calling program 2.4 us: up to two pieces per block.
+// Another block's shared memory may be written once that block runs, and must be there until the last store has arrived: one cluster barrier
+// ahead of the stores, whose arrival is given at the start so that nobody waits for it behind the sums, and one behind them.
 constexpr int kSmallBlocks = 8, kSmallPieces = 2 * kSmallBlocks;
 __global__ void __cluster_dims__(kSmallBlocks, 1, 1) __launch_bounds__(kClipThreads, kClipBlocksPerSm)
     grad_small_kernel(const __grid_constant__ GradParams<kFewTensors> p) {
   __shared__ double shared[kClipThreads / 32];
   __shared__ double all[kSmallBlocks];
   __shared__ Share<kFewTensors> share;
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   early_launch_wait();
   share.fill(p);
   const double s = block_sum(share_squares(p, share, blockIdx.x, kSmallBlocks), shared);
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   if (threadIdx.x < kSmallBlocks) {  // into every block's list
     uint32_t to;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&all[blockIdx.x])), "r"(threadIdx.x));

@@ -1,0 +1,62 @@
+"""Gradient clipping in the forms of a training step: next to other work, in place, the norm alone, constant and extreme values.
+
+Tolerances as in test_gpu_grad_clip.py: the norm is its fp64 value rounded to fp32 (1e-7 relative), an fp32 gradient is g times the fp32
+coefficient (1.3e-7 relative, 1e-45 absolute), a 16-bit one that product rounded once more."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.helpers import mfet
+from tests.lowbit_reference import within
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+REL, ABS = 1.3e-7, 1e-45
+
+
+class Clip:
+    """One list of gradients with its buffers."""
+
+    def __init__(self, src, dst, counts=None):
+        m = mfet()
+        self.grads = m.make_grads(src, dst, counts)
+        self.scratch = torch.full((m.mfet_grad_clip_bytes(len(src)),), 0xFF, dtype=torch.uint8, device="cuda")
+        self.norm = torch.full((1,), -1.0, device="cuda")
+
+    def __call__(self, max_norm, stream=None):
+        s = torch.cuda.current_stream() if stream is None else stream
+        mfet().mfet_grad_clip(self.grads, max_norm, self.norm, self.scratch, self.scratch.numel(), s.cuda_stream)
+        return self.norm
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def test_one_launch_calls_next_to_a_busy_stream():
+    """The blocks of the one-launch form's cluster start when the SMs have room: results are those of a quiet GPU."""
+    torch.manual_seed(0)
+    xs = [torch.randn(n, device="cuda") * 0.01 for n in (5, 4000, 65536, 120_000)]
+    ys = [torch.empty_like(x) for x in xs]
+    calls = [Clip([x], [y]) for x, y in zip(xs, ys)]
+    quiet = []
+    for c, y in zip(calls, ys):
+        c(0.05)
+        quiet.append((c.norm.clone(), y.clone()))
+    torch.cuda.synchronize()
+    a = torch.randn(4096, 4096, device="cuda").bfloat16()
+    busy, s = torch.cuda.Stream(), torch.cuda.Stream()
+    for rep in range(100):
+        with torch.cuda.stream(busy):
+            a @ a
+        for c, y in zip(calls, ys):
+            with torch.cuda.stream(s):
+                y.zero_()
+            c(0.05, s)
+        if rep % 10 == 9:
+            s.synchronize()
+            assert all(torch.equal(c.norm, n) and torch.equal(y, q) for c, y, (n, q) in zip(calls, ys, quiet))
+    torch.cuda.synchronize()

@@ -1,0 +1,38 @@
+"""Rules of the kernels of the clipping, row and matrix calls that no run on a GPU can show: read from the sources (no GPU needed)."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2508_05700_b200", "csrc")
+
+
+def code(name):
+    """A source file without its comments."""
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//[^\n]*|/\*.*?\*/", "", f.read(), flags=re.S)
+
+
+def body(text, name):
+    """The braces of the function `name`, its last definition."""
+    at = [m.start() for m in re.finditer(r"\b%s\(" % name, text)][-1]
+    start = text.index("{", text.index(")", at))
+    depth = 0
+    for i in range(start, len(text)):
+        depth += {"{": 1, "}": -1}.get(text[i], 0)
+        if depth == 0:
+            return text[start:i + 1]
+    raise AssertionError(name)
+
+
+def test_a_cluster_has_started_before_its_shared_memory_is_written():
+    """Memory of another block of the cluster exists once that block runs: a barrier comes ahead of the first access and one behind the last."""
+    found = 0
+    for name in sorted(os.listdir(CSRC)):
+        text = code(name) if name.endswith((".cu", ".cuh")) else ""
+        for kernel in re.findall(r"__cluster_dims__[^{;]*?(\w+)\(const", text, flags=re.S):
+            b = body(text, kernel)
+            first, last = b.index("shared::cluster"), b.rindex("st.shared::cluster")
+            waits = [m.start() for m in re.finditer(r"barrier\.cluster\.wait", b)]
+            assert waits and waits[0] < first, kernel
+            assert waits[-1] > last, kernel
+            found += 1
+    assert found == 1
