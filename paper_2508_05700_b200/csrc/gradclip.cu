@@ -189,7 +189,7 @@ __device__ __forceinline__ int64_t edge_element(const GradDev& t, int64_t v0, in
   return tail >= v0 && tail < v0 + kPieceVecs && !(tail == 0 && t.lead > 0) ? e : -1;
 }
 
-// 16 bytes through the read-only path, kept in L2 or among the first to leave it
+// 16 bytes, kept in L2 or among the first to leave it. (Not through the read-only path: one kernel may read and write a gradient.)
 __device__ __forceinline__ uint64_t l2_policy(bool keep) {
   uint64_t p;
   if (keep) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
@@ -198,7 +198,7 @@ __device__ __forceinline__ uint64_t l2_policy(bool keep) {
 }
 __device__ __forceinline__ uint4 load_with(const uint4* p, uint64_t policy) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                : "l"(p), "l"(policy));
   return v;
@@ -226,7 +226,7 @@ __device__ __forceinline__ double piece_squares(const GradDev& t, int64_t n, int
     uint4 v[kClipInFlight];
 #pragma unroll
     for (int j = 0; j < kClipInFlight; ++j)
-      v[j] = whole_vector<V>(t, v0 + j * kClipThreads + threadIdx.x, end) ? __ldg(at + j * kClipThreads) : make_uint4(0, 0, 0, 0);
+      v[j] = whole_vector<V>(t, v0 + j * kClipThreads + threadIdx.x, end) ? __ldcg(at + j * kClipThreads) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
     const int64_t e = edge_element<V>(t, v0, end);

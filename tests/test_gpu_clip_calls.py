@@ -60,3 +60,21 @@ def test_one_launch_calls_next_to_a_busy_stream():
             s.synchronize()
             assert all(torch.equal(c.norm, n) and torch.equal(y, q) for c, y, (n, q) in zip(calls, ys, quiet))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 7, 4096, 131_071, 400_003])
+def test_in_place_above_and_below_the_limit(n, dtype):
+    torch.manual_seed(n)
+    keep = (torch.randn(n + 3, device="cuda") * 0.01).to(DTYPES[dtype])
+    for shift in (0, 1):
+        x = keep.clone()
+        v = x[shift:shift + n]
+        total = math.sqrt(math.fsum(np.square(f64(v)).tolist()))
+        for limit in (total / 3, total * 3):
+            v.copy_(keep[shift:shift + n])
+            got = float(Clip([v], [v])(limit).item())
+            assert abs(got - total) <= 1e-7 * total
+            want = f64(keep[shift:shift + n]) * min(1.0, float(np.float32(limit)) / total)
+            assert within(v, want, ABS + REL * np.abs(want))
+            assert torch.equal(x[:shift], keep[:shift]) and torch.equal(x[shift + n:], keep[shift + n:])

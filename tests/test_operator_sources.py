@@ -36,3 +36,9 @@ def test_a_cluster_has_started_before_its_shared_memory_is_written():
             assert waits[-1] > last, kernel
             found += 1
     assert found == 1
+
+
+def test_gradients_are_not_read_through_the_read_only_path():
+    """Clipping in place writes what the same kernel has read, which that path does not allow for."""
+    text = code("gradclip.cu")
+    assert "ld.global.nc" not in text and "__ldg(" not in text
