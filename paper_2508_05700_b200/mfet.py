@@ -328,8 +328,9 @@ def dtype_of(t) -> int:
 
 def make_grads(src, dst, counts=None):
     """The list of gradient tensors of mfet_grad_clip, to be kept and used for every step: `src` and `dst` (entries may be
-    None, or the source itself) are torch tensors of one or two dimensions whose last one is dense; counts: i64 device
-    tensor with the number of live rows of every tensor, or None."""
+    None, or the source itself) are torch tensors of one or two dimensions whose last one is dense and whose rows do not overlap
+    (an expanded tensor is refused: make it contiguous first); counts: i64 device tensor with the number of live rows of every
+    tensor, or None."""
     arr = (Grad * max(len(src), 1))()
     for i, (a, b) in enumerate(zip(src, dst)):
         if b is not None and (b.dtype != a.dtype or b.shape != a.shape or b.stride() != a.stride()):
@@ -338,6 +339,8 @@ def make_grads(src, dst, counts=None):
         if two is None or (two.shape[1] > 1 and two.stride(1) != 1):
             raise MfetError(ERR_INVALID_ARG, "make_grads: tensor %d is not rows of neighbouring elements" % i)
         rows, cols = two.shape
+        if rows > 1 and two.stride(0) < cols:  # an expanded tensor: its stride of 0 would mean `cols` to the library
+            raise MfetError(ERR_INVALID_ARG, "make_grads: rows of tensor %d share memory" % i)
         ld = two.stride(0) if rows > 1 else cols
         arr[i] = Grad(_ptr(a), _ptr(b), rows, cols, ld, None if counts is None else _ptr(counts) + 8 * i, dtype_of(a), 0)
     return arr, len(src)

@@ -130,3 +130,19 @@ def test_mx4_refusals():
 def test_struct_layout():
     m = mfet()
     assert C.sizeof(m.Grad) == 56 and m.Grad.n_rows.offset == 40 and m.Grad.dtype.offset == 48
+
+
+def test_make_grads_refuses_rows_that_share_memory():
+    """An expanded tensor's rows are one row in memory; as a stride of 0 it would be read as rows one behind the other."""
+    import torch
+    m = mfet()
+    w = torch.zeros(4, 6, requires_grad=True)
+    grad, = torch.autograd.grad((w.sum(0) * torch.arange(6.0)).sum(), w)
+    assert grad.stride() == (0, 1)
+    for t in (grad, torch.zeros(64).expand(10, 64), torch.zeros(1, 1).expand(5, 1), torch.zeros(20).as_strided((4, 6), (3, 1)),
+              torch.zeros(1).expand(7)):
+        assert status(m.make_grads, [t], [None]) == m.ERR_INVALID_ARG
+        assert status(m.make_grads, [t], [t]) == m.ERR_INVALID_ARG
+    for t in (torch.zeros(64).expand(1, 64), torch.zeros(0, 6), torch.zeros(4, 0), torch.zeros(()), torch.zeros(2, 3, 4), torch.zeros(5, 1)):
+        arr, n = m.make_grads([t], [t])
+        assert n == 1 and arr[0].rows * arr[0].cols == t.numel() and (arr[0].rows < 2 or arr[0].ld >= arr[0].cols)
