@@ -329,8 +329,12 @@ def dtype_of(t) -> int:
 def make_grads(src, dst, counts=None):
     """The list of gradient tensors of mfet_grad_clip, to be kept and used for every step: `src` and `dst` (entries may be
     None, or the source itself) are torch tensors of one or two dimensions whose last one is dense and whose rows do not overlap
-    (an expanded tensor is refused: make it contiguous first); counts: i64 device tensor with the number of live rows of every
-    tensor, or None."""
+    (an expanded tensor is refused: make it contiguous first); counts: dense i64 tensor on their device with the number of
+    live rows of every tensor, or None."""
+    if counts is not None:
+        elsewhere = {t.device for t in src} - {counts.device}
+        if str(counts.dtype) != "torch.int64" or not counts.is_contiguous() or counts.numel() < len(src) or elsewhere:
+            raise MfetError(ERR_INVALID_ARG, "make_grads: counts is not a dense int64 tensor of %d entries beside the gradients" % len(src))
     arr = (Grad * max(len(src), 1))()
     for i, (a, b) in enumerate(zip(src, dst)):
         if b is not None and (b.dtype != a.dtype or b.shape != a.shape or b.stride() != a.stride()):

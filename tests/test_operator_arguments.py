@@ -146,3 +146,16 @@ def test_make_grads_refuses_rows_that_share_memory():
     for t in (torch.zeros(64).expand(1, 64), torch.zeros(0, 6), torch.zeros(4, 0), torch.zeros(()), torch.zeros(2, 3, 4), torch.zeros(5, 1)):
         arr, n = m.make_grads([t], [t])
         assert n == 1 and arr[0].rows * arr[0].cols == t.numel() and (arr[0].rows < 2 or arr[0].ld >= arr[0].cols)
+
+
+def test_make_grads_looks_at_the_counts():
+    """The library reads one 64-bit count per tensor, 8 bytes apart."""
+    import torch
+    m = mfet()
+    a, b = torch.zeros(4, 6), torch.zeros(5, 3)
+    for counts in (torch.zeros(2, dtype=torch.int32), torch.zeros(2), torch.zeros(1, dtype=torch.int64), torch.zeros(4, dtype=torch.int64)[::2],
+                   torch.zeros(0, dtype=torch.int64), torch.zeros(1, dtype=torch.int64).expand(2), torch.zeros(2, dtype=torch.int64, device="meta")):
+        assert status(m.make_grads, [a, b], [None, None], counts) == m.ERR_INVALID_ARG
+    for counts in (torch.zeros(2, dtype=torch.int64), torch.zeros(3, dtype=torch.int64), torch.zeros(2, 1, dtype=torch.int64)):
+        arr, n = m.make_grads([a, b], [None, b], counts)
+        assert n == 2 and [arr[i].n_rows for i in range(2)] == [counts.data_ptr(), counts.data_ptr() + 8]
