@@ -331,14 +331,16 @@ def make_grads(src, dst, counts=None):
     None, or the source itself) are torch tensors of one or two dimensions whose last one is dense and whose rows do not overlap
     (an expanded tensor is refused: make it contiguous first); counts: dense i64 tensor on their device with the number of
     live rows of every tensor, or None."""
+    if len(src) != len(dst):
+        raise MfetError(ERR_INVALID_ARG, "make_grads: %d tensors and %d destinations" % (len(src), len(dst)))
     if counts is not None:
         elsewhere = {t.device for t in src} - {counts.device}
         if str(counts.dtype) != "torch.int64" or not counts.is_contiguous() or counts.numel() < len(src) or elsewhere:
             raise MfetError(ERR_INVALID_ARG, "make_grads: counts is not a dense int64 tensor of %d entries beside the gradients" % len(src))
     arr = (Grad * max(len(src), 1))()
     for i, (a, b) in enumerate(zip(src, dst)):
-        if b is not None and (b.dtype != a.dtype or b.shape != a.shape or b.stride() != a.stride()):
-            raise MfetError(ERR_INVALID_ARG, "make_grads: tensor %d and its destination differ in type, shape or strides" % i)
+        if b is not None and (b.dtype != a.dtype or b.shape != a.shape or b.stride() != a.stride() or b.device != a.device):
+            raise MfetError(ERR_INVALID_ARG, "make_grads: tensor %d and its destination differ in type, shape, strides or device" % i)
         two = a if a.dim() == 2 else a.reshape(1, -1) if a.is_contiguous() else None
         if two is None or (two.shape[1] > 1 and two.stride(1) != 1):
             raise MfetError(ERR_INVALID_ARG, "make_grads: tensor %d is not rows of neighbouring elements" % i)

@@ -159,3 +159,20 @@ def test_make_grads_looks_at_the_counts():
     for counts in (torch.zeros(2, dtype=torch.int64), torch.zeros(3, dtype=torch.int64), torch.zeros(2, 1, dtype=torch.int64)):
         arr, n = m.make_grads([a, b], [None, b], counts)
         assert n == 2 and [arr[i].n_rows for i in range(2)] == [counts.data_ptr(), counts.data_ptr() + 8]
+
+
+def test_make_grads_wants_a_destination_for_every_tensor():
+    """A list that ends early would drop the tensors behind its end from the norm."""
+    import torch
+    m = mfet()
+    a, b = torch.zeros(4, 6), torch.zeros(5, 3)
+    for src, dst in (([a, b], [a]), ([a], [a, b]), ([], [None]), ([a], [])):
+        assert status(m.make_grads, src, dst) == m.ERR_INVALID_ARG
+    assert m.make_grads([], [])[1] == 0
+
+
+def test_make_grads_wants_a_destination_on_the_same_device():
+    import torch
+    m = mfet()
+    a = torch.zeros(4, 6)
+    assert status(m.make_grads, [a], [torch.zeros(4, 6, device="meta")]) == m.ERR_INVALID_ARG
