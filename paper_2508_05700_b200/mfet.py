@@ -330,7 +330,8 @@ def make_grads(src, dst, counts=None):
     """The list of gradient tensors of mfet_grad_clip, to be kept and used for every step: `src` and `dst` (entries may be
     None, or the source itself) are torch tensors of one or two dimensions whose last one is dense and whose rows do not overlap
     (an expanded tensor is refused: make it contiguous first); counts: dense i64 tensor on their device with the number of
-    live rows of every tensor, or None."""
+    live rows of every tensor, or None. The list keeps the tensors alive and goes on using their memory: a program whose
+    gradients are new tensors in every step (zero_grad(set_to_none=True)) makes a new list in every step."""
     if len(src) != len(dst):
         raise MfetError(ERR_INVALID_ARG, "make_grads: %d tensors and %d destinations" % (len(src), len(dst)))
     if counts is not None:
@@ -349,6 +350,7 @@ def make_grads(src, dst, counts=None):
             raise MfetError(ERR_INVALID_ARG, "make_grads: rows of tensor %d share memory" % i)
         ld = two.stride(0) if rows > 1 else cols
         arr[i] = Grad(_ptr(a), _ptr(b), rows, cols, ld, None if counts is None else _ptr(counts) + 8 * i, dtype_of(a), 0)
+    arr.tensors = (list(src), list(dst), counts)  # what the addresses point at lives as long as the list
     return arr, len(src)
 
 

@@ -176,3 +176,22 @@ def test_make_grads_wants_a_destination_on_the_same_device():
     m = mfet()
     a = torch.zeros(4, 6)
     assert status(m.make_grads, [a], [torch.zeros(4, 6, device="meta")]) == m.ERR_INVALID_ARG
+
+
+def test_make_grads_keeps_what_its_addresses_point_at():
+    """The list is kept from step to step: the memory behind it must not be handed to somebody else meanwhile."""
+    import gc
+    import weakref
+
+    import torch
+    m = mfet()
+
+    def make():
+        src, dst, counts = [torch.zeros(4, 6), torch.zeros(7)], [torch.zeros(4, 6), None], torch.zeros(2, dtype=torch.int64)
+        return m.make_grads(src, dst, counts), [weakref.ref(t) for t in src + dst[:1] + [counts]]
+    grads, held = make()
+    gc.collect()
+    assert all(r() is not None for r in held)
+    del grads
+    gc.collect()
+    assert all(r() is None for r in held)
