@@ -380,7 +380,8 @@ MFET_API int mfet_tables_version(const mfet_tables_t* t, uint64_t* version /*hos
 /* ---- after the backward pass: clipping, writing rows back, the first dense layer ----
  * These calls take no handle: they work on caller memory of the current GPU, with the
  * sizes, formats and lists that the calls above use. They are asynchronous on `stream`.
- * `status` is a device word (or NULL) into which the kernels OR MFET_DEV_* bits. */
+ * `status` is a device word (or NULL) into which the kernels OR MFET_DEV_* bits. An address that is not aligned
+ * to its type (lists and counts to 8 bytes, status, bias and norm to 4) is MFET_ERR_ALIGNMENT. */
 
 /* One gradient tensor: rows x cols elements of dtype MFET_F32 / MFET_F16 / MFET_BF16, `ld`
  * elements apart (0 = cols). n_rows: NULL, or a device count of which at most `rows` rows

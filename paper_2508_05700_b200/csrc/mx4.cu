@@ -819,7 +819,9 @@ int mfet_mx4_matmul(const void* a_codes, const void* a_scales, int64_t m, const 
   if (rc != MFET_OK) return rc;
   if (m == 0 || n == 0) return MFET_OK;
   if (!a_codes || !a_scales || !w_codes || !w_scales) return MFET_ERR_INVALID_ARG;
-  if (!aligned(a_codes, 16) || !aligned(a_scales, 16) || !aligned(w_codes, 16) || !aligned(w_scales, 16)) return MFET_ERR_ALIGNMENT;
+  if (!aligned(a_codes, 16) || !aligned(a_scales, 16) || !aligned(w_codes, 16) || !aligned(w_scales, 16) ||
+      !aligned(status, 4))
+    return MFET_ERR_ALIGNMENT;
   const OutParams out{(uint8_t*)y, y_ld, bias, y_dtype, act == MFET_ACT_RELU};
   return product(a_codes, a_scales, m, w_codes, w_scales, n, k, out, status, (cudaStream_t)stream);
 }
@@ -837,7 +839,7 @@ int mfet_mx4_linear(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t m, co
   if (rc != MFET_OK) return rc;
   if (m == 0 || n == 0) return MFET_OK;
   if (!x || !w_codes || !w_scales) return MFET_ERR_INVALID_ARG;
-  if (!aligned(x, size_of(x_dtype)) || !aligned(w_codes, 16) || !aligned(w_scales, 16)) return MFET_ERR_ALIGNMENT;
+  if (!aligned(x, size_of(x_dtype)) || !aligned(w_codes, 16) || !aligned(w_scales, 16) || !aligned(status, 4)) return MFET_ERR_ALIGNMENT;
   const OutParams out{(uint8_t*)y, y_ld, bias, y_dtype, act == MFET_ACT_RELU};
   const Dims d = dims_of(k);
   cudaStream_t s = (cudaStream_t)stream;

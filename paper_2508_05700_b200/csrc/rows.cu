@@ -345,6 +345,7 @@ int run_rows(const mfet_table_desc_t* d, const int64_t* list, int64_t n, const i
   RowsParams p;
   const int rc = check(d, list, n, mem, mem_dtype, ld, &p);
   if (rc != MFET_OK) return rc;
+  if (((uintptr_t)list & 7u) || ((uintptr_t)n_dev & 7u) || ((uintptr_t)status & 3u)) return MFET_ERR_ALIGNMENT;
   if (n == 0) return MFET_OK;
   p.n_dev = n_dev;
   p.status = status;

@@ -195,3 +195,18 @@ def test_make_grads_keeps_what_its_addresses_point_at():
     del grads
     gc.collect()
     assert all(r() is None for r in held)
+
+
+def test_lists_counts_and_status_words_are_aligned():
+    """A kernel reads them as 64-bit and 32-bit words: an address between two words is refused like any other."""
+    m = mfet()
+    A = 1 << 20
+    d = m.TableDesc(A, 100, 64, m.MXFP4, m.LOC_DEVICE, 0, 0, 0)
+    for call in (m.mfet_rows_write, m.mfet_rows_read):
+        for off in (1, 4):
+            assert status(call, d, A + off, 5, None, A, m.F32, 64) == m.ERR_ALIGNMENT
+            assert status(call, d, A, 5, A + off, A, m.F32, 64) == m.ERR_ALIGNMENT
+        assert status(call, d, A, 5, None, A, m.F32, 64, A + 2) == m.ERR_ALIGNMENT
+    assert status(m.mfet_mx4_matmul, A, A, 200, A, A, 64, 64, None, 0, A, m.F32, 64, A + 2) == m.ERR_ALIGNMENT
+    assert status(m.mfet_mx4_linear, A, m.F32, 64, 200, A, A, 64, 64, None, 0, A, m.F32, 64, A, 1 << 20, A + 1) == m.ERR_ALIGNMENT
+    assert status(m.mfet_mx4_linear, A, m.F32, 64, 2, A, A, 64, 64, None, 0, A, m.F32, 64, None, 0, A + 1) == m.ERR_ALIGNMENT
