@@ -27,11 +27,14 @@ static struct {
 static PyObject *fail, *data_ptr;
 
 /* The n arguments of `name`, of which the last may be left out down to `least`: kinds p = address, i = integer, f = float,
- * b = an object that lends its memory (a ctypes structure or array), o = any object. */
-typedef union {
-  long long i;
-  void* p;
-  double f;
+ * b = an object that lends its memory (a ctypes structure or array; `bytes` is its length), o = any object. */
+typedef struct {
+  union {
+    long long i;
+    void* p;
+    double f;
+  };
+  Py_ssize_t bytes;
 } arg_t;
 
 static int address(PyObject* o, void** p) {
@@ -73,6 +76,7 @@ static int parse(const char* name, const char* kinds, Py_ssize_t least, PyObject
           Py_buffer view; /* the caller's reference keeps the memory for the length of the call */
           if (PyObject_GetBuffer(args[k], &view, PyBUF_SIMPLE) != 0) return 0;
           a[k].p = view.buf;
+          a[k].bytes = view.len;
           PyBuffer_Release(&view);
         }
         break;
@@ -112,6 +116,8 @@ static PyObject* py_grad_clip(PyObject* self, PyObject* const* args, Py_ssize_t 
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "mfet_grad_clip: what make_grads gave is wanted");
     return NULL;
   }
+  /* a list that is shorter than it says */
+  if (g[0].p && g[1].i > g[0].bytes / (Py_ssize_t)sizeof(mfet_grad_t)) return done(MFET_ERR_INVALID_ARG, name);
   RUN(lib.grad_clip((const mfet_grad_t*)g[0].p, (int32_t)g[1].i, (float)a[1].f, (float*)a[2].p, a[3].p, (uint64_t)a[4].i, a[5].p));
   return done(status, name);
 }
@@ -119,6 +125,7 @@ static PyObject* py_grad_clip(PyObject* self, PyObject* const* args, Py_ssize_t 
 static PyObject* rows(rows_fn f, const char* name, PyObject* const* args, Py_ssize_t n) {
   arg_t a[9];
   if (!parse(name, "bpippiipp", 7, args, n, a)) return NULL;
+  if (a[0].p && a[0].bytes < (Py_ssize_t)sizeof(mfet_table_desc_t)) return done(MFET_ERR_INVALID_ARG, name);
   RUN(f((const mfet_table_desc_t*)a[0].p, (const int64_t*)a[1].p, a[2].i, (const int64_t*)a[3].p, a[4].p, (uint32_t)a[5].i, a[6].i,
         (uint32_t*)a[7].p, a[8].p));
   return done(status, name);

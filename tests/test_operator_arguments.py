@@ -210,3 +210,17 @@ def test_lists_counts_and_status_words_are_aligned():
     assert status(m.mfet_mx4_matmul, A, A, 200, A, A, 64, 64, None, 0, A, m.F32, 64, A + 2) == m.ERR_ALIGNMENT
     assert status(m.mfet_mx4_linear, A, m.F32, 64, 200, A, A, 64, 64, None, 0, A, m.F32, 64, A, 1 << 20, A + 1) == m.ERR_ALIGNMENT
     assert status(m.mfet_mx4_linear, A, m.F32, 64, 2, A, A, 64, 64, None, 0, A, m.F32, 64, None, 0, A + 1) == m.ERR_ALIGNMENT
+
+
+def test_descriptors_shorter_than_their_structure():
+    """The library reads whole structures: what lends less memory than that is refused."""
+    m = mfet()
+    A = 1 << 20
+    for call in (m.mfet_rows_write, m.mfet_rows_read):
+        for short in (b"", bytes(47), bytearray(16)):
+            assert status(call, short, A, 5, None, A, m.F32, 64) == m.ERR_INVALID_ARG
+        assert status(call, None, A, 5, None, A, m.F32, 64) == m.ERR_INVALID_ARG
+    one = (m.Grad * 1)(m.Grad(A, A, 4, 8, 0, None, m.F32, 0))
+    for n in (2, 1000, 2**31 - 1):
+        assert status(m.mfet_grad_clip, (one, n), 1.0, A, A, 1 << 20) == m.ERR_INVALID_ARG
+    assert status(m.mfet_grad_clip, (bytes(55), 1), 1.0, A, A, 1 << 20) == m.ERR_INVALID_ARG
