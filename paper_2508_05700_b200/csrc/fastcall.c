@@ -26,8 +26,9 @@ static struct {
 } lib;
 static PyObject *fail, *data_ptr;
 
-/* The n arguments of `name`, of which the last may be left out down to `least`: kinds p = address, i = integer, f = float,
- * b = an object that lends its memory (a ctypes structure or array; `bytes` is its length), o = any object. */
+/* The n arguments of `name`, of which the last may be left out down to `least`: kinds p = address, i = integer (u: of 32 bits
+ * without a sign, d: with one, z: not negative; another value is MFET_ERR_INVALID_ARG), f = float, b = an object that lends its memory
+ * (a ctypes structure or array; `bytes` is its length), o = any object. */
 typedef struct {
   union {
     long long i;
@@ -51,6 +52,16 @@ static int address(PyObject* o, void** p) {
   const int ok = !PyErr_Occurred();
   if (v != o) Py_DECREF(v);
   return ok;
+}
+
+static PyObject* done(int status, const char* name) {
+  if (status == MFET_OK) Py_RETURN_NONE;
+  PyObject* r = PyObject_CallFunction(fail, "is", status, name);
+  if (r) {
+    Py_DECREF(r);
+    PyErr_Format(PyExc_RuntimeError, "%s: status %d", name, status);
+  }
+  return NULL;
 }
 
 static int parse(const char* name, const char* kinds, Py_ssize_t least, PyObject* const* args, Py_ssize_t n, arg_t* a) {
@@ -85,19 +96,14 @@ static int parse(const char* name, const char* kinds, Py_ssize_t least, PyObject
       default:
         a[k].i = PyLong_AsLongLong(args[k]);
         if (a[k].i == -1 && PyErr_Occurred()) return 0;
+        if ((kinds[k] == 'u' && (a[k].i < 0 || a[k].i > (long long)UINT32_MAX)) ||
+            (kinds[k] == 'd' && (a[k].i < INT32_MIN || a[k].i > INT32_MAX)) || (kinds[k] == 'z' && a[k].i < 0)) {
+          done(MFET_ERR_INVALID_ARG, name);
+          return 0;
+        }
     }
   }
   return 1;
-}
-
-static PyObject* done(int status, const char* name) {
-  if (status == MFET_OK) Py_RETURN_NONE;
-  PyObject* r = PyObject_CallFunction(fail, "is", status, name);
-  if (r) {
-    Py_DECREF(r);
-    PyErr_Format(PyExc_RuntimeError, "%s: status %d", name, status);
-  }
-  return NULL;
 }
 
 #define RUN(call)          \
@@ -109,10 +115,10 @@ static PyObject* done(int status, const char* name) {
 static PyObject* py_grad_clip(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   static const char name[] = "mfet_grad_clip";
   arg_t a[6];
-  if (!parse(name, "ofppip", 5, args, n, a)) return NULL;
+  if (!parse(name, "ofppzp", 5, args, n, a)) return NULL;
   PyObject* list = args[0];
   arg_t g[2];
-  if (!PyTuple_Check(list) || !parse(name, "bi", 2, &PyTuple_GET_ITEM(list, 0), PyTuple_GET_SIZE(list), g)) {
+  if (!PyTuple_Check(list) || !parse(name, "bd", 2, &PyTuple_GET_ITEM(list, 0), PyTuple_GET_SIZE(list), g)) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "mfet_grad_clip: what make_grads gave is wanted");
     return NULL;
   }
@@ -124,7 +130,7 @@ static PyObject* py_grad_clip(PyObject* self, PyObject* const* args, Py_ssize_t 
 
 static PyObject* rows(rows_fn f, const char* name, PyObject* const* args, Py_ssize_t n) {
   arg_t a[9];
-  if (!parse(name, "bpippiipp", 7, args, n, a)) return NULL;
+  if (!parse(name, "bpippuipp", 7, args, n, a)) return NULL;
   if (a[0].p && a[0].bytes < (Py_ssize_t)sizeof(mfet_table_desc_t)) return done(MFET_ERR_INVALID_ARG, name);
   RUN(f((const mfet_table_desc_t*)a[0].p, (const int64_t*)a[1].p, a[2].i, (const int64_t*)a[3].p, a[4].p, (uint32_t)a[5].i, a[6].i,
         (uint32_t*)a[7].p, a[8].p));
@@ -136,7 +142,7 @@ static PyObject* py_rows_read(PyObject* self, PyObject* const* args, Py_ssize_t 
 static PyObject* py_quantize(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   static const char name[] = "mfet_mx4_quantize";
   arg_t a[8];
-  if (!parse(name, "piiiippp", 7, args, n, a)) return NULL;
+  if (!parse(name, "puiiippp", 7, args, n, a)) return NULL;
   RUN(lib.quantize(a[0].p, (uint32_t)a[1].i, a[2].i, a[3].i, a[4].i, a[5].p, a[6].p, a[7].p));
   return done(status, name);
 }
@@ -144,7 +150,7 @@ static PyObject* py_quantize(PyObject* self, PyObject* const* args, Py_ssize_t n
 static PyObject* py_matmul(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   static const char name[] = "mfet_mx4_matmul";
   arg_t a[14];
-  if (!parse(name, "ppippiipipiipp", 12, args, n, a)) return NULL;
+  if (!parse(name, "ppippiipupuipp", 12, args, n, a)) return NULL;
   RUN(lib.matmul(a[0].p, a[1].p, a[2].i, a[3].p, a[4].p, a[5].i, a[6].i, (const float*)a[7].p, (uint32_t)a[8].i, a[9].p,
                  (uint32_t)a[10].i, a[11].i, (uint32_t*)a[12].p, a[13].p));
   return done(status, name);
@@ -153,7 +159,7 @@ static PyObject* py_matmul(PyObject* self, PyObject* const* args, Py_ssize_t n) 
 static PyObject* py_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   static const char name[] = "mfet_mx4_linear";
   arg_t a[17];
-  if (!parse(name, "piiippiipipiipipp", 15, args, n, a)) return NULL;
+  if (!parse(name, "puiippiipupuipzpp", 15, args, n, a)) return NULL;
   RUN(lib.linear(a[0].p, (uint32_t)a[1].i, a[2].i, a[3].i, a[4].p, a[5].p, a[6].i, a[7].i, (const float*)a[8].p, (uint32_t)a[9].i,
                  a[10].p, (uint32_t)a[11].i, a[12].i, a[13].p, (uint64_t)a[14].i, (uint32_t*)a[15].p, a[16].p));
   return done(status, name);

@@ -224,3 +224,25 @@ def test_descriptors_shorter_than_their_structure():
     for n in (2, 1000, 2**31 - 1):
         assert status(m.mfet_grad_clip, (one, n), 1.0, A, A, 1 << 20) == m.ERR_INVALID_ARG
     assert status(m.mfet_grad_clip, (bytes(55), 1), 1.0, A, A, 1 << 20) == m.ERR_INVALID_ARG
+
+
+def test_integers_that_do_not_fit_their_argument():
+    """2^32 is no dtype 0, and -1 bytes of scratch are not 2^64 - 1."""
+    m = mfet()
+    A, big = 1 << 20, 1 << 32
+    d = m.TableDesc(A, 100, 64, m.MXFP4, m.LOC_DEVICE, 0, 0, 0)
+    for wrong in (big, big + 2, -big, -1, 2**62):
+        for call in (m.mfet_rows_write, m.mfet_rows_read):
+            assert status(call, d, A, 5, None, A, wrong, 64) == m.ERR_INVALID_ARG
+        assert status(m.mfet_mx4_quantize, A, wrong, 64, 4, 64, A, A) == m.ERR_INVALID_ARG
+        assert status(m.mfet_mx4_matmul, A, A, 200, A, A, 64, 64, None, wrong, A, m.F32, 64) == m.ERR_INVALID_ARG
+        assert status(m.mfet_mx4_matmul, A, A, 200, A, A, 64, 64, None, 0, A, wrong, 64) == m.ERR_INVALID_ARG
+        for at in (1, 9, 11):
+            args = [A, m.F32, 64, 200, A, A, 64, 64, None, 0, A, m.F32, 64, A, 1 << 20]
+            args[at] = wrong
+            assert status(m.mfet_mx4_linear, *args) == m.ERR_INVALID_ARG
+        assert status(m.mfet_grad_clip, (None, -big + (wrong & 1)), 1.0, A, A, 1 << 20) == m.ERR_INVALID_ARG
+    for nbytes in (-1, -2**63):
+        one = (m.Grad * 1)(m.Grad(A, A, 4, 8, 0, None, m.F32, 0))
+        assert status(m.mfet_grad_clip, (one, 1), 1.0, A, A, nbytes) == m.ERR_INVALID_ARG
+        assert status(m.mfet_mx4_linear, A, m.F32, 64, 200, A, A, 64, 64, None, 0, A, m.F32, 64, A, nbytes) == m.ERR_INVALID_ARG
