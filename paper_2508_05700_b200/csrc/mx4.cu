@@ -488,11 +488,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
   // made it slower (8192 x 896 x 1024 with its quantisation: 21 instead of 17 us).
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
+  uint64_t filled = 0;  // stages that this lane has asked for
+  bool issues = false;  // this lane issues the products
   if (warp == 0) {
     // One lane runs this role from end to end: what it does per stage is on the critical path of a product with many tiles.
     if (elect_one()) {
       uint32_t st = 0, phase = 1;  // an empty barrier's phase before the first is taken as complete
-      uint64_t filled = 0;
       bool ok = true;
       for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next()) {
         const int32_t ya = (int32_t)(w.tm * kTileM), yb = (int32_t)(w.tn * TN);
@@ -511,18 +512,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
           if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
         }
       }
-      // Every copy that this lane started has to land before the block ends. The products wait for each of them; only
-      // when a wait has run out are they waited for here.
-      if (!ok || dead) {
-        volatile int none = 0;
-        const uint64_t from = filled > G::stages ? filled - G::stages : 0;
-        for (uint64_t i = from; i < filled; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
-      }
     }
   } else if (warp == 1) {
     // One lane runs this role from end to end. The tensor cores' queue is short, so what the lane does between the instructions of two
     // stages has to be short too: stage and phase are counted along, and the next stage's barrier is asked between this one's instructions.
     if (elect_one()) {
+      issues = true;
       uint32_t st = 0, phase = 0, done = 0, set = 0;
       bool ok = true, ready = false;
       for (TileWalk w(p.n_tiles); ok && w.t < p.tiles; w.next(), ++done) {
@@ -564,11 +559,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
           mma_commit(this_empty);
           if (s + 1 == p.stages_k) mma_commit(acc_full(acc));
         }
-      }
-      if (!ok || dead) {  // the products under way read shared memory and write tensor memory: let them end
-        volatile int none = 0;
-        mma_commit(drained);
-        bar_wait(drained, 0, &none);
       }
     }
   } else {
@@ -638,7 +628,20 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  if (dead && threadIdx.x == 0 && p.status) atomicOr(p.status, (uint32_t)MFET_DEV_STALLED);
+  // Without a stall every copy and product has been waited for by the role that needed it. After one, whoever was ahead of the role that
+  // gave up has left some under way: all roles have ended here, so what is waited for now (with the same limit) is the last of them.
+  if (dead) {
+    volatile int none = 0;
+    const uint64_t from = filled > G::stages ? filled - G::stages : 0;
+    for (uint64_t i = from; i < filled; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
+    if (issues) {
+      mma_commit(drained);
+      bar_wait(drained, 0, &none);
+    }
+    if (threadIdx.x == 0 && p.status) atomicOr(p.status, (uint32_t)MFET_DEV_STALLED);
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  }
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 

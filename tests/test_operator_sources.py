@@ -42,3 +42,14 @@ def test_gradients_are_not_read_through_the_read_only_path():
     """Clipping in place writes what the same kernel has read, which that path does not allow for."""
     text = code("gradclip.cu")
     assert "ld.global.nc" not in text and "__ldg(" not in text
+
+
+def test_the_product_ends_with_nothing_under_way():
+    """When a wait of the product has run out in one role, the other roles may have ended before: copies and products are waited for once all roles
+    have, and only then is the tensor memory freed."""
+    b = body(code("mx4.cu"), "mx4_gemm_kernel")
+    last_role = b.index("cp.async.bulk.wait_group.read 0;")
+    joined = b.index("__syncthreads();", last_role)
+    copies, products = b.rindex("bar_wait(full("), b.rindex("mma_commit(drained)")
+    assert joined < copies and joined < products
+    assert b.index("bar_wait(drained", products) < b.index("__syncthreads();", max(copies, products)) < b.index("tcgen05.dealloc")
