@@ -124,6 +124,7 @@ constexpr int kFewMost = 8;  // rows of x
 // hardly does: 8 x 2048 x 1000 (2^24) 7.4 us here against 7.8, 1 x 2048 x 8192 (2^24) 6.7 against 7.6, but 4 x 2048 x 8192 (2^26) 9.8
 // against 8.2 and 8 x 2048 x 8192 17.5 against 8.3; 1 x 896 x 1024 2.5 against 5.0. A second launch costs a calling program 2.4 us besides.
 constexpr int64_t kFewWork = 1ll << 25;
+constexpr uint32_t kFewSmem = 96 * 1024;  // the quantised x has to fit this (k up to 10,000 for 8 rows)
 
 struct FewParams {
   const uint8_t* x;
@@ -724,6 +725,20 @@ bool out_map(CUtensorMap* map, const OutParams& o, int64_t m, int64_t n, uint32_
            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Lets a kernel use `bytes` of dynamic shared memory on the current GPU: always the same number for a kernel, so that no thread takes away
+// what another one is about to launch with. ready: one bit per GPU where that is done.
+template <typename K>
+cudaError_t allow_smem(K kernel, uint32_t bytes, std::atomic<uint64_t>* ready) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (ready->load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) ready->fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 template <int TN, int DT>
 int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
          uint32_t* status, cudaStream_t s) {
@@ -745,16 +760,8 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   p.bulk_y = aligned(out.y, 16) && (uint64_t)out.ld * size_of(out.dtype) % 16 == 0;
   if (!p.bulk_y) y = a;  // not used
   else if (!out_map(&y, out, m, n, GemmShape<TN, DT>::piece_row)) return MFET_ERR_CUDA;
-  static std::atomic<uint64_t> ready{0};  // one bit per GPU: the kernel may use this much shared memory there
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return MFET_ERR_CUDA;
-  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-  if (!(ready.load(std::memory_order_relaxed) & bit)) {
-    if (cudaFuncSetAttribute(mx4_gemm_kernel<TN, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GemmShape<TN, DT>::smem) !=
-        cudaSuccess)
-      return MFET_ERR_CUDA;
-    ready.fetch_or(bit, std::memory_order_relaxed);
-  }
+  static std::atomic<uint64_t> ready{0};
+  if (allow_smem(mx4_gemm_kernel<TN, DT>, GemmShape<TN, DT>::smem, &ready) != cudaSuccess) return MFET_ERR_CUDA;
   const unsigned blocks = (unsigned)(p.tiles < sm_count() ? p.tiles : sm_count());
   return launch_early(mx4_gemm_kernel<TN, DT>, blocks, kGemmThreads, GemmShape<TN, DT>::smem, s, a, b, y, p) == cudaSuccess ? MFET_OK
                                                                                                                         : MFET_ERR_CUDA;
@@ -783,10 +790,9 @@ template <int MT>
 cudaError_t launch_few(const FewParams& p, cudaStream_t s) {
   const size_t padded = (p.blocks + 31) & ~31u;
   const size_t smem = MT * padded * (32 + 4);
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(mx4_few_kernel<MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem(mx4_few_kernel<MT>, kFewSmem, &ready);
+  if (e != cudaSuccess) return e;
   const int64_t want = (p.n + kFewThreads / 32 - 1) / (kFewThreads / 32), most = (int64_t)sm_count() * 4;
   return launch_early(mx4_few_kernel<MT>, (unsigned)(want < most ? want : most), kFewThreads, smem, s, p);
 }
@@ -846,9 +852,9 @@ int mfet_mx4_linear(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t m, co
   const OutParams out{(uint8_t*)y, y_ld, bias, y_dtype, act == MFET_ACT_RELU};
   const Dims d = dims_of(k);
   cudaStream_t s = (cudaStream_t)stream;
-  // a few rows and little work; the quantised x has to fit shared memory (k up to 10,000 for 8 rows)
+  // a few rows and little work
   const uint32_t mt = m == 1 ? 1 : m == 2 ? 2 : m <= 4 ? 4 : 8;
-  if (m <= kFewMost && mt * n <= kFewWork / k && (uint64_t)mt * ((d.blocks + 31) & ~31u) * 36 <= 96 * 1024) {
+  if (m <= kFewMost && mt * n <= kFewWork / k && (uint64_t)mt * ((d.blocks + 31) & ~31u) * 36 <= kFewSmem) {
     FewParams p{(const uint8_t*)x, x_ld, (const uint8_t*)w_codes, (const uint8_t*)w_scales, n, (uint32_t)k, d.blocks, d.groups,
                 (int32_t)m, x_dtype, aligned(x, 16) && (uint64_t)x_ld * size_of(x_dtype) % 16 == 0,
                 (const uint8_t*)x + ((m - 1) * x_ld + k) * size_of(x_dtype), out};
