@@ -469,7 +469,8 @@ int run_clip(const mfet_grad_t* g, int32_t n_grads, double max_norm, float* norm
     if (launch_scale(p, s) != cudaSuccess) return MFET_ERR_CUDA;
     p.norm = nullptr;  // written once
   }
-  if (p.norm) {  // nothing to scale: the norm alone
+  if (p.norm) {  // nothing to scale: the norm alone, from the sums; no block looks at the tensors again
+    p.n = 0;
     p.pieces = 0;
     if (launch_scale(p, s) != cudaSuccess) return MFET_ERR_CUDA;
   }

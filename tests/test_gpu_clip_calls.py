@@ -78,3 +78,26 @@ def test_in_place_above_and_below_the_limit(n, dtype):
             want = f64(keep[shift:shift + n]) * min(1.0, float(np.float32(limit)) / total)
             assert within(v, want, ABS + REL * np.abs(want))
             assert torch.equal(x[:shift], keep[:shift]) and torch.equal(x[shift + n:], keep[shift + n:])
+
+
+def device_us(call, reps=20):
+    for _ in range(3):
+        call()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    for _ in range(reps):
+        call()
+    b.record()
+    b.synchronize()
+    return a.elapsed_time(b) * 1e3 / reps
+
+
+def test_the_norm_alone_costs_one_pass():
+    """It reads every gradient once; clipping reads twice and writes once."""
+    x = torch.randn(150_000_000, device="cuda", dtype=torch.bfloat16)
+    y = torch.empty_like(x)
+    full, norm = Clip([x], [y]), Clip([x], [None])
+    full(0.1)
+    norm(0.1)
+    assert torch.equal(full.norm, norm.norm)
+    assert device_us(lambda: norm(0.1)) < 0.75 * device_us(lambda: full(0.1))
