@@ -5,7 +5,8 @@
 // Two launches over the same pieces of 32 KB. The first adds up the squares in fp64, a few of them at a time in fp32, and leaves one
 // sum per block. The second adds those sums up - every block the same ones in the same order, which costs less than another launch or
 // a count of finished blocks - and scales. It walks the pieces from the last to the first, because the end of what the first launch has
-// read is still in L2, which is told to keep the last 64 MB and let the rest go (214 instead of 222 us for 200 M bf16 values).
+// read is still in L2: all but the last 64 MB are read as what leaves it first (214 instead of 222 us for 200 M bf16 values). Marking the
+// last 64 MB to stay as well took 215 us, and those lines stayed behind when nothing was scaled.
 // Bound by DRAM in three passes, two of which the result needs: 33 M fp32 values in twelve lists 65 us (6.1 TB/s over the three), 200 M
 // bf16 values in 300 tensors 214 us. Nothing depends on which block finishes when: equal inputs give equal bits.
 #include <cmath>
@@ -22,7 +23,7 @@ constexpr int kClipThreads = 256;
 constexpr int kClipInFlight = 8;                                  // 16-byte loads that a thread requests together
 constexpr int kPieceVecs = kClipThreads * kClipInFlight;          // 16-byte vectors per piece
 constexpr int kClipBlocksPerSm = 4;
-constexpr int kKeepPieces = 2048;                                 // 64 MB: what L2 can be made to keep for the second launch
+constexpr int kKeepPieces = 2048;                                 // 64 MB: what is still in L2 for the second launch
 
 struct GradDev {
   const uint8_t* src;
@@ -189,10 +190,10 @@ __device__ __forceinline__ int64_t edge_element(const GradDev& t, int64_t v0, in
   return tail >= v0 && tail < v0 + kPieceVecs && !(tail == 0 && t.lead > 0) ? e : -1;
 }
 
-// 16 bytes, kept in L2 or among the first to leave it. (Not through the read-only path: one kernel may read and write a gradient.)
+// 16 bytes, among the first to leave L2 or not. (Not through the read-only path: one kernel may read and write a gradient.)
 __device__ __forceinline__ uint64_t l2_policy(bool keep) {
   uint64_t p;
-  if (keep) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  if (keep) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
   else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
   return p;
 }

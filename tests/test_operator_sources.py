@@ -53,3 +53,10 @@ def test_the_product_ends_with_nothing_under_way():
     copies, products = b.rindex("bar_wait(full("), b.rindex("mma_commit(drained)")
     assert joined < copies and joined < products
     assert b.index("bar_wait(drained", products) < b.index("__syncthreads();", max(copies, products)) < b.index("tcgen05.dealloc")
+
+
+def test_no_line_of_the_l2_cache_is_kept_beyond_a_call():
+    """A line that is marked to leave last stays in the way of the next kernels when the second pass does not read it."""
+    for name in sorted(os.listdir(CSRC)):
+        if name.endswith((".cu", ".cuh")):
+            assert "evict_last" not in code(name), name
