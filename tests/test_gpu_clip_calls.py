@@ -101,3 +101,12 @@ def test_the_norm_alone_costs_one_pass():
     norm(0.1)
     assert torch.equal(full.norm, norm.norm)
     assert device_us(lambda: norm(0.1)) < 0.75 * device_us(lambda: full(0.1))
+
+
+@pytest.mark.parametrize("dtype,value", [("f16", 0.01398468), ("bf16", 0.0123), ("f32", 0.1), ("f32", 0.013984681), ("f16", 3e-7), ("f32", 7e-23)])
+@pytest.mark.parametrize("n", [8000, 300_007, 5_000_000])
+def test_equal_values_do_not_add_up_their_roundings(n, dtype, value):
+    x = torch.full((n,), value, device="cuda").to(DTYPES[dtype])
+    total = float(x[:1].double().item()) * math.sqrt(n)
+    got = float(Clip([x], [None])(1.0).item())
+    assert abs(got - total) <= 1e-7 * total
