@@ -152,14 +152,15 @@ __device__ __forceinline__ double vec_squares(const uint4& w) {
   return s;
 }
 
-// x * coef rounded to its type; without clipping the bits are handed on (a product with 1 would change a NaN's)
+// x * coef rounded to its type; without clipping the bits are handed on (a product with 1 would change a NaN's). A coefficient below
+// fp32's normal range (gradients near the largest values) is taken in two factors, of which the first, a power of two, is 1 otherwise.
 struct Factor {
   bool clip;
-  float coef;
+  float power, coef;
 };
 template <int DT>
 __device__ __forceinline__ typename Elem<DT>::T scaled(typename Elem<DT>::T x, Factor f) {
-  return f.clip ? Elem<DT>::from(to_float<DT>(x) * f.coef) : x;
+  return f.clip ? Elem<DT>::from(to_float<DT>(x) * f.power * f.coef) : x;
 }
 template <int DT>
 __device__ __forceinline__ uint4 scaled16(const uint4& w, Factor f) {
@@ -168,7 +169,7 @@ __device__ __forceinline__ uint4 scaled16(const uint4& w, Factor f) {
   float v[V];
   widen16<DT>(w, v);
 #pragma unroll
-  for (int j = 0; j < V; ++j) v[j] *= f.coef;
+  for (int j = 0; j < V; ++j) v[j] = v[j] * f.power * f.coef;
   return narrow16<DT>(v);
 }
 
@@ -314,7 +315,9 @@ __device__ __forceinline__ void share_scale(const GradParams<N>& p, const Share<
   if (p.norm && b == 0 && threadIdx.x == 0) *p.norm = (float)norm;
   // a norm that is infinite or NaN leaves the gradients as they are
   const bool clip = norm > p.max_norm && norm < INFINITY;
-  Factor f{clip, (float)(p.max_norm / norm)};
+  const double coef = p.max_norm / norm;
+  const bool tiny = coef < 0x1p-126;
+  Factor f{clip, tiny ? 0x1p-126f : 1.f, (float)(tiny ? coef * 0x1p126 : coef)};
   asm volatile("" : "+f"(f.coef));  // else "clip ? x * coef : x" may be folded into one product
   int32_t k = b < share.total ? (share.total - 1 - b) / g * g + b : -1;
   for (int i = k >= 0 ? share.tensor_of(p.n, k) : 0; k >= 0; k -= g) {

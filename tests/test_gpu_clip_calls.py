@@ -110,3 +110,16 @@ def test_equal_values_do_not_add_up_their_roundings(n, dtype, value):
     total = float(x[:1].double().item()) * math.sqrt(n)
     got = float(Clip([x], [None])(1.0).item())
     assert abs(got - total) <= 1e-7 * total
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("limit", [1.0, 1e-10, 1e-30])
+def test_coefficients_below_fp32(dtype, limit):
+    """Gradients near the largest values: the coefficient has no normal fp32 value, g * coef has."""
+    torch.manual_seed(5)
+    x = (torch.randn(20_000, device="cuda", dtype=torch.float64).clamp(-3, 3) * 1e38).float().to(DTYPES[dtype])
+    y = torch.empty_like(x)
+    total = math.sqrt(math.fsum(np.square(f64(x)).tolist()))
+    Clip([x], [y])(limit)
+    want = f64(x) * (float(np.float32(limit)) / total)
+    assert within(y, want, ABS + REL * np.abs(want))
