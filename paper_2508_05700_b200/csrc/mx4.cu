@@ -226,7 +226,10 @@ __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_const
     for (int r = 0; r < MT; ++r) acc[r] = 0.f;
     for (uint32_t b = lane; b < padded; b += 32) {
       const uint4 wn = w;
-      const float sw = mx_scale(s) * 0.25f;  // both factors of the integer product are doubled
+      // Both factors of the integer product are doubled. It goes up to 4608: under the largest weights' scales (2^116 and above) it is held
+      // 2^12 smaller until x's scale is in, else it would leave fp32's range where the product of all three does not.
+      const bool large = s > 242u;
+      const float sw = mx_scale(s) * (large ? 0x1p-14f : 0x1p-2f), back = large ? 0x1p12f : 1.f;
       // the next block's weights, or the next column's first ones
       if (b + 32 < padded) weights(j, b + 32, &w, &s);
       else weights(j + step, lane, &w, &s);
@@ -245,7 +248,7 @@ __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_const
         d = __dp4a((int)v[5], x1.y, d);
         d = __dp4a((int)v[6], x1.z, d);
         d = __dp4a((int)v[7], x1.w, d);
-        acc[r] = fmaf((float)d * sw, ss[r * padded + b], acc[r]);
+        acc[r] = fmaf((float)d * sw * ss[r * padded + b], back, acc[r]);
       }
     }
 #pragma unroll

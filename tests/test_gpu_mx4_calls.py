@@ -78,3 +78,11 @@ def test_threads_with_rows_of_different_lengths():
     torch.cuda.synchronize()
     assert not errors, errors[0]
     assert all(torch.equal(c.y, w) for c, w in zip(calls, want))
+
+
+@pytest.mark.parametrize("m_", [1, 2, 3, 8, 9, 200])
+@pytest.mark.parametrize("x_size,w_size", [(1e-30, 2e38), (2e38, 1e-30), (1e-38, 2e38), (2e38, 1e-38), (1e-20, 1e-15)])
+def test_products_of_large_and_small_operands(m_, x_size, w_size):
+    """Every product and sum is far inside fp32's range, although one factor is not."""
+    call = Linear(np.random.default_rng(m_), m_, 70, 300, x_size, w_size)
+    check(call(), call.a, call.w)
