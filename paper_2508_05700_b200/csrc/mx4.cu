@@ -121,8 +121,10 @@ __device__ __forceinline__ void put(const OutParams& o, int64_t i, int64_t j, fl
 constexpr int kFewThreads = 256;
 constexpr int kFewMost = 8;  // rows of x
 // The most work, in multiply-adds, with the rows counted up to a power of two. The integer products grow with it and the two-launch form
-// hardly does: 8 x 2048 x 1000 (2^24) 7.4 us here against 7.8, 1 x 2048 x 8192 (2^24) 6.7 against 7.6, but 4 x 2048 x 8192 (2^26) 9.8
-// against 8.2 and 8 x 2048 x 8192 17.5 against 8.3; 1 x 896 x 1024 2.5 against 5.0. A second launch costs a calling program 2.4 us besides.
+// hardly does; a second launch costs a calling program 2.4 us besides its time on the device. On the device: 1 x 896 x 1024 2.5 us here
+// against 4.8; at 2^24 7 x 2048 x 1000 6.9 against 7.6, 2 x 2048 x 4096 5.2 against 6.3; at the limit 4 x 2048 x 4096 6.8 against 6.6,
+// 1 x 2048 x 16384 9.4 against 8.3, 8 x 2048 x 2048 8.8 against 6.3 (with the launch about even); beyond it 4 x 2048 x 8192 (2^26) 9.8
+// against 8.2 and 8 x 2048 x 8192 17.5 against 8.3.
 constexpr int64_t kFewWork = 1ll << 25;
 constexpr uint32_t kFewSmem = 96 * 1024;  // the quantised x has to fit this (k up to 10,000 for 8 rows)
 
@@ -195,8 +197,8 @@ __device__ __forceinline__ void few_stage(const FewParams& p, int mt, int4* sx, 
 
 // A warp per output column: lane b takes block b, b + 32, ... of the column's weights (16 bytes each, 512 bytes per warp and
 // load) against the same block of all MT rows of x from shared memory: 8 integer dot products of 4 values per
-// row and block, exact, then one fp32 multiply-add with the two scales. Latency: 2.5 us for 1 x 896 x 1024 (0.5 MB of weights, 0.1 us of
-// bandwidth), of which a launch is most; 7.2 us for 7 x 2048 x 1000, where every block quantises all of x for itself.
+// row and block, exact, then the two scales and an fp32 addition. Latency: 2.5 us for 1 x 896 x 1024 (0.5 MB of weights, 0.1 us of
+// bandwidth), of which a launch is most; 6.9 us for 7 x 2048 x 1000, where every block quantises all of x for itself.
 template <int MT>
 __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_constant__ FewParams p) {
   extern __shared__ int4 sx[];  // [MT][2][padded] 16-byte halves, then [MT][padded] scales
