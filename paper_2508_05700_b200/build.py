@@ -21,14 +21,21 @@ def _newest(paths):
     return max(os.path.getmtime(p) for p in paths)
 
 
-def build_fastcall(force: bool = False) -> str:
-    """The binding's extension (host code: csrc/fastcall.c)."""
+def build_fastcall(force: bool = False) -> str | None:
+    """The binding's extension (host code: csrc/fastcall.c). Where it cannot be built (no compiler or headers for this Python) there is none:
+    the binding then makes its calls through ctypes."""
     src = os.path.join(CSRC, "fastcall.c")
     deps = [src, os.path.join(HERE, "..", "include", "mfet.h")]
     if force or not os.path.exists(FASTCALL) or os.path.getmtime(FASTCALL) < _newest(deps):
         tmp = FASTCALL + ".tmp.%d" % os.getpid()
-        subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
-                               src, "-o", tmp])
+        try:
+            subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
+                                   src, "-o", tmp])
+        except (OSError, subprocess.CalledProcessError) as e:
+            sys.stderr.write("no extension for the binding, its calls go through ctypes: %s\n" % e)
+            if os.path.exists(FASTCALL):  # of an older source
+                os.remove(FASTCALL)
+            return None
         os.replace(tmp, FASTCALL)
     return FASTCALL
 

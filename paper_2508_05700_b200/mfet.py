@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from operator import index
 from typing import Optional, Sequence
 
 import numpy as np
@@ -68,7 +69,10 @@ if not os.path.exists(LIB_PATH):
     raise ImportError("libmfet.so is missing: build it with `python -m paper_2508_05700_b200.build` "
                       "(there is no fallback path)")
 _lib = C.CDLL(LIB_PATH)
-from . import _fastcall  # noqa: E402  (built with the library)
+try:
+    from . import _fastcall  # noqa: E402  (built with the library, for the Python that built it)
+except ImportError:
+    _fastcall = None
 
 _P = C.c_void_p
 _lib.mfet_row_bytes.restype = C.c_uint64
@@ -370,17 +374,55 @@ def mfet_mx4_linear_bytes(m: int, k: int) -> int:
     return int(_lib.mfet_mx4_linear_bytes(m, k))
 
 
-# The calls that a step makes many times go through a small extension instead of ctypes (csrc/fastcall.c): same names, arguments
-# and errors.
+# The calls that a step makes many times go through a small extension instead of ctypes (csrc/fastcall.c). It is built for one version of
+# Python; another one makes the same calls, with the same names, arguments and errors, through ctypes. Per call: the kinds of its arguments
+# (as in fastcall.c) and how many of them have to be given.
+_FAST = {"mfet_grad_clip": ("ofppzp", 5), "mfet_rows_write": ("bpippuipp", 7), "mfet_rows_read": ("bpippuipp", 7),
+         "mfet_mx4_quantize": ("puiiippp", 7), "mfet_mx4_matmul": ("ppippiipupuipp", 12), "mfet_mx4_linear": ("puiippiipupuipzpp", 15)}
+_KINDS = {"p": C.c_void_p, "b": C.c_void_p, "f": C.c_float, "i": C.c_int64, "u": C.c_uint32, "d": C.c_int32, "z": C.c_uint64}
+_RANGES = {"i": (-2**63, 2**63), "u": (0, 2**32), "d": (-2**31, 2**31), "z": (0, 2**63)}
+
+
 def _fail(status: int, where: str) -> None:
     raise MfetError(status, where)
 
 
-_FAST = ("mfet_grad_clip", "mfet_rows_write", "mfet_rows_read", "mfet_mx4_quantize", "mfet_mx4_matmul", "mfet_mx4_linear")
-_fastcall.bind(_fail, *(C.cast(getattr(_lib, _n), C.c_void_p).value for _n in _FAST))
-mfet_grad_clip = _fastcall.mfet_grad_clip
-mfet_rows_write = _fastcall.mfet_rows_write
-mfet_rows_read = _fastcall.mfet_rows_read
-mfet_mx4_quantize = _fastcall.mfet_mx4_quantize
-mfet_mx4_matmul = _fastcall.mfet_mx4_matmul
-mfet_mx4_linear = _fastcall.mfet_mx4_linear
+def _through_ctypes(name: str):
+    kinds, least = _FAST[name]
+    in_c = kinds.replace("o", "bd")  # a list of gradients: its memory and its length
+    size = C.sizeof(Grad if "o" in kinds else TableDesc)
+    fn = getattr(_lib, name)
+    fn.argtypes = [_KINDS[k] for k in in_c]
+
+    def convert(kind, v):
+        if kind == "p":
+            return v if v is None or isinstance(v, int) else v.data_ptr()
+        if kind == "f":
+            return float(v)
+        if kind == "b":
+            return v if v is None else np.frombuffer(v, np.uint8).ctypes.data
+        v, (lo, hi) = index(v), _RANGES[kind]
+        if not lo <= v < hi:
+            _fail(ERR_INVALID_ARG, name)
+        return v
+
+    def call(*args):
+        if not least <= len(args) <= len(kinds):
+            raise TypeError("%s takes %d to %d arguments (%d given)" % (name, least, len(kinds), len(args)))
+        args += (None,) * (len(kinds) - len(args))
+        if "o" in kinds:
+            if not isinstance(args[0], tuple) or len(args[0]) != 2:
+                raise TypeError("%s: what make_grads gave is wanted" % name)
+            args = args[0] + args[1:]
+        lent = args[0]
+        if "b" in in_c and lent is not None and memoryview(lent).nbytes < size * (args[1] if "o" in kinds else 1):
+            _fail(ERR_INVALID_ARG, name)
+        _check(fn(*[convert(k, v) for k, v in zip(in_c, args)]), name)
+    call.__name__ = name
+    return call
+
+
+if _fastcall is not None:
+    _fastcall.bind(_fail, *(C.cast(getattr(_lib, _n), C.c_void_p).value for _n in _FAST))
+mfet_grad_clip, mfet_rows_write, mfet_rows_read, mfet_mx4_quantize, mfet_mx4_matmul, mfet_mx4_linear = (
+    _through_ctypes(_n) if _fastcall is None else getattr(_fastcall, _n) for _n in _FAST)
