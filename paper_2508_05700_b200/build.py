@@ -42,7 +42,8 @@ def build_fastcall(force: bool = False) -> str | None:
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
     """Builds (if out of date) and returns the library; checked=True: the bounds-checked build, in
-    which every kernel tests its indices and reports a violation through MFET_DEV_BOUNDS."""
+    which the kernels test the indices of their loads and stores and report a violation through MFET_DEV_BOUNDS (what the tensor-map
+    copies of the MXFP4 product reach is clipped by the map)."""
     build_fastcall(force)
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     srcs = [os.path.join(CSRC, s) for s in SOURCES]

@@ -76,7 +76,7 @@ struct Share {
     for (int j = 0; j < kPer; ++j) {
       const int i = (int)threadIdx.x * kPer + j;
       mine[j] = 0;
-      if (i < p.n) {
+      if (i < p.n && MFET_INSIDE(nullptr, i < N)) {
         const GradDev& t = entries[i];
         int64_t r = t.rows;
         if (t.n_rows) {
@@ -188,6 +188,16 @@ __device__ __forceinline__ int64_t edge_element(const GradDev& t, int64_t v0, in
   return tail >= v0 && tail < v0 + kPieceVecs && !(tail == 0 && t.lead > 0) ? e : -1;
 }
 
+#ifdef MFET_CHECKED
+// What the checked build tests: vector `vec`, element `e` counted from the boundary, or element `at` of rows `ld` apart lies in the tensor
+template <int V>
+__device__ __forceinline__ bool holds_vector(const GradDev& t, int64_t vec) {
+  return vec * V >= t.lead && (vec + 1) * V - t.lead <= t.rows * t.cols;
+}
+__device__ __forceinline__ bool holds_element(const GradDev& t, int64_t e) { return e >= t.lead && e - t.lead < t.rows * t.cols; }
+__device__ __forceinline__ bool holds_strided(const GradDev& t, int64_t at) { return at >= 0 && at < (t.rows - 1) * t.ld + t.cols; }
+#endif
+
 // 16 bytes, among the first to leave L2 or not. (Not through the read-only path: one kernel may read and write a gradient.)
 __device__ __forceinline__ uint64_t l2_policy(bool keep) {
   uint64_t p;
@@ -217,7 +227,9 @@ __device__ __forceinline__ double piece_squares(const GradDev& t, int64_t n, int
     if (v0 * V >= t.lead && (v0 + kPieceVecs) * V <= end) {  // a whole piece
       uint4 v[kClipInFlight];
 #pragma unroll
-      for (int j = 0; j < kClipInFlight; ++j) v[j] = load_with(at + j * kClipThreads, policy);
+      for (int j = 0; j < kClipInFlight; ++j)
+        v[j] = MFET_INSIDE(nullptr, holds_vector<V>(t, v0 + j * kClipThreads + threadIdx.x)) ? load_with(at + j * kClipThreads, policy)
+                                                                                            : make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
       return s;
@@ -225,17 +237,22 @@ __device__ __forceinline__ double piece_squares(const GradDev& t, int64_t n, int
     uint4 v[kClipInFlight];
 #pragma unroll
     for (int j = 0; j < kClipInFlight; ++j)
-      v[j] = whole_vector<V>(t, v0 + j * kClipThreads + threadIdx.x, end) ? __ldcg(at + j * kClipThreads) : make_uint4(0, 0, 0, 0);
+      v[j] = whole_vector<V>(t, v0 + j * kClipThreads + threadIdx.x, end) &&
+                     MFET_INSIDE(nullptr, holds_vector<V>(t, v0 + j * kClipThreads + threadIdx.x))
+                 ? __ldcg(at + j * kClipThreads)
+                 : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int j = 0; j < kClipInFlight; ++j) s += vec_squares<DT>(v[j]);
     const int64_t e = edge_element<V>(t, v0, end);
-    if (e >= 0) {
+    if (e >= 0 && MFET_INSIDE(nullptr, holds_element(t, e))) {
       const double x = (double)to_float<DT>(base[e]);
       s = fma(x, x, s);
     }
   } else {
     for (int64_t i = v0 * V + threadIdx.x; i < (v0 + kPieceVecs) * V && i < n; i += kClipThreads) {
-      const double x = (double)to_float<DT>(src[strided(t, i)]);
+      const int64_t at = strided(t, i);
+      if (!MFET_INSIDE(nullptr, holds_strided(t, at))) continue;
+      const double x = (double)to_float<DT>(src[at]);
       s = fma(x, x, s);
     }
   }
@@ -259,19 +276,24 @@ __device__ __forceinline__ void piece_scale(const GradDev& t, int64_t n, int64_t
     if (same && v0 * V >= t.lead && (v0 + kPieceVecs) * V <= end) {
       uint4 v[kClipInFlight];
 #pragma unroll
-      for (int j = 0; j < kClipInFlight; ++j) v[j] = __ldcs(in + j * kClipThreads);
+      for (int j = 0; j < kClipInFlight; ++j)
+        if (MFET_INSIDE(nullptr, holds_vector<V>(t, v0 + j * kClipThreads + threadIdx.x))) v[j] = __ldcs(in + j * kClipThreads);
 #pragma unroll
-      for (int j = 0; j < kClipInFlight; ++j) __stcs(out + j * kClipThreads, scaled16<DT>(v[j], f));
+      for (int j = 0; j < kClipInFlight; ++j)
+        if (MFET_INSIDE(nullptr, holds_vector<V>(t, v0 + j * kClipThreads + threadIdx.x)))
+          __stcs(out + j * kClipThreads, scaled16<DT>(v[j], f));
       return;
     }
     uint4 v[kClipInFlight];
 #pragma unroll
     for (int j = 0; j < kClipInFlight; ++j)
-      if (whole_vector<V>(t, v0 + j * kClipThreads + threadIdx.x, end)) v[j] = __ldcs(in + j * kClipThreads);
+      if (whole_vector<V>(t, v0 + j * kClipThreads + threadIdx.x, end) &&
+          MFET_INSIDE(nullptr, holds_vector<V>(t, v0 + j * kClipThreads + threadIdx.x)))
+        v[j] = __ldcs(in + j * kClipThreads);
 #pragma unroll
     for (int j = 0; j < kClipInFlight; ++j) {
       const int64_t vec = v0 + j * kClipThreads + threadIdx.x;
-      if (!whole_vector<V>(t, vec, end)) continue;
+      if (!whole_vector<V>(t, vec, end) || !MFET_INSIDE(nullptr, holds_vector<V>(t, vec))) continue;
       const uint4 r = scaled16<DT>(v[j], f);
       if (same) {
         __stcs(out + j * kClipThreads, r);
@@ -283,11 +305,11 @@ __device__ __forceinline__ void piece_scale(const GradDev& t, int64_t n, int64_t
       }
     }
     const int64_t e = edge_element<V>(t, v0, end);
-    if (e >= 0) to[e] = scaled<DT>(from[e], f);
+    if (e >= 0 && MFET_INSIDE(nullptr, holds_element(t, e))) to[e] = scaled<DT>(from[e], f);
   } else {
     for (int64_t i = v0 * V + threadIdx.x; i < (v0 + kPieceVecs) * V && i < n; i += kClipThreads) {
       const int64_t at = strided(t, i);
-      dst[at] = scaled<DT>(src[at], f);
+      if (MFET_INSIDE(nullptr, holds_strided(t, at))) dst[at] = scaled<DT>(src[at], f);
     }
   }
 }
@@ -338,7 +360,7 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) grad_squares_k
   early_launch_wait();
   share.fill(p);
   const double s = block_sum(share_squares(p, share, blockIdx.x, gridDim.x), shared);
-  if (threadIdx.x == 0) p.sums[p.first_sum + blockIdx.x] = s;
+  if (threadIdx.x == 0 && MFET_INSIDE(nullptr, p.first_sum + (int)blockIdx.x < p.n_sums)) p.sums[p.first_sum + blockIdx.x] = s;
 }
 
 template <int N>

@@ -11,7 +11,24 @@
 
 #include "common.cuh"
 
+#ifdef MFET_CHECKED
+#include <cstdio>
+#endif
+
 namespace mfet {
+
+// The bounds-checked build's test ahead of an access, for kernels without a handle's error word: what lies outside is printed, sets
+// MFET_DEV_BOUNDS in the call's status word if it has one, and is skipped. The normal build has `true` in its place.
+#ifdef MFET_CHECKED
+static __device__ __noinline__ bool out_of_bounds(uint32_t* status, const char* where, int line) {
+  printf("mfet: index out of bounds, %s:%d\n", where, line);
+  if (status) atomicOr(status, (uint32_t)MFET_DEV_BOUNDS);
+  return false;
+}
+#define MFET_INSIDE(status, cond) ((cond) || out_of_bounds((status), __FILE__, __LINE__))
+#else
+#define MFET_INSIDE(status, cond) true
+#endif
 
 constexpr int kMxBlock = 32;         // values per scale
 constexpr uint32_t kMxNan = 255u;    // scale byte of a block with a value that is not finite

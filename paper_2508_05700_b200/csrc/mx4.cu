@@ -62,7 +62,8 @@ __global__ void __launch_bounds__(kQuantThreads, 4) mx4_quantize_kernel(const __
       c[u] = (uint32_t)(i - row[u] * per_row);
       const uint32_t at = c[u] * 32;
       const int count = i < p.units && at < p.k ? (int)min(32u, p.k - at) : 0;
-      if (count > 0) raw[u] = load_any<DT, 32, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count, p.x, p.x_end, p.wide);
+      if (count > 0 && MFET_INSIDE(nullptr, row[u] * per_row + c[u] < p.units && at + count <= p.k))
+        raw[u] = load_any<DT, 32, VEC>(reinterpret_cast<const T*>(p.x) + row[u] * p.ld + at, count, p.x, p.x_end, p.wide);
       else memset(&raw[u], 0, sizeof(raw[u]));
     }
 #pragma unroll
@@ -83,9 +84,9 @@ __global__ void __launch_bounds__(kQuantThreads, 4) mx4_quantize_kernel(const __
       }
       if (e == kMxNan) codes[0] = codes[1] = codes[2] = codes[3] = 0u;
       if (u0 + 32 * u + lane < p.units) {
-        if (c[u] < p.blocks)
+        if (c[u] < p.blocks && MFET_INSIDE(nullptr, row[u] * per_row < p.units))
           *reinterpret_cast<uint4*>(p.codes + (row[u] * p.blocks + c[u]) * 16) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
-        if ((lane & 3) == 0)
+        if ((lane & 3) == 0 && MFET_INSIDE(nullptr, row[u] * per_row < p.units && (c[u] >> 2) < p.groups))
           *reinterpret_cast<uint32_t*>(p.scales + ((row[u] >> 7) * p.groups + (c[u] >> 2)) * 512 + (row[u] & 31) * 16 +
                                        ((row[u] & 127) >> 5) * 4) = word;
       }
@@ -169,7 +170,8 @@ __device__ __forceinline__ void few_stage(const FewParams& p, int mt, int4* sx, 
     for (int u = 0; u < U; ++u) {
       const uint32_t i = i0 + u * kFewThreads, row = i / (padded * 4), c = i - row * padded * 4;
       const int count = i < units && (int)row < p.m && c * 8 < p.k ? (int)min(8u, p.k - c * 8) : 0;
-      if (count > 0) raw[u] = load_any<DT, 8, VEC>(reinterpret_cast<const T*>(p.x) + (int64_t)row * p.ld + c * 8, count, p.x, p.x_end);
+      if (count > 0 && MFET_INSIDE(nullptr, (int)row < p.m && c * 8 + count <= p.k))
+        raw[u] = load_any<DT, 8, VEC>(reinterpret_cast<const T*>(p.x) + (int64_t)row * p.ld + c * 8, count, p.x, p.x_end);
       else memset(&raw[u], 0, sizeof(raw[u]));
     }
 #pragma unroll
@@ -183,6 +185,7 @@ __device__ __forceinline__ void few_stage(const FewParams& p, int mt, int4* sx, 
       m = max(m, __shfl_xor_sync(kAll, m, 2));
       const uint32_t s = mx_scale_byte(m);
       const uint32_t codes = s == kMxNan ? 0u : mx_encode8(v, mx_inv_scale(s));
+      if (!MFET_INSIDE(nullptr, (int)row < mt && (c >> 2) < padded)) continue;
       uint2* dst = reinterpret_cast<uint2*>(sx + (row * 2 + ((c >> 1) & 1)) * padded + (c >> 2)) + (c & 1);
       *dst = make_uint2(twice4(codes), twice4(codes >> 16));
       if ((c & 3) == 0) ss[row * padded + (c >> 2)] = mx_scale(s);
@@ -208,7 +211,7 @@ __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_const
   const int64_t first = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5);
   const int64_t step = (int64_t)gridDim.x * (kFewThreads / 32);
   auto weights = [&](int64_t j, uint32_t b, uint4* w, uint32_t* s) {
-    const bool in = j < p.n && b < p.blocks;
+    const bool in = j < p.n && b < p.blocks && MFET_INSIDE(nullptr, j >= 0 && (b >> 2) < p.groups);
     *w = in ? __ldg(reinterpret_cast<const uint4*>(p.codes + (j * p.blocks + b) * 16)) : make_uint4(0, 0, 0, 0);
     *s = in ? (uint32_t)__ldg(p.scales + ((j >> 7) * p.groups + (b >> 2)) * 512 + (j & 31) * 16 + ((j & 127) >> 5) * 4 + (b & 3))
             : 0u;
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_const
 #pragma unroll
     for (int r = 1; r < MT; ++r)
       if (lane == r) mine = acc[r];
-    if (lane < p.m) put(p.out, lane, j, activate(mine, p.out.bias ? p.out.bias[j] : 0.f, p.out.relu));
+    if (lane < p.m && MFET_INSIDE(nullptr, j >= 0 && j < p.n && j < p.out.ld)) put(p.out, lane, j, activate(mine, p.out.bias ? p.out.bias[j] : 0.f, p.out.relu));
   }
 }
 
@@ -507,6 +510,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
         const uint8_t* sb = p.b_scales + (size_t)((uint32_t)yb >> 7) * p.groups * 512;
         for (uint32_t s = 0; s < p.stages_k; ++s) {
           if (!(ok = bar_wait(empty(st), phase, &dead))) break;
+          // the scale tiles that are read here; codes outside their operand read as 0
+          if (!MFET_INSIDE(p.status, 2 * s < p.groups && (int64_t)w.tm * kTileM < p.m && (int64_t)yb < p.n)) {
+            ok = false;
+            dead = 1;
+            break;
+          }
           const uint32_t at = base + st * G::stage_bytes, bar = full(st);
           const uint32_t sc = min(2u, p.groups - 2 * s) * 512;  // scale bytes per operand
           bar_expect(bar, G::a_bytes + G::b_bytes + 2 * sc);
@@ -622,7 +631,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
 #pragma unroll 8
           for (int i = 0; i < 32; ++i) {  // a warp writes a row's 32 columns
             const T x = *reinterpret_cast<const T*>(to + G::at(i, lane / kPer) + lane % kPer * sizeof(T));
-            if (i0 + i < p.m && j1 + lane < p.n) y[i * p.out.ld] = x;
+            if (i0 + i < p.m && j1 + lane < p.n && MFET_INSIDE(p.status, i0 >= 0 && j1 >= 0 && j1 + lane < p.out.ld)) y[i * p.out.ld] = x;
           }
           __syncwarp();
         }

@@ -44,8 +44,17 @@ __device__ __forceinline__ int64_t live_count(const RowsParams& p) {
 
 // Entry i of the list; -1 beyond its end
 __device__ __forceinline__ int64_t entry(const RowsParams& p, int64_t i, int64_t n) {
-  return i < n ? (p.list ? __ldg(reinterpret_cast<const long long*>(p.list) + i) : i) : -1;
+  return i < n && MFET_INSIDE(p.status, i >= 0 && i < p.n) ? (p.list ? __ldg(reinterpret_cast<const long long*>(p.list) + i) : i) : -1;
 }
+#ifdef MFET_CHECKED
+// What the checked build tests: `count` values from column `at` of value row i, or bytes [from, to) of a table row
+__device__ __forceinline__ bool holds_values(const RowsParams& p, int64_t i, uint32_t at, int count) {
+  return i >= 0 && i < p.n && (uint64_t)at + count <= p.dim;
+}
+__device__ __forceinline__ bool holds_bytes(const RowsParams& p, int64_t r, uint64_t from, uint64_t to) {
+  return (uint64_t)r < p.rows && from <= to && to <= p.row_bytes;
+}
+#endif
 // The table row that an entry names, or -1: a negative entry, or one past the table, which is reported
 __device__ __forceinline__ int64_t checked(const RowsParams& p, int64_t r) {
   if (r < 0) return -1;
@@ -100,7 +109,8 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
         Raw<SD, E> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (count > 0) raw[u] = load_any<SD, E, VEC>(src[u] + at, count, p.mem, p.mem_end, p.wide);
+          if (count > 0 && MFET_INSIDE(p.status, holds_values(p, (src[u] - reinterpret_cast<const S*>(p.mem)) / p.ld, at, count)))
+            raw[u] = load_any<SD, E, VEC>(src[u] + at, count, p.mem, p.mem_end, p.wide);
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (count > 0) {
@@ -129,7 +139,8 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
       Raw<SD, E> raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (count > 0) raw[u] = load_any<SD, E, VEC>(src[u] + at, count, p.mem, p.mem_end, p.wide);  // does not wait for the list entry
+        if (count > 0 && MFET_INSIDE(p.status, holds_values(p, (src[u] - reinterpret_cast<const S*>(p.mem)) / p.ld, at, count)))
+          raw[u] = load_any<SD, E, VEC>(src[u] + at, count, p.mem, p.mem_end, p.wide);  // does not wait for the list entry
         else memset(&raw[u], 0, sizeof(raw[u]));
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -148,7 +159,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
           float v[E];
           widen_raw<SD, E>(raw[u], v);
           const float inv = b == kMxNan ? 0.f : mx_inv_scale(b);
-          if (ok && count > 0) {
+          if (ok && count > 0 && MFET_INSIDE(p.status, holds_bytes(p, r, at / 2, (at + count) / 2))) {
             uint32_t codes[E / 8];
 #pragma unroll
             for (int j = 0; j < E / 8; ++j) codes[j] = b == kMxNan ? 0u : mx_encode8(v + 8 * j, inv);
@@ -160,7 +171,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
             uint32_t* tail = reinterpret_cast<uint32_t*>(out + p.dim / 2);
             const uint32_t tail_words = (p.row_bytes - p.dim / 2) / 4, data_words = (p.dim + 127) / 128;
             const uint32_t w = c / (4 * LPB);
-            if (c % (4 * LPB) == 0 && w < data_words) tail[w] = word;
+            if (c % (4 * LPB) == 0 && w < data_words && MFET_INSIDE(p.status, w < tail_words && r < (int64_t)p.rows)) tail[w] = word;
             if (rd + 1 == rounds)
               for (uint32_t x = data_words + sub; x < tail_words; x += lanes) tail[x] = 0u;  // the padding
           }
@@ -178,7 +189,8 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
 #pragma unroll
               for (int j = 0; j < 8; ++j) word |= int4_code(v[8 * q + j], scale, bias, inv) << (4 * j);
             }
-            if (ok && count >= 8 * (q + 1)) reinterpret_cast<uint32_t*>(out + at / 2)[q] = word;
+            if (ok && count >= 8 * (q + 1) && MFET_INSIDE(p.status, holds_bytes(p, r, at / 2 + 4 * q, at / 2 + 4 * q + 4)))
+              reinterpret_cast<uint32_t*>(out + at / 2)[q] = word;
           }
           // scale and bias, then zeros up to the row's end
           if (ok && rd == 0)
@@ -188,7 +200,8 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_write_ker
         } else {
           float v[E];
           widen_raw<SD, E>(raw[u], v);
-          if (ok && count > 0) store_values<TD, E, true>(reinterpret_cast<typename Elem<TD>::T*>(out) + at, v, count);
+          if (ok && count > 0 && MFET_INSIDE(p.status, holds_bytes(p, r, 0, (uint64_t)(at + count) * sizeof(typename Elem<TD>::T))))
+            store_values<TD, E, true>(reinterpret_cast<typename Elem<TD>::T*>(out) + at, v, count);
         }
       }
     }
@@ -230,7 +243,10 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_read_kern
 #pragma unroll
         for (int j = 0; j < E / 8; ++j) codes[u][j] = 0;
         meta[u] = 0;
-        if (row[u] >= 0 && count > 0) {
+        if (row[u] >= 0 && count > 0 &&
+            MFET_INSIDE(p.status, kCodes ? holds_bytes(p, row[u], at / 2, at / 2 + E / 2) &&
+                                               holds_bytes(p, row[u], p.dim / 2, p.dim / 2 + (TD == MFET_MXFP4 ? c / LPB + 1 : 4))
+                                         : holds_bytes(p, row[u], 0, (uint64_t)(at + count) * sizeof(typename Elem<kTable>::T)))) {
           const uint8_t* from = p.table + (uint64_t)row[u] * p.stride;
           if constexpr (kCodes) {
             // 16 codes are read together; behind the last 8 of a row lie its scales, which are not used as codes
@@ -265,6 +281,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm) rows_read_kern
             widen_raw<kTable, E>(raw[u], v);
           }
         }
+        if (!MFET_INSIDE(p.status, holds_values(p, i, at, count))) continue;
         store_values<DD, E, VEC>(reinterpret_cast<D*>(p.mem) + i * p.ld + at, v, count, p.wide);
       }
     }
