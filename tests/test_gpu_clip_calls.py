@@ -123,3 +123,15 @@ def test_coefficients_below_fp32(dtype, limit):
     Clip([x], [y])(limit)
     want = f64(x) * (float(np.float32(limit)) / total)
     assert within(y, want, ABS + REL * np.abs(want))
+
+
+def test_more_than_2_to_the_32_elements():
+    n = 2**32 + 100_003
+    x = torch.full((n,), 0.01, device="cuda", dtype=torch.bfloat16)
+    x[-5:] = 100.0
+    v = float(x[0].double().item())
+    total = math.sqrt((n - 5) * v * v + 5 * 100.0**2)
+    c = Clip([x], [x])
+    c(total / 4)  # in place, by a power of two
+    assert abs(float(c.norm.item()) - total) <= 1e-7 * total
+    assert float(x[-1].item()) == 25.0 and float(x[0].double().item()) == v / 4 and bool((x[:-5] == x[0]).all())
