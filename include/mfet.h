@@ -402,8 +402,10 @@ typedef struct {
  * with the ranking model, so the gradients of tables and dense parameters are clipped together):
  *   norm = sqrt(sum of g^2 over all elements of all tensors)
  *   dst  = g * (norm > max_norm ? max_norm / norm : 1), rounded to the tensor's dtype.
- * Squares and sums are fp64, in an order that depends only on the list and the GPU. When norm is NaN or
- * infinite the gradients are passed on unchanged; the caller sees it in *norm.
+ * Squares, sums and the norm are fp64, in an order that depends only on the list and the GPU; max_norm / norm is rounded
+ * to fp32 (in two factors where fp32 has no normal value for it). When a gradient is NaN or infinite, so is *norm, and
+ * the gradients are passed on unchanged. A finite norm beyond fp32's range is infinity in *norm and clips all the same.
+ * Tensors of which one is written must not overlap (a parameter that two layers share is listed once).
  *   grads    host mfet_grad_t[n_grads]; n_grads == 0 gives norm 0
  *   norm     dev f32[1], or NULL;  max_norm >= 0; infinity: the norm only, dst = g
  *   scratch  dev, 8-byte aligned, mfet_grad_clip_bytes(n_grads) bytes; needs no initialisation
@@ -455,7 +457,7 @@ MFET_API int mfet_mx4_quantize(const void* x, uint32_t dtype, int64_t ld, int64_
 /* y[i, j] = act(sum over k of a[i, k] * w[j, k] + bias[j]), i < m, j < n, for two operands of k
  * columns; products exact, fp32 sums, rounded once to y's dtype. bias dev f32[n] or NULL; act
  * MFET_ACT_NONE / MFET_ACT_RELU; y dev [m, n] of dtype MFET_F32 / F16 / BF16, y_ld >= n elements between rows (what
- * lies between is not written). MFET_DEV_STALLED in *status: a wait inside the kernel ran out (two
+ * lies between is not written; it must not overlap the operands, x, bias or scratch). MFET_DEV_STALLED in *status: a wait inside the kernel ran out (two
  * seconds) and y is incomplete. Errors: INVALID_ARG, ALIGNMENT, CUDA. */
 MFET_API int mfet_mx4_matmul(const void* a_codes, const void* a_scales, int64_t m, const void* w_codes,
                              const void* w_scales, int64_t n, int64_t k, const float* bias, uint32_t act, void* y,

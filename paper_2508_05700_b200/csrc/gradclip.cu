@@ -8,7 +8,7 @@
 // the last 64 MB are read as what leaves it first (9 us less for 200 M bf16 values). Marking the last 64 MB to stay as well gained
 // nothing more, and those lines stayed behind when nothing was scaled.
 // Bound by DRAM, most of three passes, two of which the result needs: 33 M fp32 values in twelve lists 66 us (338 MB of traffic, 5.1 TB/s: 56 of
-// the 132 MB of the second read come from L2), 200 M bf16 values in 300 tensors 217 us (1.16 GB, 5.3 TB/s: 45 MB come from L2); the norm of
+// the 132 MB of the second read come from L2), 200 M bf16 values in 300 tensors 218 us (1.16 GB, 5.3 TB/s: 45 MB come from L2); the norm of
 // 200 M bf16 values alone 62 us (6.4 TB/s). Nothing depends on which block finishes when: equal inputs give equal bits.
 #include <cmath>
 #include <cstring>
@@ -139,7 +139,7 @@ __device__ __forceinline__ int64_t strided(const GradDev& t, int64_t i) {
 }
 
 // Sum of the squares of 16 bytes, in fp64 like all sums of the norm: a square of an fp32 value is exact there, and nothing leaves the range.
-// (Adding the four or eight squares in fp32 first takes 213 instead of 217 us for 200 M bf16 values in 300 tensors, and the norm alone 56
+// (Adding the four or eight squares in fp32 first takes 213 instead of 218 us for 200 M bf16 values in 300 tensors, and the norm alone 56
 // instead of 62, but equal values, whose roundings do not cancel, put the norm off by up to 2^-23.)
 template <int DT>
 __device__ __forceinline__ double vec_squares(const uint4& w) {
