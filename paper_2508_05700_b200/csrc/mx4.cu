@@ -10,12 +10,9 @@
 // Two kernels for the product. A few rows (mx4_few_kernel): the weights are read once and nothing else costs bandwidth,
 // so a warp per output column and integer dot products suffice, and x is quantised in the same launch. More rows
 // (mx4_gemm_kernel): block-scaled 5th-generation tensor-core instructions.
-#include <cuda.h>
-
-#include <atomic>
 #include <cstring>
 
-#include "lowbit.cuh"
+#include "tensor.cuh"
 
 using namespace mfet;
 
@@ -274,7 +271,6 @@ __global__ void __launch_bounds__(kFewThreads) mx4_few_kernel(const __grid_const
 constexpr int kGemmThreads = 320;  // warp 0 loads, warp 1 issues the products, warps 2..9 write results
 constexpr int kTileM = 128;        // rows of x per tile: lanes of tensor memory
 constexpr int kSlab = 256;         // k per stage: 128 bytes of codes per row, four instructions of k = 64
-constexpr uint64_t kStallNs = 2000000000ull;
 
 template <int TN, int DT>  // output columns per tile: 64 or 128; type of y
 struct GemmShape {
@@ -307,21 +303,12 @@ struct GemmParams {
   uint32_t k, groups, stages_k;  // stages_k: stages that cover k
   uint32_t n_tiles;
   uint32_t bulk_y;          // every row of y starts on a 16-byte boundary
+  uint32_t whole_y;         // ... and ends on one: bulk copies write whole units of 16 bytes, also where a row ends inside one
   int64_t tiles;
   uint32_t* status;
   OutParams out;
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-// True in one lane of a converged warp. Instructions of the tensor cores and the copy engine take their operands from uniform
-// registers; under a branch on this the compiler knows that one lane runs and moves them there directly (under `lane == 0`
-// each such instruction took 110 cycles to issue).
-__device__ __forceinline__ bool elect_one() {
-  uint32_t r;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-  return r != 0;
-}
 // The tiles of a block, one after the other: column tiles run fastest
 struct TileWalk {
   int64_t t;
@@ -340,61 +327,9 @@ struct TileWalk {
   }
 };
 
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\t"
-               "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-               "selp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok)
-               : "r"(bar), "r"(parity)
-               : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ uint64_t now_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-  return t;
-}
-// Waits for the phase `parity` of a barrier, two seconds at most; false: it did not come (or another role gave up). It polls (a
-// suspended wait took longer to come back: 2 us of 47 for a 16384 x 2048 x 2048 product), and reads the clock rarely.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  uint64_t t0 = 0;
-  for (uint32_t i = 1;; ++i) {
-    if (bar_try(bar, parity)) return true;
-    if ((i & 0xFFFF) == 0) {
-      if (*dead) return false;
-      const uint64_t t = now_ns();
-      if (t0 == 0) t0 = t;
-      if (t - t0 > kStallNs) {
-        *dead = 1;
-        return false;
-      }
-    }
-  }
-}
-
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-               "l"(map), "r"(x), "r"(y), "r"(bar)
-               : "memory");
-}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
                "r"(bytes), "r"(bar)
-               : "memory");
-}
-
-__device__ __forceinline__ void bulk_store(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
                : "memory");
 }
 
@@ -428,23 +363,6 @@ __device__ __forceinline__ void mma_mx4(uint32_t d, uint32_t a_lo, uint32_t b_lo
                "r"(a_lo), "r"(b_lo), "r"(inst), "r"(sa), "r"(sb), "r"(add), "n"(kTileDescHi)
                : "memory");
 }
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"  // in one statement: nothing may use the registers before the wait
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(addr)
-      : "memory");
-}
-
 // One block per SM walks over the tiles (128 rows of x times TN output columns); output columns run fastest, so that the blocks
 // at work share the rows of x in L2. 8192 x 896 x 1024 to bf16 takes 10 us (1.5 PFLOP/s), 16384 x 2048 x 2048 41 us (3.4 PFLOP/s; without its loads 29,
 // without its stores 36: it is bound by what loads, stores and scales share, not by the tensor cores, which are busy 44 % of the time).
@@ -619,12 +537,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
 #pragma unroll
         for (int q = 0; q < 32; q += kPer) *reinterpret_cast<uint4*>(to + G::at(lane, q / kPer)) = narrow16<DT>(v + q);
         const int64_t j1 = j0 + c;
-        if (p.bulk_y) {
+        if (p.bulk_y && (p.whole_y || j1 + 32 <= p.n)) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (i0 < p.m && j1 < p.n && elect_one()) bulk_store(&y_map, out_at + piece, (int32_t)j1, (int32_t)i0);
           __syncwarp();
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         } else {
           __syncwarp();
           T* y = reinterpret_cast<T*>(p.out.y) + i0 * p.out.ld + j1 + lane;
@@ -635,6 +552,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) mx4_gemm_kernel(const __grid_
           }
           __syncwarp();
         }
+        if (p.bulk_y) asm volatile("cp.async.bulk.commit_group;" ::: "memory");  // one per piece, which the wait above counts on
       }
     }
     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // shared memory outlives the copies that read it
@@ -672,9 +590,6 @@ bool bad_size(int64_t rows, int64_t k) { return rows < 0 || rows >= (1ll << 31) 
 uint64_t code_bytes(int64_t rows, int64_t k) { return (uint64_t)rows * dims_of(k).blocks * 16; }
 uint64_t scale_bytes(int64_t rows, int64_t k) { return (uint64_t)((rows + 127) / 128) * dims_of(k).groups * 512; }
 
-bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-uint32_t size_of(uint32_t dtype) { return dtype == MFET_F32 ? 4 : 2; }
-
 template <int DT>
 cudaError_t launch_quantize(const QuantParams& p, bool vec, cudaStream_t s) {
   const int64_t want = (p.units + kQuantThreads - 1) / kQuantThreads, most = (int64_t)sm_count() * 16;
@@ -695,24 +610,6 @@ int quantize(const void* x, uint32_t dtype, int64_t rows, int64_t k, int64_t ld,
     default: e = launch_quantize<MFET_BF16>(p, vec, s); break;
   }
   return e == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-  static std::atomic<void*> found{nullptr};
-  void* f = found.load(std::memory_order_acquire);
-  if (!f) {
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      return nullptr;
-    }
-    found.store(f, std::memory_order_release);
-  }
-  return reinterpret_cast<EncodeTiled>(f);
 }
 
 // codes [rows, blocks * 16 bytes] read in boxes of `box` rows x 128 bytes; what lies outside reads as code 0
@@ -739,20 +636,6 @@ bool out_map(CUtensorMap* map, const OutParams& o, int64_t m, int64_t n, uint32_
            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Lets a kernel use `bytes` of dynamic shared memory on the current GPU: always the same number for a kernel, so that no thread takes away
-// what another one is about to launch with. ready: one bit per GPU where that is done.
-template <typename K>
-cudaError_t allow_smem(K kernel, uint32_t bytes, std::atomic<uint64_t>* ready) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-  if (ready->load(std::memory_order_relaxed) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e == cudaSuccess) ready->fetch_or(bit, std::memory_order_relaxed);
-  return e;
-}
-
 template <int TN, int DT>
 int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* ws, int64_t n, int64_t k, const OutParams& out,
          uint32_t* status, cudaStream_t s) {
@@ -772,6 +655,7 @@ int gemm(const void* xc, const void* xs, int64_t m, const void* wc, const void* 
   p.status = status;
   p.out = out;
   p.bulk_y = aligned(out.y, 16) && (uint64_t)out.ld * size_of(out.dtype) % 16 == 0;
+  p.whole_y = n * size_of(out.dtype) % 16 == 0;
   if (!p.bulk_y) y = a;  // not used
   else if (!out_map(&y, out, m, n, GemmShape<TN, DT>::piece_row)) return MFET_ERR_CUDA;
   static std::atomic<uint64_t> ready{0};
