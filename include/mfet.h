@@ -44,7 +44,8 @@ typedef struct mfet_tables mfet_tables_t; /* opaque, library-owned */
 typedef void* mfet_stream_t;              /* a cudaStream_t */
 
 enum { MFET_F32 = 0, MFET_F16 = 1, MFET_BF16 = 2, MFET_INT4 = 3, MFET_MXFP4 = 4 };
-enum { MFET_ACT_NONE = 0, MFET_ACT_RELU = 1 };
+enum { MFET_ACT_NONE = 0, MFET_ACT_RELU = 1, /* of the gated block alone: */
+       MFET_ACT_SILU = 2, MFET_ACT_GELU = 3, MFET_ACT_SIGMOID = 4 };
 enum { MFET_POOL_SUM = 0, MFET_POOL_MEAN = 1, MFET_POOL_WSUM = 2 };
 enum { MFET_LOC_DEVICE = 0, MFET_LOC_HOST = 1 };
 enum { MFET_VAL_NORMAL = 0, MFET_VAL_GRID = 1 };
@@ -473,6 +474,66 @@ MFET_API int mfet_mx4_linear(const void* x, uint32_t x_dtype, int64_t x_ld, int6
                              const void* w_scales, int64_t n, int64_t k, const float* bias, uint32_t act, void* y,
                              uint32_t y_dtype, int64_t y_ld, void* scratch, uint64_t scratch_bytes, uint32_t* status,
                              mfet_stream_t stream);
+
+/* ---- between the pooled features and the upper layers: layer norm, gated block, their training ----
+ * As above: no handle, caller memory of the current GPU, asynchronous on `stream`, `status` a device word or NULL.
+ * Matrices are row-major, `ld` elements between rows (at least the row's length; what lies between is not written), at any address
+ * of their element type. Outputs must not overlap inputs, scratch or one another. Calls that are captured into a graph use their
+ * scratch in every replay: two graphs that may run at the same time need one each. Results depend on the arguments and the GPU alone, not on timing. */
+
+/* Layer norm over the columns, and its backward pass (paper, Section 2.2: features of several tables, of very different scale,
+ * feed one ranking model). With mu and v the mean and the variance (sum of squares / cols) of a row, r = 1 / sqrt(v + eps), xh = (x - mu) r:
+ *   y  = xh * weight + bias
+ *   t  = dy * weight;  dx = r * (t - mean(t) - xh * mean(t * xh))
+ *   dweight = sum over rows of dy * xh;  dbias = sum over rows of dy
+ * fp32 inside (squares that leave its range are not caught), rounded once. The backward pass computes mu and r again: nothing has to be kept but x.
+ *   x, y, dy  dev [rows, cols] of dtype MFET_F32 / F16 / BF16 each; dx: of x's dtype
+ *   weight, bias, dweight, dbias  dev f32[cols]; NULL: 1, 0, not wanted, not wanted
+ *   scratch   dev, 4-byte aligned, mfet_layer_norm_backward_bytes(rows, cols) bytes; needs no initialisation; may be NULL
+ *             when neither dweight nor dbias is wanted
+ * rows >= 0 (no rows: the sums are 0), 1 <= cols < 2^30, eps >= 0. Errors: INVALID_ARG, ALIGNMENT, WORKSPACE, CUDA. */
+MFET_API int mfet_layer_norm(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t rows, int64_t cols, const float* weight,
+                             const float* bias, float eps, void* y, uint32_t y_dtype, int64_t y_ld, mfet_stream_t stream);
+MFET_API uint64_t mfet_layer_norm_backward_bytes(int64_t rows, int64_t cols);
+MFET_API int mfet_layer_norm_backward(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t rows, int64_t cols, const float* weight,
+                                      float eps, const void* dy, uint32_t dy_dtype, int64_t dy_ld, void* dx, int64_t dx_ld,
+                                      float* dweight, float* dbias, void* scratch, uint64_t scratch_bytes, mfet_stream_t stream);
+
+/* The gated linear block h = act(G) * U with G = x w_gate^T, U = x w_up^T, and its backward pass:
+ *   dG = dh * U * act'(G), dU = dh * act(G);  dx = dG w_gate + dU w_up;  dw_gate = dG^T x, dw_up = dU^T x
+ * fp32 sums; h and the gradients rounded once; dG and dU are rounded to the dtype before the products that use them. The backward pass
+ * computes G and U again: nothing has to be kept but x.
+ *   dtype    MFET_F16 or MFET_BF16, of all matrices: x, dx dev [m, k]; w_gate, w_up, dw_gate, dw_up dev [n, k]; h, dh dev [m, n]
+ *   act      MFET_ACT_*: NONE, RELU (slope 0 at 0), SILU g / (1 + e^-g), GELU g Phi(g), SIGMOID
+ *   dx, or dw_gate and dw_up, may be NULL: not wanted
+ *   scratch  dev, 16-byte aligned, mfet_gated_linear_bytes / mfet_gated_linear_backward_bytes bytes; needs no initialisation. The
+ *            forward call needs none (NULL) when x, w_gate and w_up start, and their rows follow, on 16-byte boundaries; otherwise
+ *            it holds copies of them that do.
+ * m, n >= 0 (sums over nothing are 0), k >= 1. MFET_DEV_STALLED in *status: a wait inside a kernel ran out (two seconds) and the results are incomplete.
+ * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE, CUDA. */
+MFET_API uint64_t mfet_gated_linear_bytes(int64_t m, int64_t n, int64_t k);
+MFET_API int mfet_gated_linear(const void* x, uint32_t dtype, int64_t x_ld, int64_t m, const void* w_gate, int64_t wg_ld,
+                               const void* w_up, int64_t wu_ld, int64_t n, int64_t k, uint32_t act, void* h, int64_t h_ld,
+                               void* scratch, uint64_t scratch_bytes, uint32_t* status, mfet_stream_t stream);
+MFET_API uint64_t mfet_gated_linear_backward_bytes(int64_t m, int64_t n, int64_t k);
+MFET_API int mfet_gated_linear_backward(const void* x, uint32_t dtype, int64_t x_ld, int64_t m, const void* w_gate, int64_t wg_ld,
+                                        const void* w_up, int64_t wu_ld, int64_t n, int64_t k, uint32_t act, const void* dh,
+                                        int64_t dh_ld, void* dx, int64_t dx_ld, void* dw_gate, int64_t dwg_ld, void* dw_up,
+                                        int64_t dwu_ld, void* scratch, uint64_t scratch_bytes, uint32_t* status, mfet_stream_t stream);
+
+/* An update orthogonalised, as an optimiser does with the gradients of the block's weights: X = g / |g| with |g| the root of the sum of
+ * squares; then `steps` times, with A = X X^T where rows <= cols and A = X^T X otherwise,
+ *   X <- a X + (b A + c A A) X   (or a X + X (b A + c A A));   out = scale * X
+ *   coefficients  host f32[3 * steps]: a, b, c of each step; NULL: 3.4445, -4.775, 2.0315 in every step
+ *   g, out        dev [rows, cols] of dtype MFET_F32 / F16 / BF16 each
+ *   scratch       dev, 16-byte aligned, mfet_orthogonalize_bytes(rows, cols) bytes; needs no initialisation
+ * Matrices between the products are held to 22 bits or more, |g| and its squares in fp64: the result is about as near as one computed in fp32
+ * throughout. A g of zeros gives zeros; one with a NaN or an infinity gives NaN throughout. 1 <= steps <= 64; coefficients that let
+ * a singular value grow beyond 2^20 are INVALID_ARG. Errors: INVALID_ARG, ALIGNMENT, WORKSPACE, CUDA; MFET_DEV_STALLED as above. */
+MFET_API uint64_t mfet_orthogonalize_bytes(int64_t rows, int64_t cols);
+MFET_API int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, int64_t cols, const float* coefficients,
+                                int32_t steps, float scale, void* out, uint32_t out_dtype, int64_t out_ld, void* scratch,
+                                uint64_t scratch_bytes, uint32_t* status, mfet_stream_t stream);
 
 /* Number of kernels the library has launched on behalf of this handle. */
 MFET_API int mfet_launch_count(const mfet_tables_t* t, uint64_t* launches /*host*/);

@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libmfet.so")
 LIB_CHECKED = os.path.join(HERE, "libmfet_checked.so")  # the same library with -DMFET_CHECKED (see common.cuh)
 FASTCALL = os.path.join(HERE, "_fastcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))  # Python entry of the hot calls
 SOURCES = ["api.cu", "bag.cu", "hash_fill.cu", "dedup.cu", "hostpath.cu", "backward.cu", "rows.cu",
-           "gradclip.cu", "mx4.cu"]
+           "gradclip.cu", "mx4.cu", "norm.cu", "gated.cu", "ortho.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O3", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--fmad=true"]
 
@@ -48,7 +48,7 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
     deps = srcs + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "dedup_layout.cuh"), os.path.join(CSRC, "lowbit.cuh"),
-                   os.path.join(CSRC, "tensor.cuh"),
+                   os.path.join(CSRC, "tensor.cuh"), os.path.join(CSRC, "gemm16.cuh"),
                    os.path.join(HERE, "..", "include", "mfet.h")]
     lib = LIB_CHECKED if checked else LIB
     if not force and os.path.exists(lib) and os.path.getmtime(lib) >= _newest(deps):

@@ -1,5 +1,6 @@
 /* Python entry of the calls that are made many times per step: mfet_grad_clip, mfet_rows_write, mfet_rows_read,
- * mfet_mx4_quantize, mfet_mx4_matmul and mfet_mx4_linear, argument for argument as in mfet.h, without the per-argument
+ * mfet_mx4_quantize, mfet_mx4_matmul, mfet_mx4_linear, mfet_layer_norm, mfet_layer_norm_backward, mfet_gated_linear,
+ * mfet_gated_linear_backward and mfet_orthogonalize, argument for argument as in mfet.h, without the per-argument
  * cost of ctypes (17 arguments: 3.0 us there, 0.5 us here; the kernels of a small call take as long). Marshalling only: an argument that
  * is an address may be a tensor (its data_ptr() is taken), an int or None. The addresses of the functions come from the library that the
  * binding has loaded. A status other than MFET_OK goes to the binding's error function, which raises. */
@@ -17,12 +18,29 @@ typedef int (*matmul_fn)(const void*, const void*, int64_t, const void*, const v
 typedef int (*linear_fn)(const void*, uint32_t, int64_t, int64_t, const void*, const void*, int64_t, int64_t, const float*, uint32_t,
                          void*, uint32_t, int64_t, void*, uint64_t, uint32_t*, mfet_stream_t);
 
+typedef int (*norm_fn)(const void*, uint32_t, int64_t, int64_t, int64_t, const float*, const float*, float, void*, uint32_t, int64_t,
+                       mfet_stream_t);
+typedef int (*norm_back_fn)(const void*, uint32_t, int64_t, int64_t, int64_t, const float*, float, const void*, uint32_t, int64_t, void*,
+                            int64_t, float*, float*, void*, uint64_t, mfet_stream_t);
+typedef int (*gated_fn)(const void*, uint32_t, int64_t, int64_t, const void*, int64_t, const void*, int64_t, int64_t, int64_t, uint32_t,
+                        void*, int64_t, void*, uint64_t, uint32_t*, mfet_stream_t);
+typedef int (*gated_back_fn)(const void*, uint32_t, int64_t, int64_t, const void*, int64_t, const void*, int64_t, int64_t, int64_t,
+                             uint32_t, const void*, int64_t, void*, int64_t, void*, int64_t, void*, int64_t, void*, uint64_t, uint32_t*,
+                             mfet_stream_t);
+typedef int (*orthogonalize_fn)(const void*, uint32_t, int64_t, int64_t, int64_t, const float*, int32_t, float, void*, uint32_t, int64_t,
+                                void*, uint64_t, uint32_t*, mfet_stream_t);
+
 static struct {
   grad_clip_fn grad_clip;
   rows_fn rows_write, rows_read;
   quantize_fn quantize;
   matmul_fn matmul;
   linear_fn linear;
+  norm_fn norm;
+  norm_back_fn norm_back;
+  gated_fn gated;
+  gated_back_fn gated_back;
+  orthogonalize_fn orthogonalize;
 } lib;
 static PyObject *fail, *data_ptr;
 
@@ -165,14 +183,60 @@ static PyObject* py_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) 
   return done(status, name);
 }
 
-/* bind(fail, grad_clip, rows_write, rows_read, quantize, matmul, linear): the error function and the library's addresses */
+static PyObject* py_norm(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  static const char name[] = "mfet_layer_norm";
+  arg_t a[12];
+  if (!parse(name, "puiiippfpuip", 11, args, n, a)) return NULL;
+  RUN(lib.norm(a[0].p, (uint32_t)a[1].i, a[2].i, a[3].i, a[4].i, (const float*)a[5].p, (const float*)a[6].p, (float)a[7].f, a[8].p,
+               (uint32_t)a[9].i, a[10].i, a[11].p));
+  return done(status, name);
+}
+
+static PyObject* py_norm_back(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  static const char name[] = "mfet_layer_norm_backward";
+  arg_t a[17];
+  if (!parse(name, "puiiipfpuipipppzp", 16, args, n, a)) return NULL;
+  RUN(lib.norm_back(a[0].p, (uint32_t)a[1].i, a[2].i, a[3].i, a[4].i, (const float*)a[5].p, (float)a[6].f, a[7].p, (uint32_t)a[8].i,
+                    a[9].i, a[10].p, a[11].i, (float*)a[12].p, (float*)a[13].p, a[14].p, (uint64_t)a[15].i, a[16].p));
+  return done(status, name);
+}
+
+static PyObject* py_gated(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  static const char name[] = "mfet_gated_linear";
+  arg_t a[17];
+  if (!parse(name, "puiipipiiiupipzpp", 15, args, n, a)) return NULL;
+  RUN(lib.gated(a[0].p, (uint32_t)a[1].i, a[2].i, a[3].i, a[4].p, a[5].i, a[6].p, a[7].i, a[8].i, a[9].i, (uint32_t)a[10].i, a[11].p,
+                a[12].i, a[13].p, (uint64_t)a[14].i, (uint32_t*)a[15].p, a[16].p));
+  return done(status, name);
+}
+
+static PyObject* py_gated_back(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  static const char name[] = "mfet_gated_linear_backward";
+  arg_t a[23];
+  if (!parse(name, "puiipipiiiupipipipipzpp", 21, args, n, a)) return NULL;
+  RUN(lib.gated_back(a[0].p, (uint32_t)a[1].i, a[2].i, a[3].i, a[4].p, a[5].i, a[6].p, a[7].i, a[8].i, a[9].i, (uint32_t)a[10].i, a[11].p,
+                     a[12].i, a[13].p, a[14].i, a[15].p, a[16].i, a[17].p, a[18].i, a[19].p, (uint64_t)a[20].i, (uint32_t*)a[21].p,
+                     a[22].p));
+  return done(status, name);
+}
+
+static PyObject* py_orthogonalize(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  static const char name[] = "mfet_orthogonalize";
+  arg_t a[15];
+  if (!parse(name, "puiiipdfpuipzpp", 13, args, n, a)) return NULL;
+  RUN(lib.orthogonalize(a[0].p, (uint32_t)a[1].i, a[2].i, a[3].i, a[4].i, (const float*)a[5].p, (int32_t)a[6].i, (float)a[7].f, a[8].p,
+                        (uint32_t)a[9].i, a[10].i, a[11].p, (uint64_t)a[12].i, (uint32_t*)a[13].p, a[14].p));
+  return done(status, name);
+}
+
+/* bind(fail, grad_clip, rows_write, ..., orthogonalize): the error function and the library's addresses, in the order of `lib` */
 static PyObject* py_bind(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-  if (n != 7) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 7 arguments");
+  if (n != 12) {
+    PyErr_SetString(PyExc_TypeError, "bind takes 12 arguments");
     return NULL;
   }
-  void* p[6];
-  for (int k = 0; k < 6; ++k)
+  void* p[11];
+  for (int k = 0; k < 11; ++k)
     if (!address(args[k + 1], &p[k])) return NULL;
   lib.grad_clip = (grad_clip_fn)p[0];
   lib.rows_write = (rows_fn)p[1];
@@ -180,6 +244,11 @@ static PyObject* py_bind(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   lib.quantize = (quantize_fn)p[3];
   lib.matmul = (matmul_fn)p[4];
   lib.linear = (linear_fn)p[5];
+  lib.norm = (norm_fn)p[6];
+  lib.norm_back = (norm_back_fn)p[7];
+  lib.gated = (gated_fn)p[8];
+  lib.gated_back = (gated_back_fn)p[9];
+  lib.orthogonalize = (orthogonalize_fn)p[10];
   Py_INCREF(args[0]);
   Py_XSETREF(fail, args[0]);
   Py_RETURN_NONE;
@@ -200,6 +269,19 @@ static PyMethodDef methods[] = {
     METHOD("mfet_mx4_linear", py_linear,
            "mfet_mx4_linear(x, x_dtype, x_ld, m, w_codes, w_scales, n, k, bias, act, y, y_dtype, y_ld, scratch, scratch_bytes,\n"
            "                status=None, stream=None)"),
+    METHOD("mfet_layer_norm", py_norm, "mfet_layer_norm(x, x_dtype, x_ld, rows, cols, weight, bias, eps, y, y_dtype, y_ld, stream=None)"),
+    METHOD("mfet_layer_norm_backward", py_norm_back,
+           "mfet_layer_norm_backward(x, x_dtype, x_ld, rows, cols, weight, eps, dy, dy_dtype, dy_ld, dx, dx_ld, dweight, dbias, scratch,\n"
+           "                         scratch_bytes, stream=None)"),
+    METHOD("mfet_gated_linear", py_gated,
+           "mfet_gated_linear(x, dtype, x_ld, m, w_gate, wg_ld, w_up, wu_ld, n, k, act, h, h_ld, scratch, scratch_bytes,\n"
+           "                  status=None, stream=None)"),
+    METHOD("mfet_gated_linear_backward", py_gated_back,
+           "mfet_gated_linear_backward(x, dtype, x_ld, m, w_gate, wg_ld, w_up, wu_ld, n, k, act, dh, dh_ld, dx, dx_ld, dw_gate, dwg_ld,\n"
+           "                           dw_up, dwu_ld, scratch, scratch_bytes, status=None, stream=None)"),
+    METHOD("mfet_orthogonalize", py_orthogonalize,
+           "mfet_orthogonalize(g, dtype, ld, rows, cols, coefficients, steps, scale, out, out_dtype, out_ld, scratch, scratch_bytes,\n"
+           "                   status=None, stream=None)\n\ncoefficients: an address, or None."),
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

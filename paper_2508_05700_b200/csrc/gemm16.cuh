@@ -1,0 +1,690 @@
+// Products of 16-bit matrices on the tensor cores, with what follows them done on the accumulators:
+//
+//   acc[i, j] = sum over segments s, sum over k of A_s[i, k] * B_s[j, k]      (fp32)
+//
+// An operand lies K-major (rows of neighbouring k: x and W in x W^T) or MN-major (k runs over its rows: dG and x in dG^T x); the tensor
+// cores read both, so nothing is transposed in memory. Segments add up products of several pairs of matrices in one accumulator
+// (dG Wg + dU Wu; the three products of numbers held in two words).
+//
+// A tile is computed by one block, or by a pair of blocks that shares its operands (CTAS = 2: each loads its 128 rows of A and half of
+// B, one issues the instructions of both; a pair reads 64 bytes per SM and cycle at full rate where a block alone would need 96).
+// Copies of tiles go through a ring of shared memory; two accumulators in tensor memory, so that one tile is written while the next
+// one is computed. With few tiles, `split` blocks (pairs) of a cluster take a part of k each, leave their sums in shared memory, and
+// each adds up its share of the columns over all of them, in the order of k: the result does not depend on who is first.
+#pragma once
+
+#include <cstring>
+
+#include "tensor.cuh"
+
+namespace mfet {
+namespace gemm16 {
+
+constexpr int kThreads = 320;  // warp 0 loads, warp 1 issues the products, warps 2..9 write results
+constexpr int kSlab = 64;      // k per stage: 128 bytes of a K-major row
+constexpr unsigned kAllLanes = 0xFFFFFFFFu;
+
+enum Mode {
+  kGated,      // columns are units: h = act(g) * u
+  kGatedBack,  // ... with the gradient of h: dG and dU
+  kOut,        // the accumulator, rounded
+  kPair,       // v = alpha * C + beta * acc in two fp16 words
+  kPairOut     // the same, rounded to the type of the result
+};
+
+template <int CTAS, int TN, int MODE, int DT>
+struct Shape {
+  static constexpr bool dual = MODE == kGated || MODE == kGatedBack;  // half of the columns of B come from a second matrix
+  static constexpr int outs = MODE == kGatedBack || MODE == kPair ? 2 : 1;
+  static constexpr int b_rows = TN / CTAS;
+  static constexpr uint32_t a_bytes = 128 * 128, b_bytes = b_rows * 128, stage_bytes = a_bytes + b_bytes;
+  // Results leave in pieces of 32 rows x 32 columns; a warp has room for two of each output
+  static constexpr int piece_row = 32 * (int)sizeof(typename Elem<DT>::T);
+  static constexpr uint32_t piece = 32 * piece_row;
+  static constexpr uint32_t warp_out = 2 * outs * piece;
+  static constexpr int stages = (int)((226u * 1024 - 1024 - 8 * warp_out) / stage_bytes);
+  static constexpr uint32_t out_at = stages * stage_bytes;
+  static constexpr uint32_t smem = out_at + 8 * warp_out + 1024;  // + room to align to 1024
+  static constexpr int width = dual ? TN / 2 : TN;                // output columns of a tile
+  static constexpr uint32_t tmem_cols = 2 * TN;
+  static_assert(tmem_cols <= 512 && stages >= 4, "tensor memory, stages");
+  static_assert((uint32_t)stages * stage_bytes >= 128u * TN * 4, "the ring holds a tile of sums");
+  // the 16 bytes `q` of row `row` of a piece, where the bulk copy's swizzle expects them
+  static __device__ __forceinline__ int at(int row, int q) {
+    return row * piece_row + ((piece_row == 128 ? q ^ (row & 7) : q ^ ((row >> 1) & 3)) << 4);
+  }
+};
+
+struct Maps {
+  CUtensorMap a[2], b[2], out[2];
+};
+
+struct Params {
+  int64_t m, n;             // rows and columns of the result (units, where dual)
+  uint32_t m_tiles, n_tiles, tiles;  // tiles of one result; of all results
+  uint32_t band;            // tiles of rows that are walked through together, so that the blocks at work share operands in L2
+  uint32_t kb, iters;       // blocks of k per segment; of all segments
+  uint32_t tail;            // instructions (k = 16) in the last block of a segment
+  uint32_t split;
+  uint32_t a_mn, b_mn;      // MN-major operands
+  uint32_t inst;            // instruction descriptor
+  uint32_t seg_a, seg_b;    // operand of segment s: bits 4s..
+  uint32_t act;
+  uint32_t bulk;            // bit z: rows of output z start on 16-byte boundaries; bit 2 + z: ... and may be written up to one (bulk copies
+                            // write whole units of 16 bytes, also where a row ends inside one)
+  void* out[2];
+  int64_t out_ld[2];
+  const void* c0;           // kGatedBack: gradient of h; kPair*: high words of C, or NULL
+  const void* c1;           // low words of C
+  int64_t c_ld;
+  uint32_t c_vec;           // rows of c0 start on 16-byte boundaries
+  float alpha, beta;        // alpha has C's scale in it, beta the product's; both the result's
+  uint32_t* status;
+};
+
+// ------------------------------------------------------------------ instructions ----
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// the address of the same place in the shared memory of block `rank` of the cluster
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float peer_load(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void peer_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// a tile into this block's memory; the barrier may be the pair's other block's
+template <int CTAS>
+__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
+  if constexpr (CTAS == 1) {
+    tma_load(dst, map, x, y, bar);
+  } else {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+  }
+}
+
+// Shared-memory matrix descriptors, 128-byte swizzle. K-major: groups of 8 rows 1024 bytes apart. MN-major: boxes of 64 elements x 64 k,
+// 8192 bytes apart, groups of 8 k 1024 bytes apart. (In a cluster an address in shared memory has the block's rank above its 18 bits.)
+constexpr uint32_t kDescHi = 64u | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t mn) { return ((addr & 0x3FFFFu) >> 4) | ((mn ? 512u : 1u) << 16); }
+
+template <int CTAS>
+__device__ __forceinline__ void mma16(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t inst, uint32_t add) {
+  if constexpr (CTAS == 1)
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
+                 "mov.b64 a, {%1, %5};\n\t"
+                 "mov.b64 b, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+                 "r"(a_lo), "r"(b_lo), "r"(inst), "r"(add), "n"(kDescHi)
+                 : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
+                 "mov.b64 a, {%1, %5};\n\t"
+                 "mov.b64 b, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+                 "r"(a_lo), "r"(b_lo), "r"(inst), "r"(add), "n"(kDescHi)
+                 : "memory");
+}
+// arrives at the barrier (of both blocks of a pair) when the products issued so far are done
+template <int CTAS>
+__device__ __forceinline__ void commit(uint32_t bar, uint32_t mask) {
+  if constexpr (CTAS == 1)
+    mma_commit(bar);
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)mask)
+                 : "memory");
+}
+
+// ------------------------------------------------------------------ activations ----
+
+// act(g), and its derivative. The exponential's error (2^-17 at the ends of its range, 2^-21 in the middle) is far below a 16-bit result's.
+template <bool SLOPE>
+__device__ __forceinline__ float gate(uint32_t act, float g, float* slope) {
+  switch (act) {
+    case MFET_ACT_RELU: {
+      float r = g;
+      asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(r));
+      if (SLOPE) *slope = g > 0.f ? 1.f : 0.f;
+      return r;
+    }
+    case MFET_ACT_SILU: {
+      const float s = __fdividef(1.f, 1.f + __expf(-g));
+      if (SLOPE) *slope = s * (1.f + g * (1.f - s));
+      return g * s;
+    }
+    case MFET_ACT_SIGMOID: {
+      const float e = __expf(-g), s = __fdividef(1.f, 1.f + e);
+      if (SLOPE) *slope = s * (1.f - s);
+      return s;
+    }
+    case MFET_ACT_GELU: {
+      const float c = 0.5f * erfcf(g * -0.70710678118654752f);  // no cancellation for negative g
+      if (SLOPE) *slope = c + g * 0.3989422804014327f * __expf(-0.5f * g * g);
+      return g * c;
+    }
+    default:
+      if (SLOPE) *slope = 1.f;
+      return g;
+  }
+}
+
+// ------------------------------------------------------------------ the kernel ----
+
+struct Tile {
+  uint32_t z, tm, tn;
+};
+__device__ __forceinline__ Tile tile_at(const Params& p, uint32_t t) {
+  const uint32_t per = p.m_tiles * p.n_tiles, z = t / per, r = t - z * per;
+  const uint32_t band = r / (p.band * p.n_tiles), in = r - band * p.band * p.n_tiles;
+  const uint32_t rows = min(p.band, p.m_tiles - band * p.band);
+  const uint32_t tn = in / rows;
+  return {z, band * p.band + (in - tn * rows), tn};
+}
+
+// 32 neighbouring values of a row, 0 behind its end
+template <int DT>
+__device__ __forceinline__ void load_row32(const void* base, int64_t at, int64_t left, uint32_t vec, float* v) {
+  using T = typename Elem<DT>::T;
+  const T* p = reinterpret_cast<const T*>(base) + at;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (vec && left >= 8 * q + 8) {
+      widen16<DT>(*reinterpret_cast<const uint4*>(p + 8 * q), v + 8 * q);
+    } else {
+#pragma unroll
+      for (int j = 8 * q; j < 8 * q + 8; ++j) v[j] = j < left ? to_float<DT>(p[j]) : 0.f;
+    }
+  }
+}
+
+template <int CTAS, int TN, int MODE, int DT>
+__global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
+  using G = Shape<CTAS, TN, MODE, DT>;
+  using T = typename Elem<DT>::T;
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ __align__(8) uint64_t bars[2 * G::stages + 5];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int dead;
+  const uint32_t base = (smem_addr(raw_smem) + 1023) & ~1023u;  // the same in all blocks
+  uint8_t* const smem = raw_smem + (base - smem_addr(raw_smem));
+  const uint32_t bar0 = smem_addr(bars);
+  auto full = [&](int s) { return bar0 + 8 * s; };
+  auto empty = [&](int s) { return bar0 + 8 * (G::stages + s); };
+  auto acc_full = [&](int a) { return bar0 + 8 * (2 * G::stages + a); };
+  auto acc_empty = [&](int a) { return bar0 + 8 * (2 * G::stages + 2 + a); };
+  const uint32_t drained = bar0 + 8 * (2 * G::stages + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool clustered = CTAS * p.split > 1;
+  const uint32_t rank = clustered ? cluster_rank() : 0u;
+  const uint32_t part = rank / CTAS, half = rank % CTAS, leader = rank - half;
+  const uint32_t pair_mask = (CTAS == 2 ? 3u : 1u) << leader;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < G::stages; ++s) bar_init(full(s), 1), bar_init(empty(s), 1);
+    for (int a = 0; a < 2; ++a) bar_init(acc_full(a), 1), bar_init(acc_empty(a), 8 * CTAS);
+    bar_init(drained, 1);
+    dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    if constexpr (CTAS == 1) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "n"(G::tmem_cols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "n"(G::tmem_cols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (clustered) cluster_sync();  // the barriers of the other blocks exist, and so do the blocks
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  const uint32_t members = CTAS * p.split;
+  const uint32_t first = blockIdx.x / members, step = gridDim.x / members;
+  // this part of k
+  const uint32_t k0 = (uint32_t)((uint64_t)p.iters * part / p.split), k1 = (uint32_t)((uint64_t)p.iters * (part + 1) / p.split);
+
+  uint64_t filled = 0;  // stages that this lane has asked for
+  bool issues = false;  // this lane issues the products
+  if (warp == 0) {
+    if (elect_one()) {
+      uint32_t st = 0, phase = 1;  // an empty barrier's phase before the first is taken as complete
+      bool ok = true;
+      for (uint32_t t = first; ok && t < p.tiles; t += step) {
+        const Tile w = tile_at(p, t);
+        const int32_t row = (int32_t)((w.tm * CTAS + half) * 128);
+        uint32_t seg = k0 / p.kb, kk = k0 - seg * p.kb;
+        for (uint32_t i = k0; i < k1; ++i) {
+          if (!(ok = bar_wait(empty(st), phase, &dead))) break;
+          // tiles and blocks of k outside their matrix read as 0
+          if (!MFET_INSIDE(p.status, seg < 3 && w.z < 2 && (int64_t)row < p.m + 128 && w.tn < p.n_tiles)) {
+            ok = false;
+            dead = 1;
+            break;
+          }
+          const uint32_t at = base + st * G::stage_bytes;
+          const uint32_t bar = CTAS == 1 ? full(st) : peer_addr(full(st), leader);
+          if (half == 0) bar_expect(full(st), CTAS * G::stage_bytes);
+          const CUtensorMap* a = &maps.a[((p.seg_a >> (4 * seg)) & 15u) + w.z];
+          const int32_t k = (int32_t)(kk * kSlab);
+          if (p.a_mn) {
+            tile_load<CTAS>(at, a, row, k, bar);
+            tile_load<CTAS>(at + 8192, a, row + 64, k, bar);
+          } else {
+            tile_load<CTAS>(at, a, k, row, bar);
+          }
+          if constexpr (G::dual) {
+            const int32_t unit = (int32_t)(w.tn * G::width);
+            if constexpr (CTAS == 2) {
+              tile_load<CTAS>(at + G::a_bytes, &maps.b[half], k, unit, bar);
+            } else {
+              tile_load<CTAS>(at + G::a_bytes, &maps.b[0], k, unit, bar);
+              tile_load<CTAS>(at + G::a_bytes + G::b_bytes / 2, &maps.b[1], k, unit, bar);
+            }
+          } else {
+            const CUtensorMap* b = &maps.b[(p.seg_b >> (4 * seg)) & 15u];
+            const int32_t col = (int32_t)(w.tn * TN + half * G::b_rows);
+            if (p.b_mn) {
+#pragma unroll
+              for (int j = 0; j < G::b_rows / 64; ++j) tile_load<CTAS>(at + G::a_bytes + 8192 * j, b, col + 64 * j, k, bar);
+            } else {
+              tile_load<CTAS>(at + G::a_bytes, b, k, col, bar);
+            }
+          }
+          ++filled;
+          if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
+          if (++kk == p.kb) kk = 0, ++seg;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (half == 0 && elect_one()) {
+      issues = true;
+      uint32_t st = 0, phase = 0, done = 0;
+      bool ok = true, ready = false;
+      const uint32_t a_step = p.a_mn ? 128u : 2u, b_step = p.b_mn ? 128u : 2u;
+      for (uint32_t t = first; ok && t < p.tiles; t += step, ++done) {
+        const int acc = done & 1;
+        if (done >= 2 && !(ok = bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem + acc * TN;
+        uint32_t kk = k0 % p.kb;
+        for (uint32_t i = k0; i < k1; ++i) {
+          if (!ready && !(ok = bar_wait(full(st), phase, &dead))) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t at = base + st * G::stage_bytes;
+          const uint32_t this_empty = empty(st);
+          const uint32_t a_lo = desc_lo(at, p.a_mn), b_lo = desc_lo(at + G::a_bytes, p.b_mn);
+          if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
+          const bool last = ++kk == p.kb;
+          if (last) kk = 0;
+          if (!last || p.tail == 4) {
+            mma16<CTAS>(d, a_lo, b_lo, p.inst, i != k0);
+            mma16<CTAS>(d, a_lo + a_step, b_lo + b_step, p.inst, 1);
+            ready = bar_try(full(st), phase);
+            mma16<CTAS>(d, a_lo + 2 * a_step, b_lo + 2 * b_step, p.inst, 1);
+            mma16<CTAS>(d, a_lo + 3 * a_step, b_lo + 3 * b_step, p.inst, 1);
+          } else {
+            for (uint32_t j = 0; j < p.tail; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, p.inst, (i != k0) | j);
+            ready = bar_try(full(st), phase);
+          }
+          commit<CTAS>(this_empty, pair_mask);
+          if (i + 1 == k1) commit<CTAS>(acc_full(acc), pair_mask);
+        }
+      }
+    }
+  }
+  const int quarter = warp & 3;            // the 32 lanes of tensor memory that this warp may read
+  const int second = warp >= 6 ? 1 : 0;    // two warps share them and take every other 32 columns
+  uint8_t* const out_ptr = smem + G::out_at + (warp - 2) * G::warp_out;
+  const uint32_t out_at = base + G::out_at + (warp - 2) * G::warp_out;
+  uint32_t turn = 0;
+  // 32 columns `v` of this lane's row, from column j1 on, to output o of the result (i0: the warp's first row)
+  auto put = [&](float* v, int o, int64_t i0, int64_t j1) {
+    constexpr int kPer = 16 / (int)sizeof(T);  // values per 16 bytes
+    const uint32_t piece = (turn * G::outs + (G::outs == 2 ? o : 0)) * G::piece;
+    uint8_t* const to = out_ptr + piece;
+#pragma unroll
+    for (int q = 0; q < 32; q += kPer) *reinterpret_cast<uint4*>(to + G::at(lane, q / kPer)) = narrow16<DT>(v + q);
+    if (((p.bulk >> o) & 1) && (j1 + 32 <= p.n || ((p.bulk >> o) & 4))) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (i0 < p.m && j1 < p.n && elect_one()) bulk_store(&maps.out[o], out_at + piece, (int32_t)j1, (int32_t)i0);
+      __syncwarp();
+    } else {
+      __syncwarp();
+      T* y = reinterpret_cast<T*>(p.out[o]) + i0 * p.out_ld[o] + j1 + lane;
+#pragma unroll 8
+      for (int i = 0; i < 32; ++i) {  // a warp writes a row's 32 columns
+        const T x = *reinterpret_cast<const T*>(to + G::at(i, lane / kPer) + lane % kPer * sizeof(T));
+        if (i0 + i < p.m && j1 + lane < p.n && MFET_INSIDE(p.status, i0 >= 0 && j1 >= 0 && j1 + lane < p.out_ld[o])) y[i * p.out_ld[o]] = x;
+      }
+      __syncwarp();
+    }
+  };
+  auto put_begin = [&]() {  // what the memory of the pieces held before has left
+    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    __syncwarp();
+  };
+  auto put_end = [&]() {
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    turn ^= 1;
+  };
+  // what becomes of 32 columns of the accumulator (and of the same units' other half, where dual): x is what c0 (c1) held there
+  auto finish = [&](float* v, float* u, float* x, int z, int64_t i0, int64_t j1) {
+    put_begin();
+    if constexpr (MODE == kGated) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = gate<false>(p.act, v[j], nullptr) * u[j];
+      put(v, 0, i0, j1);
+    } else if constexpr (MODE == kGatedBack) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        float slope;
+        const float a = gate<true>(p.act, v[j], &slope);
+        v[j] = x[j] * u[j] * slope;
+        u[j] = x[j] * a;
+      }
+      put(v, 0, i0, j1);
+      put(u, 1, i0, j1);
+    } else if constexpr (MODE == kOut) {
+      put(v, z, i0, j1);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], p.beta, x[j] * p.alpha);
+      if constexpr (MODE == kPair) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = v[j] - __half2float(__float2half_rn(v[j]));
+        put(v, 0, i0, j1);
+        put(x, 1, i0, j1);
+      } else {
+        put(v, 0, i0, j1);
+      }
+    }
+    put_end();
+  };
+  auto other = [&](float* x, int64_t i, int64_t j1) {  // what stands beside 32 columns of row i
+#pragma unroll
+    for (int j = 0; j < 32; ++j) x[j] = 0.f;
+    if constexpr (MODE == kGatedBack) {
+      if (i < p.m && MFET_INSIDE(p.status, j1 >= 0 && i >= 0)) load_row32<DT>(p.c0, i * p.c_ld + j1, p.n - j1, p.c_vec, x);
+    } else if constexpr (MODE == kPair || MODE == kPairOut) {
+      if (p.c0 && i < p.m && MFET_INSIDE(p.status, j1 >= 0 && i >= 0)) {
+        float lo[32];
+        load_row32<MFET_F16>(p.c0, i * p.c_ld + j1, p.n - j1, p.c_vec, x);
+        load_row32<MFET_F16>(p.c1, i * p.c_ld + j1, p.n - j1, p.c_vec, lo);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] += lo[j];
+      }
+    }
+  };
+  if (warp >= 2) {
+    uint32_t done = 0;
+    for (uint32_t t = first; t < p.tiles; t += step, ++done) {
+      const Tile w = tile_at(p, t);
+      const int acc = done & 1;
+      const int64_t i0 = (int64_t)(w.tm * CTAS + half) * 128 + quarter * 32, j0 = (int64_t)w.tn * G::width;
+      const uint32_t from = tmem + acc * TN + ((uint32_t)(quarter * 32) << 16);
+      float x[32];
+      if (p.split == 1) other(x, i0 + lane, j0 + 32 * second);  // under way while the tile is computed
+      const bool ok = bar_wait(acc_full(acc), (done / 2) & 1, &dead);
+      if (!__all_sync(kAllLanes, ok)) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      if (p.split > 1) {  // one tile per block: its sums go to shared memory, where the ring was
+#pragma unroll 1
+        for (int c = 32 * second; c < TN; c += 64) {
+          uint32_t r[32];
+          tmem_load32(from + c, r);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) *reinterpret_cast<uint32_t*>(smem + ((c + j) * 128 + quarter * 32 + lane) * 4) = r[j];
+        }
+        break;
+      }
+#pragma unroll 1
+      for (int c = 32 * second; c < G::width; c += 64) {
+        uint32_t r[32], r2[32];
+        tmem_load32(from + c, r);
+        if constexpr (G::dual) tmem_load32(from + G::width + c, r2);
+        if (c + 64 >= G::width) {  // the accumulator is read: the next tile but one may overwrite it
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (CTAS == 1) bar_arrive(acc_empty(acc));
+            else peer_arrive(peer_addr(acc_empty(acc), leader));
+          }
+        }
+        finish(reinterpret_cast<float*>(r), reinterpret_cast<float*>(r2), x, (int)w.z, i0, j0 + c);
+        if (c + 64 < G::width) other(x, i0 + lane, j0 + c + 64);
+      }
+    }
+  }
+  __syncwarp();  // the one lane that loaded or issued rejoins its warp
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (clustered) cluster_sync();  // of a split: all sums are in shared memory
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (p.split > 1) {
+    if (warp >= 2 && !dead && first < p.tiles) {
+      const Tile w = tile_at(p, first);
+      const int64_t i0 = (int64_t)(w.tm * CTAS + half) * 128 + quarter * 32, j0 = (int64_t)w.tn * G::width;
+      const int share = G::width / (int)p.split;
+#pragma unroll 1
+      for (int c = (int)part * share + 32 * second; c < (int)(part + 1) * share; c += 64) {
+        float x[32], v[32], u[32];
+        other(x, i0 + lane, j0 + c);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = 0.f, u[j] = 0.f;
+        for (uint32_t s = 0; s < p.split; ++s) {
+          const uint32_t src = peer_addr(base + (c * 128 + quarter * 32 + lane) * 4, s * CTAS + half);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] += peer_load(src + j * 512);
+          if constexpr (G::dual) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[j] += peer_load(src + (G::width + j) * 512);
+          }
+        }
+        finish(v, u, x, (int)w.z, i0, j0 + c);
+      }
+    }
+    __syncwarp();
+    cluster_sync();  // nobody's shared memory goes while another block reads it
+  }
+  if (warp >= 2) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // shared memory outlives the copies that read it
+  // Without a stall every copy and product has been waited for by the role that needed it. After one, whoever was ahead of the role that
+  // gave up has left some under way: all roles have ended here, so what is waited for now (with the same limit) is the last of them.
+  if (dead) {
+    volatile int none = 0;
+    if (half == 0) {
+      const uint64_t from = filled > G::stages ? filled - G::stages : 0;
+      for (uint64_t i = from; i < filled; ++i) bar_wait(full(i % G::stages), (i / G::stages) & 1, &none);
+    }
+    if (issues) {
+      commit<CTAS>(drained, pair_mask);
+      bar_wait(drained, 0, &none);
+    }
+    if (threadIdx.x == 0 && p.status) atomicOr(p.status, (uint32_t)MFET_DEV_STALLED);
+  }
+  __syncthreads();
+  if (clustered) cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 1) {
+    if constexpr (CTAS == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(G::tmem_cols));
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(G::tmem_cols));
+  }
+}
+
+// ------------------------------------------------------------------ host side ----
+
+// `outer` rows of `inner` neighbouring 16-bit values, `ld` apart
+struct Matrix {
+  const void* p;
+  int64_t inner, outer, ld;
+  bool spare = false;  // what lies between its rows is the library's own
+};
+
+inline bool tile_map(CUtensorMap* map, const Matrix& x, uint32_t dtype, uint32_t rows, uint32_t cols, CUtensorMapSwizzle swizzle, bool load) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const uint32_t size = size_of(dtype);
+  const int64_t ld = x.outer == 1 ? (x.inner * size + 15) / 16 * 16 / size : x.ld;  // of one row: not used
+  const cuuint64_t dims[2] = {(cuuint64_t)x.inner, (cuuint64_t)x.outer}, stride[1] = {(cuuint64_t)ld * size};
+  const cuuint32_t box[2] = {cols, rows}, ones[2] = {1, 1};
+  const CUtensorMapDataType t = dtype == MFET_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                : dtype == MFET_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                    : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return f(map, t, 2, const_cast<void*>(x.p), dims, stride, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+           load ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// may a bulk copy write (or read) its rows?
+inline bool on_16(const Matrix& x, uint32_t dtype) {
+  return aligned(x.p, 16) && (x.outer == 1 || (uint64_t)x.ld * size_of(dtype) % 16 == 0);
+}
+
+struct Problem {
+  uint32_t dtype = MFET_F16;  // of the operands
+  Matrix a[2] = {}, b[2] = {}, out[2] = {};
+  int n_a = 1, n_b = 1, n_out = 1, results = 1;
+  int64_t k = 0;              // of one segment
+  int segs = 1;
+  uint32_t out_dtype = MFET_F16;
+  Params p = {};              // majors, segments' operands, epilogue
+};
+
+template <int CTAS, int TN, int MODE, int DT>
+int launch(const Problem& q, uint32_t split, cudaStream_t s) {
+  using G = Shape<CTAS, TN, MODE, DT>;
+  Maps maps;
+  memset(&maps, 0, sizeof(maps));
+  Params p = q.p;
+  const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
+  for (int i = 0; i < q.n_a; ++i)
+    if (!tile_map(&maps.a[i], q.a[i], q.dtype, p.a_mn ? 64 : 128, 64, sw, true)) return MFET_ERR_CUDA;
+  for (int i = 0; i < q.n_b; ++i)
+    if (!tile_map(&maps.b[i], q.b[i], q.dtype, p.b_mn ? 64 : G::dual ? TN / 2 : G::b_rows, 64, sw, true)) return MFET_ERR_CUDA;
+  p.bulk = 0;
+  for (int i = 0; i < q.n_out; ++i) {
+    p.out[i] = const_cast<void*>(q.out[i].p);
+    p.out_ld[i] = q.out[i].ld;
+    if (!on_16(q.out[i], q.out_dtype)) continue;
+    p.bulk |= (q.out[i].spare || q.out[i].inner * size_of(q.out_dtype) % 16 == 0 ? 5u : 1u) << i;
+    if (!tile_map(&maps.out[i], q.out[i], q.out_dtype, 32, 32, G::piece_row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, false))
+      return MFET_ERR_CUDA;
+  }
+  p.m_tiles = (uint32_t)((p.m + CTAS * 128 - 1) / (CTAS * 128));
+  p.n_tiles = (uint32_t)((p.n + G::width - 1) / G::width);
+  p.tiles = p.m_tiles * p.n_tiles * (uint32_t)q.results;
+  p.band = 8;
+  p.kb = (uint32_t)((q.k + kSlab - 1) / kSlab);
+  p.iters = p.kb * (uint32_t)q.segs;
+  p.tail = (uint32_t)((q.k - (int64_t)(p.kb - 1) * kSlab + 15) / 16);
+  p.split = split;
+  const uint32_t fmt = q.dtype == MFET_BF16 ? 1u : 0u;
+  p.inst = (1u << 4) | (fmt << 7) | (fmt << 10) | (p.a_mn << 15) | (p.b_mn << 16) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(CTAS * 128 >> 4) << 24);
+  static std::atomic<uint64_t> ready{0};
+  if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return MFET_ERR_CUDA;
+  const uint32_t members = CTAS * split, at_once = (uint32_t)sm_count() / members;
+  const uint32_t clusters = split > 1 || p.tiles < at_once ? p.tiles : at_once;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = members;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(clusters * members);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = G::smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = members > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, TN, MODE, DT>, maps, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+}
+
+// The form for a problem: a cost in cycles for each, the least wins. Per block of k and tile a pair takes 512 cycles for 256 x 256 (its
+// instructions' time), a block 400 for 128 x 128 (256 for the instructions; loads bound it); setting up, the first loads and the last results 3000.
+template <int MODE, int DT>
+int run(const Problem& q, cudaStream_t s) {
+  constexpr bool dual = MODE == kGated || MODE == kGatedBack;
+  const int64_t iters = (q.k + kSlab - 1) / kSlab * q.segs;
+  const int64_t sms = sm_count();
+  auto tiles = [&](int64_t rows, int64_t cols) { return (q.p.m + rows - 1) / rows * ((q.p.n + cols - 1) / cols) * q.results; };
+  int best = 0;
+  uint32_t best_split = 1;
+  double least = 1e300;
+  for (int form = 0; form < 2; ++form) {
+    const int64_t ctas = form == 0 ? 2 : 1, width = (form == 0 ? 256 : 128) / (dual ? 2 : 1);
+    const int64_t t = tiles(128 * ctas, width);
+    for (uint32_t split = 1; split * ctas <= 8 && split * 32 <= width && (int64_t)split <= iters; split *= 2) {
+      const int64_t at_once = sms / (ctas * split), waves = (t + at_once - 1) / at_once;
+      if (split > 1 && waves > 1) break;
+      const double cost = (double)waves * ((iters + split - 1) / split) * (form == 0 ? 512 : 400) + (split > 1 ? 2500.0 : 0.0);
+      if (cost < least) least = cost, best = form, best_split = split;
+    }
+  }
+  return best == 0 ? launch<2, 256, MODE, DT>(q, best_split, s) : launch<1, 128, MODE, DT>(q, best_split, s);
+}
+
+// ------------------------------------------------------------------ rows that no bulk copy can read ----
+
+struct PackParams {
+  const uint8_t* src;
+  uint8_t* dst;
+  int64_t rows, cols, src_ld, dst_ld;
+};
+
+// 16-bit rows at any address into rows on 16-byte boundaries
+static __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackParams p) {
+  early_launch_wait();
+  const int64_t per_row = p.dst_ld / 8, units = p.rows * per_row;
+  const uint16_t* src = reinterpret_cast<const uint16_t*>(p.src);
+  const void* end = src + (p.rows - 1) * p.src_ld + p.cols;
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
+    const int64_t row = u / per_row, c = (u - row * per_row) * 8;
+    const int count = (int)(p.cols - c < 8 ? p.cols - c : 8);
+    if (!MFET_INSIDE(nullptr, row < p.rows && count > 0 && c + 8 <= p.dst_ld)) continue;
+    const Raw<MFET_F16, 8> r = load_shifted<MFET_F16, 8>(reinterpret_cast<const __half*>(src + row * p.src_ld + c), count, src, end);
+    *reinterpret_cast<uint4*>(p.dst + (row * p.dst_ld + c) * 2) = r.w[0];
+  }
+}
+
+inline int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+inline uint64_t packed_bytes(int64_t rows, int64_t cols) { return ((uint64_t)rows * up8(cols) * 2 + 15) / 16 * 16; }
+
+// x itself, or its copy at *to (which moves on behind it)
+inline cudaError_t packed(Matrix* x, uint8_t** to, cudaStream_t s) {
+  if (on_16(*x, MFET_F16)) return cudaSuccess;
+  PackParams p{(const uint8_t*)x->p, *to, x->outer, x->inner, x->ld, up8(x->inner)};
+  *to += packed_bytes(x->outer, x->inner);
+  x->p = p.dst;
+  x->ld = p.dst_ld;
+  const int64_t want = (x->outer * (p.dst_ld / 8) + 255) / 256, most = (int64_t)sm_count() * 16;
+  return launch_early(pack_kernel, (unsigned)(want < most ? want : most), 256, 0, s, p);
+}
+
+}  // namespace gemm16
+}  // namespace mfet

@@ -20,7 +20,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("MFET_LIBRARY") or os.path.join(_HERE, "libmfet.so")
 
 F32, F16, BF16, INT4, MXFP4 = 0, 1, 2, 3, 4
-ACT_NONE, ACT_RELU = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_SIGMOID = 0, 1, 2, 3, 4
 POOL_SUM, POOL_MEAN, POOL_WSUM = 0, 1, 2
 LOC_DEVICE, LOC_HOST = 0, 1
 VAL_NORMAL, VAL_GRID = 0, 1
@@ -44,6 +44,8 @@ EXPORTS = [
     "mfet_host_path_result", "mfet_host_fetch_rows",
     "mfet_grad_clip_bytes", "mfet_grad_clip", "mfet_rows_write", "mfet_rows_read", "mfet_mx4_code_bytes",
     "mfet_mx4_scale_bytes", "mfet_mx4_quantize", "mfet_mx4_matmul", "mfet_mx4_linear_bytes", "mfet_mx4_linear",
+    "mfet_layer_norm", "mfet_layer_norm_backward_bytes", "mfet_layer_norm_backward", "mfet_gated_linear_bytes", "mfet_gated_linear",
+    "mfet_gated_linear_backward_bytes", "mfet_gated_linear_backward", "mfet_orthogonalize_bytes", "mfet_orthogonalize",
 ]
 BATCH_IDS_ARE_ROWS, BATCH_PREFETCHED = 1, 2
 STATIC_DEDUP_MAX_IDS = 262144
@@ -107,10 +109,11 @@ _lib.mfet_tables_version.argtypes = [_P, C.POINTER(C.c_uint64)]
 _lib.mfet_host_prefetch.argtypes = [_P, C.POINTER(BatchShape), _P, _P, _P, _P]
 _lib.mfet_embedding_bag_backward.argtypes = [_P, C.POINTER(BatchShape), _P, _P, _P, _P, _P, _P, C.c_int32, _P, _P, _P, _P]
 _lib.mfet_launch_count.argtypes = [_P, C.POINTER(C.c_uint64)]
-_BYTES = ("mfet_grad_clip_bytes", "mfet_mx4_code_bytes", "mfet_mx4_scale_bytes", "mfet_mx4_linear_bytes")
+_BYTES = ("mfet_grad_clip_bytes", "mfet_mx4_code_bytes", "mfet_mx4_scale_bytes", "mfet_mx4_linear_bytes", "mfet_layer_norm_backward_bytes",
+          "mfet_gated_linear_bytes", "mfet_gated_linear_backward_bytes", "mfet_orthogonalize_bytes")
 for _n in _BYTES:
     getattr(_lib, _n).restype = C.c_uint64
-    getattr(_lib, _n).argtypes = [C.c_int32] if _n == "mfet_grad_clip_bytes" else [C.c_int64, C.c_int64]
+    getattr(_lib, _n).argtypes = [C.c_int32] if _n == "mfet_grad_clip_bytes" else [C.c_int64] * (3 if "gated" in _n else 2)
 for _n in EXPORTS:
     if _n not in ("mfet_row_bytes", "mfet_status_string") + _BYTES:
         getattr(_lib, _n).restype = C.c_int
@@ -374,11 +377,41 @@ def mfet_mx4_linear_bytes(m: int, k: int) -> int:
     return int(_lib.mfet_mx4_linear_bytes(m, k))
 
 
+def mfet_layer_norm_backward_bytes(rows: int, cols: int) -> int:
+    return int(_lib.mfet_layer_norm_backward_bytes(rows, cols))
+
+
+def mfet_gated_linear_bytes(m: int, n: int, k: int) -> int:
+    return int(_lib.mfet_gated_linear_bytes(m, n, k))
+
+
+def mfet_gated_linear_backward_bytes(m: int, n: int, k: int) -> int:
+    return int(_lib.mfet_gated_linear_backward_bytes(m, n, k))
+
+
+def mfet_orthogonalize_bytes(rows: int, cols: int) -> int:
+    return int(_lib.mfet_orthogonalize_bytes(rows, cols))
+
+
+def mfet_orthogonalize(g, dtype: int, ld: int, rows: int, cols: int, coefficients, steps: int, scale: float, out, out_dtype: int, out_ld: int,
+                       scratch, scratch_bytes: int, status=None, stream=None) -> None:
+    """coefficients: None, or a, b, c of every step (any host sequence or array of 3 * steps numbers)."""
+    if coefficients is not None:
+        coefficients = np.ascontiguousarray(coefficients, dtype=np.float32)
+        if coefficients.size != 3 * steps:
+            _fail(ERR_INVALID_ARG, "mfet_orthogonalize")
+    _orthogonalize(g, dtype, ld, rows, cols, None if coefficients is None else coefficients.ctypes.data, steps, scale, out, out_dtype, out_ld,
+                   scratch, scratch_bytes, status, stream)
+
+
 # The calls that a step makes many times go through a small extension instead of ctypes (csrc/fastcall.c). It is built for one version of
 # Python; another one makes the same calls, with the same names, arguments and errors, through ctypes. Per call: the kinds of its arguments
 # (as in fastcall.c) and how many of them have to be given.
 _FAST = {"mfet_grad_clip": ("ofppzp", 5), "mfet_rows_write": ("bpippuipp", 7), "mfet_rows_read": ("bpippuipp", 7),
-         "mfet_mx4_quantize": ("puiiippp", 7), "mfet_mx4_matmul": ("ppippiipupuipp", 12), "mfet_mx4_linear": ("puiippiipupuipzpp", 15)}
+         "mfet_mx4_quantize": ("puiiippp", 7), "mfet_mx4_matmul": ("ppippiipupuipp", 12), "mfet_mx4_linear": ("puiippiipupuipzpp", 15),
+         "mfet_layer_norm": ("puiiippfpuip", 11), "mfet_layer_norm_backward": ("puiiipfpuipipppzp", 16),
+         "mfet_gated_linear": ("puiipipiiiupipzpp", 15), "mfet_gated_linear_backward": ("puiipipiiiupipipipipzpp", 21),
+         "mfet_orthogonalize": ("puiiipdfpuipzpp", 13)}
 _KINDS = {"p": C.c_void_p, "b": C.c_void_p, "f": C.c_float, "i": C.c_int64, "u": C.c_uint32, "d": C.c_int32, "z": C.c_uint64}
 _RANGES = {"i": (-2**63, 2**63), "u": (0, 2**32), "d": (-2**31, 2**31), "z": (0, 2**63)}
 
@@ -424,5 +457,6 @@ def _through_ctypes(name: str):
 
 if _fastcall is not None:
     _fastcall.bind(_fail, *(C.cast(getattr(_lib, _n), C.c_void_p).value for _n in _FAST))
-mfet_grad_clip, mfet_rows_write, mfet_rows_read, mfet_mx4_quantize, mfet_mx4_matmul, mfet_mx4_linear = (
+(mfet_grad_clip, mfet_rows_write, mfet_rows_read, mfet_mx4_quantize, mfet_mx4_matmul, mfet_mx4_linear, mfet_layer_norm, mfet_layer_norm_backward,
+ mfet_gated_linear, mfet_gated_linear_backward, _orthogonalize) = (
     _through_ctypes(_n) if _fastcall is None else getattr(_fastcall, _n) for _n in _FAST)
