@@ -98,14 +98,14 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ float peer_load(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void peer_load(uint32_t addr, float* v) {
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void peer_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 // a tile into this block's memory; the barrier may be the pair's other block's
 template <int CTAS>
@@ -157,34 +157,58 @@ __device__ __forceinline__ void commit(uint32_t bar, uint32_t mask) {
 
 // ------------------------------------------------------------------ activations ----
 
+// erfc(z), called: 32 copies of it in a row would not fit the instruction cache
+static __device__ __noinline__ float erfc_of(float z) { return erfcf(z); }
+
 // act(g), and its derivative. The exponential's error (2^-17 at the ends of its range, 2^-21 in the middle) is far below a 16-bit result's.
-template <bool SLOPE>
-__device__ __forceinline__ float gate(uint32_t act, float g, float* slope) {
-  switch (act) {
-    case MFET_ACT_RELU: {
-      float r = g;
-      asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(r));
-      if (SLOPE) *slope = g > 0.f ? 1.f : 0.f;
-      return r;
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float gate(float g, float* slope) {
+  if constexpr (ACT == MFET_ACT_RELU) {
+    float r = g;
+    asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(r));
+    if (SLOPE) *slope = g > 0.f ? 1.f : 0.f;
+    return r;
+  } else if constexpr (ACT == MFET_ACT_SILU) {
+    const float s = __fdividef(1.f, 1.f + __expf(-g));
+    if (SLOPE) *slope = s * (1.f + g * (1.f - s));
+    return g * s;
+  } else if constexpr (ACT == MFET_ACT_SIGMOID) {
+    const float s = __fdividef(1.f, 1.f + __expf(-g));
+    if (SLOPE) *slope = s * (1.f - s);
+    return s;
+  } else if constexpr (ACT == MFET_ACT_GELU) {
+    const float c = 0.5f * erfc_of(g * -0.70710678118654752f);  // no cancellation for negative g
+    if (SLOPE) *slope = c + g * 0.3989422804014327f * __expf(-0.5f * g * g);
+    return g * c;
+  } else {
+    if (SLOPE) *slope = 1.f;
+    return g;
+  }
+}
+
+// 32 gates `v` and up units `u` to results: h in v; or, with the gradient x of h beside them, dG in v and dU in u
+template <int ACT, bool BACK>
+__device__ __forceinline__ void gates32(float* v, float* u, const float* x) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    if constexpr (BACK) {
+      float slope;
+      const float a = gate<ACT, true>(v[j], &slope);
+      v[j] = x[j] * u[j] * slope;
+      u[j] = x[j] * a;
+    } else {
+      v[j] = gate<ACT, false>(v[j], nullptr) * u[j];
     }
-    case MFET_ACT_SILU: {
-      const float s = __fdividef(1.f, 1.f + __expf(-g));
-      if (SLOPE) *slope = s * (1.f + g * (1.f - s));
-      return g * s;
-    }
-    case MFET_ACT_SIGMOID: {
-      const float e = __expf(-g), s = __fdividef(1.f, 1.f + e);
-      if (SLOPE) *slope = s * (1.f - s);
-      return s;
-    }
-    case MFET_ACT_GELU: {
-      const float c = 0.5f * erfcf(g * -0.70710678118654752f);  // no cancellation for negative g
-      if (SLOPE) *slope = c + g * 0.3989422804014327f * __expf(-0.5f * g * g);
-      return g * c;
-    }
-    default:
-      if (SLOPE) *slope = 1.f;
-      return g;
+  }
+}
+template <bool BACK>
+__device__ __forceinline__ void gates32(uint32_t act, float* v, float* u, const float* x) {
+  switch (act) {  // once per 32 columns: a choice per value made the code outgrow the instruction cache (8192 x 896 x 1024 backward: 71 us)
+    case MFET_ACT_RELU: return gates32<MFET_ACT_RELU, BACK>(v, u, x);
+    case MFET_ACT_SILU: return gates32<MFET_ACT_SILU, BACK>(v, u, x);
+    case MFET_ACT_GELU: return gates32<MFET_ACT_GELU, BACK>(v, u, x);
+    case MFET_ACT_SIGMOID: return gates32<MFET_ACT_SIGMOID, BACK>(v, u, x);
+    default: return gates32<MFET_ACT_NONE, BACK>(v, u, x);
   }
 }
 
@@ -239,6 +263,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   const uint32_t part = rank / CTAS, half = rank % CTAS, leader = rank - half;
   const uint32_t pair_mask = (CTAS == 2 ? 3u : 1u) << leader;
 
+  if (threadIdx.x == 64) {
+    prefetch_map(&maps.a[0]);
+    prefetch_map(&maps.b[0]);
+    if (G::dual || (p.seg_b >> 4)) prefetch_map(&maps.b[1]);
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < G::stages; ++s) bar_init(full(s), 1), bar_init(empty(s), 1);
     for (int a = 0; a < 2; ++a) bar_init(acc_full(a), 1), bar_init(acc_empty(a), 8 * CTAS);
@@ -398,17 +427,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   auto finish = [&](float* v, float* u, float* x, int z, int64_t i0, int64_t j1) {
     put_begin();
     if constexpr (MODE == kGated) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = gate<false>(p.act, v[j], nullptr) * u[j];
+      gates32<false>(p.act, v, u, x);
       put(v, 0, i0, j1);
     } else if constexpr (MODE == kGatedBack) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        float slope;
-        const float a = gate<true>(p.act, v[j], &slope);
-        v[j] = x[j] * u[j] * slope;
-        u[j] = x[j] * a;
-      }
+      gates32<true>(p.act, v, u, x);
       put(v, 0, i0, j1);
       put(u, 1, i0, j1);
     } else if constexpr (MODE == kOut) {
@@ -460,7 +482,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
           uint32_t r[32];
           tmem_load32(from + c, r);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) *reinterpret_cast<uint32_t*>(smem + ((c + j) * 128 + quarter * 32 + lane) * 4) = r[j];
+          for (int j = 0; j < 32; j += 4)
+            *reinterpret_cast<uint4*>(smem + (((c + j) >> 2) * 128 + quarter * 32 + lane) * 16) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
         }
         break;
       }
@@ -494,17 +517,24 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       const int share = G::width / (int)p.split;
 #pragma unroll 1
       for (int c = (int)part * share + 32 * second; c < (int)(part + 1) * share; c += 64) {
-        float x[32], v[32], u[32];
+        float x[32], v[32], u[32], t[32];
+        // the sums of one part after the other: of columns `from` on, four columns of a row in 16 bytes
+        auto fetch = [&](float* to, uint32_t s, int from) {
+          const uint32_t src = peer_addr(base + ((from >> 2) * 128 + quarter * 32 + lane) * 16, s * CTAS + half);
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) peer_load(src + j * 512, to + j);
+        };
+        fetch(v, 0, c);
+        if constexpr (G::dual) fetch(u, 0, G::width + c);
         other(x, i0 + lane, j0 + c);
+        for (uint32_t s = 1; s < p.split; ++s) {
+          fetch(t, s, c);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = 0.f, u[j] = 0.f;
-        for (uint32_t s = 0; s < p.split; ++s) {
-          const uint32_t src = peer_addr(base + (c * 128 + quarter * 32 + lane) * 4, s * CTAS + half);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] += peer_load(src + j * 512);
+          for (int j = 0; j < 32; ++j) v[j] += t[j];
           if constexpr (G::dual) {
+            fetch(t, s, G::width + c);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) u[j] += peer_load(src + (G::width + j) * 512);
+            for (int j = 0; j < 32; ++j) u[j] += t[j];
           }
         }
         finish(v, u, x, (int)w.z, i0, j0 + c);
@@ -607,7 +637,7 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   p.inst = (1u << 4) | (fmt << 7) | (fmt << 10) | (p.a_mn << 15) | (p.b_mn << 16) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(CTAS * 128 >> 4) << 24);
   static std::atomic<uint64_t> ready{0};
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return MFET_ERR_CUDA;
-  const uint32_t members = CTAS * split, at_once = (uint32_t)sm_count() / members;
+  const uint32_t members = CTAS * split, at_once = (uint32_t)clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, members, G::smem);
   const uint32_t clusters = split > 1 || p.tiles < at_once ? p.tiles : at_once;
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -625,28 +655,63 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, TN, MODE, DT>, maps, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
 }
 
-// The form for a problem: a cost in cycles for each, the least wins. Per block of k and tile a pair takes 512 cycles for 256 x 256 (its
-// instructions' time), a block 400 for 128 x 128 (256 for the instructions; loads bound it); setting up, the first loads and the last results 3000.
+// Clusters of 1, 2, 4 or 8 blocks that the current GPU runs at a time (148 SMs are not 18 clusters of 8: parts of the chip have odd numbers
+// of them; one cluster too many doubled a product's time).
+template <typename K>
+int64_t clusters_at_once(K kernel, uint32_t members, uint32_t smem) {
+  if (members == 1) return sm_count();
+  static std::atomic<int> known[64][4];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / (members + 1);
+  std::atomic<int>& k = known[dev][members == 2 ? 1 : members == 4 ? 2 : 3];
+  n = k.load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = members;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(members * (unsigned)sm_count());
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return sm_count() / (members + 1);  // not remembered: asked again next time
+  }
+  k.store(n, std::memory_order_relaxed);
+  return n;
+}
+
+template <int CTAS, int TN, int MODE, int DT>
+double cost(const Problem& q, uint32_t split) {
+  using G = Shape<CTAS, TN, MODE, DT>;
+  const int64_t iters = (q.k + kSlab - 1) / kSlab * q.segs;
+  if (split > 1 && (split * CTAS > 8 || split * 32 > (uint32_t)G::width || (int64_t)split > iters)) return 1e300;
+  const int64_t tiles = (q.p.m + CTAS * 128 - 1) / (CTAS * 128) * ((q.p.n + G::width - 1) / G::width) * q.results;
+  static std::atomic<uint64_t> ready{0};
+  if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
+  const int64_t at_once = clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, CTAS * split, G::smem), waves = (tiles + at_once - 1) / at_once;
+  if (split > 1 && waves > 1) return 1e300;
+  const double base = CTAS == 2 ? 7.0 : 5.9, each = CTAS == 2 ? 0.28 : tiles * split > at_once / 2 ? 0.155 : 0.14;
+  return base + (double)waves * ((iters + split - 1) / split) * each + (split == 1 ? 0.0 : split == 2 ? 2.5 : 5.0);
+}
+
+// The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 7.0 for pairs, 5.9
+// for blocks; a block of k 0.28 for 256 x 256 by a pair, 0.14 for 128 x 128 by a block (0.155 when L2 serves all SMs); joining two parts
+// 2.5, four 5. (1 x 896 x 1024 forward: blocks 7.8, in two parts 9.9, pairs 11.0; 8192 x 896 x 1024 backward: pairs 93, blocks 114.)
 template <int MODE, int DT>
 int run(const Problem& q, cudaStream_t s) {
-  constexpr bool dual = MODE == kGated || MODE == kGatedBack;
-  const int64_t iters = (q.k + kSlab - 1) / kSlab * q.segs;
-  const int64_t sms = sm_count();
-  auto tiles = [&](int64_t rows, int64_t cols) { return (q.p.m + rows - 1) / rows * ((q.p.n + cols - 1) / cols) * q.results; };
-  int best = 0;
-  uint32_t best_split = 1;
   double least = 1e300;
-  for (int form = 0; form < 2; ++form) {
-    const int64_t ctas = form == 0 ? 2 : 1, width = (form == 0 ? 256 : 128) / (dual ? 2 : 1);
-    const int64_t t = tiles(128 * ctas, width);
-    for (uint32_t split = 1; split * ctas <= 8 && split * 32 <= width && (int64_t)split <= iters; split *= 2) {
-      const int64_t at_once = sms / (ctas * split), waves = (t + at_once - 1) / at_once;
-      if (split > 1 && waves > 1) break;
-      const double cost = (double)waves * ((iters + split - 1) / split) * (form == 0 ? 512 : 400) + (split > 1 ? 2500.0 : 0.0);
-      if (cost < least) least = cost, best = form, best_split = split;
-    }
+  int form = 0;
+  uint32_t split = 1;
+  for (uint32_t part = 1; part <= 4; part *= 2) {
+    const double pair = cost<2, 256, MODE, DT>(q, part), block = cost<1, 128, MODE, DT>(q, part);
+    if (pair < least) least = pair, form = 0, split = part;
+    if (block < least) least = block, form = 1, split = part;
   }
-  return best == 0 ? launch<2, 256, MODE, DT>(q, best_split, s) : launch<1, 128, MODE, DT>(q, best_split, s);
+  return form == 0 ? launch<2, 256, MODE, DT>(q, split, s) : launch<1, 128, MODE, DT>(q, split, s);
 }
 
 // ------------------------------------------------------------------ rows that no bulk copy can read ----
