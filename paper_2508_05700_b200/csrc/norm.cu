@@ -3,8 +3,9 @@
 //   mu = mean(x), r = 1 / sqrt(mean((x - mu)^2) + eps), xh = (x - mu) r, y = xh w + b
 //   t = dy w:  dx = r (t - mean(t) - xh mean(t xh)),  dw = sum over rows of dy xh,  db = sum over rows of dy
 //
-// Both are bound by memory: x is read once and kept in registers, the variance is taken of the differences from the mean (no
-// cancellation for rows far from 0), and the backward pass computes mu and r from x again instead of reading them. Everything is fp32 inside.
+// Bound by memory: x is read once and kept in registers, the variance is taken of the differences d = x - mu (no cancellation for rows far
+// from 0), and the backward pass computes mu and r from x again instead of reading them. Two rounds of sums a row: the mean,
+// then the squares of d and, backward, t and t d with them (mean(t xh) is r mean(t d)). Everything is fp32 inside.
 #include <type_traits>
 
 #include "tensor.cuh"
@@ -15,23 +16,20 @@ namespace mfet {
 namespace {
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
-constexpr int kChunk = 8;            // neighbouring columns of a thread
-constexpr int64_t kMostHeld = 16384; // columns of the longest row that is held in registers
-constexpr int64_t kMostFast = 8192;   // ... by the kernel for rows on 16-byte boundaries, whose rows and weights are in shared memory
+constexpr int kChunk = 8;             // neighbouring columns of a thread, for rows of more than
+constexpr int64_t kMostHeld = 16384;  // columns: the longest row that registers hold
 constexpr int kLongThreads = 512;
 
 struct NormParams {
   const void *x, *dy;  // dy: backward
   void* y;             // forward: y; backward: dx, of x's type
   const float *w, *b;
-  float* partial;      // backward: [blocks][2][cols] sums of dy xh, of dy; NULL: no sums wanted
+  float* partial;      // backward: the blocks' sums of dy xh and of dy; NULL: no sums wanted
   int64_t rows, cols, x_ld, y_ld, dy_ld;
   const void *x_end, *dy_end;
   float eps;
   uint32_t dy_dtype, y_dtype;
   bool x_vec, y_vec, dy_vec, w_vec, b_vec;  // rows start on 16-byte boundaries
-  int tpr, groups;  // threads of a row; rows of a block at a time
-  int stage_bytes;  // shared memory of a group for rows of results
 };
 
 template <int DT>
@@ -88,214 +86,10 @@ __device__ __forceinline__ void params8(const float* w, int64_t c, int64_t cols,
   for (int j = 0; j < kChunk; ++j) v[j] = w && c + j < cols ? __ldg(w + c + j) : none;
 }
 
-// A row of results at an address that is not on 16 bytes: value by value to shared memory, under the same address modulo 16, and from there in
-// whole units; the units at its ends value by value. (8 values a thread straight to memory: eight times the transactions.)
-template <int DT>
-__device__ __forceinline__ void values_to(uint8_t* row, int64_t c, const float* v, int count) {
-  typename Elem<DT>::T* to = reinterpret_cast<typename Elem<DT>::T*>(row) + c;
-#pragma unroll
-  for (int j = 0; j < kChunk; ++j)
-    if (j < count) to[j] = Elem<DT>::from(v[j]);
-}
-__device__ __forceinline__ void values_any(uint32_t dtype, uint8_t* row, int64_t c, const float* v, int count) {
-  if (dtype == MFET_F32) values_to<MFET_F32>(row, c, v, count);
-  else if (dtype == MFET_F16) values_to<MFET_F16>(row, c, v, count);
-  else values_to<MFET_BF16>(row, c, v, count);
-}
-__device__ __forceinline__ void row_out(uint8_t* to, const uint8_t* from, uint32_t head, uint32_t bytes, uint32_t size, int lane, int threads) {
-  const uint32_t units = (head + bytes + 15) / 16;
-  for (uint32_t u = lane; u < units; u += threads) {
-    const uint32_t lo = max(16 * u, head), hi = min(16 * u + 16, head + bytes);
-    if (hi - lo == 16) {
-      *reinterpret_cast<uint4*>(to + 16 * u - head) = *reinterpret_cast<const uint4*>(from + 16 * u);
-    } else if (size == 4) {
-      for (uint32_t i = lo; i < hi; i += 4) *reinterpret_cast<uint32_t*>(to + i - head) = *reinterpret_cast<const uint32_t*>(from + i);
-    } else {
-      for (uint32_t i = lo; i < hi; i += 2) *reinterpret_cast<uint16_t*>(to + i - head) = *reinterpret_cast<const uint16_t*>(from + i);
-    }
-  }
-}
-
 // s / n, rounded like a quotient (one correction): the mean of equal values is that value
 __device__ __forceinline__ float over(float s, float n, float inv_n) {
   const float q = s * inv_n;
   return fmaf(fmaf(-q, n, s), inv_n, q);
-}
-
-// The block's sums for dw and db into its part of `partial`, as its threads hold them: word (which * chunks + i) * PER + j of thread `lane` of a row is
-// at that word times tpr plus lane (the kernel that adds up the blocks puts columns in order). Several groups leave theirs in shared memory
-// (`sums`: 2 PER NCH words a thread) first, and each word is added up over them in their order.
-template <int NCH, int PER, int GROUPS, int TPR, typename W, typename B>  // groups of a block and threads of a group, 0: known at run time
-__device__ __forceinline__ void block_sums(const NormParams& p, float* sums, int group, int lane, W dw, B db) {
-  if (!p.partial) return;
-  constexpr int kWords = 2 * NCH * PER;
-  const int groups = GROUPS ? GROUPS : p.groups, tpr = TPR ? TPR : p.tpr;
-  float* const to = p.partial + (int64_t)blockIdx.x * kWords * tpr + lane;
-  if (groups > 1) {
-    const int pitch = groups * tpr;
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        sums[(i * PER + j) * pitch + threadIdx.x] = dw(i, j);
-        sums[((NCH + i) * PER + j) * pitch + threadIdx.x] = db(i, j);
-      }
-    }
-    __syncthreads();
-    for (int e = group; e < kWords; e += groups) {
-      const float* from = sums + e * pitch + lane;
-      float v = from[0];
-      for (int g = 1; g < groups; ++g) v += from[g * tpr];
-      if (MFET_INSIDE(nullptr, lane < tpr)) to[e * tpr] = v;
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      if (!MFET_INSIDE(nullptr, lane < tpr)) continue;
-      to[(i * PER + j) * tpr] = dw(i, j);
-      to[((NCH + i) * PER + j) * tpr] = db(i, j);
-    }
-  }
-}
-
-// Rows that are held in registers, 8 * NCH columns a thread. As many threads as a row needs, counted up to a warp (p.tpr), are a group with its
-// barrier; a block is p.groups of them, each with a row of its own at a time, so that enough rows are under way. Two rounds of sums a row:
-// the mean, then of the differences d = x - mu their squares and, backward, t and t d together (mean(t xh) is r mean(t d)). The
-// backward pass keeps its sums for dw and db in registers from row to row and joins them per block. 8192 x 896 fp32 x, bf16 dy: 56 us with a warp
-// per row (28 columns a lane, 199 registers), 27.5 with 8 columns a thread (560 instructions per row and warp, most of them not per column).
-template <int DT, int NCH, bool BACK, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : BACK ? 2 : 3) norm_kernel(const __grid_constant__ NormParams p) {
-  constexpr int kValues = BACK ? 3 : 1;
-  __shared__ float words[2][32 * kValues];  // of a round and the one after it: a word of each warp for each sum
-  extern __shared__ __align__(16) uint8_t staged[];  // rows of results that do not start on 16 bytes; at the end: the groups' sums
-  early_launch_wait();
-  const int tpr = p.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
-  const int warps = tpr >> 5, warp0 = group * warps;
-  int turn = 0;
-  auto meet = [&]() {
-    if (warps == 1) __syncwarp();
-    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
-  };
-  // sums of v[0 .. count) over the group, the same in all its threads
-  auto total = [&](float* v, auto count) {
-    constexpr int n = decltype(count)::value;
-#pragma unroll
-    for (int i = 0; i < n; ++i) v[i] = warp_sum(v[i]);
-    if (warps == 1) return;
-    float* at = words[turn] + warp0 * kValues;
-    turn ^= 1;
-    if ((lane & 31) == 0) {
-#pragma unroll
-      for (int i = 0; i < n; ++i) at[(lane >> 5) * kValues + i] = v[i];
-    }
-    meet();
-#pragma unroll
-    for (int i = 0; i < n; ++i) v[i] = at[i];
-    for (int q = 1; q < warps; ++q) {
-#pragma unroll
-      for (int i = 0; i < n; ++i) v[i] += at[q * kValues + i];
-    }
-  };
-  const float n = (float)p.cols, inv_n = 1.f / n;
-  const uint32_t out_size = (BACK ? DT : p.y_dtype) == MFET_F32 ? 4 : 2;
-  uint8_t* const stage = staged + group * p.stage_bytes;
-  int count[NCH];
-  float w[NCH][kChunk], b[BACK ? 1 : NCH][kChunk], dw[BACK ? NCH : 1][kChunk], db[BACK ? NCH : 1][kChunk];
-#pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const int64_t c = (int64_t)(i * tpr + lane) * kChunk;
-    count[i] = c < p.cols ? (int)min((int64_t)kChunk, p.cols - c) : 0;
-    params8(p.w, c, p.cols, p.w_vec, 1.f, w[i]);
-    if constexpr (!BACK) params8(p.b, c, p.cols, p.b_vec, 0.f, b[i]);
-    if constexpr (BACK) {
-#pragma unroll
-      for (int j = 0; j < kChunk; ++j) dw[i][j] = db[i][j] = 0.f;
-    }
-  }
-  for (int64_t row = (int64_t)blockIdx.x * p.groups + group; row < p.rows; row += (int64_t)gridDim.x * p.groups) {
-    Raw<DT, kChunk> raw[NCH];
-    float v[NCH][kChunk], t[BACK ? NCH : 1][kChunk];
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int64_t c = (int64_t)(i * tpr + lane) * kChunk;
-      if (count[i] > 0 && MFET_INSIDE(nullptr, row < p.rows && c + count[i] <= p.x_ld)) raw[i] = chunk_in<DT>(p.x, row * p.x_ld + c, count[i], p.x_vec, p.x_end);
-      else memset(&raw[i], 0, sizeof(raw[i]));
-      if constexpr (BACK) {
-        if (count[i] > 0 && MFET_INSIDE(nullptr, row < p.rows && c + count[i] <= p.dy_ld)) {
-          chunk_any(p.dy_dtype, p.dy, row * p.dy_ld + c, count[i], p.dy_vec, p.dy_end, t[i]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < kChunk; ++j) t[i][j] = 0.f;
-        }
-      }
-    }
-    uint8_t* const y_row = reinterpret_cast<uint8_t*>(p.y) + row * p.y_ld * out_size;
-    const uint32_t head = (uint32_t)reinterpret_cast<uintptr_t>(y_row) & 15u;
-    float s[kValues];
-    s[0] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      widen_raw<DT, kChunk>(raw[i], v[i]);
-#pragma unroll
-      for (int j = 0; j < kChunk; ++j) s[0] += v[i][j];
-    }
-    total(s, std::integral_constant<int, 1>());
-    const float mu = over(s[0], n, inv_n);
-#pragma unroll
-    for (int k = 0; k < kValues; ++k) s[k] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-#pragma unroll
-      for (int j = 0; j < kChunk; ++j) {
-        v[i][j] = j < count[i] ? v[i][j] - mu : 0.f;
-        s[0] = fmaf(v[i][j], v[i][j], s[0]);
-        if constexpr (BACK) {
-          const float tw = t[i][j] * w[i][j];
-          s[1] += tw;
-          s[2] = fmaf(tw, v[i][j], s[2]);
-        }
-      }
-    }
-    total(s, std::integral_constant<int, kValues>());
-    const float r = rsqrtf(fmaf(s[0], inv_n, p.eps));
-    if constexpr (BACK) {
-      const float m0 = s[1] * inv_n, m1 = s[2] * inv_n * r;
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) {
-          const float xh = v[i][j] * r;
-          db[i][j] += t[i][j];
-          dw[i][j] = fmaf(t[i][j], xh, dw[i][j]);
-          v[i][j] = r * (fmaf(t[i][j], w[i][j], -m0) - xh * m1);
-        }
-        const int64_t c = (int64_t)(i * tpr + lane) * kChunk;
-        if (!p.y_vec) values_to<DT>(stage + head, c, v[i], count[i]);
-        else if (count[i] > 0 && MFET_INSIDE(nullptr, row < p.rows && c + count[i] <= p.y_ld)) chunk_out<DT>(p.y, row * p.y_ld + c, v[i], count[i], true);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) v[i][j] = fmaf(v[i][j] * r, w[i][j], b[i][j]);
-        const int64_t c = (int64_t)(i * tpr + lane) * kChunk;
-        if (!p.y_vec) values_any(p.y_dtype, stage + head, c, v[i], count[i]);
-        else if (count[i] > 0 && MFET_INSIDE(nullptr, row < p.rows && c + count[i] <= p.y_ld)) chunk_put(p.y_dtype, p.y, row * p.y_ld + c, v[i], count[i], true);
-      }
-    }
-    if (!p.y_vec) {  // what the stage held before has left: two rounds of sums lie between
-      meet();
-      if (MFET_INSIDE(nullptr, row < p.rows && p.cols <= p.y_ld)) row_out(y_row, stage, head, (uint32_t)p.cols * out_size, out_size, lane, tpr);
-      if (warps == 1) __syncwarp();
-    }
-  }
-  if constexpr (BACK) {
-    __syncthreads();
-    block_sums<NCH, kChunk, 0, 0>(p, reinterpret_cast<float*>(staged), group, lane, [&](int i, int j) { return dw[i][j]; }, [&](int i, int j) { return db[i][j]; });
-  }
 }
 
 // Two fp32 numbers in one instruction
@@ -329,32 +123,131 @@ __device__ __forceinline__ void copy_part(uint32_t to, const void* from, int byt
 __device__ __forceinline__ void store16_shared(uint32_t to, const uint4& v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+template <typename T>
+__device__ __forceinline__ void store_shared(uint32_t to, T v) {
+  if constexpr (sizeof(T) == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(reinterpret_cast<const uint32_t&>(v)) : "memory");
+  else asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(reinterpret_cast<const uint16_t&>(v)) : "memory");
+}
+__device__ __forceinline__ uint32_t load4_shared(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint4 load16_shared(uint32_t at) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
 
-// Threads of a block of the kernel below, and blocks that an SM has to hold. Backward one block, as large as its registers let it be (some 160 with
-// 32 columns a thread; at 128 it spilt: 37 us instead of 27 for 8192 x 896), since each leaves sums of all columns.
-template <int NQ, int W, bool BACK>
-constexpr int fast_threads = !BACK || W == 8 ? 256 : NQ > 4 ? 384 : 512;
-template <bool BACK>
-constexpr int fast_blocks = BACK ? 1 : 3;
+// A row of results at any address: from shared memory, where it lies under the same address modulo 16, in whole units; the units at its ends
+// value by value. (4 values a thread straight to memory: several times the transactions.)
+__device__ __forceinline__ void row_out(uint8_t* to, const uint8_t* from, uint32_t head, uint32_t bytes, uint32_t size, int lane, int threads) {
+  const uint32_t units = (head + bytes + 15) / 16;
+  for (uint32_t u = lane; u < units; u += threads) {
+    const uint32_t lo = max(16 * u, head), hi = min(16 * u + 16, head + bytes);
+    if (hi - lo == 16) {
+      *reinterpret_cast<uint4*>(to + 16 * u - head) = *reinterpret_cast<const uint4*>(from + 16 * u);
+    } else if (size == 4) {
+      for (uint32_t i = lo; i < hi; i += 4) *reinterpret_cast<uint32_t*>(to + i - head) = *reinterpret_cast<const uint32_t*>(from + i);
+    } else {
+      for (uint32_t i = lo; i < hi; i += 2) *reinterpret_cast<uint16_t*>(to + i - head) = *reinterpret_cast<const uint16_t*>(from + i);
+    }
+  }
+}
 
-// 4 values of a type in shared memory
-template <int DT>
-__device__ __forceinline__ void quad_in(uint32_t at, float2* v) {
+// The block's sums for dw and db into its part of `partial`, as its threads hold them: word (which * NQ + i) * 4 + j of thread `lane` of a row is
+// at that word times TPR plus lane (the kernel that adds up the blocks puts columns in order). Several groups leave theirs in shared memory
+// (`sums`: 8 NQ words a thread) first, and each word is added up over them in their order.
+template <int NQ, int GROUPS, int TPR>  // groups of a block and threads of a group
+__device__ __forceinline__ void block_sums(const NormParams& p, float* sums, int group, int lane, const float2 (*dw)[2], const float2 (*db)[2]) {
+  if (!p.partial) return;
+  constexpr int kWords = 8 * NQ, kPitch = GROUPS * TPR;
+  float* const to = p.partial + (int64_t)blockIdx.x * kWords * TPR + lane;
+  auto word = [&](const float2 (*v)[2], int i, int j) { return j & 1 ? v[i][j >> 1].y : v[i][j >> 1].x; };
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (GROUPS > 1) {
+        sums[(i * 4 + j) * kPitch + threadIdx.x] = word(dw, i, j);
+        sums[((NQ + i) * 4 + j) * kPitch + threadIdx.x] = word(db, i, j);
+      } else if (MFET_INSIDE(nullptr, lane < TPR)) {
+        to[(i * 4 + j) * TPR] = word(dw, i, j);
+        to[((NQ + i) * 4 + j) * TPR] = word(db, i, j);
+      }
+    }
+  }
+  if constexpr (GROUPS > 1) {
+    __syncthreads();
+    for (int e = group; e < kWords; e += GROUPS) {
+      const float* from = sums + e * kPitch + lane;
+      float v = from[0];
+#pragma unroll
+      for (int g = 1; g < GROUPS; ++g) v += from[g * TPR];
+      if (MFET_INSIDE(nullptr, lane < TPR)) to[e * TPR] = v;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ rows that registers hold ----
+
+// Threads of a block of the kernel below. Backward one block per SM, as large as its registers let it be (some 160 with 32 columns a thread;
+// at 128 it spilt: 37 us instead of 27 for 8192 x 896), since each leaves sums of all columns.
+template <int NQ, int W, bool BACK>
+constexpr int norm_threads = W == 16 ? 512 : !BACK || W == 8 ? 256 : NQ > 4 ? 384 : 512;
+
+// What a block of it has in shared memory
+template <int DT, int OT, int NQ, int W, bool BACK, bool ALIGNED>
+struct NormShape {
+  static constexpr int threads = norm_threads<NQ, W, BACK>, tpr = 32 * W, groups = threads / tpr;
+  static constexpr int xs = (int)sizeof(typename Elem<DT>::T), os = (int)sizeof(typename Elem<OT>::T);
+  static constexpr uint32_t pad = ALIGNED ? 0 : 16;
+  static constexpr uint32_t x_bytes = NQ * tpr * 4 * xs + pad, dy_bytes = BACK ? NQ * tpr * 4 * os + pad : 0, stage = x_bytes + dy_bytes;  // a row
+  static constexpr int stages = W == 16 && BACK && xs + os == 8 ? 1 : 2;  // rows of a group: computed and under way
+  static constexpr uint32_t out_at = groups * stages * stage, out_bytes = ALIGNED || BACK ? 0 : NQ * tpr * 4 * os + pad;  // results (backward: over x)
+  static constexpr uint32_t w_at = out_at + groups * out_bytes, w_bytes = W <= 8 ? NQ * tpr * 16 : 0;
+  static constexpr uint32_t rows_end = w_at + w_bytes * (BACK ? 1 : 2), sums = BACK && groups > 1 ? threads * NQ * 32 : 0;
+  static constexpr uint32_t smem = rows_end > sums ? rows_end : sums;
+  static constexpr int per_sm = BACK || W == 16 ? 1 : smem <= 74 * 1024 ? 3 : smem <= 112 * 1024 ? 2 : 1;
+  // quads that are full for all threads: no more are taken than rows of a size need (see columns_of)
+  static constexpr int sure = W > 1 || NQ == 7 ? 4 : NQ == 8 ? (ALIGNED ? 7 : 4) : NQ == 4 ? (ALIGNED ? 2 : 1) : NQ / 2;
+  static constexpr int x_pieces = (NQ * xs + 3) / 4 + (ALIGNED ? 0 : 1), dy_pieces = (NQ * os + 3) / 4 + (ALIGNED ? 0 : 1);  // that a thread fetches
+  static_assert(smem <= 227 * 1024 - 1024, "shared memory of a block");
+  static_assert(W == 1 || groups < 16, "named barriers");
+};
+
+// 4 values of a type in shared memory. ALIGNED: to all of their bytes; else to their type, `odd`: not to 4 bytes.
+template <int DT, bool ALIGNED>
+__device__ __forceinline__ void quad_in(uint32_t at, bool odd, float2* v) {
   if constexpr (DT == MFET_F32) {
-    const uint4 a = load16_shared(at);
+    uint4 a;
+    if constexpr (ALIGNED) a = load16_shared(at);
+    else a = make_uint4(load4_shared(at), load4_shared(at + 4), load4_shared(at + 8), load4_shared(at + 12));
     v[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
     v[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
   } else {
     uint32_t a, b;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(at) : "memory");
+    if constexpr (ALIGNED) {
+      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(at) : "memory");
+    } else {
+      const uint32_t from = at & ~3u;
+      a = load4_shared(from);
+      b = load4_shared(from + 4);
+      if (odd) {
+        const uint32_t c = load4_shared(from + 8);
+        a = __byte_perm(a, b, 0x5432);
+        b = __byte_perm(b, c, 0x5432);
+      }
+    }
     v[0] = Elem<DT>::widen(a);
     v[1] = Elem<DT>::widen(b);
   }
+}
+__device__ __forceinline__ void keep(float2* v, int count) {  // the first `count` of 4 values, the others 0
+  if (count < 1) v[0].x = 0.f;
+  if (count < 2) v[0].y = 0.f;
+  if (count < 3) v[1].x = 0.f;
+  if (count < 4) v[1].y = 0.f;
 }
 template <int DT>
 __device__ __forceinline__ void quad_out(typename Elem<DT>::T* to, const float2* v, int count) {
@@ -367,79 +260,117 @@ __device__ __forceinline__ void quad_out(typename Elem<DT>::T* to, const float2*
     if (count > 2) to[2] = Elem<DT>::from(v[1].x);
   }
 }
+// ... to shared memory, at any address of the type
+template <int DT>
+__device__ __forceinline__ void quad_stage(uint32_t to, bool odd, const float2* v, int count) {
+  constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
+  if (DT != MFET_F32 && !odd && count == 4) {
+    if constexpr (DT != MFET_F32) {
+      store_shared(to, Elem<DT>::pack(v[0].x, v[0].y));
+      store_shared(to + 4, Elem<DT>::pack(v[1].x, v[1].y));
+    }
+    return;
+  }
+  if (count > 0) store_shared(to, Elem<DT>::from(v[0].x));
+  if (count > 1) store_shared(to + kSize, Elem<DT>::from(v[0].y));
+  if (count > 2) store_shared(to + 2 * kSize, Elem<DT>::from(v[1].x));
+  if (count > 3) store_shared(to + 3 * kSize, Elem<DT>::from(v[1].y));
+}
 
-// The same where all rows start on 16-byte boundaries. A warp takes up to 1024 columns (most instructions of a row do not depend on its columns:
-// sums over lanes, barriers, addresses), a lane 4 neighbouring ones of every 128, so that every access of a warp is whole lines of memory
-// and of shared memory (8 neighbouring ones: fp32 rows were fetched by halves of sectors, twice). The next row is under way to shared
-// memory in pieces of 16 bytes; arithmetic goes two columns an instruction, and all distances are known to the compiler (with
-// the threads of a row and of a block known at run time, 500 of a row's 1140 instructions formed addresses). Columns
-// behind the row's end are zeros with weight 0 and mean 0, so that nothing asks for them but the stores.
-template <int DT, int OT, int NQ, int W, bool BACK>
-__global__ void __launch_bounds__((fast_threads<NQ, W, BACK>), fast_blocks<BACK>) norm_fast_kernel(const __grid_constant__ NormParams p) {
-  constexpr int kThreads = fast_threads<NQ, W, BACK>, tpr = 32 * W, kGroups = kThreads / tpr;
-  constexpr int kXs = (int)sizeof(typename Elem<DT>::T), kOs = (int)sizeof(typename Elem<OT>::T);
-  constexpr uint32_t kXb = NQ * tpr * 4 * kXs, kStage = kXb + (BACK ? NQ * tpr * 4 * kOs : 0);  // of a group: x (and dy) of a row
-  constexpr int kXn = (NQ * kXs + 3) / 4, kOn = (NQ * kOs + 3) / 4;                            // pieces of 16 bytes that a thread fetches
-  constexpr int kSure = W > 1 || NQ == 7 ? 4 : NQ == 8 ? 7 : NQ / 2;                           // quads that are full for all threads
+// W warps take a row of up to 1024 W columns (most instructions of a row do not depend on its columns: sums over lanes, barriers, addresses), a
+// lane 4 neighbouring ones of every 128 W, so that every access of a warp is whole lines of memory and of shared memory (8 neighbouring ones:
+// fp32 rows were fetched by halves of sectors, twice). The next row is under way to shared memory in pieces of 16 bytes; arithmetic
+// goes two columns an instruction, and all distances are known to the compiler (with the threads of a row and of a block known at run
+// time, 500 of a row's 1140 instructions formed addresses). Rows on 16-byte boundaries: columns behind the row's end are
+// zeros with weight 0 and mean 0, so that nothing asks for them but the stores. Other rows are fetched in the pieces that hold them, read
+// from shared memory where their values lie, and written from there.
+// Backward, 8192 x 896, fp32 x, bf16 dy: a warp per row with its row in registers 56 us, 16 columns a thread 25, this 13 and the sum of the blocks
+// 4; the loop over 16384 x 2048 bf16 runs at 6.5 TB/s.
+template <int DT, int OT, int NQ, int W, bool BACK, bool ALIGNED>
+__global__ void __launch_bounds__((norm_threads<NQ, W, BACK>), BACK || W == 16 ? 1 : 3) norm_kernel(const __grid_constant__ NormParams p) {
+  using S = NormShape<DT, OT, NQ, W, BACK, ALIGNED>;
+  constexpr int tpr = S::tpr, kXs = S::xs, kOs = S::os, kYs = BACK ? kXs : kOs, kType = BACK ? DT : OT;
   __shared__ float words[2][16][4];
-  extern __shared__ __align__(16) uint8_t ring[];  // two rows of each group, weight and bias; at the end: the groups' sums
+  extern __shared__ __align__(16) uint8_t ring[];
   early_launch_wait();
   const int group = threadIdx.x / tpr, lane = threadIdx.x % tpr, warp0 = group * W;
-  const uint32_t mine = smem_addr(ring) + group * 2 * kStage;
-  const uint32_t w_at = smem_addr(ring) + kGroups * 2 * kStage + lane * 16, b_at = w_at + NQ * tpr * 16;
+  const uint32_t base = smem_addr(ring), mine = base + group * S::stages * S::stage;
+  const uint32_t w_at = base + S::w_at + lane * 16, b_at = w_at + S::w_bytes;
   const bool ragged = p.cols % 4 != 0;
+  const int cols = (int)p.cols;
   int count[NQ];  // columns of a quad
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int64_t c = (int64_t)(i * tpr + lane) * 4;
-    count[i] = i < kSure ? 4 : c < p.cols ? (int)min((int64_t)4, p.cols - c) : 0;
-  }
-  const int64_t row0 = (int64_t)blockIdx.x * kGroups + group, step = (int64_t)gridDim.x * kGroups;
-  const uint8_t* x_at = reinterpret_cast<const uint8_t*>(p.x) + row0 * p.x_ld * kXs + lane * 16;  // of the next row to be asked for
-  const uint8_t* dy_at = reinterpret_cast<const uint8_t*>(p.dy) + row0 * p.dy_ld * kOs + lane * 16;
-  uint8_t* y_at = reinterpret_cast<uint8_t*>(p.y) + (row0 * p.y_ld + lane * 4) * (BACK ? kXs : kOs);  // of the row that is computed
-  const int64_t x_step = step * p.x_ld * kXs, dy_step = step * p.dy_ld * kOs, y_step = step * p.y_ld * (BACK ? kXs : kOs);
-  int64_t left = row0 < p.rows ? (p.rows - row0 + step - 1) / step : 0, ask = left;  // rows of this group: to compute, to ask for
-  const int x_bytes = (int)p.cols * kXs - lane * 16, dy_bytes = (int)p.cols * kOs - lane * 16;  // of a row from this thread's first piece on
+  for (int i = 0; i < NQ; ++i) count[i] = i < S::sure ? 4 : max(0, min(4, cols - (i * tpr + lane) * 4));
+  const int64_t row0 = (int64_t)blockIdx.x * S::groups + group, step = (int64_t)gridDim.x * S::groups;
+  // of the row that is computed; the one that is asked for next is `ahead` rows of this group further on
+  const uint8_t* x_row = reinterpret_cast<const uint8_t*>(p.x) + row0 * p.x_ld * kXs;
+  const uint8_t* dy_row = BACK ? reinterpret_cast<const uint8_t*>(p.dy) + row0 * p.dy_ld * kOs : nullptr;
+  uint8_t* y_row = reinterpret_cast<uint8_t*>(p.y) + row0 * p.y_ld * kYs;
+  const int64_t x_step = step * p.x_ld * kXs, dy_step = BACK ? step * p.dy_ld * kOs : 0, y_step = step * p.y_ld * kYs;
+  int64_t left = row0 < p.rows ? (p.rows - row0 + step - 1) / step : 0;  // rows of this group
   auto meet = [&]() {
     if constexpr (W == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(tpr) : "memory");
   };
-  // zeros behind the rows' ends: nothing else is written there
-  for (int at = lane * 16; at < (int)(2 * kStage); at += tpr * 16) store16_shared(mine + at, make_uint4(0, 0, 0, 0));
-  meet();
-  auto fetch = [&](uint32_t to, const uint8_t* from, int bytes, auto pieces) {
+  if constexpr (ALIGNED) {  // zeros behind the rows' ends: nothing else is written there
+    for (int at = lane * 16; at < (int)(S::stages * S::stage); at += tpr * 16) store16_shared(mine + at, make_uint4(0, 0, 0, 0));
+    meet();
+  }
+  // the row at `row` into the pieces of 16 bytes from `to` on (from the piece that its first value is in)
+  auto fetch = [&](uint32_t to, const uint8_t* row, const void* lo, int size, auto pieces) {
+    const int head = ALIGNED ? 0 : (int)(reinterpret_cast<uintptr_t>(row) & 15), bytes = head + cols * size - lane * 16;
+    const uint8_t* from = row - head + lane * 16;
 #pragma unroll
     for (int k = 0; k < decltype(pieces)::value; ++k) {
       const int n = bytes - k * tpr * 16;
-      if (n >= 16) copy16(to + k * tpr * 16, from + k * tpr * 16);
-      else if (n > 0) copy_part(to + k * tpr * 16, from + k * tpr * 16, n);
+      const uint32_t at = to + (lane + k * tpr) * 16;
+      if (!ALIGNED && k == 0 && lane == 0 && from < static_cast<const uint8_t*>(lo)) {  // the array begins inside this piece
+        for (int e = head; e < 16 && e < n; e += size) {
+          if (size == 4) store_shared(at + e, *reinterpret_cast<const uint32_t*>(from + e));
+          else store_shared(at + e, *reinterpret_cast<const uint16_t*>(from + e));
+        }
+      } else if (n >= 16) {
+        copy16(at, from + k * tpr * 16);
+      } else if (n > 0) {
+        copy_part(at, from + k * tpr * 16, n);
+      }
     }
   };
-  auto request = [&](uint32_t to) {
-    if (ask > 0 && MFET_INSIDE(nullptr, p.cols <= p.x_ld && p.cols <= NQ * tpr * 4)) {
-      fetch(to + lane * 16, x_at, x_bytes, std::integral_constant<int, kXn>());
-      if constexpr (BACK) fetch(to + kXb + lane * 16, dy_at, dy_bytes, std::integral_constant<int, kOn>());
-      --ask;
-      x_at += x_step;
-      if constexpr (BACK) dy_at += dy_step;
+  auto request = [&](uint32_t to, bool any, int64_t ahead) {
+    if (any && MFET_INSIDE(nullptr, p.cols <= p.x_ld && p.cols <= NQ * tpr * 4)) {
+      fetch(to, x_row + ahead * x_step, p.x, kXs, std::integral_constant<int, S::x_pieces>());
+      if constexpr (BACK) fetch(to + S::x_bytes, dy_row + ahead * dy_step, p.dy, kOs, std::integral_constant<int, S::dy_pieces>());
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  request(mine);
+  request(mine, left > 0, 0);
   // weight and bias as a group's threads read them; every group writes the same values
+  auto param = [&](const float* v, float none, int i, float* a) {
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int64_t c = (int64_t)(i * tpr + lane) * 4;
-    float a[4], b[4];
+    for (int j = 0; j < 4; ++j) a[j] = j < count[i] ? (v ? __ldg(v + (i * tpr + lane) * 4 + j) : none) : 0.f;
+  };
+  if constexpr (W <= 8) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      a[j] = j < count[i] ? (p.w ? __ldg(p.w + c + j) : 1.f) : 0.f;
-      b[j] = j < count[i] && p.b ? __ldg(p.b + c + j) : 0.f;
+    for (int i = 0; i < NQ; ++i) {
+      float a[4];
+      param(p.w, 1.f, i, a);
+      store16_shared(w_at + i * tpr * 16, narrow16<MFET_F32>(a));
+      if constexpr (!BACK) {
+        param(p.b, 0.f, i, a);
+        store16_shared(b_at + i * tpr * 16, narrow16<MFET_F32>(a));
+      }
     }
-    store16_shared(w_at + i * tpr * 16, narrow16<MFET_F32>(a));
-    if constexpr (!BACK) store16_shared(b_at + i * tpr * 16, narrow16<MFET_F32>(b));
   }
+  auto weights = [&](uint32_t at, const float* from, float none, int i, float2* v) {
+    if constexpr (W <= 8) {
+      quad_in<MFET_F32, true>(at + i * tpr * 16, false, v);
+    } else {  // no room for them
+      float a[4];
+      param(from, none, i, a);
+      v[0] = make_float2(a[0], a[1]);
+      v[1] = make_float2(a[2], a[3]);
+    }
+  };
   float2 dw[BACK ? NQ : 1][2], db[BACK ? NQ : 1][2];
 #pragma unroll
   for (int i = 0; i < (BACK ? NQ : 0); ++i) dw[i][0] = dw[i][1] = db[i][0] = db[i][1] = both(0.f);
@@ -470,34 +401,35 @@ __global__ void __launch_bounds__((fast_threads<NQ, W, BACK>), fast_blocks<BACK>
     }
     return r;
   };
-  const float n = (float)p.cols, inv_n = 1.f / n;
-  uint32_t from = mine, to = mine + kStage;
+  const float n = (float)cols, inv_n = 1.f / n;
+  uint32_t from = mine, to = mine + (S::stages - 1) * S::stage;
   __syncthreads();  // the weights
   for (; left > 0; --left) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     meet();  // this row has arrived for all, and the last one is done with
-    request(to);
+    if constexpr (S::stages == 2) request(to, left > 1, 1);
+    const uint32_t x_head = ALIGNED ? 0 : (uint32_t)reinterpret_cast<uintptr_t>(x_row) & 15, dy_head = ALIGNED ? 0 : (uint32_t)reinterpret_cast<uintptr_t>(dy_row) & 15;
+    const uint32_t x_at = from + x_head + lane * 4 * kXs, dy_at = from + S::x_bytes + dy_head + lane * 4 * kOs;
+    const bool x_odd = x_head & 2, dy_odd = dy_head & 2;
     float2 v[NQ][2], s = both(0.f);
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-      quad_in<DT>(from + (i * tpr + lane) * 4 * kXs, v[i]);
+      quad_in<DT, ALIGNED>(x_at + i * tpr * 4 * kXs, x_odd, v[i]);
+      if (!ALIGNED && i >= S::sure) keep(v[i], count[i]);
       s = add2(s, add2(v[i][0], v[i][1]));
     }
     const float mu = over(joined(warp_sum(s.x + s.y), std::false_type()).x, n, inv_n);
     float2 s0 = both(0.f), s1 = both(0.f), s2 = both(0.f), t[2], w[2];
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-      const float2 minus = both(i < kSure || count[i] > 0 ? -mu : 0.f);
+      const float2 minus = both(i < S::sure || count[i] > 0 ? -mu : 0.f);
       v[i][0] = add2(v[i][0], minus);
       v[i][1] = add2(v[i][1], minus);
-      if (i >= kSure && ragged && count[i] > 0) {  // the row may end inside this quad
-        if (count[i] < 2) v[i][0].y = 0.f;
-        if (count[i] < 3) v[i][1].x = 0.f;
-        if (count[i] < 4) v[i][1].y = 0.f;
-      }
+      if (i >= S::sure && ragged) keep(v[i], count[i]);  // the row may end inside this quad
       if constexpr (BACK) {
-        quad_in<OT>(from + kXb + (i * tpr + lane) * 4 * kOs, t);
-        quad_in<MFET_F32>(w_at + i * tpr * 16, w);
+        quad_in<OT, ALIGNED>(dy_at + i * tpr * 4 * kOs, dy_odd, t);
+        if (!ALIGNED && i >= S::sure) keep(t, count[i]);
+        weights(w_at, p.w, 1.f, i, w);
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -526,14 +458,19 @@ __global__ void __launch_bounds__((fast_threads<NQ, W, BACK>), fast_blocks<BACK>
     }
     const float r = rsqrtf(fmaf(q.x, inv_n, p.eps));
     const float2 rr = both(r), rm0 = both(-r * (q.y * inv_n)), rm1 = both(-r * (q.z * inv_n * r));
-    constexpr int kType = BACK ? DT : OT;
-    typename Elem<kType>::T* const out = reinterpret_cast<typename Elem<kType>::T*>(y_at);
+    const uint32_t y_head = (uint32_t)reinterpret_cast<uintptr_t>(y_row) & 15;
+    // all have read this row's x by now: backward, the results take its place
+    const uint32_t stage = BACK ? from - base : S::out_at + group * S::out_bytes;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       float2 b[2], o[2];
-      quad_in<MFET_F32>(w_at + i * tpr * 16, w);
-      if constexpr (BACK) quad_in<OT>(from + kXb + (i * tpr + lane) * 4 * kOs, t);
-      else quad_in<MFET_F32>(b_at + i * tpr * 16, b);
+      weights(w_at, p.w, 1.f, i, w);
+      if constexpr (BACK) {
+        quad_in<OT, ALIGNED>(dy_at + i * tpr * 4 * kOs, dy_odd, t);
+        if (!ALIGNED && i >= S::sure) keep(t, count[i]);
+      } else {
+        weights(b_at, p.b, 0.f, i, b);
+      }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const float2 xh = mul2(v[i][j], rr);
@@ -545,18 +482,29 @@ __global__ void __launch_bounds__((fast_threads<NQ, W, BACK>), fast_blocks<BACK>
           o[j] = fma2(xh, w[j], b[j]);
         }
       }
-      if (MFET_INSIDE(nullptr, (int64_t)(i * tpr + lane) * 4 + count[i] <= p.y_ld || count[i] == 0)) quad_out<kType>(out + i * tpr * 4, o, i < kSure ? 4 : count[i]);
+      const int c = (i * tpr + lane) * 4, live = i < S::sure ? 4 : count[i];
+      if constexpr (!ALIGNED) quad_stage<kType>(base + stage + y_head + c * kYs, y_head & 2, o, live);
+      else if (MFET_INSIDE(nullptr, c + live <= p.y_ld || live == 0)) quad_out<kType>(reinterpret_cast<typename Elem<kType>::T*>(y_row) + c, o, live);
+    }
+    if constexpr (!ALIGNED) {
+      meet();
+      if (MFET_INSIDE(nullptr, p.cols <= p.y_ld)) row_out(y_row, ring + stage, y_head, (uint32_t)(cols * kYs), kYs, lane, tpr);
+    }
+    if constexpr (S::stages == 1) {
+      meet();
+      request(from, left > 1, 1);
     }
     const uint32_t next = to;
     to = from;
     from = next;
-    y_at += y_step;
+    x_row += x_step;
+    if constexpr (BACK) dy_row += dy_step;
+    y_row += y_step;
   }
   if constexpr (BACK) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
-    block_sums<NQ, 4, kGroups, tpr>(p, reinterpret_cast<float*>(ring), group, lane, [&](int i, int j) { return j & 1 ? dw[i][j >> 1].y : dw[i][j >> 1].x; },
-                                    [&](int i, int j) { return j & 1 ? db[i][j >> 1].y : db[i][j >> 1].x; });
+    block_sums<NQ, S::groups, tpr>(p, reinterpret_cast<float*>(ring), group, lane, dw, db);
   }
 }
 
@@ -638,7 +586,7 @@ struct SumParams {
   float *dw, *db;
   int64_t cols;
   uint32_t blocks;
-  int words, tpr, chunks, per;  // words of a block; how they belong to columns (chunks = 0: dw's columns, then db's)
+  int words, tpr, nq;  // words of a block; how they belong to columns (nq = 0: dw's columns, then db's)
 };
 __global__ void __launch_bounds__(32 * kSumWords) norm_sum_kernel(const __grid_constant__ SumParams p) {
   __shared__ float part[32][kSumWords + 1];
@@ -659,10 +607,10 @@ __global__ void __launch_bounds__(32 * kSumWords) norm_sum_kernel(const __grid_c
   if ((threadIdx.x & 31) == 0 && mine < p.words) {
     int64_t c = mine;
     bool bias;
-    if (p.chunks) {
-      const int e = (int)(mine / p.tpr), lane = (int)(mine - (int64_t)e * p.tpr), i = e / p.per % p.chunks;
-      bias = e / p.per >= p.chunks;
-      c = (int64_t)(i * p.tpr + lane) * p.per + e % p.per;
+    if (p.nq) {
+      const int e = (int)(mine / p.tpr), lane = (int)(mine - (int64_t)e * p.tpr), i = e / 4 % p.nq;
+      bias = e / 4 >= p.nq;
+      c = (int64_t)(i * p.tpr + lane) * 4 + e % 4;
     } else {
       bias = mine >= p.cols;
       c = bias ? mine - p.cols : mine;
@@ -682,108 +630,83 @@ bool bad_matrix(int64_t rows, int64_t cols, int64_t ld, uint32_t dtype) {
   return dtype > MFET_BF16 || rows < 0 || rows >= (1ll << 31) || cols < 1 || cols >= (1ll << 30) || ld < cols || ld >= (1ll << 31);
 }
 
-// How a row is spread over threads, and rows over blocks
-struct Split {
-  bool fast, held;          // which kernel
-  int chunks, per, tpr, groups;  // chunks a thread, columns of a chunk, threads of a row, rows of a block
-  int64_t at_once;          // blocks of the backward pass that the GPU holds
+// How a row is spread over threads: quads of each, warps of a row (0: the kernel for longer rows)
+struct Columns {
+  int nq, w;
 };
-Split split_of(int64_t cols, bool fast, bool back) {
-  Split s{};
-  s.held = cols <= kMostHeld;
-  s.fast = fast && cols <= kMostFast;
-  if (s.fast) {
-    s.tpr = cols <= 1024 ? 32 : cols <= 2048 ? 64 : cols <= 4096 ? 128 : 256;
-    s.per = 4;
-    s.chunks = s.tpr > 32 || cols > 896 ? 8 : cols > 512 ? 7 : cols > 256 ? 4 : cols > 128 ? 2 : 1;
-    s.groups = (!back || s.tpr == 256 ? 256 : s.chunks > 4 ? 384 : 512) / s.tpr;  // as fast_threads
-    s.at_once = sm_count();
-  } else {
-    s.per = kChunk;
-    s.chunks = cols > 256 ? 2 : 1;
-    const int64_t threads = (cols + kChunk * s.chunks - 1) / (kChunk * s.chunks);
-    s.tpr = s.held ? (int)((threads + 31) / 32 * 32) : kLongThreads;
-    s.groups = s.tpr > 128 ? 1 : 256 / s.tpr;
-    s.at_once = (int64_t)sm_count() * (s.tpr > 256 ? 1 : 2);
-  }
-  return s;
+Columns columns_of(int64_t cols, bool aligned_rows) {
+  if (cols > kMostHeld) return {0, 0};
+  if (cols > 1024) return {8, cols <= 2048 ? 2 : cols <= 4096 ? 4 : cols <= 8192 ? 8 : 16};
+  if (cols <= 128) return {1, 1};
+  if (cols <= 512) return {aligned_rows && cols <= 256 ? 2 : 4, 1};
+  return {aligned_rows && cols <= 896 ? 7 : 8, 1};
+}
+// rows of a block at a time, backward
+int groups_of(const Columns& c) { return c.w == 0 ? 1 : (c.w == 16 ? 512 : c.w == 8 ? 256 : c.nq > 4 ? 384 : 512) / (32 * c.w); }
+int64_t back_blocks(int64_t rows, const Columns& c) {
+  const int64_t want = (rows + groups_of(c) - 1) / groups_of(c), most = (int64_t)sm_count() * (c.w == 0 ? 2 : 1);
+  return want < most ? want : most;
 }
 // sums that a block of the backward pass leaves
-int64_t words_of(int64_t cols, const Split& s) { return s.held ? 2ll * s.chunks * s.per * s.tpr : 2 * cols; }
-int64_t blocks_of(int64_t rows, const Split& s) {
-  const int64_t want = (rows + s.groups - 1) / s.groups;
-  return want < s.at_once ? want : s.at_once;
-}
+int64_t words_of(int64_t cols, const Columns& c) { return c.w ? 8ll * c.nq * 32 * c.w : 2 * cols; }
 
-template <int DT, int OT, int NQ, int W, bool BACK>
-cudaError_t launch_fast(const NormParams& p, unsigned blocks, cudaStream_t s) {
-  constexpr int threads = fast_threads<NQ, W, BACK>;
-  constexpr uint32_t row = NQ * 4 * (uint32_t)(sizeof(typename Elem<DT>::T) + (BACK ? sizeof(typename Elem<OT>::T) : 0));  // of a thread
-  constexpr uint32_t ring = threads * 2 * row + 32 * W * NQ * 16 * (BACK ? 1 : 2), sums = BACK ? threads * 2 * NQ * 16 : 0;
-  constexpr uint32_t smem = ring > sums ? ring : sums;
+template <int DT, int OT, int NQ, int W, bool BACK, bool ALIGNED>
+cudaError_t launch_norm(const NormParams& p, cudaStream_t s) {
+  using S = NormShape<DT, OT, NQ, W, BACK, ALIGNED>;
   static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem(norm_fast_kernel<DT, OT, NQ, W, BACK>, smem, &ready);
-  return e != cudaSuccess ? e : launch_early(norm_fast_kernel<DT, OT, NQ, W, BACK>, blocks, threads, smem, s, p);
+  const cudaError_t e = allow_smem(norm_kernel<DT, OT, NQ, W, BACK, ALIGNED>, S::smem, &ready);
+  const int64_t want = (p.rows + S::groups - 1) / S::groups, most = (int64_t)sm_count() * S::per_sm;
+  return e != cudaSuccess ? e : launch_early(norm_kernel<DT, OT, NQ, W, BACK, ALIGNED>, (unsigned)(want < most ? want : most), S::threads, S::smem, s, p);
 }
 template <int DT, int OT, bool BACK>
-cudaError_t launch_fast(const NormParams& p, const Split& q, unsigned blocks, cudaStream_t s) {
-  switch (q.tpr + q.chunks) {
-    case 33: return launch_fast<DT, OT, 1, 1, BACK>(p, blocks, s);
-    case 34: return launch_fast<DT, OT, 2, 1, BACK>(p, blocks, s);
-    case 36: return launch_fast<DT, OT, 4, 1, BACK>(p, blocks, s);
-    case 39: return launch_fast<DT, OT, 7, 1, BACK>(p, blocks, s);
-    case 40: return launch_fast<DT, OT, 8, 1, BACK>(p, blocks, s);
-    case 72: return launch_fast<DT, OT, 8, 2, BACK>(p, blocks, s);
-    case 136: return launch_fast<DT, OT, 8, 4, BACK>(p, blocks, s);
-    default: return launch_fast<DT, OT, 8, 8, BACK>(p, blocks, s);
-  }
-}
-
-template <int DT, bool BACK>
-cudaError_t launch_held(const NormParams& p, const Split& q, cudaStream_t s) {
-  const unsigned threads = (unsigned)(q.tpr * q.groups);
-  int64_t blocks = blocks_of(p.rows, q);
-  if (!BACK && q.tpr <= 256) {  // no sums to join: as many blocks as fit
-    const int64_t want = (p.rows + q.groups - 1) / q.groups, most = (int64_t)sm_count() * (768 / threads);
-    blocks = want < most ? want : most;
-  }
-  if (q.fast) {
-    switch (BACK ? p.dy_dtype : p.y_dtype) {
-      case MFET_F32: return launch_fast<DT, MFET_F32, BACK>(p, q, (unsigned)blocks, s);
-      case MFET_F16: return launch_fast<DT, MFET_F16, BACK>(p, q, (unsigned)blocks, s);
-      default: return launch_fast<DT, MFET_BF16, BACK>(p, q, (unsigned)blocks, s);
+cudaError_t launch_types(const NormParams& p, bool aligned_rows, cudaStream_t s) {
+  const Columns c = columns_of(p.cols, aligned_rows);
+  if (aligned_rows) {
+    switch (c.w * 16 + c.nq) {
+      case 17: return launch_norm<DT, OT, 1, 1, BACK, true>(p, s);
+      case 18: return launch_norm<DT, OT, 2, 1, BACK, true>(p, s);
+      case 20: return launch_norm<DT, OT, 4, 1, BACK, true>(p, s);
+      case 23: return launch_norm<DT, OT, 7, 1, BACK, true>(p, s);
+      case 24: return launch_norm<DT, OT, 8, 1, BACK, true>(p, s);
+      case 40: return launch_norm<DT, OT, 8, 2, BACK, true>(p, s);
+      case 72: return launch_norm<DT, OT, 8, 4, BACK, true>(p, s);
+      case 136: return launch_norm<DT, OT, 8, 8, BACK, true>(p, s);
+      default: return launch_norm<DT, OT, 8, 16, BACK, true>(p, s);
     }
   }
-  size_t stage = p.y_vec ? 0 : (size_t)p.stage_bytes * q.groups;
-  if (BACK && q.groups > 1 && stage < (size_t)threads * 2 * kChunk * q.chunks * 4) stage = (size_t)threads * 2 * kChunk * q.chunks * 4;
-  auto go = [&](auto kernel) { return launch_early(kernel, (unsigned)blocks, threads, stage, s, p); };
-  if (q.chunks == 1) return go(norm_kernel<DT, 1, BACK, 256>);
-  if (threads <= 256) return go(norm_kernel<DT, 2, BACK, 256>);
-  if (threads <= 512) return go(norm_kernel<DT, 2, BACK, 512>);  // 32 KB of shared memory at most
-  static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem(norm_kernel<DT, 2, BACK, 1024>, 4 * (uint32_t)kMostHeld + 32, &ready);
-  return e != cudaSuccess ? e : go(norm_kernel<DT, 2, BACK, 1024>);
+  switch (c.w * 16 + c.nq) {
+    case 17: return launch_norm<DT, OT, 1, 1, BACK, false>(p, s);
+    case 20: return launch_norm<DT, OT, 4, 1, BACK, false>(p, s);
+    case 24: return launch_norm<DT, OT, 8, 1, BACK, false>(p, s);
+    case 40: return launch_norm<DT, OT, 8, 2, BACK, false>(p, s);
+    case 72: return launch_norm<DT, OT, 8, 4, BACK, false>(p, s);
+    case 136: return launch_norm<DT, OT, 8, 8, BACK, false>(p, s);
+    default: return launch_norm<DT, OT, 8, 16, BACK, false>(p, s);
+  }
 }
-template <int DT>
-cudaError_t launch_dt(const NormParams& p, const Split& q, bool back, cudaStream_t s) {
-  return back ? launch_held<DT, true>(p, q, s) : launch_held<DT, false>(p, q, s);
+template <int DT, bool BACK>
+cudaError_t launch_dt(const NormParams& p, bool aligned_rows, cudaStream_t s) {
+  switch (BACK ? p.dy_dtype : p.y_dtype) {
+    case MFET_F32: return launch_types<DT, MFET_F32, BACK>(p, aligned_rows, s);
+    case MFET_F16: return launch_types<DT, MFET_F16, BACK>(p, aligned_rows, s);
+    default: return launch_types<DT, MFET_BF16, BACK>(p, aligned_rows, s);
+  }
 }
-Split how(const NormParams& p, bool back) {
-  return split_of(p.cols, p.x_vec && p.y_vec && (!back || p.dy_vec), back);
-}
-cudaError_t launch(NormParams& p, uint32_t x_dtype, bool back, cudaStream_t s) {
-  const Split q = how(p, back);
-  p.tpr = q.tpr;
-  p.groups = q.groups;
-  p.stage_bytes = (int)((p.cols * (back ? size_of(x_dtype) : size_of(p.y_dtype)) + 31) / 16 * 16);
+bool all_aligned(const NormParams& p) { return p.x_vec && p.y_vec && (!p.dy || p.dy_vec); }
+template <bool BACK>
+cudaError_t launch(NormParams& p, uint32_t x_dtype, cudaStream_t s) {
   p.w_vec = aligned(p.w, 16);
   p.b_vec = aligned(p.b, 16);
-  if (p.cols > kMostHeld)
-    return launch_early(back ? norm_long_kernel<true> : norm_long_kernel<false>, (unsigned)blocks_of(p.rows, q), kLongThreads, 0, s, p, x_dtype);
+  if (p.cols > kMostHeld) {
+    const int64_t most = (int64_t)sm_count() * 4;
+    const int64_t blocks = BACK ? back_blocks(p.rows, columns_of(p.cols, false)) : p.rows < most ? p.rows : most;
+    return launch_early(norm_long_kernel<BACK>, (unsigned)blocks, kLongThreads, 0, s, p, x_dtype);
+  }
+  const bool a = all_aligned(p);
   switch (x_dtype) {
-    case MFET_F32: return launch_dt<MFET_F32>(p, q, back, s);
-    case MFET_F16: return launch_dt<MFET_F16>(p, q, back, s);
-    default: return launch_dt<MFET_BF16>(p, q, back, s);
+    case MFET_F32: return launch_dt<MFET_F32, BACK>(p, a, s);
+    case MFET_F16: return launch_dt<MFET_F16, BACK>(p, a, s);
+    default: return launch_dt<MFET_BF16, BACK>(p, a, s);
   }
 }
 
@@ -812,15 +735,15 @@ int mfet_layer_norm(const void* x, uint32_t x_dtype, int64_t x_ld, int64_t rows,
   p.y_dtype = y_dtype;
   p.x_vec = on_16(x, x_ld, x_dtype);
   p.y_vec = on_16(y, y_ld, y_dtype);
-  return launch(p, x_dtype, false, (cudaStream_t)stream) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+  return launch<false>(p, x_dtype, (cudaStream_t)stream) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
 }
 
 uint64_t mfet_layer_norm_backward_bytes(int64_t rows, int64_t cols) {
   if (bad_matrix(rows, cols, cols, MFET_F32)) return 0;
   uint64_t most = 0;  // over the alignments that a call may have
-  for (int fast = 0; fast < 2; ++fast) {
-    const Split s = split_of(cols, fast, true);
-    const uint64_t b = (uint64_t)blocks_of(rows, s) * words_of(cols, s) * 4;
+  for (int a = 0; a < 2; ++a) {
+    const Columns c = columns_of(cols, a);
+    const uint64_t b = (uint64_t)back_blocks(rows, c) * words_of(cols, c) * 4;
     most = b > most ? b : most;
   }
   return most;
@@ -860,11 +783,11 @@ int mfet_layer_norm_backward(const void* x, uint32_t x_dtype, int64_t x_ld, int6
   p.x_vec = on_16(x, x_ld, x_dtype);
   p.y_vec = on_16(dx, dx_ld, x_dtype);
   p.dy_vec = on_16(dy, dy_ld, dy_dtype);
-  if (launch(p, x_dtype, true, (cudaStream_t)stream) != cudaSuccess) return MFET_ERR_CUDA;
+  if (launch<true>(p, x_dtype, (cudaStream_t)stream) != cudaSuccess) return MFET_ERR_CUDA;
   if (!sums) return MFET_OK;
-  const Split done = how(p, true);
-  const int64_t words = words_of(cols, done);
-  const SumParams q{(const float*)scratch, dweight, dbias, cols, (uint32_t)blocks_of(rows, done), (int)words, done.tpr, done.held ? done.chunks : 0, done.per};
+  const Columns c = columns_of(cols, all_aligned(p));
+  const int64_t words = words_of(cols, c);
+  const SumParams q{(const float*)scratch, dweight, dbias, cols, (uint32_t)back_blocks(rows, c), (int)words, 32 * c.w, c.nq};
   return launch_early(norm_sum_kernel, (unsigned)((words + kSumWords - 1) / kSumWords), 32 * kSumWords, 0, (cudaStream_t)stream, q) == cudaSuccess
              ? MFET_OK
              : MFET_ERR_CUDA;
