@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   if (clustered) cluster_sync();  // the barriers of the other blocks exist, and so do the blocks
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  early_launch_wait();
 
   const uint32_t members = CTAS * p.split;
   const uint32_t first = blockIdx.x / members, step = gridDim.x / members;
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
         const int32_t row = (int32_t)((w.tm * CTAS + half) * 128);
         uint32_t seg = k0 / p.kb, kk = k0 - seg * p.kb;
         for (uint32_t i = k0; i < k1; ++i) {
-          if (!(ok = bar_wait(empty(st), phase, &dead))) break;
+          if (!(ok = bar_sleep(empty(st), phase, &dead))) break;
           // tiles and blocks of k outside their matrix read as 0
           if (!MFET_INSIDE(p.status, seg < 3 && w.z < 2 && (int64_t)row < p.m + 128 && w.tn < p.n_tiles)) {
             ok = false;
@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       const uint32_t from = tmem + acc * TN + ((uint32_t)(quarter * 32) << 16);
       float x[32];
       if (p.split == 1) other(x, i0 + lane, j0 + 32 * second);  // under way while the tile is computed
-      const bool ok = bar_wait(acc_full(acc), (done / 2) & 1, &dead);
+      const bool ok = bar_sleep(acc_full(acc), (done / 2) & 1, &dead);
       if (!__all_sync(kAllLanes, ok)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (p.split > 1) {  // one tile per block: its sums go to shared memory, where the ring was

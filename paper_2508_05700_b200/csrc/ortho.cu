@@ -43,14 +43,24 @@ __device__ __forceinline__ void eight(const LoadParams& p, int64_t row, int64_t 
   else widen_raw<DT, 8>(load_shifted<DT, 8>(at, count, p.g, p.end), v);
 }
 
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double s, double* words) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(kAllLanes, s, d);
   if ((threadIdx.x & 31) == 0) words[threadIdx.x >> 5] = s;
   __syncthreads();
   s = 0.0;
-  for (int i = 0; i < kSumThreads / 32; ++i) s += words[i];
+  for (int i = 0; i < THREADS / 32; ++i) s += words[i];
   return s;
+}
+
+// what G is multiplied by, from its sum of squares: 0 for 0, NaN if G has a value that is not finite
+__device__ __forceinline__ double factor_of(double squares, double scale) {
+  return squares > 0.0 ? (isinf(squares) ? NAN : scale / sqrt(squares)) : (squares == 0.0 ? 0.0 : squares);
+}
+__device__ __forceinline__ void cluster_or_block_sync(bool cluster) {
+  __syncthreads();
+  if (cluster) cluster_sync();
 }
 
 // squares in fp64: no overflow, whatever the scale of the gradients
@@ -67,7 +77,7 @@ __global__ void __launch_bounds__(kSumThreads) squares_kernel(const __grid_const
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = fma((double)v[j], (double)v[j], s);
   }
-  s = block_sum(s, words);
+  s = block_sum<kSumThreads>(s, words);
   if (threadIdx.x == 0 && MFET_INSIDE(nullptr, blockIdx.x < p.n_parts)) p.parts[blockIdx.x] = s;
 }
 
@@ -78,8 +88,8 @@ __global__ void __launch_bounds__(kSumThreads) scale_kernel(const __grid_constan
   early_launch_wait();
   double total = 0.0;
   for (uint32_t i = threadIdx.x; i < p.n_parts; i += kSumThreads) total += p.parts[i];
-  total = block_sum(total, words);
-  const double f = total > 0.0 ? (isinf(total) ? NAN : p.scale / sqrt(total)) : (total == 0.0 ? 0.0 : total);
+  total = block_sum<kSumThreads>(total, words);
+  const double f = factor_of(total, p.scale);
   const int64_t per_row = p.x_ld / 8, units = p.rows * per_row;
   for (int64_t u = (int64_t)blockIdx.x * kSumThreads + threadIdx.x; u < units; u += (int64_t)gridDim.x * kSumThreads) {
     const int64_t row = u / per_row, c = (u - row * per_row) * 8;
@@ -94,6 +104,353 @@ __global__ void __launch_bounds__(kSumThreads) scale_kernel(const __grid_constan
     *reinterpret_cast<uint4*>(p.hi + row * p.x_ld + c) = narrow16<MFET_F16>(v);
     *reinterpret_cast<uint4*>(p.lo + row * p.x_ld + c) = narrow16<MFET_F16>(lo);
   }
+}
+
+// ------------------------------------------------------------------ a short side of at most 128 ----
+
+// All of the call in one launch: the long side in slices of up to 256 columns (of X with the short side as its rows), one per block of a
+// cluster. A block has its slice of X in shared memory, in two words and in the order of the tensor cores: rows of 64 columns, 128 bytes with
+// the 128-byte swizzle, are K-major for X X^T and, the other way round, MN-major for B X. A step: the slice's X X^T, summed over the cluster
+// (each block adds up a share of the columns in the order of the slices and hands it to all), B by every block for itself, and the slice of
+// a X + B X over the old one. What costs is the chain: three products, each waited for, and three turns from tensor memory to shared memory.
+// 48 x 192: 25 us, 97 as seventeen launches.
+constexpr int kSmallThreads = 512;
+constexpr int kSmallSide = 128, kSlice = 256, kMostSlices = 8;
+constexpr uint32_t kBlock = 128 * 128;                    // 128 rows x 64 columns
+constexpr uint32_t kXLo = kSlice / 64 * kBlock, kAHi = 2 * kXLo, kALo = kAHi + 2 * kBlock, kSmallBytes = kALo + 2 * kBlock;
+constexpr uint32_t kSmallSmem = kSmallBytes + 1024;
+static_assert(kALo - kAHi == 32768 && 2 * (kALo - kAHi) == 128 * 128 * 4, "partial sums in fp32 take the place of A");
+
+struct SmallStep {
+  float a_beta, b_alpha, b_beta, x_alpha, x_beta;
+};
+struct SmallParams {
+  const uint8_t* g;
+  void* out;
+  int64_t ld, out_ld;
+  int64_t long_side;
+  int32_t d, slices, steps;
+  uint32_t tall;       // the short side is the columns of g
+  bool vec;            // rows of g start on 16-byte boundaries
+  const void* end;     // of g
+  uint32_t out_dtype;
+  uint32_t* status;
+  double scale;        // 2^e of X's words
+  SmallStep step[kMostSteps];
+};
+
+// where 8 columns from c on of row r are in a matrix of blocks
+__device__ __forceinline__ uint32_t words_offset(int r, int c) { return (uint32_t)(c >> 6) * kBlock + r * 128 + ((((c >> 3) & 7) ^ (r & 7)) << 4); }
+
+// X[i][c .. c + 8) before it is scaled, 0 behind its end; false: all of it is behind
+template <int DT>
+__device__ __forceinline__ bool eight_of(const SmallParams& p, int i, int64_t c, float* v) {
+  using T = typename Elem<DT>::T;
+  const int64_t left = p.long_side - c;
+  if (i >= p.d || left <= 0) return false;
+  const int count = left < 8 ? (int)left : 8;
+  const T* g = reinterpret_cast<const T*>(p.g);
+  if (!MFET_INSIDE(p.status, (p.tall ? i + 1 : c + count) <= p.ld)) return false;
+  if (p.tall) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < count ? to_float<DT>(g[(c + j) * p.ld + i]) : 0.f;
+  } else if (p.vec) {
+    widen_raw<DT, 8>(load_raw<DT, 8, true>(g + i * p.ld + c, count), v);
+  } else {
+    widen_raw<DT, 8>(load_shifted<DT, 8>(g + i * p.ld + c, count, p.g, p.end), v);
+  }
+  return true;
+}
+
+__device__ __forceinline__ void put_words(uint8_t* hi, uint8_t* lo, float* v) {  // 8 values, 16 bytes each
+  float r[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = v[j] - __half2float(__float2half_rn(v[j]));
+  *reinterpret_cast<uint4*>(hi) = narrow16<MFET_F16>(v);
+  *reinterpret_cast<uint4*>(lo) = narrow16<MFET_F16>(r);
+}
+__device__ __forceinline__ void get_words(const uint8_t* hi, const uint8_t* lo, float* v) {
+  float r[8];
+  widen16<MFET_F16>(*reinterpret_cast<const uint4*>(hi), v);
+  widen16<MFET_F16>(*reinterpret_cast<const uint4*>(lo), r);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] += r[j];
+}
+__device__ __forceinline__ void peer_store8(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void mma_small(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t b_hi, uint32_t inst, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+               "setp.ne.b32 p, %5, 0;\n\t"
+               "mov.b64 a, {%1, %6};\n\t"
+               "mov.b64 b, {%2, %3};\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d),
+               "r"(a_lo), "r"(b_lo), "r"(b_hi), "r"(inst), "r"(add), "n"(kDescHi)
+               : "memory");
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __grid_constant__ SmallParams p) {
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ __align__(8) uint64_t bar_word;
+  __shared__ double sums[kSmallThreads / 32];
+  __shared__ double total_of_block;
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int dead;
+  const uint32_t base = (smem_addr(raw_smem) + 1023) & ~1023u;
+  uint8_t* const smem = raw_smem + (base - smem_addr(raw_smem));
+  const uint32_t bar = smem_addr(&bar_word);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int slices = p.slices;
+  const uint32_t rank = slices > 1 ? cluster_rank() : 0u;
+  if (tid == 0) {
+    bar_init(bar, 1);
+    dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot, acc_x = tmem + 128;
+  early_launch_wait();
+
+  // this block's columns of X, in whole blocks of 64
+  const int64_t all = (p.long_side + 63) / 64;
+  const int64_t c0 = all * rank / slices * 64;
+  const int width = (int)((all * (rank + 1) / slices) * 64 - c0);
+  const int d16 = (p.d + 15) & ~15;
+
+  // squares of the slice, then of all of G; 8 neighbouring columns of a row at a time
+  double s = 0.0;
+  const int units = 128 * (width / 8);
+  const uint32_t per = (uint32_t)width / 8;
+  auto place = [&](int u, int* i, int* c) {
+    *i = p.tall ? u & 127 : (int)((uint32_t)u / per);
+    *c = (p.tall ? u >> 7 : u - *i * (int)per) * 8;
+  };
+  for (int u = tid; u < units; u += kSmallThreads) {
+    int i, c;
+    place(u, &i, &c);
+    float v[8];
+    if (!eight_of<DT>(p, i, c0 + c, v)) continue;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fma((double)v[j], (double)v[j], s);
+  }
+  s = block_sum<kSmallThreads>(s, sums);
+  if (slices > 1) {
+    if (tid == 0) total_of_block = s;
+    __syncthreads();
+    cluster_sync();
+    s = 0.0;
+    for (int q = 0; q < slices; ++q) {
+      double v;
+      asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(peer_addr(smem_addr(&total_of_block), q)) : "memory");
+      s += v;
+    }
+  }
+  const double f = factor_of(s, p.scale);
+  for (int u = tid; u < units; u += kSmallThreads) {
+    int i, c;
+    place(u, &i, &c);
+    float v[8];
+    const bool any = eight_of<DT>(p, i, c0 + c, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = any && c0 + c + j < p.long_side ? (float)(v[j] * f) : 0.f;
+    const uint32_t at = words_offset(i, c);
+    put_words(smem + at, smem + kXLo + at, v);
+  }
+
+  uint32_t phase = 0;
+  auto ready = [&]() {  // what this block's threads have written is there for the tensor cores
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  };
+  auto done = [&]() {  // the products that one lane has issued
+    bar_wait(bar, phase, &dead);
+    phase ^= 1;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  };
+  const uint32_t inst_a = (1u << 4) | ((uint32_t)(d16 >> 3) << 17) | (8u << 24);
+  const uint32_t inst_x = (1u << 4) | (1u << 16) | ((uint32_t)(width >> 3) << 17) | (8u << 24);
+  const uint32_t xs[2] = {base, base + kXLo}, as[2] = {base + kAHi, base + kALo};
+  const int quarter = warp & 3, row = quarter * 32 + lane, turn = warp >> 2;  // four warps share the lanes of tensor memory
+  const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+  cluster_or_block_sync(slices > 1);
+
+#pragma unroll 1
+  for (int step = 0; step < p.steps; ++step) {
+    const SmallStep k = p.step[step];
+    ready();
+    // A = X X^T over the slice
+    if (warp == 0) {
+      if (elect_one()) {
+        uint32_t any = 0;
+        for (int t = 0; t < 3; ++t) {  // high x high, high x low, low x high
+          const uint32_t a = xs[t == 2], b = xs[t == 1];
+          for (int q = 0; q < width / 16; ++q, any = 1) {
+            const uint32_t off = (uint32_t)(q >> 2) * kBlock + (q & 3) * 32;
+            mma_small(tmem, desc_lo(a + off, 0), desc_lo(b + off, 0), kDescHi, inst_a, any);
+          }
+        }
+        mma_commit(bar);
+      }
+      __syncwarp();
+    }
+    done();
+    if (slices == 1) {
+#pragma unroll 1
+      for (int c = 32 * turn; c < d16; c += 128) {
+        uint32_t r[32];
+        tmem_load32(tmem + lanes + c, r);
+        float* v = reinterpret_cast<float*>(r);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] *= k.a_beta;
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+          const uint32_t at = words_offset(row, c + j);
+          put_words(smem + kAHi + at, smem + kALo + at, v + j);
+        }
+      }
+    } else {
+      // the slice's sums, four columns of a row in 16 bytes, where A was
+#pragma unroll 1
+      for (int c = 32 * turn; c < d16; c += 128) {
+        uint32_t r[32];
+        tmem_load32(tmem + lanes + c, r);
+#pragma unroll
+        for (int j = 0; j < 32; j += 4)
+          *reinterpret_cast<uint4*>(smem + kAHi + (((c + j) >> 2) * 128 + row) * 16) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
+      }
+      cluster_sync();
+      // every block adds up each `slices`-th group of columns, four warps of a row in turn
+      constexpr int kMostGroups = 4;  // 32 groups, two blocks at least and four warps
+      float v[kMostGroups][4];
+#pragma unroll
+      for (int q = 0; q < kMostGroups; ++q) {
+        const int group = (int)rank + slices * (4 * q + turn);
+        if (group * 4 >= d16) break;
+        const uint32_t at = base + kAHi + (group * 128 + row) * 16;
+        peer_load(peer_addr(at, 0), v[q]);
+        for (int z = 1; z < slices; ++z) {
+          float t[4];
+          peer_load(peer_addr(at, z), t);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[q][j] += t[j];
+        }
+      }
+      cluster_sync();  // all sums have been read: A goes to their place, in all blocks
+#pragma unroll
+      for (int q = 0; q < kMostGroups; ++q) {
+        const int group = (int)rank + slices * (4 * q + turn), c = group * 4;
+        if (c >= d16) break;
+        float lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[q][j] *= k.a_beta;
+          lo[j] = v[q][j] - __half2float(__float2half_rn(v[q][j]));
+        }
+        const uint32_t at = words_offset(row, c) + (c & 4) * 2;
+        const uint32_t h0 = Elem<MFET_F16>::pack(v[q][0], v[q][1]), h1 = Elem<MFET_F16>::pack(v[q][2], v[q][3]);
+        const uint32_t l0 = Elem<MFET_F16>::pack(lo[0], lo[1]), l1 = Elem<MFET_F16>::pack(lo[2], lo[3]);
+        for (int z = 0; z < slices; ++z) {
+          const uint32_t to = peer_addr(base + at, z);
+          peer_store8(to + kAHi, h0, h1);
+          peer_store8(to + kALo, l0, l1);
+        }
+      }
+      asm volatile("fence.proxy.async;" ::: "memory");
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      cluster_sync();
+    }
+    ready();
+    // A A, A being symmetric
+    if (warp == 0) {
+      if (elect_one()) {
+        uint32_t any = 0;
+        for (int t = 0; t < 3; ++t) {
+          const uint32_t a = as[t == 2], b = as[t == 1];
+          for (int q = 0; q < d16 / 16; ++q, any = 1) {
+            const uint32_t off = (uint32_t)(q >> 2) * kBlock + (q & 3) * 32;
+            mma_small(tmem, desc_lo(a + off, 0), desc_lo(b + off, 0), kDescHi, inst_a, any);
+          }
+        }
+        mma_commit(bar);
+      }
+      __syncwarp();
+    }
+    done();
+    // B = b A + c A A over A
+#pragma unroll 1
+    for (int c = 32 * turn; c < d16; c += 128) {
+      uint32_t r[32];
+      tmem_load32(tmem + lanes + c, r);
+#pragma unroll
+      for (int j = 0; j < 32; j += 8) {
+        if (c + j >= d16) break;
+        const uint32_t at = words_offset(row, c + j);
+        float a[8];
+        get_words(smem + kAHi + at, smem + kALo + at, a);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = fmaf(__uint_as_float(r[j + e]), k.b_beta, a[e] * k.b_alpha);
+        put_words(smem + kAHi + at, smem + kALo + at, a);
+      }
+    }
+    ready();
+    // B X
+    if (warp == 0) {
+      if (elect_one()) {
+        uint32_t any = 0;
+        for (int t = 0; t < 3; ++t) {
+          const uint32_t a = as[t == 2], b = xs[t == 1];
+          for (int q = 0; q < d16 / 16; ++q, any = 1) {
+            const uint32_t b_lo = (((b + q * 2048) & 0x3FFFFu) >> 4) | ((kBlock >> 4) << 16);
+            mma_small(acc_x, desc_lo(a + (uint32_t)(q >> 2) * kBlock + (q & 3) * 32, 0), b_lo, kDescHi, inst_x, any);
+          }
+        }
+        mma_commit(bar);
+      }
+      __syncwarp();
+    }
+    done();
+    const bool last = step + 1 == p.steps;
+#pragma unroll 1
+    for (int c = 32 * turn; c < width; c += 128) {
+      uint32_t r[32];
+      tmem_load32(acc_x + lanes + c, r);
+#pragma unroll
+      for (int j = 0; j < 32; j += 8) {
+        const uint32_t at = words_offset(row, c + j);
+        float x[8];
+        get_words(smem + at, smem + kXLo + at, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(__uint_as_float(r[j + e]), k.x_beta, x[e] * k.x_alpha);
+        if (!last) {
+          put_words(smem + at, smem + kXLo + at, x);
+        } else if (row < p.d) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int64_t col = c0 + c + j + e, to = p.tall ? col * p.out_ld + row : row * p.out_ld + col;
+            if (col >= p.long_side || !MFET_INSIDE(p.status, (p.tall ? row : col) < p.out_ld)) continue;
+            if (p.out_dtype == MFET_F32) reinterpret_cast<float*>(p.out)[to] = x[e];
+            else if (p.out_dtype == MFET_F16) reinterpret_cast<__half*>(p.out)[to] = __float2half_rn(x[e]);
+            else reinterpret_cast<__nv_bfloat16*>(p.out)[to] = __float2bfloat16_rn(x[e]);
+          }
+        }
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  cluster_or_block_sync(slices > 1);
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (tid == 0 && dead && p.status) atomicOr(p.status, (uint32_t)MFET_DEV_STALLED);
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 // ------------------------------------------------------------------ host side ----
@@ -144,6 +501,26 @@ double bound_of(double c0, double c1, double c2, double s) {
 }
 
 constexpr float kUsual[3] = {3.4445f, -4.775f, 2.0315f};
+
+template <int DT>
+int launch_small(const SmallParams& p, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  if (allow_smem(ortho_small_kernel<DT>, kSmallSmem, &ready) != cudaSuccess) return MFET_ERR_CUDA;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)p.slices;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)p.slices);
+  cfg.blockDim = dim3(kSmallThreads);
+  cfg.dynamicSmemBytes = kSmallSmem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.slices > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, ortho_small_kernel<DT>, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+}
 
 template <int DT>
 cudaError_t load(const LoadParams& p, unsigned blocks, cudaStream_t s) {
@@ -213,7 +590,37 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
   if (!scratch || scratch_bytes < mfet_orthogonalize_bytes(rows, cols)) return MFET_ERR_WORKSPACE;
   if (!aligned(scratch, 16)) return MFET_ERR_ALIGNMENT;
   const cudaStream_t st = (cudaStream_t)stream;
-  const int64_t d = rows < cols ? rows : cols;
+  const int64_t d = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
+  const bool tall = rows > cols;
+  if (d <= kSmallSide && l <= kSlice * kMostSlices) {
+    SmallParams q{};
+    q.g = (const uint8_t*)g;
+    q.out = out;
+    q.ld = ld, q.out_ld = out_ld;
+    q.long_side = l;
+    q.d = (int32_t)d;
+    q.slices = l <= kSlice ? 1 : l <= 2 * kSlice ? 2 : l <= 4 * kSlice ? 4 : 8;
+    q.steps = steps;
+    q.tall = tall;
+    q.vec = aligned(g, 16) && (uint64_t)ld * size_of(dtype) % 16 == 0;
+    q.end = (const uint8_t*)g + ((rows - 1) * ld + cols) * size_of(dtype);
+    q.out_dtype = out_dtype;
+    q.status = status;
+    int ex = exponent_for(s[0]);
+    q.scale = std::ldexp(1.0, ex);
+    for (int i = 0; i < steps; ++i) {
+      const float* c = coefficients ? coefficients + 3 * i : kUsual;
+      const int ea = exponent_for(s[i] * s[i]), eb = exponent_for(b_most[i]), next = exponent_for(s[i + 1]);
+      const bool last = i + 1 == steps;
+      q.step[i].a_beta = (float)std::ldexp(1.0, ea - 2 * ex);
+      q.step[i].b_alpha = (float)std::ldexp((double)c[1], eb - ea);
+      q.step[i].b_beta = (float)std::ldexp((double)c[2], eb - 2 * ea);
+      q.step[i].x_alpha = (float)std::ldexp(last ? (double)c[0] * scale : (double)c[0], (last ? 0 : next) - ex);
+      q.step[i].x_beta = (float)std::ldexp(last ? (double)scale : 1.0, (last ? 0 : next) - eb - ex);
+      ex = next;
+    }
+    return dtype == MFET_F32 ? launch_small<MFET_F32>(q, st) : dtype == MFET_F16 ? launch_small<MFET_F16>(q, st) : launch_small<MFET_BF16>(q, st);
+  }
   uint8_t* to = (uint8_t*)scratch + kMostParts * 8;
   Words x[2] = {words_at(&to, rows, cols), words_at(&to, rows, cols)};
   Words a = words_at(&to, d, d), b = words_at(&to, d, d);
@@ -237,7 +644,6 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
                                             : load<MFET_BF16>(p, blocks, st);
   if (e != cudaSuccess) return MFET_ERR_CUDA;
 
-  const bool tall = rows > cols;
   for (int i = 0; i < steps; ++i) {
     const float* c = coefficients ? coefficients + 3 * i : kUsual;
     const Words& from = x[i & 1];

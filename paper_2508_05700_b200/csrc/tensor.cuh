@@ -65,6 +65,31 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   }
 }
 
+// The same for a role that may be late by a microsecond: its warp sleeps on the barrier instead of polling it, and what it does not issue is
+// power that the tensor cores' clock gets.
+__device__ __forceinline__ bool bar_sleep(uint32_t bar, uint32_t parity, volatile int* dead) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 1;; ++i) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    if (ok) return true;
+    if ((i & 0xFF) == 0) {
+      if (*dead) return false;
+      const uint64_t t = now_ns();
+      if (t0 == 0) t0 = t;
+      if (t - t0 > kStallNs) {
+        *dead = 1;
+        return false;
+      }
+    }
+  }
+}
+
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(bar)
