@@ -160,44 +160,66 @@ __device__ __forceinline__ void commit(uint32_t bar, uint32_t mask) {
 // erfc(z), called: 32 copies of it in a row would not fit the instruction cache
 static __device__ __noinline__ float erfc_of(float z) { return erfcf(z); }
 
-// act(g), and its derivative. The exponential's error (2^-17 at the ends of its range, 2^-21 in the middle) is far below a 16-bit result's.
+// 1 / (1 + e^-g): two instructions of the special functions, whose results are off by 2^-22; e^-g beyond fp32 gives 0
+__device__ __forceinline__ float2 sigmoid2(float2 g) {
+  const float2 t = mul2(g, both(-1.4426950408889634f));
+  float2 e, s;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(t.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(t.y));
+  e = add2(e, both(1.f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(e.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(e.y));
+  return s;
+}
+
+// act(g) of two gates, and its derivative. What the functions are off by (2^-17 where e^-g is large, 2^-21 in the middle) is far below
+// a 16-bit result's rounding.
 template <int ACT, bool SLOPE>
-__device__ __forceinline__ float gate(float g, float* slope) {
+__device__ __forceinline__ float2 gate2(float2 g, float2* slope) {
   if constexpr (ACT == MFET_ACT_RELU) {
-    float r = g;
-    asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(r));
-    if (SLOPE) *slope = g > 0.f ? 1.f : 0.f;
+    float2 r = g;
+    asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(r.x));
+    asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(r.y));
+    if (SLOPE) *slope = make_float2(g.x > 0.f ? 1.f : 0.f, g.y > 0.f ? 1.f : 0.f);
     return r;
   } else if constexpr (ACT == MFET_ACT_SILU) {
-    const float s = __fdividef(1.f, 1.f + __expf(-g));
-    if (SLOPE) *slope = s * (1.f + g * (1.f - s));
-    return g * s;
+    const float2 s = sigmoid2(g);
+    if (SLOPE) *slope = mul2(s, fma2(g, fma2(s, both(-1.f), both(1.f)), both(1.f)));
+    return mul2(g, s);
   } else if constexpr (ACT == MFET_ACT_SIGMOID) {
-    const float s = __fdividef(1.f, 1.f + __expf(-g));
-    if (SLOPE) *slope = s * (1.f - s);
+    const float2 s = sigmoid2(g);
+    if (SLOPE) *slope = mul2(s, fma2(s, both(-1.f), both(1.f)));
     return s;
   } else if constexpr (ACT == MFET_ACT_GELU) {
-    const float c = 0.5f * erfc_of(g * -0.70710678118654752f);  // no cancellation for negative g
-    if (SLOPE) *slope = c + g * 0.3989422804014327f * __expf(-0.5f * g * g);
-    return g * c;
+    const float2 z = mul2(g, both(-0.70710678118654752f));
+    const float2 c = mul2(make_float2(erfc_of(z.x), erfc_of(z.y)), both(0.5f));  // no cancellation for negative g
+    if (SLOPE) {
+      const float2 d = make_float2(__expf(-0.5f * g.x * g.x), __expf(-0.5f * g.y * g.y));
+      *slope = fma2(mul2(g, both(0.3989422804014327f)), d, c);
+    }
+    return mul2(g, c);
   } else {
-    if (SLOPE) *slope = 1.f;
+    if (SLOPE) *slope = both(1.f);
     return g;
   }
 }
 
-// 32 gates `v` and up units `u` to results: h in v; or, with the gradient x of h beside them, dG in v and dU in u
+// 32 gates `v` and up units `u` to results, two an instruction: h in v; or, with the gradient x of h beside them, dG in v and dU in u. (One
+// at a time: 87 cycles a gate and SM quarter, backward, as much as the products take.)
 template <int ACT, bool BACK>
 __device__ __forceinline__ void gates32(float* v, float* u, const float* x) {
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
+  for (int j = 0; j < 32; j += 2) {
+    const float2 g = make_float2(v[j], v[j + 1]), w = make_float2(u[j], u[j + 1]);
     if constexpr (BACK) {
-      float slope;
-      const float a = gate<ACT, true>(v[j], &slope);
-      v[j] = x[j] * u[j] * slope;
-      u[j] = x[j] * a;
+      float2 slope;
+      const float2 a = gate2<ACT, true>(g, &slope), d = make_float2(x[j], x[j + 1]);
+      const float2 dg = mul2(mul2(d, w), slope), du = mul2(d, a);
+      v[j] = dg.x, v[j + 1] = dg.y;
+      u[j] = du.x, u[j + 1] = du.y;
     } else {
-      v[j] = gate<ACT, false>(v[j], nullptr) * u[j];
+      const float2 h = mul2(gate2<ACT, false>(g, nullptr), w);
+      v[j] = h.x, v[j + 1] = h.y;
     }
   }
 }
@@ -225,18 +247,21 @@ __device__ __forceinline__ Tile tile_at(const Params& p, uint32_t t) {
   return {z, band * p.band + (in - tn * rows), tn};
 }
 
-// 32 neighbouring values of a row, 0 behind its end
-template <int DT>
-__device__ __forceinline__ void load_row32(const void* base, int64_t at, int64_t left, uint32_t vec, float* v) {
-  using T = typename Elem<DT>::T;
-  const T* p = reinterpret_cast<const T*>(base) + at;
+// 32 neighbouring 16-bit values of a row on its way to registers, 0 behind its end. vec: rows start on 16-byte boundaries.
+struct Row32 {
+  uint4 w[4];
+};
+__device__ __forceinline__ void fetch_row32(const void* base, int64_t at, int64_t left, uint32_t vec, Row32* r) {
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + at;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     if (vec && left >= 8 * q + 8) {
-      widen16<DT>(*reinterpret_cast<const uint4*>(p + 8 * q), v + 8 * q);
+      r->w[q] = *reinterpret_cast<const uint4*>(p + 8 * q);
     } else {
+      uint32_t v[8];
 #pragma unroll
-      for (int j = 8 * q; j < 8 * q + 8; ++j) v[j] = j < left ? to_float<DT>(p[j]) : 0.f;
+      for (int j = 0; j < 8; ++j) v[j] = 8 * q + j < left ? p[8 * q + j] : 0;
+      r->w[q] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
     }
   }
 }
@@ -449,30 +474,48 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
     }
     put_end();
   };
-  auto other = [&](float* x, int64_t i, int64_t j1) {  // what stands beside 32 columns of row i
+  // What stands beside 32 columns of row i: asked for a chunk ahead (waiting for it took longer than all else that is done with a chunk: 4.4 us
+  // a tile of 128 x 64 units, backward, where its products take 2.2)
+  constexpr bool kBeside = MODE == kGatedBack || MODE == kPair || MODE == kPairOut;
+  constexpr int kBesides = MODE == kPair || MODE == kPairOut ? 2 : 1;
+  auto ask = [&](Row32* r, int64_t i, int64_t j1) {
+    if constexpr (kBeside) {
+      if (i < p.m && j1 < p.n && p.c0 && MFET_INSIDE(p.status, j1 >= 0 && i >= 0)) {
+        fetch_row32(p.c0, i * p.c_ld + j1, p.n - j1, p.c_vec, r);
+        if constexpr (kBesides == 2) fetch_row32(p.c1, i * p.c_ld + j1, p.n - j1, p.c_vec, r + 1);
+      } else {
+        memset(r, 0, kBesides * sizeof(Row32));
+      }
+    }
+  };
+  auto got = [&](const Row32* r, float* x) {
+    if constexpr (kBeside) {
+      constexpr int kType = MODE == kGatedBack ? DT : MFET_F16;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = 0.f;
-    if constexpr (MODE == kGatedBack) {
-      if (i < p.m && MFET_INSIDE(p.status, j1 >= 0 && i >= 0)) load_row32<DT>(p.c0, i * p.c_ld + j1, p.n - j1, p.c_vec, x);
-    } else if constexpr (MODE == kPair || MODE == kPairOut) {
-      if (p.c0 && i < p.m && MFET_INSIDE(p.status, j1 >= 0 && i >= 0)) {
-        float lo[32];
-        load_row32<MFET_F16>(p.c0, i * p.c_ld + j1, p.n - j1, p.c_vec, x);
-        load_row32<MFET_F16>(p.c1, i * p.c_ld + j1, p.n - j1, p.c_vec, lo);
+      for (int q = 0; q < 4; ++q) {
+        widen16<kType>(r->w[q], x + 8 * q);
+        if constexpr (kBesides == 2) {
+          float lo[8];
+          widen16<kType>(r[1].w[q], lo);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] += lo[j];
+          for (int j = 0; j < 8; ++j) x[8 * q + j] += lo[j];
+        }
       }
     }
   };
   if (warp >= 2) {
     uint32_t done = 0;
+    Row32 next[kBesides];
+    auto row_of = [&](const Tile& w) { return (int64_t)(w.tm * CTAS + half) * 128 + quarter * 32; };
+    if (p.split == 1 && first < p.tiles) {
+      const Tile w = tile_at(p, first);
+      ask(next, row_of(w) + lane, (int64_t)w.tn * G::width + 32 * second);
+    }
     for (uint32_t t = first; t < p.tiles; t += step, ++done) {
       const Tile w = tile_at(p, t);
       const int acc = done & 1;
-      const int64_t i0 = (int64_t)(w.tm * CTAS + half) * 128 + quarter * 32, j0 = (int64_t)w.tn * G::width;
+      const int64_t i0 = row_of(w), j0 = (int64_t)w.tn * G::width;
       const uint32_t from = tmem + acc * TN + ((uint32_t)(quarter * 32) << 16);
-      float x[32];
-      if (p.split == 1) other(x, i0 + lane, j0 + 32 * second);  // under way while the tile is computed
       const bool ok = bar_sleep(acc_full(acc), (done / 2) & 1, &dead);
       if (!__all_sync(kAllLanes, ok)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -490,18 +533,25 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
 #pragma unroll 1
       for (int c = 32 * second; c < G::width; c += 64) {
         uint32_t r[32], r2[32];
+        float x[32];
         tmem_load32(from + c, r);
         if constexpr (G::dual) tmem_load32(from + G::width + c, r2);
-        if (c + 64 >= G::width) {  // the accumulator is read: the next tile but one may overwrite it
+        got(next, x);
+        if (c + 64 < G::width) {
+          ask(next, i0 + lane, j0 + c + 64);
+        } else {  // the accumulator is read: the next tile but one may overwrite it
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
             if constexpr (CTAS == 1) bar_arrive(acc_empty(acc));
             else peer_arrive(peer_addr(acc_empty(acc), leader));
           }
+          if (kBeside && t + step < p.tiles) {
+            const Tile v = tile_at(p, t + step);
+            ask(next, row_of(v) + lane, (int64_t)v.tn * G::width + 32 * second);
+          }
         }
         finish(reinterpret_cast<float*>(r), reinterpret_cast<float*>(r2), x, (int)w.z, i0, j0 + c);
-        if (c + 64 < G::width) other(x, i0 + lane, j0 + c + 64);
       }
     }
   }
@@ -524,9 +574,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
 #pragma unroll
           for (int j = 0; j < 32; j += 4) peer_load(src + j * 512, to + j);
         };
+        Row32 beside[kBesides];
+        ask(beside, i0 + lane, j0 + c);
         fetch(v, 0, c);
         if constexpr (G::dual) fetch(u, 0, G::width + c);
-        other(x, i0 + lane, j0 + c);
         for (uint32_t s = 1; s < p.split; ++s) {
           fetch(t, s, c);
 #pragma unroll
@@ -537,6 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
             for (int j = 0; j < 32; ++j) u[j] += t[j];
           }
         }
+        got(beside, x);
         finish(v, u, x, (int)w.z, i0, j0 + c);
       }
     }
@@ -694,13 +746,12 @@ double cost(const Problem& q, uint32_t split) {
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
   const int64_t at_once = clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, CTAS * split, G::smem), waves = (tiles + at_once - 1) / at_once;
   if (split > 1 && waves > 1) return 1e300;
-  const double base = CTAS == 2 ? 7.0 : 5.9, each = CTAS == 2 ? 0.28 : tiles * split > at_once / 2 ? 0.155 : 0.14;
-  return base + (double)waves * ((iters + split - 1) / split) * each + (split == 1 ? 0.0 : split == 2 ? 2.5 : 5.0);
+  return (CTAS == 2 ? 6.9 : 4.2) + (double)waves * ((iters + split - 1) / split) * (CTAS == 2 ? 0.325 : 0.25) + (split == 1 ? 0.0 : split == 2 ? 3.0 : 6.0);
 }
 
-// The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 7.0 for pairs, 5.9
-// for blocks; a block of k 0.28 for 256 x 256 by a pair, 0.14 for 128 x 128 by a block (0.155 when L2 serves all SMs); joining two parts
-// 2.5, four 5. (1 x 896 x 1024 forward: blocks 7.8, in two parts 9.9, pairs 11.0; 8192 x 896 x 1024 backward: pairs 93, blocks 114.)
+// The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 6.9 for pairs, 4.2
+// for blocks; 64 of k 0.325 for 256 x 256 by a pair, 0.25 for 128 x 128 by a block (its loads bound it); joining two parts 3, four 6.
+// Forward, k = 896, n = 1024: m = 1024 blocks 7.9, pairs 11.4; 8192 blocks 30.4, pairs 25.2. Backward 16384 x 2048 x 4096 1187 by pairs, 1803.
 template <int MODE, int DT>
 int run(const Problem& q, cudaStream_t s) {
   double least = 1e300;
