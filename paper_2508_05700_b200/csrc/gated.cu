@@ -100,9 +100,7 @@ int mfet_gated_linear(const void* x, uint32_t dtype, int64_t x_ld, int64_t m, co
   const uint64_t need = packing(in, 3);
   if (need && (!scratch || scratch_bytes < need)) return MFET_ERR_WORKSPACE;
   if (need && !aligned(scratch, 16)) return MFET_ERR_ALIGNMENT;
-  uint8_t* to = (uint8_t*)scratch;
-  for (Matrix& i : in)
-    if (packed(&i, &to, c.stream) != cudaSuccess) return MFET_ERR_CUDA;
+  if (packed(in, 3, (uint8_t*)scratch, c.stream) != cudaSuccess) return MFET_ERR_CUDA;
   const Matrix out{h, n, m, h_ld};
   return gates<kGated>(c, in[0], in[1], in[2], &out, 1, nullptr);
 }
@@ -147,8 +145,7 @@ int mfet_gated_linear_backward(const void* x, uint32_t dtype, int64_t x_ld, int6
     i = {to, n, m, up8(n), true};
     to += grad_bytes(m, n);
   }
-  for (Matrix& i : in)
-    if (packed(&i, &to, c.stream) != cudaSuccess) return MFET_ERR_CUDA;
+  if (packed(in, 4, to, c.stream) != cudaSuccess) return MFET_ERR_CUDA;
   int rc = gates<kGatedBack>(c, in[0], in[1], in[2], g, 2, &in[3]);
   if (rc == MFET_OK && dx) {
     Problem q;

@@ -431,11 +431,13 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       __syncwarp();
     } else {
       __syncwarp();
-      T* y = reinterpret_cast<T*>(p.out[o]) + i0 * p.out_ld[o] + j1 + lane;
-#pragma unroll 8
-      for (int i = 0; i < 32; ++i) {  // a warp writes a row's 32 columns
+      const int64_t ld = p.out_ld[o];
+      T* y = reinterpret_cast<T*>(p.out[o]) + i0 * ld + j1 + lane;
+      const int rows = j1 + lane < p.n && MFET_INSIDE(p.status, i0 >= 0 && j1 >= 0 && j1 + lane < ld) ? (int)(p.m - i0 < 32 ? p.m - i0 : 32) : 0;
+#pragma unroll
+      for (int i = 0; i < 32; ++i, y += ld) {  // a warp writes a row's 32 columns
         const T x = *reinterpret_cast<const T*>(to + G::at(i, lane / kPer) + lane % kPer * sizeof(T));
-        if (i0 + i < p.m && j1 + lane < p.n && MFET_INSIDE(p.status, i0 >= 0 && j1 >= 0 && j1 + lane < p.out_ld[o])) y[i * p.out_ld[o]] = x;
+        if (i < rows) *y = x;
       }
       __syncwarp();
     }
@@ -767,38 +769,52 @@ int run(const Problem& q, cudaStream_t s) {
 
 // ------------------------------------------------------------------ rows that no bulk copy can read ----
 
-struct PackParams {
-  const uint8_t* src;
+struct Pack {
+  const uint16_t* src;
   uint8_t* dst;
   int64_t rows, cols, src_ld, dst_ld;
+  int64_t first;  // of the units of all matrices
+};
+struct PackParams {
+  Pack of[4];
+  int64_t units;
 };
 
-// 16-bit rows at any address into rows on 16-byte boundaries
+// 16-bit rows at any address into rows on 16-byte boundaries, of up to four matrices in one launch: 8 values a thread
 static __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackParams p) {
   early_launch_wait();
-  const int64_t per_row = p.dst_ld / 8, units = p.rows * per_row;
-  const uint16_t* src = reinterpret_cast<const uint16_t*>(p.src);
-  const void* end = src + (p.rows - 1) * p.src_ld + p.cols;
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-    const int64_t row = u / per_row, c = (u - row * per_row) * 8;
-    const int count = (int)(p.cols - c < 8 ? p.cols - c : 8);
-    if (!MFET_INSIDE(nullptr, row < p.rows && count > 0 && c + 8 <= p.dst_ld)) continue;
-    const Raw<MFET_F16, 8> r = load_shifted<MFET_F16, 8>(reinterpret_cast<const __half*>(src + row * p.src_ld + c), count, src, end);
-    *reinterpret_cast<uint4*>(p.dst + (row * p.dst_ld + c) * 2) = r.w[0];
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < p.units; u += (int64_t)gridDim.x * 256) {
+    int z = 0;
+    while (z < 3 && u >= p.of[z + 1].first) ++z;
+    const Pack& x = p.of[z];
+    const int64_t per_row = x.dst_ld / 8, v = u - x.first;
+    const int64_t row = (uint64_t)v >> 32 ? v / per_row : (int64_t)((uint32_t)v / (uint32_t)per_row), c = (v - row * per_row) * 8;
+    const int count = (int)(x.cols - c < 8 ? x.cols - c : 8);
+    if (!MFET_INSIDE(nullptr, row < x.rows && count > 0 && c + 8 <= x.dst_ld)) continue;
+    const void* end = x.src + (x.rows - 1) * x.src_ld + x.cols;
+    const Raw<MFET_F16, 8> r = load_shifted<MFET_F16, 8>(reinterpret_cast<const __half*>(x.src + row * x.src_ld + c), count, x.src, end);
+    *reinterpret_cast<uint4*>(x.dst + (row * x.dst_ld + c) * 2) = r.w[0];
   }
 }
 
 inline int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 inline uint64_t packed_bytes(int64_t rows, int64_t cols) { return ((uint64_t)rows * up8(cols) * 2 + 15) / 16 * 16; }
 
-// x itself, or its copy at *to (which moves on behind it)
-inline cudaError_t packed(Matrix* x, uint8_t** to, cudaStream_t s) {
-  if (on_16(*x, MFET_F16)) return cudaSuccess;
-  PackParams p{(const uint8_t*)x->p, *to, x->outer, x->inner, x->ld, up8(x->inner)};
-  *to += packed_bytes(x->outer, x->inner);
-  x->p = p.dst;
-  x->ld = p.dst_ld;
-  const int64_t want = (x->outer * (p.dst_ld / 8) + 255) / 256, most = (int64_t)sm_count() * 16;
+// Those of `n` (at most four) matrices whose rows do not start on 16-byte boundaries are copied to `to`, and their entries become the copies'.
+inline cudaError_t packed(Matrix* x, int n, uint8_t* to, cudaStream_t s) {
+  PackParams p{};
+  int k = 0;
+  for (int i = 0; i < n; ++i) {
+    if (on_16(x[i], MFET_F16)) continue;
+    p.of[k++] = {(const uint16_t*)x[i].p, to, x[i].outer, x[i].inner, x[i].ld, up8(x[i].inner), p.units};
+    p.units += x[i].outer * (up8(x[i].inner) / 8);
+    x[i].p = to;
+    x[i].ld = up8(x[i].inner);
+    to += packed_bytes(x[i].outer, x[i].inner);
+  }
+  if (k == 0) return cudaSuccess;
+  for (; k < 4; ++k) p.of[k].first = p.units;
+  const int64_t want = (p.units + 255) / 256, most = (int64_t)sm_count() * 16;
   return launch_early(pack_kernel, (unsigned)(want < most ? want : most), 256, 0, s, p);
 }
 
