@@ -67,6 +67,7 @@ struct Params {
   uint32_t tail;            // instructions (k = 16) in the last block of a segment
   uint32_t split;
   uint32_t a_mn, b_mn;      // MN-major operands
+  uint32_t sym;             // the result is symmetric: tiles on and below the diagonal alone, each written to both of its places
   uint32_t inst;            // instruction descriptor
   uint32_t seg_a, seg_b;    // operand of segment s: bits 4s..
   uint32_t act;
@@ -240,6 +241,12 @@ struct Tile {
   uint32_t z, tm, tn;
 };
 __device__ __forceinline__ Tile tile_at(const Params& p, uint32_t t) {
+  if (p.sym) {  // row by row: r (r + 1) / 2 tiles lie ahead of row r
+    uint32_t r = (uint32_t)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while ((uint64_t)r * (r + 1) / 2 > t) --r;
+    while ((uint64_t)(r + 1) * (r + 2) / 2 <= t) ++r;
+    return {0, r, t - r * (r + 1) / 2};
+  }
   const uint32_t per = p.m_tiles * p.n_tiles, z = t / per, r = t - z * per;
   const uint32_t band = r / (p.band * p.n_tiles), in = r - band * p.band * p.n_tiles;
   const uint32_t rows = min(p.band, p.m_tiles - band * p.band);
@@ -442,6 +449,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       __syncwarp();
     }
   };
+  // the same with rows and columns exchanged (of a symmetric result, which has bulk copies)
+  auto put_mirror = [&](const float* v, int o, int64_t i0, int64_t j1) {
+    if constexpr (MODE == kPair) {
+      const uint32_t piece = (turn * G::outs + o) * G::piece;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) *reinterpret_cast<T*>(out_ptr + piece + G::at(j, lane >> 3) + (lane & 7) * sizeof(T)) = Elem<DT>::from(v[j]);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (i0 < p.m && j1 < p.n && elect_one()) bulk_store(&maps.out[o], out_at + piece, (int32_t)i0, (int32_t)j1);
+      __syncwarp();
+    }
+  };
   auto put_begin = [&]() {  // what the memory of the pieces held before has left
     asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
     __syncwarp();
@@ -451,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
     turn ^= 1;
   };
   // what becomes of 32 columns of the accumulator (and of the same units' other half, where dual): x is what c0 (c1) held there
-  auto finish = [&](float* v, float* u, float* x, int z, int64_t i0, int64_t j1) {
+  auto finish = [&](float* v, float* u, float* x, int z, int64_t i0, int64_t j1, bool mirror) {
     put_begin();
     if constexpr (MODE == kGated) {
       gates32<false>(p.act, v, u, x);
@@ -470,6 +489,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
         for (int j = 0; j < 32; ++j) x[j] = v[j] - __half2float(__float2half_rn(v[j]));
         put(v, 0, i0, j1);
         put(x, 1, i0, j1);
+        if (mirror) {
+          put_end();
+          put_begin();
+          put_mirror(v, 0, i0, j1);
+          put_mirror(x, 1, i0, j1);
+        }
       } else {
         put(v, 0, i0, j1);
       }
@@ -553,7 +578,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
             ask(next, row_of(v) + lane, (int64_t)v.tn * G::width + 32 * second);
           }
         }
-        finish(reinterpret_cast<float*>(r), reinterpret_cast<float*>(r2), x, (int)w.z, i0, j0 + c);
+        finish(reinterpret_cast<float*>(r), reinterpret_cast<float*>(r2), x, (int)w.z, i0, j0 + c, p.sym && w.tm != w.tn);
       }
     }
   }
@@ -591,7 +616,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
           }
         }
         got(beside, x);
-        finish(v, u, x, (int)w.z, i0, j0 + c);
+        finish(v, u, x, (int)w.z, i0, j0 + c, p.sym && w.tm != w.tn);
       }
     }
     __syncwarp();
@@ -681,7 +706,7 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   }
   p.m_tiles = (uint32_t)((p.m + CTAS * 128 - 1) / (CTAS * 128));
   p.n_tiles = (uint32_t)((p.n + G::width - 1) / G::width);
-  p.tiles = p.m_tiles * p.n_tiles * (uint32_t)q.results;
+  p.tiles = p.sym ? p.m_tiles * (p.m_tiles + 1) / 2 : p.m_tiles * p.n_tiles * (uint32_t)q.results;
   p.band = 8;
   p.kb = (uint32_t)((q.k + kSlab - 1) / kSlab);
   p.iters = p.kb * (uint32_t)q.segs;
@@ -743,7 +768,8 @@ double cost(const Problem& q, uint32_t split) {
   using G = Shape<CTAS, TN, MODE, DT>;
   const int64_t iters = (q.k + kSlab - 1) / kSlab * q.segs;
   if (split > 1 && (split * CTAS > 8 || split * 32 > (uint32_t)G::width || (int64_t)split > iters)) return 1e300;
-  const int64_t tiles = (q.p.m + CTAS * 128 - 1) / (CTAS * 128) * ((q.p.n + G::width - 1) / G::width) * q.results;
+  const int64_t rows = (q.p.m + CTAS * 128 - 1) / (CTAS * 128);
+  const int64_t tiles = q.p.sym ? rows * (rows + 1) / 2 : rows * ((q.p.n + G::width - 1) / G::width) * q.results;
   static std::atomic<uint64_t> ready{0};
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
   const int64_t at_once = clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, CTAS * split, G::smem), waves = (tiles + at_once - 1) / at_once;
@@ -754,16 +780,23 @@ double cost(const Problem& q, uint32_t split) {
 // The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 6.9 for pairs, 4.2
 // for blocks; 64 of k 0.325 for 256 x 256 by a pair, 0.25 for 128 x 128 by a block (its loads bound it); joining two parts 3, four 6.
 // Forward, k = 896, n = 1024: m = 1024 blocks 7.9, pairs 11.4; 8192 blocks 30.4, pairs 25.2. Backward 16384 x 2048 x 4096 1187 by pairs, 1803.
+// A symmetric result is computed by half where that saves a wave of tiles: writing a tile twice takes 0.8 (256 x 256: 8.2 a product for all of
+// it, 9.2; 2048 x 2048 of 4096: 52, 69).
 template <int MODE, int DT>
-int run(const Problem& q, cudaStream_t s) {
+int run(Problem q, cudaStream_t s) {
   double least = 1e300;
   int form = 0;
-  uint32_t split = 1;
-  for (uint32_t part = 1; part <= 4; part *= 2) {
-    const double pair = cost<2, 256, MODE, DT>(q, part), block = cost<1, 128, MODE, DT>(q, part);
-    if (pair < least) least = pair, form = 0, split = part;
-    if (block < least) least = block, form = 1, split = part;
+  uint32_t split = 1, half = 0;
+  for (uint32_t sym = 0; sym <= q.p.sym; ++sym) {
+    Problem r = q;
+    r.p.sym = sym;
+    for (uint32_t part = 1; part <= 4; part *= 2) {
+      const double pair = cost<2, 256, MODE, DT>(r, part) + 0.8 * sym, block = cost<1, 128, MODE, DT>(r, part) + 0.8 * sym;
+      if (pair < least) least = pair, form = 0, split = part, half = sym;
+      if (block < least) least = block, form = 1, split = part, half = sym;
+    }
   }
+  q.p.sym = half;
   return form == 0 ? launch<2, 256, MODE, DT>(q, split, s) : launch<1, 128, MODE, DT>(q, split, s);
 }
 

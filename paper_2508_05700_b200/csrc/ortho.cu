@@ -654,6 +654,7 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
     q.p.status = status;
     three(&q, from, from, tall ? rows : cols);
     q.p.a_mn = q.p.b_mn = tall;
+    q.p.sym = 1;
     combine(&q, nullptr, 0.0, 1.0, from.e, from.e, a.e);
     into(&q, a);
     int rc = run<kPair, MFET_F16>(q, st);
@@ -663,6 +664,7 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
     q = Problem();
     q.p.status = status;
     three(&q, a, a, d);
+    q.p.sym = 1;
     combine(&q, &a, c[1], c[2], a.e, a.e, b.e);
     into(&q, b);
     rc = run<kPair, MFET_F16>(q, st);
