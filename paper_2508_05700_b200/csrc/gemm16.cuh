@@ -28,6 +28,7 @@ enum Mode {
   kGated,      // columns are units: h = act(g) * u
   kGatedBack,  // ... with the gradient of h: dG and dU
   kOut,        // the accumulator, rounded
+  kOutTwo,     // ... of two products of different operands in one launch
   kPair,       // v = alpha * C + beta * acc in two fp16 words
   kPairOut     // the same, rounded to the type of the result
 };
@@ -56,25 +57,33 @@ struct Shape {
 };
 
 struct Maps {
-  CUtensorMap a[2], b[2], out[2];
+  CUtensorMap a[4], b[3], out[3];
+};
+
+// A product: one result, or two of different A (z = 0, 1)
+struct Part {
+  int64_t m, n;             // rows and columns of the result (units, where dual)
+  uint32_t m_tiles, n_tiles;
+  uint32_t kb, iters;       // blocks of k per segment; of all segments
+  uint32_t tail;            // instructions (k = 16) in the last block of a segment
+  uint32_t a_mn, b_mn;      // MN-major operands
+  uint32_t inst;            // instruction descriptor
+  uint32_t seg_a, seg_b;    // operand of segment s: bits 4s.. (A: of the first result)
+  uint32_t out;             // its first output
 };
 
 struct Params {
-  int64_t m, n;             // rows and columns of the result (units, where dual)
-  uint32_t m_tiles, n_tiles, tiles;  // tiles of one result; of all results
+  Part part[2];
+  uint32_t tiles, tiles0;   // of all results; of the first product's
+  uint32_t heavy, later;    // kOutTwo: see Walk
   uint32_t band;            // tiles of rows that are walked through together, so that the blocks at work share operands in L2
-  uint32_t kb, iters;       // blocks of k per segment; of all segments
-  uint32_t tail;            // instructions (k = 16) in the last block of a segment
   uint32_t split;
-  uint32_t a_mn, b_mn;      // MN-major operands
   uint32_t sym;             // the result is symmetric: tiles on and below the diagonal alone, each written to both of its places
-  uint32_t inst;            // instruction descriptor
-  uint32_t seg_a, seg_b;    // operand of segment s: bits 4s..
   uint32_t act;
-  uint32_t bulk;            // bit z: rows of output z start on 16-byte boundaries; bit 2 + z: ... and may be written up to one (bulk copies
+  uint32_t bulk;            // bit o: rows of output o start on 16-byte boundaries; bit 4 + o: ... and may be written up to one (bulk copies
                             // write whole units of 16 bytes, also where a row ends inside one)
-  void* out[2];
-  int64_t out_ld[2];
+  void* out[3];
+  int64_t out_ld[3];
   const void* c0;           // kGatedBack: gradient of h; kPair*: high words of C, or NULL
   const void* c1;           // low words of C
   int64_t c_ld;
@@ -82,6 +91,7 @@ struct Params {
   float alpha, beta;        // alpha has C's scale in it, beta the product's; both the result's
   uint32_t* status;
 };
+static_assert(sizeof(Maps) + sizeof(Params) <= 4000, "the kernel's parameter space");
 
 // ------------------------------------------------------------------ instructions ----
 
@@ -238,21 +248,44 @@ __device__ __forceinline__ void gates32(uint32_t act, float* v, float* u, const 
 // ------------------------------------------------------------------ the kernel ----
 
 struct Tile {
-  uint32_t z, tm, tn;
+  uint32_t z, tm, tn, part;
 };
+template <bool TWO>
 __device__ __forceinline__ Tile tile_at(const Params& p, uint32_t t) {
   if (p.sym) {  // row by row: r (r + 1) / 2 tiles lie ahead of row r
     uint32_t r = (uint32_t)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
     while ((uint64_t)r * (r + 1) / 2 > t) --r;
     while ((uint64_t)(r + 1) * (r + 2) / 2 <= t) ++r;
-    return {0, r, t - r * (r + 1) / 2};
+    return {0, r, t - r * (r + 1) / 2, 0};
   }
-  const uint32_t per = p.m_tiles * p.n_tiles, z = t / per, r = t - z * per;
-  const uint32_t band = r / (p.band * p.n_tiles), in = r - band * p.band * p.n_tiles;
-  const uint32_t rows = min(p.band, p.m_tiles - band * p.band);
+  const uint32_t part = TWO && t >= p.tiles0 ? 1 : 0;
+  if (part) t -= p.tiles0;
+  const Part& q = p.part[part];
+  const uint32_t per = q.m_tiles * q.n_tiles, z = t / per, r = t - z * per;
+  const uint32_t band = r / (p.band * q.n_tiles), in = r - band * p.band * q.n_tiles;
+  const uint32_t rows = min(p.band, q.m_tiles - band * p.band);
   const uint32_t tn = in / rows;
-  return {z, band * p.band + (in - tn * rows), tn};
+  return {z, band * p.band + (in - tn * rows), tn, part};
 }
+
+// The tiles of a block (pair), one after the other: each `step`-th. TWO: the first product's tiles are the longer ones and go first, the blocks
+// below `heavy` get one more of them than the others; the second's fill up round by round, and in the first `later` rounds the heavy
+// blocks are still busy and take none.
+template <bool TWO>
+struct Walk {
+  const Params& p;
+  uint32_t first, step, own;
+  __device__ __forceinline__ Walk(const Params& p_, uint32_t first_, uint32_t step_) : p(p_), first(first_), step(step_) {
+    own = TWO ? p.tiles0 / step + (first < p.heavy) : 0;
+  }
+  // tile k, or one beyond the last
+  __device__ __forceinline__ uint32_t operator()(uint32_t k) const {
+    if (!TWO || k < own) return first + k * step;
+    const bool heavy = first < p.heavy;
+    const uint32_t light = step - p.heavy, round = k - own + (heavy ? p.later : 0), place = heavy ? light + first : first - p.heavy;
+    return p.tiles0 + (round < p.later ? round * light + place : p.later * light + (round - p.later) * step + place);
+  }
+};
 
 // 32 neighbouring 16-bit values of a row on its way to registers, 0 behind its end. vec: rows start on 16-byte boundaries.
 struct Row32 {
@@ -296,9 +329,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   const uint32_t pair_mask = (CTAS == 2 ? 3u : 1u) << leader;
 
   if (threadIdx.x == 64) {
-    prefetch_map(&maps.a[0]);
-    prefetch_map(&maps.b[0]);
-    if (G::dual || (p.seg_b >> 4)) prefetch_map(&maps.b[1]);
+    prefetch_map(&maps.a[p.part[0].seg_a & 15u]);
+    prefetch_map(&maps.b[p.part[0].seg_b & 15u]);
+    if (G::dual || (p.part[0].seg_b >> 4)) prefetch_map(&maps.b[1]);
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < G::stages; ++s) bar_init(full(s), 1), bar_init(empty(s), 1);
@@ -325,9 +358,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   early_launch_wait();
 
   const uint32_t members = CTAS * p.split;
-  const uint32_t first = blockIdx.x / members, step = gridDim.x / members;
-  // this part of k
-  const uint32_t k0 = (uint32_t)((uint64_t)p.iters * part / p.split), k1 = (uint32_t)((uint64_t)p.iters * (part + 1) / p.split);
+  constexpr bool kTwo = MODE == kOutTwo;
+  const uint32_t first = blockIdx.x / members;
+  const Walk<kTwo> walk(p, first, gridDim.x / members);
+  auto share_begin = [&](const Part& q) { return (uint32_t)((uint64_t)q.iters * part / p.split); };  // this block's share of k
+  auto share_end = [&](const Part& q) { return (uint32_t)((uint64_t)q.iters * (part + 1) / p.split); };
 
   uint64_t filled = 0;  // stages that this lane has asked for
   bool issues = false;  // this lane issues the products
@@ -335,14 +370,17 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
     if (elect_one()) {
       uint32_t st = 0, phase = 1;  // an empty barrier's phase before the first is taken as complete
       bool ok = true;
-      for (uint32_t t = first; ok && t < p.tiles; t += step) {
-        const Tile w = tile_at(p, t);
+      uint32_t turn = 0;
+      for (uint32_t t = walk(0); ok && t < p.tiles; t = walk(++turn)) {
+        const Tile w = tile_at<kTwo>(p, t);
+        const Part& q = p.part[kTwo ? w.part : 0];
+        const uint32_t k0 = share_begin(q), k1 = share_end(q);
         const int32_t row = (int32_t)((w.tm * CTAS + half) * 128);
-        uint32_t seg = k0 / p.kb, kk = k0 - seg * p.kb;
+        uint32_t seg = k0 / q.kb, kk = k0 - seg * q.kb;
         for (uint32_t i = k0; i < k1; ++i) {
           if (!(ok = bar_sleep(empty(st), phase, &dead))) break;
           // tiles and blocks of k outside their matrix read as 0
-          if (!MFET_INSIDE(p.status, seg < 3 && w.z < 2 && (int64_t)row < p.m + 128 && w.tn < p.n_tiles)) {
+          if (!MFET_INSIDE(p.status, seg < 3 && w.z < 2 && (int64_t)row < q.m + 128 && w.tn < q.n_tiles)) {
             ok = false;
             dead = 1;
             break;
@@ -350,9 +388,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
           const uint32_t at = base + st * G::stage_bytes;
           const uint32_t bar = CTAS == 1 ? full(st) : peer_addr(full(st), leader);
           if (half == 0) bar_expect(full(st), CTAS * G::stage_bytes);
-          const CUtensorMap* a = &maps.a[((p.seg_a >> (4 * seg)) & 15u) + w.z];
+          const CUtensorMap* a = &maps.a[((q.seg_a >> (4 * seg)) & 15u) + w.z];
           const int32_t k = (int32_t)(kk * kSlab);
-          if (p.a_mn) {
+          if (q.a_mn) {
             tile_load<CTAS>(at, a, row, k, bar);
             tile_load<CTAS>(at + 8192, a, row + 64, k, bar);
           } else {
@@ -367,9 +405,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
               tile_load<CTAS>(at + G::a_bytes + G::b_bytes / 2, &maps.b[1], k, unit, bar);
             }
           } else {
-            const CUtensorMap* b = &maps.b[(p.seg_b >> (4 * seg)) & 15u];
+            const CUtensorMap* b = &maps.b[(q.seg_b >> (4 * seg)) & 15u];
             const int32_t col = (int32_t)(w.tn * TN + half * G::b_rows);
-            if (p.b_mn) {
+            if (q.b_mn) {
 #pragma unroll
               for (int j = 0; j < G::b_rows / 64; ++j) tile_load<CTAS>(at + G::a_bytes + 8192 * j, b, col + 64 * j, k, bar);
             } else {
@@ -378,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
           }
           ++filled;
           if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-          if (++kk == p.kb) kk = 0, ++seg;
+          if (++kk == q.kb) kk = 0, ++seg;
         }
       }
     }
@@ -387,30 +425,32 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       issues = true;
       uint32_t st = 0, phase = 0, done = 0;
       bool ok = true, ready = false;
-      const uint32_t a_step = p.a_mn ? 128u : 2u, b_step = p.b_mn ? 128u : 2u;
-      for (uint32_t t = first; ok && t < p.tiles; t += step, ++done) {
+      for (uint32_t t = walk(0); ok && t < p.tiles; t = walk(++done)) {
+        const Part& q = p.part[kTwo && t >= p.tiles0 ? 1 : 0];
+        const uint32_t k0 = share_begin(q), k1 = share_end(q);
+        const uint32_t a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
         const int acc = done & 1;
         if (done >= 2 && !(ok = bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + acc * TN;
-        uint32_t kk = k0 % p.kb;
+        uint32_t kk = k0 % q.kb;
         for (uint32_t i = k0; i < k1; ++i) {
           if (!ready && !(ok = bar_wait(full(st), phase, &dead))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = base + st * G::stage_bytes;
           const uint32_t this_empty = empty(st);
-          const uint32_t a_lo = desc_lo(at, p.a_mn), b_lo = desc_lo(at + G::a_bytes, p.b_mn);
+          const uint32_t a_lo = desc_lo(at, q.a_mn), b_lo = desc_lo(at + G::a_bytes, q.b_mn);
           if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-          const bool last = ++kk == p.kb;
+          const bool last = ++kk == q.kb;
           if (last) kk = 0;
-          if (!last || p.tail == 4) {
-            mma16<CTAS>(d, a_lo, b_lo, p.inst, i != k0);
-            mma16<CTAS>(d, a_lo + a_step, b_lo + b_step, p.inst, 1);
+          if (!last || q.tail == 4) {
+            mma16<CTAS>(d, a_lo, b_lo, q.inst, i != k0);
+            mma16<CTAS>(d, a_lo + a_step, b_lo + b_step, q.inst, 1);
             ready = bar_try(full(st), phase);
-            mma16<CTAS>(d, a_lo + 2 * a_step, b_lo + 2 * b_step, p.inst, 1);
-            mma16<CTAS>(d, a_lo + 3 * a_step, b_lo + 3 * b_step, p.inst, 1);
+            mma16<CTAS>(d, a_lo + 2 * a_step, b_lo + 2 * b_step, q.inst, 1);
+            mma16<CTAS>(d, a_lo + 3 * a_step, b_lo + 3 * b_step, q.inst, 1);
           } else {
-            for (uint32_t j = 0; j < p.tail; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, p.inst, (i != k0) | j);
+            for (uint32_t j = 0; j < q.tail; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, q.inst, (i != k0) | j);
             ready = bar_try(full(st), phase);
           }
           commit<CTAS>(this_empty, pair_mask);
@@ -424,6 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   uint8_t* const out_ptr = smem + G::out_at + (warp - 2) * G::warp_out;
   const uint32_t out_at = base + G::out_at + (warp - 2) * G::warp_out;
   uint32_t turn = 0;
+  const Part* q = &p.part[0];  // of the tile that is written
   // 32 columns `v` of this lane's row, from column j1 on, to output o of the result (i0: the warp's first row)
   auto put = [&](float* v, int o, int64_t i0, int64_t j1) {
     constexpr int kPer = 16 / (int)sizeof(T);  // values per 16 bytes
@@ -431,16 +472,16 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
     uint8_t* const to = out_ptr + piece;
 #pragma unroll
     for (int q = 0; q < 32; q += kPer) *reinterpret_cast<uint4*>(to + G::at(lane, q / kPer)) = narrow16<DT>(v + q);
-    if (((p.bulk >> o) & 1) && (j1 + 32 <= p.n || ((p.bulk >> o) & 4))) {
+    if (((p.bulk >> o) & 1) && (j1 + 32 <= q->n || ((p.bulk >> o) & 16))) {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (i0 < p.m && j1 < p.n && elect_one()) bulk_store(&maps.out[o], out_at + piece, (int32_t)j1, (int32_t)i0);
+      if (i0 < q->m && j1 < q->n && elect_one()) bulk_store(&maps.out[o], out_at + piece, (int32_t)j1, (int32_t)i0);
       __syncwarp();
     } else {
       __syncwarp();
       const int64_t ld = p.out_ld[o];
       T* y = reinterpret_cast<T*>(p.out[o]) + i0 * ld + j1 + lane;
-      const int rows = j1 + lane < p.n && MFET_INSIDE(p.status, i0 >= 0 && j1 >= 0 && j1 + lane < ld) ? (int)(p.m - i0 < 32 ? p.m - i0 : 32) : 0;
+      const int rows = j1 + lane < q->n && MFET_INSIDE(p.status, i0 >= 0 && j1 >= 0 && j1 + lane < ld) ? (int)(q->m - i0 < 32 ? q->m - i0 : 32) : 0;
 #pragma unroll
       for (int i = 0; i < 32; ++i, y += ld) {  // a warp writes a row's 32 columns
         const T x = *reinterpret_cast<const T*>(to + G::at(i, lane / kPer) + lane % kPer * sizeof(T));
@@ -457,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       for (int j = 0; j < 32; ++j) *reinterpret_cast<T*>(out_ptr + piece + G::at(j, lane >> 3) + (lane & 7) * sizeof(T)) = Elem<DT>::from(v[j]);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (i0 < p.m && j1 < p.n && elect_one()) bulk_store(&maps.out[o], out_at + piece, (int32_t)i0, (int32_t)j1);
+      if (i0 < q->m && j1 < q->n && elect_one()) bulk_store(&maps.out[o], out_at + piece, (int32_t)i0, (int32_t)j1);
       __syncwarp();
     }
   };
@@ -479,8 +520,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       gates32<true>(p.act, v, u, x);
       put(v, 0, i0, j1);
       put(u, 1, i0, j1);
-    } else if constexpr (MODE == kOut) {
-      put(v, z, i0, j1);
+    } else if constexpr (MODE == kOut || MODE == kOutTwo) {
+      put(v, (int)q->out + z, i0, j1);
     } else {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], p.beta, x[j] * p.alpha);
@@ -507,9 +548,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   constexpr int kBesides = MODE == kPair || MODE == kPairOut ? 2 : 1;
   auto ask = [&](Row32* r, int64_t i, int64_t j1) {
     if constexpr (kBeside) {
-      if (i < p.m && j1 < p.n && p.c0 && MFET_INSIDE(p.status, j1 >= 0 && i >= 0)) {
-        fetch_row32(p.c0, i * p.c_ld + j1, p.n - j1, p.c_vec, r);
-        if constexpr (kBesides == 2) fetch_row32(p.c1, i * p.c_ld + j1, p.n - j1, p.c_vec, r + 1);
+      if (i < q->m && j1 < q->n && p.c0 && MFET_INSIDE(p.status, j1 >= 0 && i >= 0)) {
+        fetch_row32(p.c0, i * p.c_ld + j1, q->n - j1, p.c_vec, r);
+        if constexpr (kBesides == 2) fetch_row32(p.c1, i * p.c_ld + j1, q->n - j1, p.c_vec, r + 1);
       } else {
         memset(r, 0, kBesides * sizeof(Row32));
       }
@@ -535,11 +576,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
     Row32 next[kBesides];
     auto row_of = [&](const Tile& w) { return (int64_t)(w.tm * CTAS + half) * 128 + quarter * 32; };
     if (p.split == 1 && first < p.tiles) {
-      const Tile w = tile_at(p, first);
+      const Tile w = tile_at<false>(p, first);
       ask(next, row_of(w) + lane, (int64_t)w.tn * G::width + 32 * second);
     }
-    for (uint32_t t = first; t < p.tiles; t += step, ++done) {
-      const Tile w = tile_at(p, t);
+    for (uint32_t t = walk(0); t < p.tiles; t = walk(++done)) {
+      const Tile w = tile_at<kTwo>(p, t);
+      if constexpr (kTwo) q = &p.part[w.part];
       const int acc = done & 1;
       const int64_t i0 = row_of(w), j0 = (int64_t)w.tn * G::width;
       const uint32_t from = tmem + acc * TN + ((uint32_t)(quarter * 32) << 16);
@@ -573,8 +615,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
             if constexpr (CTAS == 1) bar_arrive(acc_empty(acc));
             else peer_arrive(peer_addr(acc_empty(acc), leader));
           }
-          if (kBeside && t + step < p.tiles) {
-            const Tile v = tile_at(p, t + step);
+          if (kBeside && walk(done + 1) < p.tiles) {
+            const Tile v = tile_at<false>(p, walk(done + 1));
             ask(next, row_of(v) + lane, (int64_t)v.tn * G::width + 32 * second);
           }
         }
@@ -589,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (p.split > 1) {
     if (warp >= 2 && !dead && first < p.tiles) {
-      const Tile w = tile_at(p, first);
+      const Tile w = tile_at<kTwo>(p, first);
       const int64_t i0 = (int64_t)(w.tm * CTAS + half) * 128 + quarter * 32, j0 = (int64_t)w.tn * G::width;
       const int share = G::width / (int)p.split;
 #pragma unroll 1
@@ -676,13 +718,23 @@ inline bool on_16(const Matrix& x, uint32_t dtype) {
 
 struct Problem {
   uint32_t dtype = MFET_F16;  // of the operands
-  Matrix a[2] = {}, b[2] = {}, out[2] = {};
-  int n_a = 1, n_b = 1, n_out = 1, results = 1;
-  int64_t k = 0;              // of one segment
-  int segs = 1;
+  Matrix a[4] = {}, b[3] = {}, out[3] = {};
+  int n_a = 1, n_b = 1, n_out = 1;
+  uint32_t a_mn = 0, b_mn = 0;            // bit i: a[i] (b[i]) is MN-major
+  int64_t k[2] = {0, 0};                  // of one segment, of each product
+  int segs[2] = {1, 1}, results[2] = {1, 0};  // results of the second product: 0 where there is one product alone
   uint32_t out_dtype = MFET_F16;
-  Params p = {};              // majors, segments' operands, epilogue
+  Params p = {};                          // sizes, majors and segments' operands of the products, epilogue
 };
+
+inline int64_t tiles_of(const Problem& q, int part, int64_t rows, int64_t cols) {
+  const int64_t r = (q.p.part[part].m + rows - 1) / rows, c = (q.p.part[part].n + cols - 1) / cols;
+  return q.p.sym ? r * (r + 1) / 2 : r * c * q.results[part];
+}
+inline int64_t iters_of(const Problem& q, int part) { return (q.k[part] + kSlab - 1) / kSlab * q.segs[part]; }
+
+// rounds of the second product's tiles in which blocks with one more tile of the first take none
+inline uint32_t rounds_later(uint32_t first, uint32_t second) { return (first + second / 2) / second; }
 
 template <int CTAS, int TN, int MODE, int DT>
 int launch(const Problem& q, uint32_t split, cudaStream_t s) {
@@ -692,32 +744,40 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   Params p = q.p;
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
   for (int i = 0; i < q.n_a; ++i)
-    if (!tile_map(&maps.a[i], q.a[i], q.dtype, p.a_mn ? 64 : 128, 64, sw, true)) return MFET_ERR_CUDA;
+    if (!tile_map(&maps.a[i], q.a[i], q.dtype, (q.a_mn >> i) & 1 ? 64 : 128, 64, sw, true)) return MFET_ERR_CUDA;
   for (int i = 0; i < q.n_b; ++i)
-    if (!tile_map(&maps.b[i], q.b[i], q.dtype, p.b_mn ? 64 : G::dual ? TN / 2 : G::b_rows, 64, sw, true)) return MFET_ERR_CUDA;
+    if (!tile_map(&maps.b[i], q.b[i], q.dtype, (q.b_mn >> i) & 1 ? 64 : G::dual ? TN / 2 : G::b_rows, 64, sw, true)) return MFET_ERR_CUDA;
   p.bulk = 0;
   for (int i = 0; i < q.n_out; ++i) {
     p.out[i] = const_cast<void*>(q.out[i].p);
     p.out_ld[i] = q.out[i].ld;
     if (!on_16(q.out[i], q.out_dtype)) continue;
-    p.bulk |= (q.out[i].spare || q.out[i].inner * size_of(q.out_dtype) % 16 == 0 ? 5u : 1u) << i;
+    p.bulk |= (q.out[i].spare || q.out[i].inner * size_of(q.out_dtype) % 16 == 0 ? 17u : 1u) << i;
     if (!tile_map(&maps.out[i], q.out[i], q.out_dtype, 32, 32, G::piece_row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, false))
       return MFET_ERR_CUDA;
   }
-  p.m_tiles = (uint32_t)((p.m + CTAS * 128 - 1) / (CTAS * 128));
-  p.n_tiles = (uint32_t)((p.n + G::width - 1) / G::width);
-  p.tiles = p.sym ? p.m_tiles * (p.m_tiles + 1) / 2 : p.m_tiles * p.n_tiles * (uint32_t)q.results;
-  p.band = 8;
-  p.kb = (uint32_t)((q.k + kSlab - 1) / kSlab);
-  p.iters = p.kb * (uint32_t)q.segs;
-  p.tail = (uint32_t)((q.k - (int64_t)(p.kb - 1) * kSlab + 15) / 16);
-  p.split = split;
   const uint32_t fmt = q.dtype == MFET_BF16 ? 1u : 0u;
-  p.inst = (1u << 4) | (fmt << 7) | (fmt << 10) | (p.a_mn << 15) | (p.b_mn << 16) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(CTAS * 128 >> 4) << 24);
+  for (int i = 0; i < (MODE == kOutTwo ? 2 : 1); ++i) {
+    Part& x = p.part[i];
+    x.m_tiles = (uint32_t)((x.m + CTAS * 128 - 1) / (CTAS * 128));
+    x.n_tiles = (uint32_t)((x.n + G::width - 1) / G::width);
+    x.kb = (uint32_t)((q.k[i] + kSlab - 1) / kSlab);
+    x.iters = x.kb * (uint32_t)q.segs[i];
+    x.tail = (uint32_t)((q.k[i] - (int64_t)(x.kb - 1) * kSlab + 15) / 16);
+    x.inst = (1u << 4) | (fmt << 7) | (fmt << 10) | (x.a_mn << 15) | (x.b_mn << 16) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(CTAS * 128 >> 4) << 24);
+    p.tiles += (uint32_t)tiles_of(q, i, CTAS * 128, G::width);
+    if (i == 0) p.tiles0 = p.tiles;
+  }
+  p.band = 8;
+  p.split = split;
   static std::atomic<uint64_t> ready{0};
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return MFET_ERR_CUDA;
   const uint32_t members = CTAS * split, at_once = (uint32_t)clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, members, G::smem);
   const uint32_t clusters = split > 1 || p.tiles < at_once ? p.tiles : at_once;
+  if (MODE == kOutTwo) {
+    p.heavy = p.tiles0 % clusters;
+    p.later = p.heavy ? rounds_later(p.part[0].iters, p.part[1].iters) : 0;
+  }
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -766,10 +826,9 @@ int64_t clusters_at_once(K kernel, uint32_t members, uint32_t smem) {
 template <int CTAS, int TN, int MODE, int DT>
 double cost(const Problem& q, uint32_t split) {
   using G = Shape<CTAS, TN, MODE, DT>;
-  const int64_t iters = (q.k + kSlab - 1) / kSlab * q.segs;
+  const int64_t iters = iters_of(q, 0);
   if (split > 1 && (split * CTAS > 8 || split * 32 > (uint32_t)G::width || (int64_t)split > iters)) return 1e300;
-  const int64_t rows = (q.p.m + CTAS * 128 - 1) / (CTAS * 128);
-  const int64_t tiles = q.p.sym ? rows * (rows + 1) / 2 : rows * ((q.p.n + G::width - 1) / G::width) * q.results;
+  const int64_t tiles = tiles_of(q, 0, CTAS * 128, G::width);
   static std::atomic<uint64_t> ready{0};
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
   const int64_t at_once = clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, CTAS * split, G::smem), waves = (tiles + at_once - 1) / at_once;
@@ -780,24 +839,52 @@ double cost(const Problem& q, uint32_t split) {
 // The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 6.9 for pairs, 4.2
 // for blocks; 64 of k 0.325 for 256 x 256 by a pair, 0.25 for 128 x 128 by a block (its loads bound it); joining two parts 3, four 6.
 // Forward, k = 896, n = 1024: m = 1024 blocks 7.9, pairs 11.4; 8192 blocks 30.4, pairs 25.2. Backward 16384 x 2048 x 4096 1187 by pairs, 1803.
+// Two products in one launch, by pairs: the microseconds of it, as above
+template <int DT>
+double cost_two(const Problem& q) {
+  using G = Shape<2, 256, kOutTwo, DT>;
+  static std::atomic<uint64_t> ready{0};
+  if (allow_smem(gemm16_kernel<2, 256, kOutTwo, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
+  const int64_t pairs = clusters_at_once(gemm16_kernel<2, 256, kOutTwo, DT>, 2, G::smem);
+  const int64_t t0 = tiles_of(q, 0, 256, 256), t1 = tiles_of(q, 1, 256, 256), a = iters_of(q, 0), b = iters_of(q, 1);
+  if (t0 + t1 < pairs || t0 + t1 >= (1ll << 31)) return 1e300;
+  const int64_t heavy = t0 % pairs, light = pairs - heavy, later = heavy ? rounds_later((uint32_t)a, (uint32_t)b) : 0;
+  const int64_t rest = t1 - later * light > 0 ? t1 - later * light : 0, rounds = (rest + pairs - 1) / pairs;  // that all take part in
+  const int64_t of_light = t0 / pairs * a + (rest ? later + rounds : (t1 + light - 1) / light) * b;
+  const int64_t of_heavy = heavy ? (t0 / pairs + 1) * a + (rest > light ? rounds : rounds > 0 ? rounds - 1 : 0) * b : 0;
+  return 6.9 + 0.325 * (double)(of_light > of_heavy ? of_light : of_heavy);
+}
+
 // A symmetric result is computed by half where that saves a wave of tiles: writing a tile twice takes 0.8 (256 x 256: 8.2 a product for all of
 // it, 9.2; 2048 x 2048 of 4096: 52, 69).
+struct Choice {
+  double cost;
+  int form;  // 0: pairs, 1: blocks
+  uint32_t split, sym;
+};
 template <int MODE, int DT>
-int run(Problem q, cudaStream_t s) {
-  double least = 1e300;
-  int form = 0;
-  uint32_t split = 1, half = 0;
+Choice choose(const Problem& q) {
+  Choice c{1e300, 0, 1, 0};
   for (uint32_t sym = 0; sym <= q.p.sym; ++sym) {
     Problem r = q;
     r.p.sym = sym;
     for (uint32_t part = 1; part <= 4; part *= 2) {
       const double pair = cost<2, 256, MODE, DT>(r, part) + 0.8 * sym, block = cost<1, 128, MODE, DT>(r, part) + 0.8 * sym;
-      if (pair < least) least = pair, form = 0, split = part, half = sym;
-      if (block < least) least = block, form = 1, split = part, half = sym;
+      if (pair < c.cost) c = {pair, 0, part, sym};
+      if (block < c.cost) c = {block, 1, part, sym};
     }
   }
-  q.p.sym = half;
-  return form == 0 ? launch<2, 256, MODE, DT>(q, split, s) : launch<1, 128, MODE, DT>(q, split, s);
+  return c;
+}
+template <int MODE, int DT>
+double least_cost(const Problem& q) {
+  return choose<MODE, DT>(q).cost;
+}
+template <int MODE, int DT>
+int run(Problem q, cudaStream_t s) {
+  const Choice c = choose<MODE, DT>(q);
+  q.p.sym = c.sym;
+  return c.form == 0 ? launch<2, 256, MODE, DT>(q, c.split, s) : launch<1, 128, MODE, DT>(q, c.split, s);
 }
 
 // ------------------------------------------------------------------ rows that no bulk copy can read ----

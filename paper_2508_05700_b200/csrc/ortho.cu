@@ -532,10 +532,10 @@ cudaError_t load(const LoadParams& p, unsigned blocks, cudaStream_t s) {
 void three(Problem* q, const Words& a, const Words& b, int64_t k) {
   q->a[0] = a.hi, q->a[1] = a.lo, q->n_a = 2;
   q->b[0] = b.hi, q->b[1] = b.lo, q->n_b = 2;
-  q->segs = 3;
-  q->p.seg_a = 0x100;  // high, high, low
-  q->p.seg_b = 0x010;  // high, low, high
-  q->k = k;
+  q->segs[0] = 3;
+  q->p.part[0].seg_a = 0x100;  // high, high, low
+  q->p.part[0].seg_b = 0x010;  // high, low, high
+  q->k[0] = k;
 }
 
 // v = alpha * C + beta * (A B), to be stored under 2^e
@@ -552,8 +552,8 @@ void combine(Problem* q, const Words* c, double alpha, double beta, int e_a, int
 
 void into(Problem* q, const Words& w) {
   q->out[0] = w.hi, q->out[1] = w.lo, q->n_out = 2;
-  q->p.m = w.hi.outer;
-  q->p.n = w.hi.inner;
+  q->p.part[0].m = w.hi.outer;
+  q->p.part[0].n = w.hi.inner;
 }
 
 }  // namespace
@@ -653,7 +653,8 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
     Problem q;
     q.p.status = status;
     three(&q, from, from, tall ? rows : cols);
-    q.p.a_mn = q.p.b_mn = tall;
+    q.p.part[0].a_mn = q.p.part[0].b_mn = tall;
+    q.a_mn = q.b_mn = tall ? 3 : 0;
     q.p.sym = 1;
     combine(&q, nullptr, 0.0, 1.0, from.e, from.e, a.e);
     into(&q, a);
@@ -674,7 +675,8 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
     q.p.status = status;
     if (tall) three(&q, from, b, d);
     else three(&q, b, from, d);
-    q.p.b_mn = !tall;
+    q.p.part[0].b_mn = !tall;
+    q.b_mn = tall ? 0 : 3;
     if (i + 1 < steps) {
       next.e = exponent_for(s[i + 1]);
       combine(&q, &from, c[0], 1.0, from.e, b.e, next.e);
@@ -684,8 +686,8 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
       combine(&q, &from, (double)c[0] * scale, scale, from.e, b.e, 0);
       q.out[0] = {out, cols, rows, out_ld};
       q.out_dtype = out_dtype;
-      q.p.m = rows;
-      q.p.n = cols;
+      q.p.part[0].m = rows;
+      q.p.part[0].n = cols;
       rc = out_dtype == MFET_F32   ? run<kPairOut, MFET_F32>(q, st)
            : out_dtype == MFET_F16 ? run<kPairOut, MFET_F16>(q, st)
                                    : run<kPairOut, MFET_BF16>(q, st);

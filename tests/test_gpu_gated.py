@@ -107,6 +107,14 @@ def test_many_tiles(m, n, k):
     b.check_backward()
 
 
+@pytest.mark.parametrize("m,n,k", [(8192, 1024, 896), (5000, 1500, 700), (19000, 700, 260), (2500, 4000, 1000), (12000, 130, 2000)])
+def test_both_gradients_in_one_launch(m, n, k):
+    """More tiles of 256 x 256 than the GPU takes at a time, of products of different lengths."""
+    b = Block(m, n, k, "bf16", "relu", seed=m)
+    b.backward()
+    b.check_backward()
+
+
 @pytest.mark.parametrize("m", [4, 300])
 def test_gradients_one_by_one(m):
     for dx, dw in ((True, False), (False, True), (False, False)):
