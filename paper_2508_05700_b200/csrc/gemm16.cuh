@@ -47,7 +47,8 @@ struct Shape {
   static constexpr uint32_t out_at = stages * stage_bytes;
   static constexpr uint32_t smem = out_at + 8 * warp_out + 1024;  // + room to align to 1024
   static constexpr int width = dual ? TN / 2 : TN;                // output columns of a tile
-  static constexpr uint32_t tmem_cols = 2 * TN;
+  static constexpr bool precise = MODE == kPair || MODE == kPairOut;  // several sums of a part of k each (Params::sums)
+  static constexpr uint32_t tmem_cols = precise ? 512 : 2 * TN;
   static_assert(tmem_cols <= 512 && stages >= 4, "tensor memory, stages");
   static_assert((uint32_t)stages * stage_bytes >= 128u * TN * 4, "the ring holds a tile of sums");
   // the 16 bytes `q` of row `row` of a piece, where the bulk copy's swizzle expects them
@@ -64,7 +65,7 @@ struct Maps {
 struct Part {
   int64_t m, n;             // rows and columns of the result (units, where dual)
   uint32_t m_tiles, n_tiles;
-  uint32_t kb, iters;       // blocks of k per segment; of all segments
+  uint32_t kb, segs, iters; // blocks of k per segment; of all segments
   uint32_t tail;            // instructions (k = 16) in the last block of a segment
   uint32_t a_mn, b_mn;      // MN-major operands
   uint32_t inst;            // instruction descriptor
@@ -78,6 +79,7 @@ struct Params {
   uint32_t heavy, later;    // kOutTwo: see Walk
   uint32_t band;            // tiles of rows that are walked through together, so that the blocks at work share operands in L2
   uint32_t split;
+  uint32_t sums, buffers;   // accumulators of a tile, each of its part of k; tiles that are in tensor memory at a time
   uint32_t sym;             // the result is symmetric: tiles on and below the diagonal alone, each written to both of its places
   uint32_t act;
   uint32_t bulk;            // bit o: rows of output o start on 16-byte boundaries; bit 4 + o: ... and may be written up to one (bulk copies
@@ -361,8 +363,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   constexpr bool kTwo = MODE == kOutTwo;
   const uint32_t first = blockIdx.x / members;
   const Walk<kTwo> walk(p, first, gridDim.x / members);
-  auto share_begin = [&](const Part& q) { return (uint32_t)((uint64_t)q.iters * part / p.split); };  // this block's share of k
-  auto share_end = [&](const Part& q) { return (uint32_t)((uint64_t)q.iters * (part + 1) / p.split); };
+  auto share_begin = [&](const Part& q) { return (uint32_t)((uint64_t)q.kb * part / p.split); };  // this block's share of k, in each segment
+  auto share_end = [&](const Part& q) { return (uint32_t)((uint64_t)q.kb * (part + 1) / p.split); };
 
   uint64_t filled = 0;  // stages that this lane has asked for
   bool issues = false;  // this lane issues the products
@@ -376,8 +378,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
         const Part& q = p.part[kTwo ? w.part : 0];
         const uint32_t k0 = share_begin(q), k1 = share_end(q);
         const int32_t row = (int32_t)((w.tm * CTAS + half) * 128);
-        uint32_t seg = k0 / q.kb, kk = k0 - seg * q.kb;
-        for (uint32_t i = k0; i < k1; ++i) {
+        uint32_t seg = 0, kk = k0;
+        for (uint32_t i = (k1 - k0) * q.segs; i > 0; --i) {
           if (!(ok = bar_sleep(empty(st), phase, &dead))) break;
           // tiles and blocks of k outside their matrix read as 0
           if (!MFET_INSIDE(p.status, seg < 3 && w.z < 2 && (int64_t)row < q.m + 128 && w.tn < q.n_tiles)) {
@@ -416,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
           }
           ++filled;
           if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-          if (++kk == q.kb) kk = 0, ++seg;
+          if (++kk == k1) kk = k0, ++seg;
         }
       }
     }
@@ -429,32 +431,39 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
         const Part& q = p.part[kTwo && t >= p.tiles0 ? 1 : 0];
         const uint32_t k0 = share_begin(q), k1 = share_end(q);
         const uint32_t a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
-        const int acc = done & 1;
-        if (done >= 2 && !(ok = bar_wait(acc_empty(acc), (done / 2 - 1) & 1, &dead))) break;
+        const uint32_t acc = done % p.buffers;
+        if (done >= p.buffers && !(ok = bar_wait(acc_empty(acc), (done / p.buffers - 1) & 1, &dead))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + acc * TN;
-        uint32_t kk = k0 % q.kb;
-        for (uint32_t i = k0; i < k1; ++i) {
+        const uint32_t len = k1 - k0, sums = G::precise ? min(p.sums, len) : 1u;
+        uint32_t kk = k0, left = len * q.segs, sum = 0, fresh = 1, of_sum = 0;  // fresh: nothing has been added to this sum yet
+        for (uint32_t i = 0; left > 0; ++i) {
           if (!ready && !(ok = bar_wait(full(st), phase, &dead))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = base + st * G::stage_bytes;
           const uint32_t this_empty = empty(st);
           const uint32_t a_lo = desc_lo(at, q.a_mn), b_lo = desc_lo(at + G::a_bytes, q.b_mn);
+          const uint32_t d = tmem + (acc * (G::precise ? p.sums : 1u) + sum) * TN, add = !fresh;
+          const bool last = kk + 1 == q.kb;
           if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-          const bool last = ++kk == q.kb;
-          if (last) kk = 0;
           if (!last || q.tail == 4) {
-            mma16<CTAS>(d, a_lo, b_lo, q.inst, i != k0);
+            mma16<CTAS>(d, a_lo, b_lo, q.inst, add);
             mma16<CTAS>(d, a_lo + a_step, b_lo + b_step, q.inst, 1);
             ready = bar_try(full(st), phase);
             mma16<CTAS>(d, a_lo + 2 * a_step, b_lo + 2 * b_step, q.inst, 1);
             mma16<CTAS>(d, a_lo + 3 * a_step, b_lo + 3 * b_step, q.inst, 1);
           } else {
-            for (uint32_t j = 0; j < q.tail; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, q.inst, (i != k0) | j);
+            for (uint32_t j = 0; j < q.tail; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, q.inst, add | j);
             ready = bar_try(full(st), phase);
           }
           commit<CTAS>(this_empty, pair_mask);
-          if (i + 1 == k1) commit<CTAS>(acc_full(acc), pair_mask);
+          if (--left == 0) commit<CTAS>(acc_full(acc), pair_mask);
+          fresh = 0;
+          ++kk;
+          if constexpr (G::precise) {
+            of_sum += sums;  // block kk - k0 belongs to sum (kk - k0) * sums / len
+            if (of_sum >= len) of_sum -= len, ++sum, fresh = i + 1 < len;
+          }
+          if (kk == k1) kk = k0, sum = 0, of_sum = 0;
         }
       }
     }
@@ -574,6 +583,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   if (warp >= 2) {
     uint32_t done = 0;
     Row32 next[kBesides];
+    const uint32_t sums = G::precise ? min(p.sums, share_end(p.part[0]) - share_begin(p.part[0])) : 1u;
+    auto sums_of = [&](uint32_t at, uint32_t* r) {  // 32 columns of a tile: its sums in their order
+      tmem_load32(at, r);
+      if constexpr (G::precise) {
+        for (uint32_t z = 1; z < sums; ++z) {
+          uint32_t t[32];
+          tmem_load32(at + z * TN, t);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(t[j]));
+        }
+      }
+    };
     auto row_of = [&](const Tile& w) { return (int64_t)(w.tm * CTAS + half) * 128 + quarter * 32; };
     if (p.split == 1 && first < p.tiles) {
       const Tile w = tile_at<false>(p, first);
@@ -582,17 +603,17 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
     for (uint32_t t = walk(0); t < p.tiles; t = walk(++done)) {
       const Tile w = tile_at<kTwo>(p, t);
       if constexpr (kTwo) q = &p.part[w.part];
-      const int acc = done & 1;
+      const uint32_t acc = done % p.buffers;
       const int64_t i0 = row_of(w), j0 = (int64_t)w.tn * G::width;
-      const uint32_t from = tmem + acc * TN + ((uint32_t)(quarter * 32) << 16);
-      const bool ok = bar_sleep(acc_full(acc), (done / 2) & 1, &dead);
+      const uint32_t from = tmem + acc * (G::precise ? p.sums : 1u) * TN + ((uint32_t)(quarter * 32) << 16);
+      const bool ok = bar_sleep(acc_full(acc), (done / p.buffers) & 1, &dead);
       if (!__all_sync(kAllLanes, ok)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (p.split > 1) {  // one tile per block: its sums go to shared memory, where the ring was
 #pragma unroll 1
         for (int c = 32 * second; c < TN; c += 64) {
           uint32_t r[32];
-          tmem_load32(from + c, r);
+          sums_of(from + c, r);
 #pragma unroll
           for (int j = 0; j < 32; j += 4)
             *reinterpret_cast<uint4*>(smem + (((c + j) >> 2) * 128 + quarter * 32 + lane) * 16) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
@@ -603,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       for (int c = 32 * second; c < G::width; c += 64) {
         uint32_t r[32], r2[32];
         float x[32];
-        tmem_load32(from + c, r);
+        sums_of(from + c, r);
         if constexpr (G::dual) tmem_load32(from + G::width + c, r2);
         got(next, x);
         if (c + 64 < G::width) {
@@ -724,6 +745,7 @@ struct Problem {
   int64_t k[2] = {0, 0};                  // of one segment, of each product
   int segs[2] = {1, 1}, results[2] = {1, 0};  // results of the second product: 0 where there is one product alone
   uint32_t out_dtype = MFET_F16;
+  bool precise = false;                   // the two-word modes: for a result in fp32
   Params p = {};                          // sizes, majors and segments' operands of the products, epilogue
 };
 
@@ -762,7 +784,8 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
     x.m_tiles = (uint32_t)((x.m + CTAS * 128 - 1) / (CTAS * 128));
     x.n_tiles = (uint32_t)((x.n + G::width - 1) / G::width);
     x.kb = (uint32_t)((q.k[i] + kSlab - 1) / kSlab);
-    x.iters = x.kb * (uint32_t)q.segs[i];
+    x.segs = (uint32_t)q.segs[i];
+    x.iters = x.kb * x.segs;
     x.tail = (uint32_t)((q.k[i] - (int64_t)(x.kb - 1) * kSlab + 15) / 16);
     x.inst = (1u << 4) | (fmt << 7) | (fmt << 10) | (x.a_mn << 15) | (x.b_mn << 16) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(CTAS * 128 >> 4) << 24);
     p.tiles += (uint32_t)tiles_of(q, i, CTAS * 128, G::width);
@@ -774,6 +797,18 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return MFET_ERR_CUDA;
   const uint32_t members = CTAS * split, at_once = (uint32_t)clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, members, G::smem);
   const uint32_t clusters = split > 1 || p.tiles < at_once ? p.tiles : at_once;
+  p.sums = 1;
+  p.buffers = 2;
+  if (G::precise) {
+    // The tensor cores truncate a sum at every instruction. A sum of n instructions that grows evenly loses 0.18 n 2^-23 of what it ends at, on
+    // average over where it stands between two powers of two. Several sums of a part of k each, added up in fp32, lose as many times less; what
+    // they lose on average is put back. Results in fp32 are worth waiting with the next tile until one is written.
+    const bool one_tile = clusters == p.tiles;
+    p.buffers = one_tile || q.precise ? 1 : 2;
+    p.sums = 512 / TN / p.buffers;
+    const double len = (double)p.part[0].kb / split, of = len < p.sums ? len : p.sums;
+    p.beta = (float)(p.beta * (1.0 + 0.18 * 0x1p-23 * 4.0 * len / of));
+  }
   if (MODE == kOutTwo) {
     p.heavy = p.tiles0 % clusters;
     p.later = p.heavy ? rounds_later(p.part[0].iters, p.part[1].iters) : 0;
@@ -826,14 +861,14 @@ int64_t clusters_at_once(K kernel, uint32_t members, uint32_t smem) {
 template <int CTAS, int TN, int MODE, int DT>
 double cost(const Problem& q, uint32_t split) {
   using G = Shape<CTAS, TN, MODE, DT>;
-  const int64_t iters = iters_of(q, 0);
-  if (split > 1 && (split * CTAS > 8 || split * 32 > (uint32_t)G::width || (int64_t)split > iters)) return 1e300;
+  const int64_t kb = (q.k[0] + kSlab - 1) / kSlab;
+  if (split > 1 && (split * CTAS > 8 || split * 32 > (uint32_t)G::width || (int64_t)split > kb)) return 1e300;
   const int64_t tiles = tiles_of(q, 0, CTAS * 128, G::width);
   static std::atomic<uint64_t> ready{0};
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
   const int64_t at_once = clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, CTAS * split, G::smem), waves = (tiles + at_once - 1) / at_once;
   if (split > 1 && waves > 1) return 1e300;
-  return (CTAS == 2 ? 6.9 : 4.2) + (double)waves * ((iters + split - 1) / split) * (CTAS == 2 ? 0.325 : 0.25) + (split == 1 ? 0.0 : split == 2 ? 3.0 : 6.0);
+  return (CTAS == 2 ? 6.9 : 4.2) + (double)waves * ((kb + split - 1) / split) * q.segs[0] * (CTAS == 2 ? 0.325 : 0.25) + (split == 1 ? 0.0 : split == 2 ? 3.0 : 6.0);
 }
 
 // The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 6.9 for pairs, 4.2

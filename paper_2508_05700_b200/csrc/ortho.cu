@@ -6,7 +6,8 @@
 // values, and the errors in their directions, by a (3.4 in the usual schedule, some 480 in five steps): with operands of one 16-bit
 // word the result is off by 1e-3 (fp16) to 1e-2 (bf16) of its size. So X, A and B = b A + c A A are held as the sum of two fp16 words
 // (22 bits and more, under a power of two for each matrix that keeps its bound, known to the host, inside fp16's range), a product is three
-// (high x high, high x low, low x high) in one fp32 accumulator, and the result is as near as one computed in fp32.
+// (high x low, low x high, then high x high: the tensor cores truncate a sum after
+// every 16 products, by a part of what it is by then) in one fp32 accumulator, and the result is as near as one computed in fp32.
 #include <cmath>
 
 #include "gemm16.cuh"
@@ -216,14 +217,17 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  // accumulators of X X^T and A A: two of half of k each (what a sum loses to truncation grows with its length); of B X: two where they fit
   const uint32_t tmem = tmem_slot, acc_x = tmem + 128;
+  constexpr uint32_t kSecondA = 384, kSecondX = 128;
   early_launch_wait();
 
   // this block's columns of X, in whole blocks of 64
   const int64_t all = (p.long_side + 63) / 64;
   const int64_t c0 = all * rank / slices * 64;
   const int width = (int)((all * (rank + 1) / slices) * 64 - c0);
-  const int d16 = (p.d + 15) & ~15;
+  const int d16 = (p.d + 15) & ~15, half_d = (d16 / 16 + 1) / 2;  // instructions of the first sum over the short side
+  const bool two_d = d16 > 16, two_x = two_d && width <= (int)128;
 
   // squares of the slice, then of all of G; 8 neighbouring columns of a row at a time
   double s = 0.0;
@@ -277,6 +281,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     phase ^= 1;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   };
+  auto sums_of = [&](uint32_t at, uint32_t second, bool two, uint32_t* r) {
+    tmem_load32(at, r);
+    if (two) {
+      uint32_t t[32];
+      tmem_load32(at + second, t);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(t[j]));
+    }
+  };
   const uint32_t inst_a = (1u << 4) | ((uint32_t)(d16 >> 3) << 17) | (8u << 24);
   const uint32_t inst_x = (1u << 4) | (1u << 16) | ((uint32_t)(width >> 3) << 17) | (8u << 24);
   const uint32_t xs[2] = {base, base + kXLo}, as[2] = {base + kAHi, base + kALo};
@@ -291,12 +304,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     // A = X X^T over the slice
     if (warp == 0) {
       if (elect_one()) {
-        uint32_t any = 0;
-        for (int t = 0; t < 3; ++t) {  // high x high, high x low, low x high
-          const uint32_t a = xs[t == 2], b = xs[t == 1];
-          for (int q = 0; q < width / 16; ++q, any = 1) {
-            const uint32_t off = (uint32_t)(q >> 2) * kBlock + (q & 3) * 32;
-            mma_small(tmem, desc_lo(a + off, 0), desc_lo(b + off, 0), kDescHi, inst_a, any);
+        for (int t = 0; t < 3; ++t) {  // high x low, low x high, high x high
+          const uint32_t a = xs[t == 1], b = xs[t == 0];
+          for (int q = 0; q < width / 16; ++q) {
+            const uint32_t off = (uint32_t)(q >> 2) * kBlock + (q & 3) * 32, z = q >= width / 32;
+            mma_small(tmem + z * kSecondA, desc_lo(a + off, 0), desc_lo(b + off, 0), kDescHi, inst_a, t || (q && q != width / 32));
           }
         }
         mma_commit(bar);
@@ -308,7 +320,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
 #pragma unroll 1
       for (int c = 32 * turn; c < d16; c += 128) {
         uint32_t r[32];
-        tmem_load32(tmem + lanes + c, r);
+        sums_of(tmem + lanes + c, kSecondA, true, r);
         float* v = reinterpret_cast<float*>(r);
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] *= k.a_beta;
@@ -323,7 +335,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
 #pragma unroll 1
       for (int c = 32 * turn; c < d16; c += 128) {
         uint32_t r[32];
-        tmem_load32(tmem + lanes + c, r);
+        sums_of(tmem + lanes + c, kSecondA, true, r);
 #pragma unroll
         for (int j = 0; j < 32; j += 4)
           *reinterpret_cast<uint4*>(smem + kAHi + (((c + j) >> 2) * 128 + row) * 16) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
@@ -373,12 +385,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     // A A, A being symmetric
     if (warp == 0) {
       if (elect_one()) {
-        uint32_t any = 0;
         for (int t = 0; t < 3; ++t) {
-          const uint32_t a = as[t == 2], b = as[t == 1];
-          for (int q = 0; q < d16 / 16; ++q, any = 1) {
-            const uint32_t off = (uint32_t)(q >> 2) * kBlock + (q & 3) * 32;
-            mma_small(tmem, desc_lo(a + off, 0), desc_lo(b + off, 0), kDescHi, inst_a, any);
+          const uint32_t a = as[t == 1], b = as[t == 0];
+          for (int q = 0; q < d16 / 16; ++q) {
+            const uint32_t off = (uint32_t)(q >> 2) * kBlock + (q & 3) * 32, z = q >= half_d;
+            mma_small(tmem + z * kSecondA, desc_lo(a + off, 0), desc_lo(b + off, 0), kDescHi, inst_a, t || (q && q != half_d));
           }
         }
         mma_commit(bar);
@@ -390,7 +401,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
 #pragma unroll 1
     for (int c = 32 * turn; c < d16; c += 128) {
       uint32_t r[32];
-      tmem_load32(tmem + lanes + c, r);
+      sums_of(tmem + lanes + c, kSecondA, two_d, r);
 #pragma unroll
       for (int j = 0; j < 32; j += 8) {
         if (c + j >= d16) break;
@@ -406,12 +417,12 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     // B X
     if (warp == 0) {
       if (elect_one()) {
-        uint32_t any = 0;
         for (int t = 0; t < 3; ++t) {
-          const uint32_t a = as[t == 2], b = xs[t == 1];
-          for (int q = 0; q < d16 / 16; ++q, any = 1) {
-            const uint32_t b_lo = (((b + q * 2048) & 0x3FFFFu) >> 4) | ((kBlock >> 4) << 16);
-            mma_small(acc_x, desc_lo(a + (uint32_t)(q >> 2) * kBlock + (q & 3) * 32, 0), b_lo, kDescHi, inst_x, any);
+          const uint32_t a = as[t == 1], b = xs[t == 0];
+          for (int q = 0; q < d16 / 16; ++q) {
+            const uint32_t b_lo = (((b + q * 2048) & 0x3FFFFu) >> 4) | ((kBlock >> 4) << 16), z = two_x && q >= half_d;
+            mma_small(acc_x + z * kSecondX, desc_lo(a + (uint32_t)(q >> 2) * kBlock + (q & 3) * 32, 0), b_lo, kDescHi, inst_x,
+                      t || (q && !(two_x && q == half_d)));
           }
         }
         mma_commit(bar);
@@ -423,7 +434,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
 #pragma unroll 1
     for (int c = 32 * turn; c < width; c += 128) {
       uint32_t r[32];
-      tmem_load32(acc_x + lanes + c, r);
+      sums_of(acc_x + lanes + c, kSecondX, two_x, r);
 #pragma unroll
       for (int j = 0; j < 32; j += 8) {
         const uint32_t at = words_offset(row, c + j);
@@ -533,8 +544,8 @@ void three(Problem* q, const Words& a, const Words& b, int64_t k) {
   q->a[0] = a.hi, q->a[1] = a.lo, q->n_a = 2;
   q->b[0] = b.hi, q->b[1] = b.lo, q->n_b = 2;
   q->segs[0] = 3;
-  q->p.part[0].seg_a = 0x100;  // high, high, low
-  q->p.part[0].seg_b = 0x010;  // high, low, high
+  q->p.part[0].seg_a = 0x010;  // high, low, high
+  q->p.part[0].seg_b = 0x001;  // low, high, high
   q->k[0] = k;
 }
 
@@ -612,11 +623,13 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
       const float* c = coefficients ? coefficients + 3 * i : kUsual;
       const int ea = exponent_for(s[i] * s[i]), eb = exponent_for(b_most[i]), next = exponent_for(s[i + 1]);
       const bool last = i + 1 == steps;
-      q.step[i].a_beta = (float)std::ldexp(1.0, ea - 2 * ex);
+      // what the tensor cores' sums lose on average is put back (see launch in gemm16.cuh): sums of a slice, then of the short side
+      const double lost = 0.18 * 0x1p-23, of_l = 1.0 + lost * (double)(l / 32 / q.slices), of_d = 1.0 + lost * (double)(d / 32);
+      q.step[i].a_beta = (float)std::ldexp(of_l, ea - 2 * ex);
       q.step[i].b_alpha = (float)std::ldexp((double)c[1], eb - ea);
-      q.step[i].b_beta = (float)std::ldexp((double)c[2], eb - 2 * ea);
+      q.step[i].b_beta = (float)std::ldexp(of_d * c[2], eb - 2 * ea);
       q.step[i].x_alpha = (float)std::ldexp(last ? (double)c[0] * scale : (double)c[0], (last ? 0 : next) - ex);
-      q.step[i].x_beta = (float)std::ldexp(last ? (double)scale : 1.0, (last ? 0 : next) - eb - ex);
+      q.step[i].x_beta = (float)std::ldexp(of_d * (last ? (double)scale : 1.0), (last ? 0 : next) - eb - ex);
       ex = next;
     }
     return dtype == MFET_F32 ? launch_small<MFET_F32>(q, st) : dtype == MFET_F16 ? launch_small<MFET_F16>(q, st) : launch_small<MFET_BF16>(q, st);
@@ -652,6 +665,7 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
     a.e = exponent_for(s[i] * s[i]);
     Problem q;
     q.p.status = status;
+    q.precise = out_dtype == MFET_F32;
     three(&q, from, from, tall ? rows : cols);
     q.p.part[0].a_mn = q.p.part[0].b_mn = tall;
     q.a_mn = q.b_mn = tall ? 3 : 0;
@@ -664,6 +678,7 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
     b.e = exponent_for(b_most[i]);
     q = Problem();
     q.p.status = status;
+    q.precise = out_dtype == MFET_F32;
     three(&q, a, a, d);
     q.p.sym = 1;
     combine(&q, &a, c[1], c[2], a.e, a.e, b.e);
@@ -673,6 +688,7 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
     // X = a X + B X, or a X + X B, B being symmetric
     q = Problem();
     q.p.status = status;
+    q.precise = out_dtype == MFET_F32;
     if (tall) three(&q, from, b, d);
     else three(&q, b, from, d);
     q.p.part[0].b_mn = !tall;
