@@ -38,16 +38,19 @@ struct Shape {
   static constexpr bool dual = MODE == kGated || MODE == kGatedBack;  // half of the columns of B come from a second matrix
   static constexpr int outs = MODE == kGatedBack || MODE == kPair ? 2 : 1;
   static constexpr int b_rows = TN / CTAS;
-  static constexpr uint32_t a_bytes = 128 * 128, b_bytes = b_rows * 128, stage_bytes = a_bytes + b_bytes;
-  // Results leave in pieces of 32 rows x 32 columns; a warp has room for two of each output
+  static constexpr bool precise = MODE == kPair || MODE == kPairOut;  // two words each; several sums of a part of k each (Params::sums)
+  // With few columns the loads' latency is what a block of k takes: both words of both operands come together, and serve the three products
+  static constexpr bool fused = precise && TN == 64;
+  static constexpr uint32_t a_bytes = 128 * 128, b_bytes = b_rows * 128, stage_bytes = (a_bytes + b_bytes) * (fused ? 2 : 1);
+  // Results leave in pieces of 32 rows x 32 columns; a warp has room for two of each output, or for the one that it has of a tile of 64 columns
+  static constexpr int turns = TN == 64 ? 1 : 2;
   static constexpr int piece_row = 32 * (int)sizeof(typename Elem<DT>::T);
   static constexpr uint32_t piece = 32 * piece_row;
-  static constexpr uint32_t warp_out = 2 * outs * piece;
+  static constexpr uint32_t warp_out = turns * outs * piece;
   static constexpr int stages = (int)((226u * 1024 - 1024 - 8 * warp_out) / stage_bytes);
   static constexpr uint32_t out_at = stages * stage_bytes;
   static constexpr uint32_t smem = out_at + 8 * warp_out + 1024;  // + room to align to 1024
   static constexpr int width = dual ? TN / 2 : TN;                // output columns of a tile
-  static constexpr bool precise = MODE == kPair || MODE == kPairOut;  // several sums of a part of k each (Params::sums)
   static constexpr uint32_t tmem_cols = precise ? 512 : 2 * TN;
   static_assert(tmem_cols <= 512 && stages >= 4, "tensor memory, stages");
   static_assert((uint32_t)stages * stage_bytes >= 128u * TN * 4, "the ring holds a tile of sums");
@@ -365,6 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   const Walk<kTwo> walk(p, first, gridDim.x / members);
   auto share_begin = [&](const Part& q) { return (uint32_t)((uint64_t)q.kb * part / p.split); };  // this block's share of k, in each segment
   auto share_end = [&](const Part& q) { return (uint32_t)((uint64_t)q.kb * (part + 1) / p.split); };
+  // sums of a tile that are each of a part of `len` blocks of k (one more holds the products with low words, where they come together)
+  auto sums_for = [&](uint32_t len) { return G::precise ? min(p.sums - (G::fused ? 1u : 0u), len) : 1u; };
 
   uint64_t filled = 0;  // stages that this lane has asked for
   bool issues = false;  // this lane issues the products
@@ -379,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
         const uint32_t k0 = share_begin(q), k1 = share_end(q);
         const int32_t row = (int32_t)((w.tm * CTAS + half) * 128);
         uint32_t seg = 0, kk = k0;
-        for (uint32_t i = (k1 - k0) * q.segs; i > 0; --i) {
+        for (uint32_t i = (k1 - k0) * (G::fused ? 1 : q.segs); i > 0; --i) {
           if (!(ok = bar_sleep(empty(st), phase, &dead))) break;
           // tiles and blocks of k outside their matrix read as 0
           if (!MFET_INSIDE(p.status, seg < 3 && w.z < 2 && (int64_t)row < q.m + 128 && w.tn < q.n_tiles)) {
@@ -390,30 +395,41 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
           const uint32_t at = base + st * G::stage_bytes;
           const uint32_t bar = CTAS == 1 ? full(st) : peer_addr(full(st), leader);
           if (half == 0) bar_expect(full(st), CTAS * G::stage_bytes);
-          const CUtensorMap* a = &maps.a[((q.seg_a >> (4 * seg)) & 15u) + w.z];
           const int32_t k = (int32_t)(kk * kSlab);
-          if (q.a_mn) {
-            tile_load<CTAS>(at, a, row, k, bar);
-            tile_load<CTAS>(at + 8192, a, row + 64, k, bar);
-          } else {
-            tile_load<CTAS>(at, a, k, row, bar);
-          }
-          if constexpr (G::dual) {
-            const int32_t unit = (int32_t)(w.tn * G::width);
-            if constexpr (CTAS == 2) {
-              tile_load<CTAS>(at + G::a_bytes, &maps.b[half], k, unit, bar);
+          auto load_a = [&](const CUtensorMap* a, uint32_t to) {
+            if (q.a_mn) {
+              tile_load<CTAS>(to, a, row, k, bar);
+              tile_load<CTAS>(to + 8192, a, row + 64, k, bar);
             } else {
-              tile_load<CTAS>(at + G::a_bytes, &maps.b[0], k, unit, bar);
-              tile_load<CTAS>(at + G::a_bytes + G::b_bytes / 2, &maps.b[1], k, unit, bar);
+              tile_load<CTAS>(to, a, k, row, bar);
             }
-          } else {
-            const CUtensorMap* b = &maps.b[(q.seg_b >> (4 * seg)) & 15u];
+          };
+          auto load_b = [&](const CUtensorMap* b, uint32_t to) {
             const int32_t col = (int32_t)(w.tn * TN + half * G::b_rows);
             if (q.b_mn) {
 #pragma unroll
-              for (int j = 0; j < G::b_rows / 64; ++j) tile_load<CTAS>(at + G::a_bytes + 8192 * j, b, col + 64 * j, k, bar);
+              for (int j = 0; j < G::b_rows / 64; ++j) tile_load<CTAS>(to + 8192 * j, b, col + 64 * j, k, bar);
             } else {
-              tile_load<CTAS>(at + G::a_bytes, b, k, col, bar);
+              tile_load<CTAS>(to, b, k, col, bar);
+            }
+          };
+          if constexpr (G::fused) {
+            load_a(&maps.a[0], at);
+            load_a(&maps.a[1], at + G::a_bytes);
+            load_b(&maps.b[0], at + 2 * G::a_bytes);
+            load_b(&maps.b[1], at + 2 * G::a_bytes + G::b_bytes);
+          } else {
+            load_a(&maps.a[((q.seg_a >> (4 * seg)) & 15u) + w.z], at);
+            if constexpr (G::dual) {
+              const int32_t unit = (int32_t)(w.tn * G::width);
+              if constexpr (CTAS == 2) {
+                tile_load<CTAS>(at + G::a_bytes, &maps.b[half], k, unit, bar);
+              } else {
+                tile_load<CTAS>(at + G::a_bytes, &maps.b[0], k, unit, bar);
+                tile_load<CTAS>(at + G::a_bytes + G::b_bytes / 2, &maps.b[1], k, unit, bar);
+              }
+            } else {
+              load_b(&maps.b[(q.seg_b >> (4 * seg)) & 15u], at + G::a_bytes);
             }
           }
           ++filled;
@@ -434,18 +450,24 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
         const uint32_t acc = done % p.buffers;
         if (done >= p.buffers && !(ok = bar_wait(acc_empty(acc), (done / p.buffers - 1) & 1, &dead))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t len = k1 - k0, sums = G::precise ? min(p.sums, len) : 1u;
-        uint32_t kk = k0, left = len * q.segs, sum = 0, fresh = 1, of_sum = 0;  // fresh: nothing has been added to this sum yet
+        const uint32_t len = k1 - k0, sums = sums_for(len);
+        uint32_t kk = k0, left = len * (G::fused ? 1 : q.segs), sum = 0, fresh = 1, of_sum = 0;  // fresh: nothing has been added to this sum yet
         for (uint32_t i = 0; left > 0; ++i) {
           if (!ready && !(ok = bar_wait(full(st), phase, &dead))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = base + st * G::stage_bytes;
           const uint32_t this_empty = empty(st);
-          const uint32_t a_lo = desc_lo(at, q.a_mn), b_lo = desc_lo(at + G::a_bytes, q.b_mn);
-          const uint32_t d = tmem + (acc * (G::precise ? p.sums : 1u) + sum) * TN, add = !fresh;
+          const uint32_t a_lo = desc_lo(at, q.a_mn), b_lo = desc_lo(at + (G::fused ? 2 : 1) * G::a_bytes, q.b_mn);
+          const uint32_t first_sum = tmem + acc * (G::precise ? p.sums : 1u) * TN, d = first_sum + sum * TN, add = !fresh;
           const bool last = kk + 1 == q.kb;
           if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-          if (!last || q.tail == 4) {
+          if constexpr (G::fused) {  // high x low, low x high to a sum of their own, high x high to this part's
+            const uint32_t steps = last ? q.tail : 4u, low = first_sum + sums * TN, a2 = a_lo + (G::a_bytes >> 4), b2 = b_lo + (G::b_bytes >> 4);
+            for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(low, a_lo + j * a_step, b2 + j * b_step, q.inst, i | j);
+            for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(low, a2 + j * a_step, b_lo + j * b_step, q.inst, 1);
+            ready = bar_try(full(st), phase);
+            for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, q.inst, add | j);
+          } else if (!last || q.tail == 4) {
             mma16<CTAS>(d, a_lo, b_lo, q.inst, add);
             mma16<CTAS>(d, a_lo + a_step, b_lo + b_step, q.inst, 1);
             ready = bar_try(full(st), phase);
@@ -512,12 +534,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
     }
   };
   auto put_begin = [&]() {  // what the memory of the pieces held before has left
-    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(G::turns - 1) : "memory");
     __syncwarp();
   };
   auto put_end = [&]() {
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-    turn ^= 1;
+    if (G::turns == 2) turn ^= 1;
   };
   // what becomes of 32 columns of the accumulator (and of the same units' other half, where dual): x is what c0 (c1) held there
   auto finish = [&](float* v, float* u, float* x, int z, int64_t i0, int64_t j1, bool mirror) {
@@ -583,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   if (warp >= 2) {
     uint32_t done = 0;
     Row32 next[kBesides];
-    const uint32_t sums = G::precise ? min(p.sums, share_end(p.part[0]) - share_begin(p.part[0])) : 1u;
+    const uint32_t sums = sums_for(share_end(p.part[0]) - share_begin(p.part[0])) + (G::fused ? 1 : 0);
     auto sums_of = [&](uint32_t at, uint32_t* r) {  // 32 columns of a tile: its sums in their order
       tmem_load32(at, r);
       if constexpr (G::precise) {
@@ -806,7 +828,7 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
     const bool one_tile = clusters == p.tiles;
     p.buffers = one_tile || q.precise ? 1 : 2;
     p.sums = 512 / TN / p.buffers;
-    const double len = (double)p.part[0].kb / split, of = len < p.sums ? len : p.sums;
+    const double len = (double)p.part[0].kb / split, most = p.sums - (G::fused ? 1 : 0), of = len < most ? len : most;
     p.beta = (float)(p.beta * (1.0 + 0.18 * 0x1p-23 * 4.0 * len / of));
   }
   if (MODE == kOutTwo) {
@@ -868,12 +890,15 @@ double cost(const Problem& q, uint32_t split) {
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
   const int64_t at_once = clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, CTAS * split, G::smem), waves = (tiles + at_once - 1) / at_once;
   if (split > 1 && waves > 1) return 1e300;
-  return (CTAS == 2 ? 6.9 : 4.2) + (double)waves * ((kb + split - 1) / split) * q.segs[0] * (CTAS == 2 ? 0.325 : 0.25) + (split == 1 ? 0.0 : split == 2 ? 3.0 : 6.0);
+  if (q.p.sym && CTAS * 128 != TN) return 1e300;  // tiles are exchanged with their mirror images
+  return (CTAS == 2 ? 6.9 : TN == 128 ? 4.2 : 3.5) + (double)waves * ((kb + split - 1) / split) * q.segs[0] * (CTAS == 2 ? 0.325 : TN == 128 ? 0.25 : G::fused ? 0.135 : 0.2) + (split == 1 ? 0.0 : split == 2 ? 3.0 : 6.0);
 }
 
 // The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 6.9 for pairs, 4.2
-// for blocks; 64 of k 0.325 for 256 x 256 by a pair, 0.25 for 128 x 128 by a block (its loads bound it); joining two parts 3, four 6.
-// Forward, k = 896, n = 1024: m = 1024 blocks 7.9, pairs 11.4; 8192 blocks 30.4, pairs 25.2. Backward 16384 x 2048 x 4096 1187 by pairs, 1803.
+// for blocks of 128 columns, 3.5 for 64; 64 of k 0.325 for 256 x 256 by a pair, 0.25 for 128 x 128 by a block and 0.2 for 64 columns (its loads
+// bound it), 0.135 in each segment where three segments' tiles come together; joining two parts 3, four 6.
+// Forward, k = 896, n = 1024: m = 1024 blocks 7.9, pairs 11.4; 8192 blocks 30.4, pairs 25.2. Backward 16384 x 2048 x 4096 1187 by pairs, 1803 by
+// blocks. Orthogonalising 512 x 512: 125 with 64 columns, 183 with 128; 2048 x 2048: 538 by pairs, 920 by blocks, 966 with 64 columns.
 // Two products in one launch, by pairs: the microseconds of it, as above
 template <int DT>
 double cost_two(const Problem& q) {
@@ -894,7 +919,7 @@ double cost_two(const Problem& q) {
 // it, 9.2; 2048 x 2048 of 4096: 52, 69).
 struct Choice {
   double cost;
-  int form;  // 0: pairs, 1: blocks
+  int form;  // 0: pairs, 1: blocks, 2: blocks of 64 columns
   uint32_t split, sym;
 };
 template <int MODE, int DT>
@@ -907,6 +932,10 @@ Choice choose(const Problem& q) {
       const double pair = cost<2, 256, MODE, DT>(r, part) + 0.8 * sym, block = cost<1, 128, MODE, DT>(r, part) + 0.8 * sym;
       if (pair < c.cost) c = {pair, 0, part, sym};
       if (block < c.cost) c = {block, 1, part, sym};
+      if constexpr (!Shape<1, 128, MODE, DT>::dual) {
+        const double narrow = cost<1, 64, MODE, DT>(r, part);
+        if (narrow < c.cost) c = {narrow, 2, part, sym};
+      }
     }
   }
   return c;
@@ -919,6 +948,8 @@ template <int MODE, int DT>
 int run(Problem q, cudaStream_t s) {
   const Choice c = choose<MODE, DT>(q);
   q.p.sym = c.sym;
+  if constexpr (!Shape<1, 128, MODE, DT>::dual)
+    if (c.form == 2) return launch<1, 64, MODE, DT>(q, c.split, s);
   return c.form == 0 ? launch<2, 256, MODE, DT>(q, c.split, s) : launch<1, 128, MODE, DT>(q, c.split, s);
 }
 
