@@ -1,6 +1,6 @@
 // The gated linear block h = act(x Wg^T) * (x Wu^T) and its backward pass, 16-bit operands and fp32 sums.
 //
-// Forward: one product whose columns are pairs of a gate and an up unit, the activation and the product of the two on the accumulators.
+// Forward, a few rows: a warp per unit (gated_few_kernel). More: one product whose columns are pairs of a gate and an up unit, the activation and the product of the two on the accumulators.
 // Backward: the same product again (neither G nor U is kept between the passes; computing them costs less memory traffic than storing and
 // reading them would where k is below some 1500, and no training memory), with the gradient of h beside it:
 //   dG = dh * U * act'(G), dU = dh * act(G), rounded to the operands' type (the tensor cores take nothing wider), then
@@ -34,6 +34,140 @@ struct Call {
 };
 
 uint64_t grad_bytes(int64_t m, int64_t n) { return packed_bytes(m, n); }
+
+// ------------------------------------------------------------------ a few rows, forward ----
+
+constexpr int kFewThreads = 256;
+constexpr int kFewMost = 8;                // rows of x
+constexpr uint32_t kFewSmem = 96 * 1024;   // all of x in fp32 has to fit this
+// The most work in multiply-adds, m counted up to a power of two: 2^25, 2^24 for 5 rows and more. (us here and on the tensor cores: 1 x 896 x 1024 3.2
+// and 7.3; at the limit 4 x 2048 x 4096 13.9 and 15.0, 8 x 896 x 1024 5.3 and 7.3; beyond it 8 x 2048 x 2048 15.0 and 11.9.)
+constexpr int64_t kFewWork = 1ll << 25;
+
+struct FewParams {
+  const uint8_t *x, *wg, *wu;
+  uint8_t* h;
+  int64_t x_ld, wg_ld, wu_ld, h_ld, n;
+  const void *x_end, *wg_end, *wu_end;
+  int32_t m, k;
+  uint32_t act;
+};
+
+template <int DT>
+__device__ __forceinline__ float gate_any(uint32_t act, float g) {
+  const float2 v = make_float2(g, g);
+  switch (act) {
+    case MFET_ACT_RELU: return gate2<MFET_ACT_RELU, false>(v, nullptr).x;
+    case MFET_ACT_SILU: return gate2<MFET_ACT_SILU, false>(v, nullptr).x;
+    case MFET_ACT_GELU: return gate2<MFET_ACT_GELU, false>(v, nullptr).x;
+    case MFET_ACT_SIGMOID: return gate2<MFET_ACT_SIGMOID, false>(v, nullptr).x;
+    default: return g;
+  }
+}
+
+// A warp per unit: its lanes read 8 values of the gate's and of the up row at a time (512 bytes of each a warp), the next ones while these are
+// multiplied with the same columns of all MT rows of x, which the block has in shared memory in fp32. Bound by reading the weights (and
+// by the launch): 1 x 896 x 1024, 3.7 MB of weights, 3.2 us, 7.3 on the tensor cores, whose tiles are 128 rows high.
+template <int DT, int MT, bool VEC>
+__global__ void __launch_bounds__(kFewThreads) gated_few_kernel(const __grid_constant__ FewParams p) {
+  using T = typename Elem<DT>::T;
+  extern __shared__ float4 sx[];  // [MT][2][chunks]: the halves of 8 values of a row
+  early_launch_wait();
+  const int lane = threadIdx.x & 31, chunks = (p.k + 255) / 256 * 32;
+  const int64_t first = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5), step = (int64_t)gridDim.x * (kFewThreads / 32);
+  struct Pair {
+    Raw<DT, 8> g, u;
+  };
+  auto fetch = [&](int64_t j, int c, Pair* w) {  // chunk c of unit j; zeros behind the ends
+    const int count = j < p.n ? min(8, p.k - c * 8) : 0;
+    if (count > 0 && MFET_INSIDE(nullptr, c * 8 + count <= p.wg_ld && c * 8 + count <= p.wu_ld)) {
+      w->g = load_any<DT, 8, VEC>(reinterpret_cast<const T*>(p.wg) + j * p.wg_ld + c * 8, count, p.wg, p.wg_end);
+      w->u = load_any<DT, 8, VEC>(reinterpret_cast<const T*>(p.wu) + j * p.wu_ld + c * 8, count, p.wu, p.wu_end);
+    } else {
+      memset(w, 0, sizeof(*w));
+    }
+  };
+  Pair next[2];  // the first weights do not depend on x: they are under way while it is staged
+  fetch(first, lane, &next[0]);
+  fetch(first, lane + 32, &next[1]);
+  for (int i = threadIdx.x; i < MT * chunks; i += kFewThreads) {
+    const int row = i / chunks, c = i - row * chunks;
+    float v[8];
+    const int count = row < p.m ? min(8, p.k - c * 8) : 0;
+    if (count > 0 && MFET_INSIDE(nullptr, c * 8 + count <= p.x_ld))
+      widen_raw<DT, 8>(load_any<DT, 8, VEC>(reinterpret_cast<const T*>(p.x) + row * p.x_ld + c * 8, count, p.x, p.x_end), v);
+    else memset(v, 0, sizeof(v));
+    sx[(row * 2) * chunks + c] = make_float4(v[0], v[1], v[2], v[3]);
+    sx[(row * 2 + 1) * chunks + c] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __syncthreads();
+  for (int64_t j = first; j < p.n; j += step) {
+    float2 g[MT], u[MT];
+#pragma unroll
+    for (int r = 0; r < MT; ++r) g[r] = u[r] = both(0.f);
+    for (int c0 = lane; c0 < chunks; c0 += 64) {
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int c = c0 + 32 * z;
+        if (c >= chunks) break;  // the same for the whole warp
+        float wg[8], wu[8];
+        widen_raw<DT, 8>(next[z].g, wg);
+        widen_raw<DT, 8>(next[z].u, wu);
+        if (c + 64 < chunks) fetch(j, c + 64, &next[z]);
+        else fetch(j + step, lane + 32 * z, &next[z]);
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+          const float4 a = sx[(r * 2) * chunks + c], b = sx[(r * 2 + 1) * chunks + c];
+          const float2 x[4] = {make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            g[r] = fma2(x[q], make_float2(wg[2 * q], wg[2 * q + 1]), g[r]);
+            u[r] = fma2(x[q], make_float2(wu[2 * q], wu[2 * q + 1]), u[r]);
+          }
+        }
+      }
+    }
+    float mine_g = 0.f, mine_u = 0.f;
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+      float a = g[r].x + g[r].y, b = u[r].x + u[r].y;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) {
+        a += __shfl_xor_sync(kAllLanes, a, d);
+        b += __shfl_xor_sync(kAllLanes, b, d);
+      }
+      if (lane == r) mine_g = a, mine_u = b;
+    }
+    if (lane < p.m && MFET_INSIDE(nullptr, j < p.h_ld))
+      reinterpret_cast<T*>(p.h)[lane * p.h_ld + j] = Elem<DT>::from(gate_any<DT>(p.act, mine_g) * mine_u);
+  }
+}
+
+uint32_t few_rows(int64_t m) { return m == 1 ? 1 : m == 2 ? 2 : m <= 4 ? 4 : 8; }
+uint32_t few_smem(int64_t m, int64_t k) { return (uint32_t)((k + 255) / 256 * 32 * few_rows(m) * 32); }
+bool few(int64_t m, int64_t n, int64_t k) {
+  return m <= kFewMost && k <= kFewSmem / 4 && few_smem(m, k) <= kFewSmem && (int64_t)few_rows(m) * n <= (m <= 4 ? kFewWork : kFewWork / 2) / k;
+}
+
+template <int DT, int MT>
+int launch_few(const FewParams& p, bool vec, cudaStream_t s) {
+  static std::atomic<uint64_t> ready[2];
+  const auto kernel = vec ? gated_few_kernel<DT, MT, true> : gated_few_kernel<DT, MT, false>;
+  if (allow_smem(kernel, kFewSmem, &ready[vec]) != cudaSuccess) return MFET_ERR_CUDA;
+  const int64_t want = (p.n + kFewThreads / 32 - 1) / (kFewThreads / 32), most = (int64_t)sm_count() * 4;
+  return launch_early(kernel, (unsigned)(want < most ? want : most), kFewThreads, few_smem(MT, p.k), s, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
+}
+template <int DT>
+int launch_few(const FewParams& p, bool vec, cudaStream_t s) {
+  switch (few_rows(p.m)) {
+    case 1: return launch_few<DT, 1>(p, vec, s);
+    case 2: return launch_few<DT, 2>(p, vec, s);
+    case 4: return launch_few<DT, 4>(p, vec, s);
+    default: return launch_few<DT, 8>(p, vec, s);
+  }
+}
+
+// ------------------------------------------------------------------ products ----
 
 template <int MODE>
 int gates(const Call& c, const Matrix& x, const Matrix& wg, const Matrix& wu, const Matrix* out, int n_out, const Matrix* dh) {
@@ -114,6 +248,13 @@ int mfet_gated_linear(const void* x, uint32_t dtype, int64_t x_ld, int64_t m, co
   const uint64_t need = packing(in, 3);
   if (need && (!scratch || scratch_bytes < need)) return MFET_ERR_WORKSPACE;
   if (need && !aligned(scratch, 16)) return MFET_ERR_ALIGNMENT;
+  if (few(m, n, k)) {
+    const bool vec = on_16(in[0], dtype) && on_16(in[1], dtype) && on_16(in[2], dtype);
+    auto end = [](const Matrix& a) { return (const uint8_t*)a.p + ((a.outer - 1) * a.ld + a.inner) * 2; };
+    const FewParams p{(const uint8_t*)x, (const uint8_t*)w_gate, (const uint8_t*)w_up, (uint8_t*)h, x_ld, wg_ld, wu_ld, h_ld, n,
+                      end(in[0]), end(in[1]), end(in[2]), (int32_t)m, (int32_t)k, act};
+    return dtype == MFET_F16 ? launch_few<MFET_F16>(p, vec, c.stream) : launch_few<MFET_BF16>(p, vec, c.stream);
+  }
   if (packed(in, 3, (uint8_t*)scratch, c.stream) != cudaSuccess) return MFET_ERR_CUDA;
   const Matrix out{h, n, m, h_ld};
   return gates<kGated>(c, in[0], in[1], in[2], &out, 1, nullptr);
