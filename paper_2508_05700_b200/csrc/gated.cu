@@ -199,7 +199,7 @@ int out_product(Problem& q, const Call& c) {
 }
 
 // Both products of the backward pass in one launch, where that takes less time than one after the other: blocks that have no tile of one left
-// go on with the other (8192 x 896 x 1024: 48 us, 58 in two launches). 1: it does not.
+// go on with the other (the backward pass of 8192 x 896 x 1024: 80 us, 84 in two launches). 1: it does not.
 template <int DT>
 int out_products_dt(const Problem& both, const Problem& of_x, const Problem& of_w, cudaStream_t s) {
   return cost_two<DT>(both) < least_cost<kOut, DT>(of_x) + least_cost<kOut, DT>(of_w) ? launch<2, 256, kOutTwo, DT>(both, 1, s) : 1;

@@ -880,6 +880,11 @@ int64_t clusters_at_once(K kernel, uint32_t members, uint32_t smem) {
   return n;
 }
 
+// The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 6.9 for pairs, 4.2
+// for blocks of 128 columns, 3.5 for 64; 64 of k 0.325 for 256 x 256 by a pair, 0.25 for 128 x 128 by a block and 0.2 for 64 columns (its loads
+// bound it), 0.135 in each segment where three segments' tiles come together; joining two parts 3, four 6.
+// Forward, k = 896, n = 1024: m = 1024 blocks 7.9, pairs 11.4; 8192 blocks 30.4, pairs 25.2. Backward 16384 x 2048 x 4096 1187 by pairs, 1803 by
+// blocks. Orthogonalising 512 x 512: 125 with 64 columns, 183 with 128; 2048 x 2048: 538 by pairs, 920 by blocks, 966 with 64 columns.
 template <int CTAS, int TN, int MODE, int DT>
 double cost(const Problem& q, uint32_t split) {
   using G = Shape<CTAS, TN, MODE, DT>;
@@ -894,11 +899,6 @@ double cost(const Problem& q, uint32_t split) {
   return (CTAS == 2 ? 6.9 : TN == 128 ? 4.2 : 3.5) + (double)waves * ((kb + split - 1) / split) * q.segs[0] * (CTAS == 2 ? 0.325 : TN == 128 ? 0.25 : G::fused ? 0.135 : 0.2) + (split == 1 ? 0.0 : split == 2 ? 3.0 : 6.0);
 }
 
-// The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 6.9 for pairs, 4.2
-// for blocks of 128 columns, 3.5 for 64; 64 of k 0.325 for 256 x 256 by a pair, 0.25 for 128 x 128 by a block and 0.2 for 64 columns (its loads
-// bound it), 0.135 in each segment where three segments' tiles come together; joining two parts 3, four 6.
-// Forward, k = 896, n = 1024: m = 1024 blocks 7.9, pairs 11.4; 8192 blocks 30.4, pairs 25.2. Backward 16384 x 2048 x 4096 1187 by pairs, 1803 by
-// blocks. Orthogonalising 512 x 512: 125 with 64 columns, 183 with 128; 2048 x 2048: 538 by pairs, 920 by blocks, 966 with 64 columns.
 // Two products in one launch, by pairs: the microseconds of it, as above
 template <int DT>
 double cost_two(const Problem& q) {
@@ -915,8 +915,8 @@ double cost_two(const Problem& q) {
   return 6.9 + 0.325 * (double)(of_light > of_heavy ? of_light : of_heavy);
 }
 
-// A symmetric result is computed by half where that saves a wave of tiles: writing a tile twice takes 0.8 (256 x 256: 8.2 a product for all of
-// it, 9.2; 2048 x 2048 of 4096: 52, 69).
+// A symmetric result is computed by half where that saves a wave of tiles: writing a tile twice takes 0.8 (orthogonalising 256 x 256 with tiles of
+// 128 columns, one wave either way: 138 by half, 123 without; 4096 x 2048: 833 by half, 985 without).
 struct Choice {
   double cost;
   int form;  // 0: pairs, 1: blocks, 2: blocks of 64 columns

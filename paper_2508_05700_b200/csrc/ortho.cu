@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kSumThreads) scale_kernel(const __grid_constan
 // the 128-byte swizzle, are K-major for X X^T and, the other way round, MN-major for B X. A step: the slice's X X^T, summed over the cluster
 // (each block adds up a share of the columns in the order of the slices and hands it to all), B by every block for itself, and the slice of
 // a X + B X over the old one. What costs is the chain: three products, each waited for, and three turns from tensor memory to shared memory.
-// 48 x 192: 25 us, 97 as seventeen launches.
+// 48 x 192 in five steps: 40 us, 106 as seventeen launches.
 constexpr int kSmallThreads = 512;
 constexpr int kSmallSide = 128, kSlice = 256, kMostSlices = 8;
 constexpr uint32_t kBlock = 128 * 128;                    // 128 rows x 64 columns
