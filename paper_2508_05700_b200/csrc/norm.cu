@@ -191,7 +191,8 @@ struct NormShape {
   static constexpr int per_sm = BACK || W == 16 ? 1 : smem <= 74 * 1024 ? 3 : smem <= 112 * 1024 ? 2 : 1;
   // quads that are full for all threads: no more are taken than rows of a size need (see columns_of)
   static constexpr int sure = W > 1 || NQ == 7 ? 4 : NQ == 8 ? (ALIGNED ? 7 : 4) : NQ == 4 ? (ALIGNED ? 2 : 1) : NQ / 2;
-  static constexpr int x_pieces = (NQ * xs + 3) / 4 + (ALIGNED ? 0 : 1), dy_pieces = (NQ * os + 3) / 4 + (ALIGNED ? 0 : 1);  // that a thread fetches
+  template <int SIZE>
+  static constexpr int pieces = (NQ * SIZE + 3) / 4 + (ALIGNED ? 0 : 1);  // that a thread fetches
   static_assert(smem <= 227 * 1024 - 1024, "shared memory of a block");
   static_assert(W == 1 || groups < 16, "named barriers");
 };
@@ -318,8 +319,8 @@ __global__ void __launch_bounds__((norm_threads<NQ, W, BACK>), BACK || W == 16 ?
   };
   auto request = [&](uint32_t to, bool any, int64_t ahead) {
     if (any && MFET_INSIDE(nullptr, p.cols <= p.x_ld && p.cols <= NQ * tpr * 4)) {
-      fetch(to, x_row + ahead * x_step, p.x, kXs, std::integral_constant<int, S::x_pieces>());
-      if constexpr (BACK) fetch(to + S::x_bytes, dy_row + ahead * dy_step, p.dy, kOs, std::integral_constant<int, S::dy_pieces>());
+      fetch(to, x_row + ahead * x_step, p.x, kXs, std::integral_constant<int, S::template pieces<kXs>>());
+      if constexpr (BACK) fetch(to + S::x_bytes, dy_row + ahead * dy_step, p.dy, kOs, std::integral_constant<int, S::template pieces<kOs>>());
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -616,7 +617,9 @@ struct Columns {
 };
 Columns columns_of(int64_t cols, bool aligned_rows) {
   if (cols > kMostHeld) return {0, 0};
-  if (cols > 1024) return {8, cols <= 2048 ? 2 : cols <= 4096 ? 4 : cols <= 8192 ? 8 : 16};
+  // 6 quads in place of 8: 4099 x 1075, bf16 to fp16 at any address 11.4 us, 12.9; 8192 x 1280 of these types 12.4, 14.9, backward 20.4, 25.2
+  for (int w = 2; w <= 16; w *= 2)
+    if (cols > 512 * w && cols <= 1024 * w) return {w < 16 && cols <= 768 * w ? 6 : 8, w};
   if (cols <= 128) return {1, 1};
   if (cols <= 512) return {aligned_rows && cols <= 256 ? 2 : 4, 1};
   return {aligned_rows && cols <= 896 ? 7 : 8, 1};
@@ -648,8 +651,11 @@ cudaError_t launch_types(const NormParams& p, bool aligned_rows, cudaStream_t s)
       case 20: return launch_norm<DT, OT, 4, 1, BACK, true>(p, s);
       case 23: return launch_norm<DT, OT, 7, 1, BACK, true>(p, s);
       case 24: return launch_norm<DT, OT, 8, 1, BACK, true>(p, s);
+      case 38: return launch_norm<DT, OT, 6, 2, BACK, true>(p, s);
       case 40: return launch_norm<DT, OT, 8, 2, BACK, true>(p, s);
+      case 70: return launch_norm<DT, OT, 6, 4, BACK, true>(p, s);
       case 72: return launch_norm<DT, OT, 8, 4, BACK, true>(p, s);
+      case 134: return launch_norm<DT, OT, 6, 8, BACK, true>(p, s);
       case 136: return launch_norm<DT, OT, 8, 8, BACK, true>(p, s);
       default: return launch_norm<DT, OT, 8, 16, BACK, true>(p, s);
     }
@@ -658,8 +664,11 @@ cudaError_t launch_types(const NormParams& p, bool aligned_rows, cudaStream_t s)
     case 17: return launch_norm<DT, OT, 1, 1, BACK, false>(p, s);
     case 20: return launch_norm<DT, OT, 4, 1, BACK, false>(p, s);
     case 24: return launch_norm<DT, OT, 8, 1, BACK, false>(p, s);
+    case 38: return launch_norm<DT, OT, 6, 2, BACK, false>(p, s);
     case 40: return launch_norm<DT, OT, 8, 2, BACK, false>(p, s);
+    case 70: return launch_norm<DT, OT, 6, 4, BACK, false>(p, s);
     case 72: return launch_norm<DT, OT, 8, 4, BACK, false>(p, s);
+    case 134: return launch_norm<DT, OT, 6, 8, BACK, false>(p, s);
     case 136: return launch_norm<DT, OT, 8, 8, BACK, false>(p, s);
     default: return launch_norm<DT, OT, 8, 16, BACK, false>(p, s);
   }

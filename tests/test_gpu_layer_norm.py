@@ -47,7 +47,7 @@ def check_backward(x, w, dy, dx, dw, db, eps=EPS):
         assert ref.within(db, wb, eb + ref.rounding(wb, db.dtype))
 
 
-COLS = [1, 2, 7, 8, 31, 255, 256, 257, 512, 513, 896, 1024, 1025, 2048, 2049, 4096, 4097, 8192, 8193, 16384, 16385, 20011]
+COLS = [1, 2, 7, 8, 31, 255, 256, 257, 512, 513, 896, 1024, 1025, 1536, 1537, 2048, 2049, 2560, 3100, 4096, 4097, 5000, 6145, 8192, 8193, 16384, 16385, 20011]
 
 
 @pytest.mark.parametrize("cols", COLS)
