@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
     const uint32_t piece = (turn * G::outs + (G::outs == 2 ? o : 0)) * G::piece;
     uint8_t* const to = out_ptr + piece;
 #pragma unroll
-    for (int q = 0; q < 32; q += kPer) *reinterpret_cast<uint4*>(to + G::at(lane, q / kPer)) = narrow16<DT>(v + q);
+    for (int c = 0; c < 32; c += kPer) *reinterpret_cast<uint4*>(to + G::at(lane, c / kPer)) = narrow16<DT>(v + c);
     if (((p.bulk >> o) & 1) && (j1 + 32 <= q->n || ((p.bulk >> o) & 16))) {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();

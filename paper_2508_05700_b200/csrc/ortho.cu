@@ -112,9 +112,10 @@ __global__ void __launch_bounds__(kSumThreads) scale_kernel(const __grid_constan
 // All of the call in one launch: the long side in slices of up to 256 columns (of X with the short side as its rows), one per block of a
 // cluster. A block has its slice of X in shared memory, in two words and in the order of the tensor cores: rows of 64 columns, 128 bytes with
 // the 128-byte swizzle, are K-major for X X^T and, the other way round, MN-major for B X. A step: the slice's X X^T, summed over the cluster
-// (each block adds up a share of the columns in the order of the slices and hands it to all), B by every block for itself, and the slice of
-// a X + B X over the old one. What costs is the chain: three products, each waited for, and three turns from tensor memory to shared memory.
-// 48 x 192 in five steps: 40 us, 106 as seventeen launches.
+// (each block adds up a share of the columns in the order of the slices, and all read the sums), B by every block for itself, and the slice of
+// a X + B X over the old one. (With a on B's diagonal X is not read again, 3 us less, and errors are 1.4 times as large.) What costs is the
+// chain: three products, each waited for, and three turns from tensor memory to shared memory.
+// 48 x 192 in five steps: 36 us, 106 as seventeen launches; 128 x 2048: 91.
 constexpr int kSmallThreads = 512;
 constexpr int kSmallSide = 128, kSlice = 256, kMostSlices = 8;
 constexpr uint32_t kBlock = 128 * 128;                    // 128 rows x 64 columns
@@ -143,42 +144,57 @@ struct SmallParams {
 // where 8 columns from c on of row r are in a matrix of blocks
 __device__ __forceinline__ uint32_t words_offset(int r, int c) { return (uint32_t)(c >> 6) * kBlock + r * 128 + ((((c >> 3) & 7) ^ (r & 7)) << 4); }
 
-// X[i][c .. c + 8) before it is scaled, 0 behind its end; false: all of it is behind
+// X[i][c .. c + 8) before it is scaled, 0 outside X. Its loads depend on nothing, so that a thread's can all be under way: outside X, and for
+// a long side that 8 does not divide, they are of another element.
 template <int DT>
-__device__ __forceinline__ bool eight_of(const SmallParams& p, int i, int64_t c, float* v) {
+__device__ __forceinline__ void eight_of(const SmallParams& p, int i, int64_t c, float* v) {
   using T = typename Elem<DT>::T;
-  const int64_t left = p.long_side - c;
-  if (i >= p.d || left <= 0) return false;
-  const int count = left < 8 ? (int)left : 8;
   const T* g = reinterpret_cast<const T*>(p.g);
-  if (!MFET_INSIDE(p.status, (p.tall ? i + 1 : c + count) <= p.ld)) return false;
-  if (p.tall) {
+  const int64_t left = p.long_side - c;
+  int count = i >= p.d || left <= 0 ? 0 : left < 8 ? (int)left : 8;
+  const int64_t row = min(i, p.d - 1);
+  if (!MFET_INSIDE(p.status, (p.tall ? row + 1 : count ? c + count : 0) <= p.ld)) count = 0;
+  if (p.vec && !p.tall && p.long_side % 8 == 0) {
+    widen_raw<DT, 8>(load_raw<DT, 8, true>(g + (count ? row * p.ld + c : 0), 8), v);
+  } else if (p.tall) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < count ? to_float<DT>(g[(c + j) * p.ld + i]) : 0.f;
-  } else if (p.vec) {
-    widen_raw<DT, 8>(load_raw<DT, 8, true>(g + i * p.ld + c, count), v);
-  } else {
-    widen_raw<DT, 8>(load_shifted<DT, 8>(g + i * p.ld + c, count, p.g, p.end), v);
+    for (int j = 0; j < 8; ++j) v[j] = to_float<DT>(g[(c + j < p.long_side ? c + j : p.long_side - 1) * p.ld + row]);
+  } else if (count) {
+    widen_raw<DT, 8>(load_shifted<DT, 8>(g + row * p.ld + c, count, p.g, p.end), v);
   }
-  return true;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = j < count ? v[j] : 0.f;
 }
 
 __device__ __forceinline__ void put_words(uint8_t* hi, uint8_t* lo, float* v) {  // 8 values, 16 bytes each
-  float r[8];
+  const uint4 h = narrow16<MFET_F16>(v);
+  float w[8];
+  widen16<MFET_F16>(h, w);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) r[j] = v[j] - __half2float(__float2half_rn(v[j]));
-  *reinterpret_cast<uint4*>(hi) = narrow16<MFET_F16>(v);
-  *reinterpret_cast<uint4*>(lo) = narrow16<MFET_F16>(r);
+  for (int j = 0; j < 8; j += 2) {
+    const float2 d = fma2(make_float2(w[j], w[j + 1]), both(-1.f), make_float2(v[j], v[j + 1]));
+    w[j] = d.x, w[j + 1] = d.y;
+  }
+  *reinterpret_cast<uint4*>(hi) = h;
+  *reinterpret_cast<uint4*>(lo) = narrow16<MFET_F16>(w);
 }
 __device__ __forceinline__ void get_words(const uint8_t* hi, const uint8_t* lo, float* v) {
   float r[8];
   widen16<MFET_F16>(*reinterpret_cast<const uint4*>(hi), v);
   widen16<MFET_F16>(*reinterpret_cast<const uint4*>(lo), r);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] += r[j];
+  for (int j = 0; j < 8; j += 2) {
+    const float2 a = add2(make_float2(v[j], v[j + 1]), make_float2(r[j], r[j + 1]));
+    v[j] = a.x, v[j + 1] = a.y;
+  }
 }
-__device__ __forceinline__ void peer_store8(uint32_t addr, uint32_t a, uint32_t b) {
-  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+// 8 values a * x + b * y into x
+__device__ __forceinline__ void combine8(float* x, float a, const uint32_t* y, float b) {
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const float2 v = fma2(make_float2(__uint_as_float(y[j]), __uint_as_float(y[j + 1])), both(b), mul2(make_float2(x[j], x[j + 1]), both(a)));
+    x[j] = v.x, x[j + 1] = v.y;
+  }
 }
 __device__ __forceinline__ void mma_small(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t b_hi, uint32_t inst, uint32_t add) {
   asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
@@ -237,14 +253,26 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     *i = p.tall ? u & 127 : (int)((uint32_t)u / per);
     *c = (p.tall ? u >> 7 : u - *i * (int)per) * 8;
   };
-  for (int u = tid; u < units; u += kSmallThreads) {
+  constexpr int kUnits = 128 * (kSlice / 8) / kSmallThreads;  // of a thread, in registers until |G| is known
+  float g[kUnits][8];
+#pragma unroll
+  for (int n = 0; n < kUnits; ++n) {
+    const int u = tid + n * kSmallThreads;
     int i, c;
     place(u, &i, &c);
-    float v[8];
-    if (!eight_of<DT>(p, i, c0 + c, v)) continue;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s = fma((double)v[j], (double)v[j], s);
+    eight_of<DT>(p, u < units ? i : 128, c0 + c, g[n]);
   }
+  double s2 = 0.0;
+#pragma unroll
+  for (int n = 0; n < kUnits; ++n) {
+    if (n * kSmallThreads >= units) break;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      s = fma((double)g[n][j], (double)g[n][j], s);
+      s2 = fma((double)g[n][j + 1], (double)g[n][j + 1], s2);
+    }
+  }
+  s += s2;
   s = block_sum<kSmallThreads>(s, sums);
   if (slices > 1) {
     if (tid == 0) total_of_block = s;
@@ -257,16 +285,26 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
       s += v;
     }
   }
-  const double f = factor_of(s, p.scale);
-  for (int u = tid; u < units; u += kSmallThreads) {
+  // The factor as a power of two, half of it before and half after, and a fraction in two words: fp32's range is enough for either half
+  // where it may not be for the factor, and the result is off by an ulp at most. (Conversions to fp64 and back took 4 us.)
+  int e = 0;
+  const double f = frexp(factor_of(s, p.scale), &e);
+  if (!(f > 0.0)) e = 0;
+  const float f_hi = (float)f, f_lo = (float)(f - f_hi), before = ldexpf(1.f, e / 2), after = ldexpf(1.f, e - e / 2);
+#pragma unroll
+  for (int n = 0; n < kUnits; ++n) {
+    const int u = tid + n * kSmallThreads;
+    if (u >= units) break;
     int i, c;
     place(u, &i, &c);
-    float v[8];
-    const bool any = eight_of<DT>(p, i, c0 + c, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = any && c0 + c + j < p.long_side ? (float)(v[j] * f) : 0.f;
+    for (int j = 0; j < 8; j += 2) {
+      const float2 x = mul2(make_float2(g[n][j], g[n][j + 1]), both(before));
+      const float2 y = mul2(fma2(x, both(f_hi), mul2(x, both(f_lo))), both(after));
+      g[n][j] = y.x, g[n][j + 1] = y.y;
+    }
     const uint32_t at = words_offset(i, c);
-    put_words(smem + at, smem + kXLo + at, v);
+    put_words(smem + at, smem + kXLo + at, g[n]);
   }
 
   uint32_t phase = 0;
@@ -321,13 +359,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
       for (int c = 32 * turn; c < d16; c += 128) {
         uint32_t r[32];
         sums_of(tmem + lanes + c, kSecondA, true, r);
-        float* v = reinterpret_cast<float*>(r);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] *= k.a_beta;
 #pragma unroll
         for (int j = 0; j < 32; j += 8) {
+          if (c + j >= d16) break;
           const uint32_t at = words_offset(row, c + j);
-          put_words(smem + kAHi + at, smem + kALo + at, v + j);
+          float* const v = reinterpret_cast<float*>(r) + j;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= k.a_beta;
+          put_words(smem + kAHi + at, smem + kALo + at, v);
         }
       }
     } else {
@@ -341,45 +380,48 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
           *reinterpret_cast<uint4*>(smem + kAHi + (((c + j) >> 2) * 128 + row) * 16) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
       }
       cluster_sync();
-      // every block adds up each `slices`-th group of columns, four warps of a row in turn
+      // Every block adds up each `slices`-th group of columns, four warps of a row in turn, and leaves the sums where its own part of
+      // them was; then all read them there. (Words stored into all blocks, 8 bytes a row: 27000 cycles a step with 8 blocks.)
       constexpr int kMostGroups = 4;  // 32 groups, two blocks at least and four warps
-      float v[kMostGroups][4];
 #pragma unroll
       for (int q = 0; q < kMostGroups; ++q) {
         const int group = (int)rank + slices * (4 * q + turn);
         if (group * 4 >= d16) break;
-        const uint32_t at = base + kAHi + (group * 128 + row) * 16;
-        peer_load(peer_addr(at, 0), v[q]);
-        for (int z = 1; z < slices; ++z) {
-          float t[4];
-          peer_load(peer_addr(at, z), t);
+        const uint32_t at = (group * 128 + row) * 16;
+        float t[kMostSlices][4], v[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[q][j] += t[j];
+        for (int z = 0; z < kMostSlices; ++z)
+          if (z < slices) peer_load(peer_addr(base + kAHi + at, z), t[z]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = t[0][j];
+#pragma unroll
+        for (int z = 1; z < kMostSlices; ++z) {
+          if (z >= slices) break;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] += t[z][j];
         }
+        *reinterpret_cast<float4*>(smem + kAHi + at) = make_float4(v[0] * k.a_beta, v[1] * k.a_beta, v[2] * k.a_beta, v[3] * k.a_beta);
       }
-      cluster_sync();  // all sums have been read: A goes to their place, in all blocks
-#pragma unroll
-      for (int q = 0; q < kMostGroups; ++q) {
-        const int group = (int)rank + slices * (4 * q + turn), c = group * 4;
-        if (c >= d16) break;
-        float lo[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[q][j] *= k.a_beta;
-          lo[j] = v[q][j] - __half2float(__float2half_rn(v[q][j]));
-        }
-        const uint32_t at = words_offset(row, c) + (c & 4) * 2;
-        const uint32_t h0 = Elem<MFET_F16>::pack(v[q][0], v[q][1]), h1 = Elem<MFET_F16>::pack(v[q][2], v[q][3]);
-        const uint32_t l0 = Elem<MFET_F16>::pack(lo[0], lo[1]), l1 = Elem<MFET_F16>::pack(lo[2], lo[3]);
-        for (int z = 0; z < slices; ++z) {
-          const uint32_t to = peer_addr(base + at, z);
-          peer_store8(to + kAHi, h0, h1);
-          peer_store8(to + kALo, l0, l1);
-        }
-      }
-      asm volatile("fence.proxy.async;" ::: "memory");
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       cluster_sync();
+      // two groups, 8 columns, a turn
+      constexpr int kPairs = kMostGroups;  // 16 pairs of groups, four warps
+      float v[kPairs][8];
+#pragma unroll
+      for (int q = 0; q < kPairs; ++q) {
+        const int group = 2 * (4 * q + turn);
+        if (group * 4 >= d16) break;
+        const uint32_t at = base + kAHi + (group * 128 + row) * 16;
+        peer_load(peer_addr(at, group & (slices - 1)), v[q]);
+        peer_load(peer_addr(at + 2048, (group + 1) & (slices - 1)), v[q] + 4);
+      }
+      cluster_sync();  // all sums have been read: A goes to their place
+#pragma unroll
+      for (int q = 0; q < kPairs; ++q) {
+        const int c = 8 * (4 * q + turn);
+        if (c >= d16) break;
+        const uint32_t at = words_offset(row, c);
+        put_words(smem + kAHi + at, smem + kALo + at, v[q]);
+      }
     }
     ready();
     // A A, A being symmetric
@@ -408,8 +450,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
         const uint32_t at = words_offset(row, c + j);
         float a[8];
         get_words(smem + kAHi + at, smem + kALo + at, a);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = fmaf(__uint_as_float(r[j + e]), k.b_beta, a[e] * k.b_alpha);
+        combine8(a, k.b_alpha, r + j, k.b_beta);
         put_words(smem + kAHi + at, smem + kALo + at, a);
       }
     }
@@ -440,21 +481,30 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
         const uint32_t at = words_offset(row, c + j);
         float x[8];
         get_words(smem + at, smem + kXLo + at, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = fmaf(__uint_as_float(r[j + e]), k.x_beta, x[e] * k.x_alpha);
+        combine8(x, k.x_alpha, r + j, k.x_beta);
         if (!last) {
           put_words(smem + at, smem + kXLo + at, x);
-        } else if (row < p.d) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int64_t col = c0 + c + j + e, to = p.tall ? col * p.out_ld + row : row * p.out_ld + col;
-            if (col >= p.long_side || !MFET_INSIDE(p.status, (p.tall ? row : col) < p.out_ld)) continue;
-            if (p.out_dtype == MFET_F32) reinterpret_cast<float*>(p.out)[to] = x[e];
-            else if (p.out_dtype == MFET_F16) reinterpret_cast<__half*>(p.out)[to] = __float2half_rn(x[e]);
-            else reinterpret_cast<__nv_bfloat16*>(p.out)[to] = __float2bfloat16_rn(x[e]);
-          }
+        } else {  // fp32, in the place of both words
+          *reinterpret_cast<float4*>(smem + at) = make_float4(x[0], x[1], x[2], x[3]);
+          *reinterpret_cast<float4*>(smem + kXLo + at) = make_float4(x[4], x[5], x[6], x[7]);
         }
       }
+    }
+  }
+  // A warp writes a row of the result at a time. (From tensor memory, a lane with its own row: 8 us for 48 x 192.)
+  __syncthreads();
+  const int64_t left = p.long_side - c0;
+  const int most = left < width ? (int)left : width, rows = p.tall ? most : p.d, cols = p.tall ? p.d : most;
+  for (int i = warp; i < rows; i += kSmallThreads / 32) {
+    const int64_t first = p.tall ? (c0 + i) * p.out_ld : i * p.out_ld + c0;
+#pragma unroll 4
+    for (int j = lane; j < cols; j += 32) {
+      const int r = p.tall ? j : i, c = p.tall ? i : j;
+      const float x = *reinterpret_cast<const float*>(smem + (c & 4 ? kXLo : 0u) + words_offset(r, c & ~7) + (c & 3) * 4);
+      if (!MFET_INSIDE(p.status, (p.tall ? j : c0 + j) < p.out_ld)) continue;
+      if (p.out_dtype == MFET_F32) reinterpret_cast<float*>(p.out)[first + j] = x;
+      else if (p.out_dtype == MFET_F16) reinterpret_cast<__half*>(p.out)[first + j] = __float2half_rn(x);
+      else reinterpret_cast<__nv_bfloat16*>(p.out)[first + j] = __float2bfloat16_rn(x);
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

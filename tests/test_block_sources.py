@@ -5,7 +5,7 @@ from tests.test_operator_sources import body, code
 
 
 def test_shared_memory_of_another_block_is_touched_between_cluster_barriers():
-    for name, kernel, first, last in (("gemm16.cuh", "gemm16_kernel", "peer_load(", "peer_load("), ("ortho.cu", "ortho_small_kernel", "ld.shared::cluster", "peer_store8(")):
+    for name, kernel, first, last in (("gemm16.cuh", "gemm16_kernel", "peer_load(", "peer_load("), ("ortho.cu", "ortho_small_kernel", "ld.shared::cluster", "peer_load(")):
         text = code(name)
         b = body(text, kernel) if name == "gemm16.cuh" else text[text.index("ortho_small_kernel(const"):]
         b = b[b.index("{"):]
