@@ -917,6 +917,11 @@ double cost_two(const Problem& q) {
 
 // A symmetric result is computed by half where that saves a wave of tiles: writing a tile twice takes 0.8 (orthogonalising 256 x 256 with tiles of
 // 128 columns, one wave either way: 138 by half, 123 without; 4096 x 2048: 833 by half, 985 without).
+//
+// Pairs have tensor memory for two sums of a tile, blocks for four. Where the result is fp32, pairs are left out if one would be of more than
+// kSumOfPairs instructions, since truncation's scatter shows: 2048 x 2048 in five steps 5.5e-6 of the result and 538 us with pairs, 2.6e-6 and 610
+// without (an iteration in fp32: 3.0e-6); 2048 x 4096 5.3e-6 and 867, 1.7e-6 and 1034; 1300 x 1200, 42 instructions, 1.6e-6 with pairs.
+constexpr int kSumOfPairs = 44;
 struct Choice {
   double cost;
   int form;  // 0: pairs, 1: blocks, 2: blocks of 64 columns
@@ -930,7 +935,7 @@ Choice choose(const Problem& q) {
     r.p.sym = sym;
     for (uint32_t part = 1; part <= 4; part *= 2) {
       const double pair = cost<2, 256, MODE, DT>(r, part) + 0.8 * sym, block = cost<1, 128, MODE, DT>(r, part) + 0.8 * sym;
-      if (pair < c.cost) c = {pair, 0, part, sym};
+      if (pair < c.cost && !(q.precise && (q.k[0] + kSlab - 1) / kSlab * 2 / part > kSumOfPairs)) c = {pair, 0, part, sym};
       if (block < c.cost) c = {block, 1, part, sym};
       if constexpr (!Shape<1, 128, MODE, DT>::dual) {
         const double narrow = cost<1, 64, MODE, DT>(r, part);
