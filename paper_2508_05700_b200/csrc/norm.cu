@@ -438,7 +438,7 @@ __global__ void __launch_bounds__((norm_threads<NQ, W, BACK>), BACK || W == 16 ?
       q = joined(warp_sum(s0.x + s0.y), std::false_type());
     }
     const float r = rsqrtf(fmaf(q.x, inv_n, p.eps));
-    const float2 rr = both(r), rm0 = both(-r * (q.y * inv_n)), rm1 = both(-r * (q.z * inv_n * r));
+    const float2 rr = both(r), m0 = both(-(q.y * inv_n)), m1 = both(-(q.z * inv_n * r));
     const uint32_t y_head = (uint32_t)reinterpret_cast<uintptr_t>(y_row) & 15;
     // all have read this row's x by now: backward, the results take its place
     const uint32_t stage = BACK ? from - base : S::out_at + group * S::out_bytes;
@@ -458,7 +458,9 @@ __global__ void __launch_bounds__((norm_threads<NQ, W, BACK>), BACK || W == 16 ?
         if constexpr (BACK) {
           db[i][j] = add2(db[i][j], t[j]);
           dw[i][j] = fma2(t[j], xh, dw[i][j]);
-          o[j] = fma2(xh, rm1, fma2(mul2(t[j], w[j]), rr, rm0));
+          // t is rounded as in its mean, so that equal ones leave 0 (the two-number forms of product and sum were joined to one rounding)
+          const float2 tw = make_float2(__fmul_rn(t[j].x, w[j].x), __fmul_rn(t[j].y, w[j].y));
+          o[j] = mul2(fma2(xh, m1, add2(tw, m0)), rr);
         } else {
           o[j] = fma2(xh, w[j], b[j]);
         }

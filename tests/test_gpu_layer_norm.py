@@ -71,6 +71,25 @@ def test_both_directions(cols, xt, yt, pad, shift):
         assert bool((buf == 7.0).all())
 
 
+@pytest.mark.parametrize("xt,yt", [("f32", "f32"), ("f32", "bf16"), ("f16", "f32"), ("bf16", "f16")])
+@pytest.mark.parametrize("pad", [0, 7])
+def test_one_column_has_no_gradient(xt, yt, pad):
+    """With one column x - mu and t - mean(t) are 0, whatever their size; with two equal ones and equal gradients, too."""
+    for cols in (1, 2):
+        rows = 333
+        _, x = make(rows, cols, ref.DT[xt], pad, seed=1)
+        _, dy = make(rows, cols, ref.DT[yt], pad, seed=2, size=37.0)
+        if cols == 2:
+            x[:, 1], dy[:, 1] = x[:, 0], dy[:, 0]
+        w, b = torch.full((cols,), 1.3, device="cuda"), torch.full((cols,), 0.7, device="cuda")
+        _, y = make(rows, cols, ref.DT[yt], pad)
+        _, dx = make(rows, cols, ref.DT[xt], pad)
+        forward(x, w, b, y)
+        backward(x, w, dy, dx, None, None)
+        assert torch.equal(y, b.to(y.dtype).expand(rows, cols))
+        assert not dx.any()
+
+
 @pytest.mark.parametrize("rows", [1, 2, 8, 9, 147, 5000, 20000])
 @pytest.mark.parametrize("cols", [64, 1500])
 def test_row_counts(rows, cols):
