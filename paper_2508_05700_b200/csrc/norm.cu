@@ -458,9 +458,12 @@ __global__ void __launch_bounds__((norm_threads<NQ, W, BACK>), BACK || W == 16 ?
         if constexpr (BACK) {
           db[i][j] = add2(db[i][j], t[j]);
           dw[i][j] = fma2(t[j], xh, dw[i][j]);
-          // t is rounded as in its mean, so that equal ones leave 0 (the two-number forms of product and sum were joined to one rounding)
-          const float2 tw = make_float2(__fmul_rn(t[j].x, w[j].x), __fmul_rn(t[j].y, w[j].y));
-          o[j] = mul2(fma2(xh, m1, add2(tw, m0)), rr);
+          // Short rows: t is rounded as in its mean, so that a row of one column has the gradient 0 (the two-number forms of product and
+          // sum would be joined to one rounding; 16384 x 2048: 43.0 us, 41.6 without).
+          float2 d;
+          if constexpr (NQ == 1) d = add2(make_float2(__fmul_rn(t[j].x, w[j].x), __fmul_rn(t[j].y, w[j].y)), m0);
+          else d = fma2(t[j], w[j], m0);
+          o[j] = mul2(fma2(xh, m1, d), rr);
         } else {
           o[j] = fma2(xh, w[j], b[j]);
         }
