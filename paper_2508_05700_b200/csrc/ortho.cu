@@ -543,18 +543,15 @@ int exponent_for(double s) { return 14 - (int)std::ceil(std::log2(s > 1e-30 ? s 
 double bound_of(double c0, double c1, double c2, double s) {
   auto at = [&](double t) { return std::fabs(((c2 * t * t + c1) * t * t + c0) * t); };
   double most = at(s);
-  // where the slope c0 + 3 c1 q + 5 c2 q^2 vanishes, q = t^2
-  const double qa = 5 * c2, qb = 3 * c1;
+  // where the slope c0 + 3 c1 q + 5 c2 q^2 vanishes, q = t^2: h / (5 c2) and c0 / h. (The usual formula for the second subtracts two numbers that agree
+  // where c2 is small, and finds q = 0.)
+  const double qa = 5 * c2, qb = 3 * c1, disc = qb * qb - 4 * qa * c0;
   double q[2];
   int n = 0;
-  if (qa == 0.0) {
-    if (qb != 0.0) q[n++] = -c0 / qb;
-  } else {
-    const double disc = qb * qb - 4 * qa * c0;
-    if (disc >= 0.0) {
-      q[n++] = (-qb + std::sqrt(disc)) / (2 * qa);
-      q[n++] = (-qb - std::sqrt(disc)) / (2 * qa);
-    }
+  if (disc >= 0.0) {
+    const double h = -0.5 * (qb + std::copysign(std::sqrt(disc), qb));
+    if (qa != 0.0) q[n++] = h / qa;
+    if (h != 0.0) q[n++] = c0 / h;
   }
   for (int i = 0; i < n; ++i)
     if (q[i] > 0.0 && q[i] < s * s) most = std::fmax(most, at(std::sqrt(q[i])));
