@@ -176,20 +176,20 @@ __device__ __forceinline__ void commit(uint32_t bar, uint32_t mask) {
 // erfc(z), called: 32 copies of it in a row would not fit the instruction cache
 static __device__ __noinline__ float erfc_of(float z) { return erfcf(z); }
 
-// 1 / (1 + e^-g): two instructions of the special functions, whose results are off by 2^-22; e^-g beyond fp32 gives 0
-__device__ __forceinline__ float2 sigmoid2(float2 g) {
+// 1 / (1 + e^-g), and e^-g: two instructions of the special functions, whose results are off by 2^-22; e^-g beyond fp32 gives 0
+__device__ __forceinline__ float2 sigmoid2(float2 g, float2* e) {
   const float2 t = mul2(g, both(-1.4426950408889634f));
-  float2 e, s;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(t.x));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(t.y));
-  e = add2(e, both(1.f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(e.x));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(e.y));
+  float2 s;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e->x) : "f"(t.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e->y) : "f"(t.y));
+  const float2 d = add2(*e, both(1.f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(d.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(d.y));
   return s;
 }
 
-// act(g) of two gates, and its derivative. What the functions are off by (2^-17 where e^-g is large, 2^-21 in the middle) is far below
-// a 16-bit result's rounding.
+// act(g) of two gates, and its derivative. What the functions are off by (2^-17 of themselves where e^-g is large, 2^-21 in the middle) is far
+// below a 16-bit result's rounding.
 template <int ACT, bool SLOPE>
 __device__ __forceinline__ float2 gate2(float2 g, float2* slope) {
   if constexpr (ACT == MFET_ACT_RELU) {
@@ -199,12 +199,18 @@ __device__ __forceinline__ float2 gate2(float2 g, float2* slope) {
     if (SLOPE) *slope = make_float2(g.x > 0.f ? 1.f : 0.f, g.y > 0.f ? 1.f : 0.f);
     return r;
   } else if constexpr (ACT == MFET_ACT_SILU) {
-    const float2 s = sigmoid2(g);
+    float2 e;
+    const float2 s = sigmoid2(g, &e);
+    // 1 - s may cancel here: where it does, it stands beside 1
     if (SLOPE) *slope = mul2(s, fma2(g, fma2(s, both(-1.f), both(1.f)), both(1.f)));
     return mul2(g, s);
   } else if constexpr (ACT == MFET_ACT_SIGMOID) {
-    const float2 s = sigmoid2(g);
-    if (SLOPE) *slope = mul2(s, fma2(s, both(-1.f), both(1.f)));
+    float2 e;
+    const float2 s = sigmoid2(g, &e);
+    if (SLOPE) {  // s (1 - s), with 1 - s as e^-g s where it would cancel (from g = 12 on it was off by 1 %, from 17 on 0)
+      const float2 c = fma2(s, both(-1.f), both(1.f)), d = mul2(e, s);
+      *slope = mul2(s, make_float2(g.x > 0.f ? d.x : c.x, g.y > 0.f ? d.y : c.y));
+    }
     return s;
   } else if constexpr (ACT == MFET_ACT_GELU) {
     const float2 z = mul2(g, both(-0.70710678118654752f));
