@@ -192,24 +192,34 @@ int gates(const Call& c, const Matrix& x, const Matrix& wg, const Matrix& wu, co
   return c.dtype == MFET_F16 ? run<MODE, MFET_F16>(q, c.stream) : run<MODE, MFET_BF16>(q, c.stream);
 }
 
+template <int MODE>
 int out_product(Problem& q, const Call& c) {
   q.dtype = q.out_dtype = c.dtype;
   q.p.status = c.status;
-  return c.dtype == MFET_F16 ? run<kOut, MFET_F16>(q, c.stream) : run<kOut, MFET_BF16>(q, c.stream);
+  return c.dtype == MFET_F16 ? run<MODE, MFET_F16>(q, c.stream) : run<MODE, MFET_BF16>(q, c.stream);
 }
+
+// The weights' gradients are sums over the rows. The tensor cores truncate a sum once in 16 of them, by up to 2^-22 of what it holds (its 16 products
+// included), so that beyond some rows it loses more than its rounding to 16 bits does: fp16 products of one sign were off by 2.1e-4 of their sum for
+// 2^17 rows, 1.7e-3 for 2^20 and 6.6e-3 for 2^22 (half a step of fp16 is 4.9e-4), 64 x 64 weights in four parts of the rows. Sums over more than
+// kLongRows are taken in parts of kPartRows, which are added up in fp32, to nearest: 131072 x 1024 x 896 1132 -> 1172 us, 66000 x 100 x 5000 769 -> 844,
+// 2^20 x 64 x 64 1234 either way. (Both products in two launches: 1147 and 922; 131072 x 1024 x 2048 2298 in one, 2212 in two.)
+constexpr int64_t kLongRows = 1ll << 16, kPartRows = 1ll << 14;
 
 // Both products of the backward pass in one launch, where that takes less time than one after the other: blocks that have no tile of one left
 // go on with the other (the backward pass of 8192 x 896 x 1024: 80 us, 84 in two launches). 1: it does not.
-template <int DT>
+template <int TWO, int OF_W, int DT>
 int out_products_dt(const Problem& both, const Problem& of_x, const Problem& of_w, cudaStream_t s) {
-  return cost_two<DT>(both) < least_cost<kOut, DT>(of_x) + least_cost<kOut, DT>(of_w) ? launch<2, 256, kOutTwo, DT>(both, 1, s) : 1;
+  return cost_two<TWO, DT>(both) < least_cost<kOut, DT>(of_x) + least_cost<OF_W, DT>(of_w) ? launch<2, 256, TWO, DT>(both, 1, s) : 1;
 }
+template <int TWO, int OF_W>
 int out_products(Problem* both, Problem* of_x, Problem* of_w, const Call& c) {
   for (Problem* q : {both, of_x, of_w}) {
     q->dtype = q->out_dtype = c.dtype;
     q->p.status = c.status;
   }
-  return c.dtype == MFET_F16 ? out_products_dt<MFET_F16>(*both, *of_x, *of_w, c.stream) : out_products_dt<MFET_BF16>(*both, *of_x, *of_w, c.stream);
+  return c.dtype == MFET_F16 ? out_products_dt<TWO, OF_W, MFET_F16>(*both, *of_x, *of_w, c.stream)
+                             : out_products_dt<TWO, OF_W, MFET_BF16>(*both, *of_x, *of_w, c.stream);
 }
 
 // scratch for operands whose rows do not start on 16-byte boundaries, as they are
@@ -325,7 +335,9 @@ int mfet_gated_linear_backward(const void* x, uint32_t dtype, int64_t x_ld, int6
     q.p.part[0].a_mn = q.p.part[0].b_mn = 1;
     q.p.part[0].m = n, q.p.part[0].n = k;
   }
-  if (dx && dw_gate) {
+  const bool long_sum = m > kLongRows;
+  of_w.p.part_kb = kPartRows / kSlab;
+  if (dx && dw_gate && (!long_sum || n <= kPartRows)) {
     both = of_w;
     both.a[2] = g[0], both.a[3] = g[1], both.n_a = 4;
     both.b[1] = in[1], both.b[2] = in[2], both.n_b = 3, both.b_mn = 7;
@@ -333,11 +345,11 @@ int mfet_gated_linear_backward(const void* x, uint32_t dtype, int64_t x_ld, int6
     both.k[1] = n, both.segs[1] = 2, both.results[1] = 1;
     both.p.part[1] = of_x.p.part[0];
     both.p.part[1].seg_a = 0x32, both.p.part[1].seg_b = 0x21, both.p.part[1].out = 2;
-    rc = out_products(&both, &of_x, &of_w, c);
+    rc = long_sum ? out_products<kOutTwoLong, kOutLong>(&both, &of_x, &of_w, c) : out_products<kOutTwo, kOut>(&both, &of_x, &of_w, c);
     if (rc <= 0) return rc;
   }
-  rc = dx ? out_product(of_x, c) : MFET_OK;
-  if (rc == MFET_OK && dw_gate) rc = out_product(of_w, c);
+  rc = dx ? out_product<kOut>(of_x, c) : MFET_OK;
+  if (rc == MFET_OK && dw_gate) rc = long_sum ? out_product<kOutLong>(of_w, c) : out_product<kOut>(of_w, c);
   return rc;
 }
 

@@ -29,6 +29,8 @@ enum Mode {
   kGatedBack,  // ... with the gradient of h: dG and dU
   kOut,        // the accumulator, rounded
   kOutTwo,     // ... of two products of different operands in one launch
+  kOutLong,    // ... of a long sum: the tensor cores add up parts of k, registers the parts
+  kOutTwoLong, // both: the first product's sum is long, the second's is one part
   kPair,       // v = alpha * C + beta * acc in two fp16 words
   kPairOut     // the same, rounded to the type of the result
 };
@@ -79,10 +81,11 @@ struct Part {
 struct Params {
   Part part[2];
   uint32_t tiles, tiles0;   // of all results; of the first product's
-  uint32_t heavy, later;    // kOutTwo: see Walk
+  uint32_t heavy, later;    // two products: see Walk
   uint32_t band;            // tiles of rows that are walked through together, so that the blocks at work share operands in L2
   uint32_t split;
   uint32_t sums, buffers;   // accumulators of a tile, each of its part of k; tiles that are in tensor memory at a time
+  uint32_t part_kb;         // long sums: blocks of k in a part
   uint32_t sym;             // the result is symmetric: tiles on and below the diagonal alone, each written to both of its places
   uint32_t act;
   uint32_t bulk;            // bit o: rows of output o start on 16-byte boundaries; bit 4 + o: ... and may be written up to one (bulk copies
@@ -369,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   early_launch_wait();
 
   const uint32_t members = CTAS * p.split;
-  constexpr bool kTwo = MODE == kOutTwo;
+  constexpr bool kTwo = MODE == kOutTwo || MODE == kOutTwoLong, kLong = MODE == kOutLong || MODE == kOutTwoLong;
   const uint32_t first = blockIdx.x / members;
   const Walk<kTwo> walk(p, first, gridDim.x / members);
   auto share_begin = [&](const Part& q) { return (uint32_t)((uint64_t)q.kb * part / p.split); };  // this block's share of k, in each segment
@@ -447,52 +450,57 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   } else if (warp == 1) {
     if (half == 0 && elect_one()) {
       issues = true;
-      uint32_t st = 0, phase = 0, done = 0;
+      uint32_t st = 0, phase = 0, done = 0, unit = 0;  // unit: accumulators used so far, one a tile (a part)
       bool ok = true, ready = false;
       for (uint32_t t = walk(0); ok && t < p.tiles; t = walk(++done)) {
         const Part& q = p.part[kTwo && t >= p.tiles0 ? 1 : 0];
-        const uint32_t k0 = share_begin(q), k1 = share_end(q);
-        const uint32_t a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
-        const uint32_t acc = done % p.buffers;
-        if (done >= p.buffers && !(ok = bar_wait(acc_empty(acc), (done / p.buffers - 1) & 1, &dead))) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t len = k1 - k0, sums = sums_for(len);
-        uint32_t kk = k0, left = len * (G::fused ? 1 : q.segs), sum = 0, fresh = 1, of_sum = 0;  // fresh: nothing has been added to this sum yet
-        for (uint32_t i = 0; left > 0; ++i) {
-          if (!ready && !(ok = bar_wait(full(st), phase, &dead))) break;
+        const uint32_t a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u, end = share_end(q);
+        uint32_t k0 = share_begin(q);
+        do {
+          const uint32_t k1 = kLong ? min(k0 + p.part_kb, end) : end;
+          const uint32_t acc = unit % p.buffers;
+          if (unit >= p.buffers && !(ok = bar_wait(acc_empty(acc), (unit / p.buffers - 1) & 1, &dead))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t at = base + st * G::stage_bytes;
-          const uint32_t this_empty = empty(st);
-          const uint32_t a_lo = desc_lo(at, q.a_mn), b_lo = desc_lo(at + (G::fused ? 2 : 1) * G::a_bytes, q.b_mn);
-          const uint32_t first_sum = tmem + acc * (G::precise ? p.sums : 1u) * TN, d = first_sum + sum * TN, add = !fresh;
-          const bool last = kk + 1 == q.kb;
-          if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-          if constexpr (G::fused) {  // high x low, low x high to a sum of their own, high x high to this part's
-            const uint32_t steps = last ? q.tail : 4u, low = first_sum + sums * TN, a2 = a_lo + (G::a_bytes >> 4), b2 = b_lo + (G::b_bytes >> 4);
-            for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(low, a_lo + j * a_step, b2 + j * b_step, q.inst, i | j);
-            for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(low, a2 + j * a_step, b_lo + j * b_step, q.inst, 1);
-            ready = bar_try(full(st), phase);
-            for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, q.inst, add | j);
-          } else if (!last || q.tail == 4) {
-            mma16<CTAS>(d, a_lo, b_lo, q.inst, add);
-            mma16<CTAS>(d, a_lo + a_step, b_lo + b_step, q.inst, 1);
-            ready = bar_try(full(st), phase);
-            mma16<CTAS>(d, a_lo + 2 * a_step, b_lo + 2 * b_step, q.inst, 1);
-            mma16<CTAS>(d, a_lo + 3 * a_step, b_lo + 3 * b_step, q.inst, 1);
-          } else {
-            for (uint32_t j = 0; j < q.tail; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, q.inst, add | j);
-            ready = bar_try(full(st), phase);
+          const uint32_t len = k1 - k0, sums = sums_for(len);
+          uint32_t kk = k0, left = len * (G::fused ? 1 : q.segs), sum = 0, fresh = 1, of_sum = 0;  // fresh: nothing has been added to this sum yet
+          for (uint32_t i = 0; left > 0; ++i) {
+            if (!ready && !(ok = bar_wait(full(st), phase, &dead))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t at = base + st * G::stage_bytes;
+            const uint32_t this_empty = empty(st);
+            const uint32_t a_lo = desc_lo(at, q.a_mn), b_lo = desc_lo(at + (G::fused ? 2 : 1) * G::a_bytes, q.b_mn);
+            const uint32_t first_sum = tmem + acc * (G::precise ? p.sums : 1u) * TN, d = first_sum + sum * TN, add = !fresh;
+            const bool last = kk + 1 == q.kb;
+            if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
+            if constexpr (G::fused) {  // high x low, low x high to a sum of their own, high x high to this part's
+              const uint32_t steps = last ? q.tail : 4u, low = first_sum + sums * TN, a2 = a_lo + (G::a_bytes >> 4), b2 = b_lo + (G::b_bytes >> 4);
+              for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(low, a_lo + j * a_step, b2 + j * b_step, q.inst, i | j);
+              for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(low, a2 + j * a_step, b_lo + j * b_step, q.inst, 1);
+              ready = bar_try(full(st), phase);
+              for (uint32_t j = 0; j < steps; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, q.inst, add | j);
+            } else if (!last || q.tail == 4) {
+              mma16<CTAS>(d, a_lo, b_lo, q.inst, add);
+              mma16<CTAS>(d, a_lo + a_step, b_lo + b_step, q.inst, 1);
+              ready = bar_try(full(st), phase);
+              mma16<CTAS>(d, a_lo + 2 * a_step, b_lo + 2 * b_step, q.inst, 1);
+              mma16<CTAS>(d, a_lo + 3 * a_step, b_lo + 3 * b_step, q.inst, 1);
+            } else {
+              for (uint32_t j = 0; j < q.tail; ++j) mma16<CTAS>(d, a_lo + j * a_step, b_lo + j * b_step, q.inst, add | j);
+              ready = bar_try(full(st), phase);
+            }
+            commit<CTAS>(this_empty, pair_mask);
+            if (--left == 0) commit<CTAS>(acc_full(acc), pair_mask);
+            fresh = 0;
+            ++kk;
+            if constexpr (G::precise) {
+              of_sum += sums;  // block kk - k0 belongs to sum (kk - k0) * sums / len
+              if (of_sum >= len) of_sum -= len, ++sum, fresh = i + 1 < len;
+            }
+            if (kk == k1) kk = k0, sum = 0, of_sum = 0;
           }
-          commit<CTAS>(this_empty, pair_mask);
-          if (--left == 0) commit<CTAS>(acc_full(acc), pair_mask);
-          fresh = 0;
-          ++kk;
-          if constexpr (G::precise) {
-            of_sum += sums;  // block kk - k0 belongs to sum (kk - k0) * sums / len
-            if (of_sum >= len) of_sum -= len, ++sum, fresh = i + 1 < len;
-          }
-          if (kk == k1) kk = k0, sum = 0, of_sum = 0;
-        }
+          k0 = k1;
+          ++unit;
+        } while (kLong && ok && k0 < end);
       }
     }
   }
@@ -557,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       gates32<true>(p.act, v, u, x);
       put(v, 0, i0, j1);
       put(u, 1, i0, j1);
-    } else if constexpr (MODE == kOut || MODE == kOutTwo) {
+    } else if constexpr (MODE == kOut || kTwo || kLong) {
       put(v, (int)q->out + z, i0, j1);
     } else {
 #pragma unroll
@@ -628,13 +636,54 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       const Tile w = tile_at<false>(p, first);
       ask(next, row_of(w) + lane, (int64_t)w.tn * G::width + 32 * second);
     }
+    uint32_t unit = 0;
     for (uint32_t t = walk(0); t < p.tiles; t = walk(++done)) {
       const Tile w = tile_at<kTwo>(p, t);
       if constexpr (kTwo) q = &p.part[w.part];
-      const uint32_t acc = done % p.buffers;
+      const uint32_t len = share_end(*q) - share_begin(*q), parts = kLong ? (len + p.part_kb - 1) / p.part_kb : 1;
+      if (kLong && parts > 1) {  // a tile's parts in their order, added up in registers while the next one is computed
+        constexpr int kChunks = G::width / 64;
+        float v[kChunks][32];
+        bool ok = true;
+        for (uint32_t n = 0; n < parts; ++n, ++unit) {
+          const uint32_t acc = unit % p.buffers;
+          ok = __all_sync(kAllLanes, bar_sleep(acc_full(acc), (unit / p.buffers) & 1, &dead));
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) {
+            uint32_t r[32];
+            tmem_load32(tmem + acc * TN + ((uint32_t)(quarter * 32) << 16) + 32 * second + 64 * c, r);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[c][j] = n ? v[c][j] + __uint_as_float(r[j]) : __uint_as_float(r[j]);
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (CTAS == 1) bar_arrive(acc_empty(acc));
+            else peer_arrive(peer_addr(acc_empty(acc), leader));
+          }
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+          const int c0 = 32 * second + 64 * c;
+          if (p.split > 1) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              *reinterpret_cast<float4*>(smem + (((c0 + j) >> 2) * 128 + quarter * 32 + lane) * 16) = make_float4(v[c][j], v[c][j + 1], v[c][j + 2], v[c][j + 3]);
+          } else {
+            finish(v[c], nullptr, nullptr, (int)w.z, row_of(w), (int64_t)w.tn * G::width + c0, false);
+          }
+        }
+        if (p.split > 1) break;
+        continue;
+      }
+      const uint32_t acc = unit % p.buffers;
       const int64_t i0 = row_of(w), j0 = (int64_t)w.tn * G::width;
       const uint32_t from = tmem + acc * (G::precise ? p.sums : 1u) * TN + ((uint32_t)(quarter * 32) << 16);
-      const bool ok = bar_sleep(acc_full(acc), (done / p.buffers) & 1, &dead);
+      const bool ok = bar_sleep(acc_full(acc), (unit / p.buffers) & 1, &dead);
+      ++unit;
       if (!__all_sync(kAllLanes, ok)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (p.split > 1) {  // one tile per block: its sums go to shared memory, where the ring was
@@ -807,7 +856,8 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
       return MFET_ERR_CUDA;
   }
   const uint32_t fmt = q.dtype == MFET_BF16 ? 1u : 0u;
-  for (int i = 0; i < (MODE == kOutTwo ? 2 : 1); ++i) {
+  constexpr bool kTwo = MODE == kOutTwo || MODE == kOutTwoLong;
+  for (int i = 0; i < (kTwo ? 2 : 1); ++i) {
     Part& x = p.part[i];
     x.m_tiles = (uint32_t)((x.m + CTAS * 128 - 1) / (CTAS * 128));
     x.n_tiles = (uint32_t)((x.n + G::width - 1) / G::width);
@@ -837,7 +887,7 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
     const double len = (double)p.part[0].kb / split, most = p.sums - (G::fused ? 1 : 0), of = len < most ? len : most;
     p.beta = (float)(p.beta * (1.0 + 0.18 * 0x1p-23 * 4.0 * len / of));
   }
-  if (MODE == kOutTwo) {
+  if (kTwo) {
     p.heavy = p.tiles0 % clusters;
     p.later = p.heavy ? rounds_later(p.part[0].iters, p.part[1].iters) : 0;
   }
@@ -906,12 +956,12 @@ double cost(const Problem& q, uint32_t split) {
 }
 
 // Two products in one launch, by pairs: the microseconds of it, as above
-template <int DT>
+template <int MODE, int DT>
 double cost_two(const Problem& q) {
-  using G = Shape<2, 256, kOutTwo, DT>;
+  using G = Shape<2, 256, MODE, DT>;
   static std::atomic<uint64_t> ready{0};
-  if (allow_smem(gemm16_kernel<2, 256, kOutTwo, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
-  const int64_t pairs = clusters_at_once(gemm16_kernel<2, 256, kOutTwo, DT>, 2, G::smem);
+  if (allow_smem(gemm16_kernel<2, 256, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
+  const int64_t pairs = clusters_at_once(gemm16_kernel<2, 256, MODE, DT>, 2, G::smem);
   const int64_t t0 = tiles_of(q, 0, 256, 256), t1 = tiles_of(q, 1, 256, 256), a = iters_of(q, 0), b = iters_of(q, 1);
   if (t0 + t1 < pairs || t0 + t1 >= (1ll << 31)) return 1e300;
   const int64_t heavy = t0 % pairs, light = pairs - heavy, later = heavy ? rounds_later((uint32_t)a, (uint32_t)b) : 0;
