@@ -147,27 +147,34 @@ using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, 
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// The driver's function that describes a tile to the copy engine. It wants the GPU's context to be the calling thread's, which a thread that
-// makes its first call here does not have yet.
-inline EncodeTiled encode_tiled() {
-  static std::atomic<void*> found{nullptr};
-  static thread_local int bound = -1;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || (dev != bound && cudaSetDevice(dev) != cudaSuccess)) {
+// A function of the driver, by name; `found` keeps it
+inline void* driver_function(const char* name, std::atomic<void*>* found) {
+  void* f = found->load(std::memory_order_acquire);
+  if (f) return f;
+  cudaDriverEntryPointQueryResult r;
+  if (cudaGetDriverEntryPoint(name, &f, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
     cudaGetLastError();
     return nullptr;
   }
-  bound = dev;
-  void* f = found.load(std::memory_order_acquire);
-  if (!f) {
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+  found->store(f, std::memory_order_release);
+  return f;
+}
+
+// The driver's function that describes a tile to the copy engine. It wants a context to be the calling thread's. A thread that makes its first call here
+// may have none yet: it gets the one of its GPU. A context that the caller has made current, of whatever kind, stays.
+inline EncodeTiled encode_tiled() {
+  static std::atomic<void*> encode{nullptr}, get_current{nullptr};
+  const auto current = reinterpret_cast<CUresult (*)(CUcontext*)>(driver_function("cuCtxGetCurrent", &get_current));
+  CUcontext context = nullptr;
+  if (!current) return nullptr;
+  if (current(&context) != CUDA_SUCCESS || !context) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) {
       cudaGetLastError();
       return nullptr;
     }
-    found.store(f, std::memory_order_release);
   }
-  return reinterpret_cast<EncodeTiled>(f);
+  return reinterpret_cast<EncodeTiled>(driver_function("cuTensorMapEncodeTiled", &encode));
 }
 
 // Lets a kernel use `bytes` of dynamic shared memory on the current GPU: always the same number for a kernel, so that no thread takes away
