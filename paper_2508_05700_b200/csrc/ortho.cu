@@ -209,19 +209,20 @@ __device__ __forceinline__ void mma_small(uint32_t d, uint32_t a_lo, uint32_t b_
 template <int DT>
 __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __grid_constant__ SmallParams p) {
   extern __shared__ uint8_t raw_smem[];
-  __shared__ __align__(8) uint64_t bar_word;
+  __shared__ __align__(8) uint64_t bar_words[2];
   __shared__ double sums[kSmallThreads / 32];
   __shared__ double total_of_block;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int dead;
   const uint32_t base = (smem_addr(raw_smem) + 1023) & ~1023u;
   uint8_t* const smem = raw_smem + (base - smem_addr(raw_smem));
-  const uint32_t bar = smem_addr(&bar_word);
+  const uint32_t bar = smem_addr(bar_words), drained = bar + 8;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int slices = p.slices;
   const uint32_t rank = slices > 1 ? cluster_rank() : 0u;
   if (tid == 0) {
     bar_init(bar, 1);
+    bar_init(drained, 1);
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -308,6 +309,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
   }
 
   uint32_t phase = 0;
+  // Every product that this warp waited for has ended. Where it has not, its operands may still be read: from then on the warp issues nothing and writes
+  // no words, but comes to every barrier. (A warp that has seen the product end may go on: what it overwrites is no longer read.)
+  bool ok = true;
+  bool issues = false;  // this lane issues the products
   auto ready = [&]() {  // what this block's threads have written is there for the tensor cores
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -315,7 +320,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   };
   auto done = [&]() {  // the products that one lane has issued
-    bar_wait(bar, phase, &dead);
+    ok = __all_sync(kAllLanes, ok && bar_wait(bar, phase, &dead));
     phase ^= 1;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   };
@@ -340,8 +345,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     const SmallStep k = p.step[step];
     ready();
     // A = X X^T over the slice
-    if (warp == 0) {
+    if (warp == 0 && ok) {
       if (elect_one()) {
+        issues = true;
         for (int t = 0; t < 3; ++t) {  // high x low, low x high, high x high
           const uint32_t a = xs[t == 1], b = xs[t == 0];
           for (int q = 0; q < width / 16; ++q) {
@@ -356,7 +362,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     done();
     if (slices == 1) {
 #pragma unroll 1
-      for (int c = 32 * turn; c < d16; c += 128) {
+      for (int c = 32 * turn; ok && c < d16; c += 128) {
         uint32_t r[32];
         sums_of(tmem + lanes + c, kSecondA, true, r);
 #pragma unroll
@@ -372,7 +378,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     } else {
       // the slice's sums, four columns of a row in 16 bytes, where A was
 #pragma unroll 1
-      for (int c = 32 * turn; c < d16; c += 128) {
+      for (int c = 32 * turn; ok && c < d16; c += 128) {
         uint32_t r[32];
         sums_of(tmem + lanes + c, kSecondA, true, r);
 #pragma unroll
@@ -386,7 +392,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
 #pragma unroll
       for (int q = 0; q < kMostGroups; ++q) {
         const int group = (int)rank + slices * (4 * q + turn);
-        if (group * 4 >= d16) break;
+        if (!ok || group * 4 >= d16) break;
         const uint32_t at = (group * 128 + row) * 16;
         float t[kMostSlices][4], v[4];
 #pragma unroll
@@ -418,15 +424,16 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
 #pragma unroll
       for (int q = 0; q < kPairs; ++q) {
         const int c = 8 * (4 * q + turn);
-        if (c >= d16) break;
+        if (!ok || c >= d16) break;
         const uint32_t at = words_offset(row, c);
         put_words(smem + kAHi + at, smem + kALo + at, v[q]);
       }
     }
     ready();
     // A A, A being symmetric
-    if (warp == 0) {
+    if (warp == 0 && ok) {
       if (elect_one()) {
+        issues = true;
         for (int t = 0; t < 3; ++t) {
           const uint32_t a = as[t == 1], b = as[t == 0];
           for (int q = 0; q < d16 / 16; ++q) {
@@ -441,7 +448,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     done();
     // B = b A + c A A over A
 #pragma unroll 1
-    for (int c = 32 * turn; c < d16; c += 128) {
+    for (int c = 32 * turn; ok && c < d16; c += 128) {
       uint32_t r[32];
       sums_of(tmem + lanes + c, kSecondA, two_d, r);
 #pragma unroll
@@ -456,8 +463,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     }
     ready();
     // B X
-    if (warp == 0) {
+    if (warp == 0 && ok) {
       if (elect_one()) {
+        issues = true;
         for (int t = 0; t < 3; ++t) {
           const uint32_t a = as[t == 1], b = xs[t == 0];
           for (int q = 0; q < d16 / 16; ++q) {
@@ -473,7 +481,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     done();
     const bool last = step + 1 == p.steps;
 #pragma unroll 1
-    for (int c = 32 * turn; c < width; c += 128) {
+    for (int c = 32 * turn; ok && c < width; c += 128) {
       uint32_t r[32];
       sums_of(acc_x + lanes + c, kSecondX, two_x, r);
 #pragma unroll
@@ -507,10 +515,18 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
       else reinterpret_cast<__nv_bfloat16*>(p.out)[first + j] = __float2bfloat16_rn(x);
     }
   }
+  if (dead) {  // all threads have ended their last wait: what is waited for now, with the same limit, is the last product under way
+    volatile int none = 0;
+    if (issues) {
+      mma_commit(drained);
+      bar_wait(drained, 0, &none);
+    }
+    if (tid == 0 && p.status) atomicOr(p.status, (uint32_t)MFET_DEV_STALLED);
+  }
+  __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   cluster_or_block_sync(slices > 1);
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  if (tid == 0 && dead && p.status) atomicOr(p.status, (uint32_t)MFET_DEV_STALLED);
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
