@@ -835,6 +835,35 @@ inline int64_t iters_of(const Problem& q, int part) { return (q.k[part] + kSlab 
 // rounds of the second product's tiles in which blocks with one more tile of the first take none
 inline uint32_t rounds_later(uint32_t first, uint32_t second) { return (first + second / 2) / second; }
 
+// Clusters of 1, 2, 4 or 8 blocks that the current GPU runs at a time (148 SMs are not 18 clusters of 8: parts of the chip have odd numbers
+// of them; one cluster too many doubled a product's time).
+template <auto Kernel>  // each kernel has its own answers
+int64_t clusters_at_once(uint32_t members, uint32_t smem) {
+  if (members == 1) return sm_count();
+  static std::atomic<int> known[64][4];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / (members + 1);
+  std::atomic<int>& k = known[dev][members == 2 ? 1 : members == 4 ? 2 : 3];
+  n = k.load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = members;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(members * (unsigned)sm_count());
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, Kernel, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return sm_count() / (members + 1);  // not remembered: asked again next time
+  }
+  k.store(n, std::memory_order_relaxed);
+  return n;
+}
+
 template <int CTAS, int TN, int MODE, int DT>
 int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   using G = Shape<CTAS, TN, MODE, DT>;
@@ -873,7 +902,7 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   p.split = split;
   static std::atomic<uint64_t> ready{0};
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return MFET_ERR_CUDA;
-  const uint32_t members = CTAS * split, at_once = (uint32_t)clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, members, G::smem);
+  const uint32_t members = CTAS * split, at_once = (uint32_t)clusters_at_once<gemm16_kernel<CTAS, TN, MODE, DT>>(members, G::smem);
   const uint32_t clusters = split > 1 || p.tiles < at_once ? p.tiles : at_once;
   p.sums = 1;
   p.buffers = 2;
@@ -907,35 +936,6 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, TN, MODE, DT>, maps, p) == cudaSuccess ? MFET_OK : MFET_ERR_CUDA;
 }
 
-// Clusters of 1, 2, 4 or 8 blocks that the current GPU runs at a time (148 SMs are not 18 clusters of 8: parts of the chip have odd numbers
-// of them; one cluster too many doubled a product's time).
-template <typename K>
-int64_t clusters_at_once(K kernel, uint32_t members, uint32_t smem) {
-  if (members == 1) return sm_count();
-  static std::atomic<int> known[64][4];
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / (members + 1);
-  std::atomic<int>& k = known[dev][members == 2 ? 1 : members == 4 ? 2 : 3];
-  n = k.load(std::memory_order_relaxed);
-  if (n > 0) return n;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = members;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(members * (unsigned)sm_count());
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
-    cudaGetLastError();
-    return sm_count() / (members + 1);  // not remembered: asked again next time
-  }
-  k.store(n, std::memory_order_relaxed);
-  return n;
-}
-
 // The form for a problem: the least of the microseconds that were measured for each. A launch with a tile's start and end 6.9 for pairs, 4.2
 // for blocks of 128 columns, 3.5 for 64; 64 of k 0.325 for 256 x 256 by a pair, 0.25 for 128 x 128 by a block and 0.2 for 64 columns (its loads
 // bound it), 0.135 in each segment where three segments' tiles come together; joining two parts 3, four 6.
@@ -949,7 +949,7 @@ double cost(const Problem& q, uint32_t split) {
   const int64_t tiles = tiles_of(q, 0, CTAS * 128, G::width);
   static std::atomic<uint64_t> ready{0};
   if (allow_smem(gemm16_kernel<CTAS, TN, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
-  const int64_t at_once = clusters_at_once(gemm16_kernel<CTAS, TN, MODE, DT>, CTAS * split, G::smem), waves = (tiles + at_once - 1) / at_once;
+  const int64_t at_once = clusters_at_once<gemm16_kernel<CTAS, TN, MODE, DT>>(CTAS * split, G::smem), waves = (tiles + at_once - 1) / at_once;
   if (split > 1 && waves > 1) return 1e300;
   if (q.p.sym && CTAS * 128 != TN) return 1e300;  // tiles are exchanged with their mirror images
   return (CTAS == 2 ? 6.9 : TN == 128 ? 4.2 : 3.5) + (double)waves * ((kb + split - 1) / split) * q.segs[0] * (CTAS == 2 ? 0.325 : TN == 128 ? 0.25 : G::fused ? 0.135 : 0.2) + (split == 1 ? 0.0 : split == 2 ? 3.0 : 6.0);
@@ -961,7 +961,7 @@ double cost_two(const Problem& q) {
   using G = Shape<2, 256, MODE, DT>;
   static std::atomic<uint64_t> ready{0};
   if (allow_smem(gemm16_kernel<2, 256, MODE, DT>, G::smem, &ready) != cudaSuccess) return 1e300;
-  const int64_t pairs = clusters_at_once(gemm16_kernel<2, 256, MODE, DT>, 2, G::smem);
+  const int64_t pairs = clusters_at_once<gemm16_kernel<2, 256, MODE, DT>>(2, G::smem);
   const int64_t t0 = tiles_of(q, 0, 256, 256), t1 = tiles_of(q, 1, 256, 256), a = iters_of(q, 0), b = iters_of(q, 1);
   if (t0 + t1 < pairs || t0 + t1 >= (1ll << 31)) return 1e300;
   const int64_t heavy = t0 % pairs, light = pairs - heavy, later = heavy ? rounds_later((uint32_t)a, (uint32_t)b) : 0;
