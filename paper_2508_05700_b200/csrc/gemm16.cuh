@@ -907,14 +907,17 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
   p.sums = 1;
   p.buffers = 2;
   if (G::precise) {
-    // The tensor cores truncate a sum at every instruction. A sum of n instructions that grows evenly loses 0.18 n 2^-23 of what it ends at, on
-    // average over where it stands between two powers of two. Several sums of a part of k each, added up in fp32, lose as many times less; what
-    // they lose on average is put back. Results in fp32 are worth waiting with the next tile until one is written.
+    // The tensor cores truncate a sum at every instruction, and the products that an instruction adds to it beside each other. A sum of n instructions
+    // ends up short by 0.27 n 2^-23 of its value where signs are random, 0.33 to 0.43 in updates that many samples share, 0.45 to 0.75 where all
+    // terms have one sign (A X of 1024 x 896 to 2300 x 3000). Several sums of a part of k each, added up in fp32, lose as many times less; 0.25 of
+    // it is put back. (2300 x 3000, error of one step 1.14e-6 of the result with 0.18, 0.76e-6 with 0.25, 0.57e-6 with 0.3, in fp32 0.38e-6; of five,
+    // where large singular values end beside each other, 2.30, 2.47, 2.58 and 2.71e-6.) Results in fp32 are worth waiting with the next tile until
+    // one is written.
     const bool one_tile = clusters == p.tiles;
     p.buffers = one_tile || q.precise ? 1 : 2;
     p.sums = 512 / TN / p.buffers;
     const double len = (double)p.part[0].kb / split, most = p.sums - (G::fused ? 1 : 0), of = len < most ? len : most;
-    p.beta = (float)(p.beta * (1.0 + 0.18 * 0x1p-23 * 4.0 * len / of));
+    p.beta = (float)(p.beta * (1.0 + 0.25 * 0x1p-23 * 4.0 * len / of));
   }
   if (kTwo) {
     p.heavy = p.tiles0 % clusters;

@@ -686,7 +686,9 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
       const float* c = coefficients ? coefficients + 3 * i : kUsual;
       const int ea = exponent_for(s[i] * s[i]), eb = exponent_for(b_most[i]), next = exponent_for(s[i + 1]);
       const bool last = i + 1 == steps;
-      // what the tensor cores' sums lose on average is put back (see launch in gemm16.cuh): sums of a slice, then of the short side
+      // What the tensor cores' sums lose on average is put back (see launch in gemm16.cuh): sums of a slice, then of the short side, as of two sums each.
+      // B X of slices wider than 128 columns is one sum, of which half stays: a step of fp32 at most, and a factor beside 1 comes in such steps only
+      // (following the form changed 128 x 2048 by nothing and 48 x 192 from 1.3e-6 to 1.6e-6 of the result, which is one step in one coefficient).
       const double lost = 0.18 * 0x1p-23, of_l = 1.0 + lost * (double)(l / 32 / q.slices), of_d = 1.0 + lost * (double)(d / 32);
       q.step[i].a_beta = (float)std::ldexp(of_l, ea - 2 * ex);
       q.step[i].b_alpha = (float)std::ldexp((double)c[1], eb - ea);
