@@ -501,8 +501,10 @@ MFET_API int mfet_layer_norm_backward(const void* x, uint32_t x_dtype, int64_t x
 
 /* The gated linear block h = act(G) * U with G = x w_gate^T, U = x w_up^T, and its backward pass:
  *   dG = dh * U * act'(G), dU = dh * act(G);  dx = dG w_gate + dU w_up;  dw_gate = dG^T x, dw_up = dU^T x
- * fp32 sums; h and the gradients rounded once; dG and dU are rounded to the dtype before the products that use them. The backward pass
- * computes G and U again: nothing has to be kept but x.
+ * fp32 sums; h and the gradients rounded once; dG and dU are rounded to the dtype before the products that use them, so in fp16 they have to be inside
+ * its range (gradients are proportional to dh: a power of two on it moves them all without a rounding). The backward pass
+ * computes G and U again: nothing has to be kept but x. A sum on the tensor cores is short by up to 2^-22 of itself for every 16 values, which shows in
+ * fp16 from some 10^5 on; sums over more than 65536 rows, of the weights' gradients, are taken in parts, where it does not.
  *   dtype    MFET_F16 or MFET_BF16, of all matrices: x, dx dev [m, k]; w_gate, w_up, dw_gate, dw_up dev [n, k]; h, dh dev [m, n]
  *   act      MFET_ACT_*: NONE, RELU (slope 0 at 0), SILU g / (1 + e^-g), GELU g Phi(g), SIGMOID
  *   dx, or dw_gate and dw_up, may be NULL: not wanted
@@ -527,9 +529,12 @@ MFET_API int mfet_gated_linear_backward(const void* x, uint32_t dtype, int64_t x
  *   coefficients  host f32[3 * steps]: a, b, c of each step; NULL: 3.4445, -4.775, 2.0315 in every step
  *   g, out        dev [rows, cols] of dtype MFET_F32 / F16 / BF16 each
  *   scratch       dev, 16-byte aligned, mfet_orthogonalize_bytes(rows, cols) bytes; needs no initialisation
- * Matrices between the products are held to 22 bits or more, |g| and its squares in fp64: the result is about as near as one computed in fp32
- * throughout. A g of zeros gives zeros; one with a NaN or an infinity gives NaN throughout. 1 <= steps <= 64; coefficients that let
- * a singular value grow beyond 2^20 are INVALID_ARG. Errors: INVALID_ARG, ALIGNMENT, WORKSPACE, CUDA; MFET_DEV_STALLED as above. */
+ * |g| and its squares are fp64. Matrices between the products are held to 22 bits, but not beyond 2^-38 of what bounds their singular values: s <= 1 for
+ * the first X, s^2 for A, |b| s^2 + |c| s^4 for b A + c A A. With schedules like the usual one the result is about as near as one computed in fp32
+ * throughout (one step of large matrices: up to twice as far off); with b = 0 and singular values of 1/30 and less it is not.
+ * A g of zeros gives zeros; one with a NaN or an infinity gives NaN throughout. 1 <= steps <= 64; coefficients that let
+ * a singular value, or |b| s^2 + |c| s^4 for the largest, grow beyond 2^20 are INVALID_ARG. Errors: INVALID_ARG, ALIGNMENT, WORKSPACE, CUDA;
+ * MFET_DEV_STALLED as above. */
 MFET_API uint64_t mfet_orthogonalize_bytes(int64_t rows, int64_t cols);
 MFET_API int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, int64_t cols, const float* coefficients,
                                 int32_t steps, float scale, void* out, uint32_t out_dtype, int64_t out_ld, void* scratch,

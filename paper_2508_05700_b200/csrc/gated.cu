@@ -202,8 +202,8 @@ int out_product(Problem& q, const Call& c) {
 // The weights' gradients are sums over the rows. The tensor cores truncate a sum once in 16 of them, by up to 2^-22 of what it holds (its 16 products
 // included), so that beyond some rows it loses more than its rounding to 16 bits does: fp16 products of one sign were off by 2.1e-4 of their sum for
 // 2^17 rows, 1.7e-3 for 2^20 and 6.6e-3 for 2^22 (half a step of fp16 is 4.9e-4), 64 x 64 weights in four parts of the rows. Sums over more than
-// kLongRows are taken in parts of kPartRows, which are added up in fp32, to nearest: 131072 x 1024 x 896 1132 -> 1172 us, 66000 x 100 x 5000 769 -> 844,
-// 2^20 x 64 x 64 1234 either way. (Both products in two launches: 1147 and 922; 131072 x 1024 x 2048 2298 in one, 2212 in two.)
+// kLongRows are taken in parts of kPartRows, which are added up in fp32, to nearest: 131072 x 1024 x 896 1134 -> 1157 us, 2^20 x 64 x 64 1232 -> 1240;
+// with both products in one launch 131072 x 1024 x 2048 2271 -> 2279, 66000 x 100 x 5000 770 -> 845 (922 in two launches).
 constexpr int64_t kLongRows = 1ll << 16, kPartRows = 1ll << 14;
 
 // Both products of the backward pass in one launch, where that takes less time than one after the other: blocks that have no tile of one left

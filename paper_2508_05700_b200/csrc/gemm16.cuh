@@ -29,10 +29,10 @@ enum Mode {
   kGatedBack,  // ... with the gradient of h: dG and dU
   kOut,        // the accumulator, rounded
   kOutTwo,     // ... of two products of different operands in one launch
-  kOutLong,    // ... of a long sum: the tensor cores add up parts of k, registers the parts
-  kOutTwoLong, // both: the first product's sum is long, the second's is one part
   kPair,       // v = alpha * C + beta * acc in two fp16 words
-  kPairOut     // the same, rounded to the type of the result
+  kPairOut,    // the same, rounded to the type of the result
+  kOutLong,    // kOut of a long sum: the tensor cores add up parts of k, registers the parts
+  kOutTwoLong  // kOutTwo, of which the first product's sum is long and the second's is one part
 };
 
 template <int CTAS, int TN, int MODE, int DT>

@@ -17,7 +17,9 @@ namespace {
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kChunk = 8;             // neighbouring columns of a thread, for rows of more than
-constexpr int64_t kMostHeld = 16384;  // columns: the longest row that registers hold
+// Columns: the longest row that registers hold, of 16 warps. 1024 x 16384 to bf16: 30 us (bf16) and 35 (fp32) held, 46 and 55 by the kernel for longer rows;
+// backward 68 and 70, 272 and 285.
+constexpr int64_t kMostHeld = 16384;
 constexpr int kLongThreads = 512;
 
 struct NormParams {
@@ -266,7 +268,7 @@ __device__ __forceinline__ void quad_stage(uint32_t to, bool odd, const float2* 
 // zeros with weight 0 and mean 0, so that nothing asks for them but the stores. Other rows are fetched in the pieces that hold them, read
 // from shared memory where their values lie, and written from there.
 // Backward with the sum of the blocks' parts, 8192 x 896, fp32 x, bf16 dy: a warp per row with its row in registers 56 us, 16 columns a thread
-// 25, this 17.5; 16384 x 2048 bf16 41.6, 201 MB at 4.8 TB/s.
+// 25, this 17.5 (the same inputs again and again, of which L2 holds a part; three sets of inputs in turn 21.2); 16384 x 2048 bf16 44, 201 MB at 4.6 TB/s.
 template <int DT, int OT, int NQ, int W, bool BACK, bool ALIGNED>
 __global__ void __launch_bounds__((norm_threads<NQ, W, BACK>), BACK || W == 16 ? 1 : 3) norm_kernel(const __grid_constant__ NormParams p) {
   using S = NormShape<DT, OT, NQ, W, BACK, ALIGNED>;
@@ -495,7 +497,8 @@ __global__ void __launch_bounds__((norm_threads<NQ, W, BACK>), BACK || W == 16 ?
 }
 
 // Rows that registers do not hold: a block per row reads it once for each sum and once more for the result (from L2). BACK: the
-// block's sums over its rows stay in its part of `partial`.
+// block's sums over its rows stay in its part of `partial`. Bound by latency, with one chunk of a thread under way at a time: 1024 x 20000 to bf16 takes
+// 60 us (bf16) and 70 (fp32), floors 12.5 and 18.8; backward 322 and 339, where every row also goes through the block's sums in memory.
 template <bool BACK>
 __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const __grid_constant__ NormParams p, uint32_t x_dtype) {
   __shared__ float shared[2][kLongThreads / 32];
@@ -630,6 +633,14 @@ struct Columns {
   int nq, w;
 };
 Columns columns_of(int64_t cols, bool aligned_rows) {
+  // The fewest quads and warps that hold a row, of those that there are; figures to bf16, of bf16 and of fp32 rows, backward in brackets:
+  //   65536 x 128   one quad 14.4, 15.6 (23.6, 26.4), two 15.1, 20.9 (24.8, 27.5)
+  //   32768 x 256   two 10.4, 14.0 (16.4, 20.6), four 15.1, 17.0 (23.1, 25.1)
+  //   16384 x 512   four 11.2, 13.1 (15.9, 19.9), seven 12.7, 15.1 (22.8, 27.6)
+  //   16384 x 640   seven 13.5, 16.0 (23.6, 31.1), eight 14.6, 17.6 (27.4, 38.3)
+  //   8192 x 896    seven 10.7, 12.6 (16.3, 21.5), eight 11.3, 13.6 (18.8, 26.4), two warps 11.9, 13.9 (22.4, 24.5)
+  //   8192 x 1024   eight 11.8, 14.3 (19.5, 27.8), two warps 12.1, 14.4 (22.5, 24.6)
+  //   1024 x 8192   eight warps 12.1, 14.6 (22.5, 24.9), sixteen 22.6, 24.8 (58.5, 58.7)
   if (cols > kMostHeld) return {0, 0};
   // 6 quads in place of 8: 4099 x 1075, bf16 to fp16 at any address 11.4 us, 12.9; 8192 x 1280 of these types 12.4, 14.9, backward 20.4, 25.2
   for (int w = 2; w <= 16; w *= 2)

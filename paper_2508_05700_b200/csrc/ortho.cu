@@ -115,7 +115,8 @@ __global__ void __launch_bounds__(kSumThreads) scale_kernel(const __grid_constan
 // (each block adds up a share of the columns in the order of the slices, and all read the sums), B by every block for itself, and the slice of
 // a X + B X over the old one. (With a on B's diagonal X is not read again, 3 us less, and errors are 1.4 times as large.) What costs is the
 // chain: three products, each waited for, and three turns from tensor memory to shared memory.
-// 48 x 192 in five steps: 36 us, 106 as seventeen launches; 128 x 2048: 91.
+// In five steps, here and as seventeen launches: 48 x 192 36 and 72 us, 128 x 128 42 and 76, 128 x 512 83 and 91, 128 x 2048 92 and 127. Beyond: 129 x 512
+// 103, 129 x 2048 137 (a short side above 128 does not fit the tensor cores' 128 lanes), 128 x 4096 162 (eight blocks hold no longer side).
 constexpr int kSmallThreads = 512;
 constexpr int kSmallSide = 128, kSlice = 256, kMostSlices = 8;
 constexpr uint32_t kBlock = 128 * 128;                    // 128 rows x 64 columns
