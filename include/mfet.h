@@ -531,7 +531,7 @@ MFET_API int mfet_gated_linear_backward(const void* x, uint32_t dtype, int64_t x
  *   scratch       dev, 16-byte aligned, mfet_orthogonalize_bytes(rows, cols) bytes; needs no initialisation
  * |g| and its squares are fp64. Matrices between the products are held to 22 bits, but not beyond 2^-38 of what bounds their singular values: s <= 1 for
  * the first X, s^2 for A, |b| s^2 + |c| s^4 for b A + c A A. With schedules like the usual one the result is about as near as one computed in fp32
- * throughout (one step of large matrices: up to twice as far off); with b = 0 and singular values of 1/30 and less it is not.
+ * throughout, also where sides are long (one step of large matrices: up to twice as far off); with b = 0 and singular values of 1/30 and less it is not.
  * A g of zeros gives zeros; one with a NaN or an infinity gives NaN throughout. 1 <= steps <= 64; coefficients that let
  * a singular value, or |b| s^2 + |c| s^4 for the largest, grow beyond 2^20 are INVALID_ARG. Errors: INVALID_ARG, ALIGNMENT, WORKSPACE, CUDA;
  * MFET_DEV_STALLED as above. */

@@ -10,10 +10,12 @@
 // B, one issues the instructions of both; a pair reads 64 bytes per SM and cycle at full rate where a block alone would need 96).
 // Copies of tiles go through a ring of shared memory; two accumulators in tensor memory, so that one tile is written while the next
 // one is computed. With few tiles, `split` blocks (pairs) of a cluster take a part of k each, leave their sums in shared memory, and
-// each adds up its share of the columns over all of them, in the order of k: the result does not depend on who is first.
+// each adds up its share of the columns over all of them, in the order of k: the result does not depend on who is first. The tensor cores truncate a
+// running sum; long ones are taken in parts, in the two accumulators in turn, that the writing warps add up in registers (the modes *Long).
 #pragma once
 
 #include <cstring>
+#include <type_traits>
 
 #include "tensor.cuh"
 
@@ -32,15 +34,25 @@ enum Mode {
   kPair,       // v = alpha * C + beta * acc in two fp16 words
   kPairOut,    // the same, rounded to the type of the result
   kOutLong,    // kOut of a long sum: the tensor cores add up parts of k, registers the parts
-  kOutTwoLong  // kOutTwo, of which the first product's sum is long and the second's is one part
+  kOutTwoLong, // kOutTwo, of which the first product's sum is long and the second's is one part
+  kPairLong,   // kPair and kPairOut of a long sum
+  kPairOutLong
 };
+template <int MODE>
+constexpr bool is_long = MODE >= kOutLong;
+template <int MODE>
+constexpr bool is_two = MODE == kOutTwo || MODE == kOutTwoLong;
+template <int MODE>
+constexpr bool is_pair = MODE == kPair || MODE == kPairLong;
+template <int MODE>
+constexpr bool is_pair_out = MODE == kPairOut || MODE == kPairOutLong;
 
 template <int CTAS, int TN, int MODE, int DT>
 struct Shape {
   static constexpr bool dual = MODE == kGated || MODE == kGatedBack;  // half of the columns of B come from a second matrix
-  static constexpr int outs = MODE == kGatedBack || MODE == kPair ? 2 : 1;
+  static constexpr int outs = MODE == kGatedBack || is_pair<MODE> ? 2 : 1;
   static constexpr int b_rows = TN / CTAS;
-  static constexpr bool precise = MODE == kPair || MODE == kPairOut;  // two words each; several sums of a part of k each (Params::sums)
+  static constexpr bool precise = is_pair<MODE> || is_pair_out<MODE>;  // two words each; several sums of a part of k each (Params::sums)
   // With few columns the loads' latency is what a block of k takes: both words of both operands come together, and serve the three products
   static constexpr bool fused = precise && TN == 64;
   static constexpr uint32_t a_bytes = 128 * 128, b_bytes = b_rows * 128, stage_bytes = (a_bytes + b_bytes) * (fused ? 2 : 1);
@@ -172,6 +184,38 @@ __device__ __forceinline__ void commit(uint32_t bar, uint32_t mask) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
                  "h"((uint16_t)mask)
                  : "memory");
+}
+
+// 16 columns of two and of four sums, `apart` columns from one to the next: while products are under way a load takes 0.4 us to come back
+__device__ __forceinline__ void tmem_load16x2(uint32_t addr, uint32_t apart, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr), "r"(addr + apart)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_load16x4(uint32_t addr, uint32_t apart, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%64];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%65];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47}, [%66];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%67];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]),
+        "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]),
+        "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]),
+        "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]),
+        "=r"(r[63])
+      : "r"(addr), "r"(addr + apart), "r"(addr + 2 * apart), "r"(addr + 3 * apart)
+      : "memory");
 }
 
 // ------------------------------------------------------------------ activations ----
@@ -372,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   early_launch_wait();
 
   const uint32_t members = CTAS * p.split;
-  constexpr bool kTwo = MODE == kOutTwo || MODE == kOutTwoLong, kLong = MODE == kOutLong || MODE == kOutTwoLong;
+  constexpr bool kTwo = is_two<MODE>, kLong = is_long<MODE>;
   const uint32_t first = blockIdx.x / members;
   const Walk<kTwo> walk(p, first, gridDim.x / members);
   auto share_begin = [&](const Part& q) { return (uint32_t)((uint64_t)q.kb * part / p.split); };  // this block's share of k, in each segment
@@ -392,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
         const Part& q = p.part[kTwo ? w.part : 0];
         const uint32_t k0 = share_begin(q), k1 = share_end(q);
         const int32_t row = (int32_t)((w.tm * CTAS + half) * 128);
-        uint32_t seg = 0, kk = k0;
+        uint32_t seg = 0, kk = k0, from = k0, to = kLong ? min(k0 + p.part_kb, k1) : k1;  // of a part
         for (uint32_t i = (k1 - k0) * (G::fused ? 1 : q.segs); i > 0; --i) {
           if (!(ok = bar_sleep(empty(st), phase, &dead))) break;
           // tiles and blocks of k outside their matrix read as 0
@@ -443,7 +487,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
           }
           ++filled;
           if (++st == (uint32_t)G::stages) st = 0, phase ^= 1;
-          if (++kk == k1) kk = k0, ++seg;
+          if (++kk == to) {
+            kk = from, ++seg;
+            if (kLong && seg == (G::fused ? 1 : q.segs)) seg = 0, kk = from = to, to = min(to + p.part_kb, k1);
+          }
         }
       }
     }
@@ -537,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   };
   // the same with rows and columns exchanged (of a symmetric result, which has bulk copies)
   auto put_mirror = [&](const float* v, int o, int64_t i0, int64_t j1) {
-    if constexpr (MODE == kPair) {
+    if constexpr (is_pair<MODE>) {
       const uint32_t piece = (turn * G::outs + o) * G::piece;
 #pragma unroll
       for (int j = 0; j < 32; ++j) *reinterpret_cast<T*>(out_ptr + piece + G::at(j, lane >> 3) + (lane & 7) * sizeof(T)) = Elem<DT>::from(v[j]);
@@ -565,12 +612,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       gates32<true>(p.act, v, u, x);
       put(v, 0, i0, j1);
       put(u, 1, i0, j1);
-    } else if constexpr (MODE == kOut || kTwo || kLong) {
+    } else if constexpr (!G::precise) {
       put(v, (int)q->out + z, i0, j1);
     } else {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], p.beta, x[j] * p.alpha);
-      if constexpr (MODE == kPair) {
+      if constexpr (is_pair<MODE>) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) x[j] = v[j] - __half2float(__float2half_rn(v[j]));
         put(v, 0, i0, j1);
@@ -589,8 +636,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
   };
   // What stands beside 32 columns of row i: asked for a chunk ahead (waiting for it took longer than all else that is done with a chunk: 4.4 us
   // a tile of 128 x 64 units, backward, where its products take 2.2)
-  constexpr bool kBeside = MODE == kGatedBack || MODE == kPair || MODE == kPairOut;
-  constexpr int kBesides = MODE == kPair || MODE == kPairOut ? 2 : 1;
+  constexpr bool kBeside = MODE == kGatedBack || G::precise;
+  constexpr int kBesides = G::precise ? 2 : 1;
   auto ask = [&](Row32* r, int64_t i, int64_t j1) {
     if constexpr (kBeside) {
       if (i < q->m && j1 < q->n && p.c0 && MFET_INSIDE(p.status, j1 >= 0 && i >= 0)) {
@@ -643,7 +690,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
       const uint32_t len = share_end(*q) - share_begin(*q), parts = kLong ? (len + p.part_kb - 1) / p.part_kb : 1;
       if (kLong && parts > 1) {  // a tile's parts in their order, added up in registers while the next one is computed
         constexpr int kChunks = G::width / 64;
-        float v[kChunks][32];
+        // (64 columns leave room for fp64, whose additions cost nothing beside the products: the longest sums are the narrowest ones)
+        std::conditional_t<G::fused, double, float> v[kChunks][32];
         bool ok = true;
         for (uint32_t n = 0; n < parts; ++n, ++unit) {
           const uint32_t acc = unit % p.buffers;
@@ -652,10 +700,29 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
           for (int c = 0; c < kChunks; ++c) {
-            uint32_t r[32];
-            tmem_load32(tmem + acc * TN + ((uint32_t)(quarter * 32) << 16) + 32 * second + 64 * c, r);
+            const uint32_t from = tmem + acc * (G::precise ? p.sums : 1u) * TN + ((uint32_t)(quarter * 32) << 16) + 32 * second + 64 * c;
+            if constexpr (G::precise) {
+              constexpr int kSums = G::fused ? 4 : 2;  // Params::sums; the last part may have fewer
+              const uint32_t sums = sums_for(min(p.part_kb, len - n * p.part_kb)) + (G::fused ? 1 : 0);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[c][j] = n ? v[c][j] + __uint_as_float(r[j]) : __uint_as_float(r[j]);
+              for (int h = 0; h < 32; h += 16) {
+                uint32_t r[16 * kSums];
+                if constexpr (G::fused) tmem_load16x4(from + h, TN, r);
+                else tmem_load16x2(from + h, TN, r);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                  float t = __uint_as_float(r[j]);
+#pragma unroll
+                  for (int z = 1; z < kSums; ++z) t += z < sums ? __uint_as_float(r[16 * z + j]) : 0.f;
+                  v[c][h + j] = n ? v[c][h + j] + t : t;
+                }
+              }
+            } else {
+              uint32_t r[32];
+              tmem_load32(from, r);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[c][j] = n ? v[c][j] + __uint_as_float(r[j]) : __uint_as_float(r[j]);
+            }
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
@@ -668,12 +735,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm16_kernel(const __grid_consta
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
           const int c0 = 32 * second + 64 * c;
+          float r[32], x[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) r[j] = (float)v[c][j];
           if (p.split > 1) {
 #pragma unroll
             for (int j = 0; j < 32; j += 4)
-              *reinterpret_cast<float4*>(smem + (((c0 + j) >> 2) * 128 + quarter * 32 + lane) * 16) = make_float4(v[c][j], v[c][j + 1], v[c][j + 2], v[c][j + 3]);
+              *reinterpret_cast<float4*>(smem + (((c0 + j) >> 2) * 128 + quarter * 32 + lane) * 16) = make_float4(r[j], r[j + 1], r[j + 2], r[j + 3]);
           } else {
-            finish(v[c], nullptr, nullptr, (int)w.z, row_of(w), (int64_t)w.tn * G::width + c0, false);
+            const int64_t i0 = row_of(w), j1 = (int64_t)w.tn * G::width + c0;
+            ask(next, i0 + lane, j1);
+            got(next, x);
+            finish(r, nullptr, x, (int)w.z, i0, j1, p.sym && w.tm != w.tn);
           }
         }
         if (p.split > 1) break;
@@ -885,7 +958,7 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
       return MFET_ERR_CUDA;
   }
   const uint32_t fmt = q.dtype == MFET_BF16 ? 1u : 0u;
-  constexpr bool kTwo = MODE == kOutTwo || MODE == kOutTwoLong;
+  constexpr bool kTwo = is_two<MODE>;
   for (int i = 0; i < (kTwo ? 2 : 1); ++i) {
     Part& x = p.part[i];
     x.m_tiles = (uint32_t)((x.m + CTAS * 128 - 1) / (CTAS * 128));
@@ -914,9 +987,13 @@ int launch(const Problem& q, uint32_t split, cudaStream_t s) {
     // where large singular values end beside each other, 2.30, 2.47, 2.58 and 2.71e-6.) Results in fp32 are worth waiting with the next tile until
     // one is written.
     const bool one_tile = clusters == p.tiles;
-    p.buffers = one_tile || q.precise ? 1 : 2;
+    p.buffers = !is_long<MODE> && (one_tile || q.precise) ? 1 : 2;
     p.sums = 512 / TN / p.buffers;
-    const double len = (double)p.part[0].kb / split, most = p.sums - (G::fused ? 1 : 0), of = len < most ? len : most;
+    double len = (double)p.part[0].kb / split, most = p.sums - (G::fused ? 1 : 0), of = len < most ? len : most;
+    if (is_long<MODE>) {  // two blocks of k a sum, and the next part's sums while these are added up
+      p.part_kb = 2 * (uint32_t)most;
+      len = 2 * (of = most);
+    }
     p.beta = (float)(p.beta * (1.0 + 0.25 * 0x1p-23 * 4.0 * len / of));
   }
   if (kTwo) {
@@ -986,15 +1063,20 @@ struct Choice {
   int form;  // 0: pairs, 1: blocks, 2: blocks of 64 columns
   uint32_t split, sym;
 };
+template <int MODE>
+constexpr bool has_pairs = !(Shape<2, 256, MODE, MFET_F16>::precise && is_long<MODE>);  // no room for several sums and the next part's
 template <int MODE, int DT>
 Choice choose(const Problem& q) {
-  Choice c{1e300, 0, 1, 0};
+  Choice c{1e300, has_pairs<MODE> ? 0 : 1, 1, 0};
   for (uint32_t sym = 0; sym <= q.p.sym; ++sym) {
     Problem r = q;
     r.p.sym = sym;
     for (uint32_t part = 1; part <= 4; part *= 2) {
-      const double pair = cost<2, 256, MODE, DT>(r, part) + 0.8 * sym, block = cost<1, 128, MODE, DT>(r, part) + 0.8 * sym;
-      if (pair < c.cost && !(q.precise && (q.k[0] + kSlab - 1) / kSlab * 2 / part > kSumOfPairs)) c = {pair, 0, part, sym};
+      if constexpr (has_pairs<MODE>) {
+        const double pair = cost<2, 256, MODE, DT>(r, part) + 0.8 * sym;
+        if (pair < c.cost && !(q.precise && (q.k[0] + kSlab - 1) / kSlab * 2 / part > kSumOfPairs)) c = {pair, 0, part, sym};
+      }
+      const double block = cost<1, 128, MODE, DT>(r, part) + 0.8 * sym;
       if (block < c.cost) c = {block, 1, part, sym};
       if constexpr (!Shape<1, 128, MODE, DT>::dual) {
         const double narrow = cost<1, 64, MODE, DT>(r, part);
@@ -1014,7 +1096,9 @@ int run(Problem q, cudaStream_t s) {
   q.p.sym = c.sym;
   if constexpr (!Shape<1, 128, MODE, DT>::dual)
     if (c.form == 2) return launch<1, 64, MODE, DT>(q, c.split, s);
-  return c.form == 0 ? launch<2, 256, MODE, DT>(q, c.split, s) : launch<1, 128, MODE, DT>(q, c.split, s);
+  if constexpr (has_pairs<MODE>)
+    if (c.form == 0) return launch<2, 256, MODE, DT>(q, c.split, s);
+  return launch<1, 128, MODE, DT>(q, c.split, s);
 }
 
 // ------------------------------------------------------------------ rows that no bulk copy can read ----

@@ -7,7 +7,7 @@
 // word the result is off by 1e-3 (fp16) to 1e-2 (bf16) of its size. So X, A and B = b A + c A A are held as the sum of two fp16 words
 // (22 bits and more, under a power of two for each matrix that keeps its bound, known to the host, inside fp16's range), a product is three
 // (high x low, low x high, then high x high: the tensor cores truncate a sum after
-// every 16 products, by a part of what it is by then) in one fp32 accumulator, and the result is as near as one computed in fp32.
+// every 16 products, by a part of what it is by then) in fp32 accumulators of a part of the sum each, and the result is as near as one computed in fp32.
 #include <cmath>
 
 #include "gemm16.cuh"
@@ -603,6 +603,12 @@ cudaError_t load(const LoadParams& p, unsigned blocks, cudaStream_t s) {
   return e != cudaSuccess ? e : launch_early(scale_kernel<DT>, blocks, kSumThreads, 0, s, p);
 }
 
+// Sums that are longer are taken in parts of few instructions each, which are added up outside the tensor cores: with fp32 results, and with 16-bit ones.
+// Error of five steps to fp32 in one run of sums, in parts and of an iteration in fp32: 64 x 2^20 2.1e-4 of the result, 1.5e-6, 0.9e-6; 500 x 40000 5.4e-6,
+// 3.3e-6, 2.5e-6; 2048 x 16384 1.3e-5, 2.2e-6, 3.1e-6. Time: 17.3 -> 21.4 ms, 1.21 -> 1.41, 3.53 -> 3.72 (a part's sums are read while the next part's
+// products are under way, which takes longer than these do).
+constexpr int64_t kLongSum = 4096, kLongSum16 = 65536;
+
 // the three products of two matrices in two words
 void three(Problem* q, const Words& a, const Words& b, int64_t k) {
   q->a[0] = a.hi, q->a[1] = a.lo, q->n_a = 2;
@@ -723,6 +729,8 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
                                             : load<MFET_BF16>(p, blocks, st);
   if (e != cudaSuccess) return MFET_ERR_CUDA;
 
+  const bool precise = out_dtype == MFET_F32;
+  auto words_of = [&](const Problem& q) { return q.k[0] > (precise ? kLongSum : kLongSum16) ? run<kPairLong, MFET_F16>(q, st) : run<kPair, MFET_F16>(q, st); };
   for (int i = 0; i < steps; ++i) {
     const float* c = coefficients ? coefficients + 3 * i : kUsual;
     const Words& from = x[i & 1];
@@ -731,30 +739,30 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
     a.e = exponent_for(s[i] * s[i]);
     Problem q;
     q.p.status = status;
-    q.precise = out_dtype == MFET_F32;
+    q.precise = precise;
     three(&q, from, from, tall ? rows : cols);
     q.p.part[0].a_mn = q.p.part[0].b_mn = tall;
     q.a_mn = q.b_mn = tall ? 3 : 0;
     q.p.sym = 1;
     combine(&q, nullptr, 0.0, 1.0, from.e, from.e, a.e);
     into(&q, a);
-    int rc = run<kPair, MFET_F16>(q, st);
+    int rc = words_of(q);
     if (rc != MFET_OK) return rc;
     // B = b A + c A A, A being symmetric
     b.e = exponent_for(b_most[i]);
     q = Problem();
     q.p.status = status;
-    q.precise = out_dtype == MFET_F32;
+    q.precise = precise;
     three(&q, a, a, d);
     q.p.sym = 1;
     combine(&q, &a, c[1], c[2], a.e, a.e, b.e);
     into(&q, b);
-    rc = run<kPair, MFET_F16>(q, st);
+    rc = words_of(q);
     if (rc != MFET_OK) return rc;
     // X = a X + B X, or a X + X B, B being symmetric
     q = Problem();
     q.p.status = status;
-    q.precise = out_dtype == MFET_F32;
+    q.precise = precise;
     if (tall) three(&q, from, b, d);
     else three(&q, b, from, d);
     q.p.part[0].b_mn = !tall;
@@ -763,14 +771,14 @@ int mfet_orthogonalize(const void* g, uint32_t dtype, int64_t ld, int64_t rows, 
       next.e = exponent_for(s[i + 1]);
       combine(&q, &from, c[0], 1.0, from.e, b.e, next.e);
       into(&q, next);
-      rc = run<kPair, MFET_F16>(q, st);
+      rc = words_of(q);
     } else {
       combine(&q, &from, (double)c[0] * scale, scale, from.e, b.e, 0);
       q.out[0] = {out, cols, rows, out_ld};
       q.out_dtype = out_dtype;
       q.p.part[0].m = rows;
       q.p.part[0].n = cols;
-      rc = out_dtype == MFET_F32   ? run<kPairOut, MFET_F32>(q, st)
+      rc = precise                 ? (d > kLongSum ? run<kPairOutLong, MFET_F32>(q, st) : run<kPairOut, MFET_F32>(q, st))
            : out_dtype == MFET_F16 ? run<kPairOut, MFET_F16>(q, st)
                                    : run<kPairOut, MFET_BF16>(q, st);
     }

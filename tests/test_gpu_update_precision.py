@@ -52,6 +52,19 @@ def test_as_near_as_an_iteration_in_fp32(rows, cols, steps):
     assert sorted(off)[2] <= 2 * sorted(by)[2] + 2.0**-24 + short
 
 
+@pytest.mark.parametrize("rows,cols", [(64, 8192), (8200, 60), (300, 4097), (500, 40000), (40001, 129), (1000, 20000), (64, 2**17 + 9), (2**20, 64), (1, 2**22),
+                                       (2048, 16384), (4500, 5000)])
+@pytest.mark.parametrize("steps", [1, 5])
+def test_long_sides(rows, cols, steps):
+    """The same where the sums over the long side (and over a short one of more than 4096) are long."""
+    test_as_near_as_an_iteration_in_fp32(rows, cols, steps)
+
+
+@pytest.mark.parametrize("rows,cols", [(100, 70000), (66000, 300), (1500, 66000)])
+def test_long_sides_in_16_bits(rows, cols):
+    test_results_in_16_bits_element_by_element(rows, cols, "f16")
+
+
 @pytest.mark.parametrize("rows,cols", [(1700, 1600), (3000, 2300), (2300, 3000)])
 @pytest.mark.parametrize("dst", ["bf16", "f16"])
 def test_results_in_16_bits_element_by_element(rows, cols, dst):
